@@ -1,0 +1,920 @@
+// Attention and its backward pass on the fifth-generation tensor cores.
+//
+// Forward, one CTA per 128 queries of a head: S = Q K^T into tensor memory, a thread per query takes its row through
+// the online softmax, P goes back into tensor memory as the left operand of O += P V.  The running maximum is only moved
+// (and O rescaled) when it grows by more than 2^8: P stays below 256, which both 16-bit types hold.
+//
+// Backward, two kernels without atomics, so that gradients are the same bits every time:
+//   dK, dV: a CTA keeps 128 keys and walks the queries of its group's heads, 64 at a time.  It works on the transposes,
+//           S^T = K Q^T and dP^T = V dO^T, so that P^T and dS^T are left operands in tensor memory: nothing is staged
+//           in shared memory between the products.
+//   dQ:     a CTA keeps 128 queries and walks the keys, 64 at a time: S, dP, and dQ += dS K with dS in tensor memory.
+// That is 7 products per pair of tiles where adding dQ up by atomics would take 5; what it saves is the 32-bit dQ
+// in memory, its clearing and conversion, and the order of its sums.
+//
+// Roles in a CTA: warps of 4 take the rows (thread = tensor memory lane), one warp issues the bulk copies, one the products.
+#include "step_tcgen05.cuh"
+
+#include <limits.h>
+#include <math.h>
+
+namespace halos_step {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kRecord = 64;   // queries to a record
+
+// What the backward pass knows of 64 queries of a head before it starts.  A query that sees nothing, or is none, has
+// lse2 = infinity: its probabilities are 0.
+struct Record {
+    float lse2[kRecord];      // log2 of the sum of exponentials
+    float delta[kRecord];     // dout . o
+    int lo[kRecord], hi[kRecord];
+};
+static_assert(sizeof(Record) == 1024, "one bulk copy");
+// The keys that a batch row's 64 queries see, in four numbers: some of them see [min_lo, max_hi), all of them see
+// [max_lo, min_hi).  max_lo = INT_MAX: one of them sees nothing.
+struct Reach { int min_lo, max_hi, max_lo, min_hi; };
+
+struct AttentionParams {
+    int sq, sk, head_dim, n_q, group, batch, causal, q_tiles, k_tiles, records;
+    float scale, scale2;              // scale2 = scale log2(e)
+    const int32_t *doc_start, *lens;
+    const char *q, *k, *v, *o_in, *dout;
+    char *o, *dq, *dk, *dv;
+    float* lse;
+    Record* record;                   // [batch, n_q, records]
+    Reach* reach;                     // [batch, records]
+    int* fault;
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3], dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];  // in elements
+};
+
+__device__ int g_fault;
+
+// The keys [lo, hi) that query i of batch row b sees; lo = INT_MAX, hi = 0 if none.
+__device__ __forceinline__ void seen_by(const AttentionParams& P, int b, int i, int& lo, int& hi) {
+    lo = INT_MAX, hi = 0;
+    if (i >= P.sq) return;
+    const int t = i + P.sk - P.sq;
+    int n = P.sk;
+    if (P.lens) n = min(max(P.lens[b], 0), P.sk);
+    if (t >= n) return;
+    const int h = P.causal ? min(n, t + 1) : n;
+    const int l = P.doc_start ? max(P.doc_start[(int64_t)b * P.sq + i], 0) : 0;
+    if (l < h) lo = l, hi = h;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(char* base, int64_t at, int head_dim, const uint32_t* words, int first) {
+    // `words`: 16 packed pairs, elements first .. first + 32 of the row at element `at`
+    T* row = reinterpret_cast<T*>(base) + at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (first + 8 * i < head_dim)
+            *reinterpret_cast<uint4*>(row + first + 8 * i) = make_uint4(words[4 * i], words[4 * i + 1], words[4 * i + 2], words[4 * i + 3]);
+}
+
+// Zeroes rows of a tile in shared memory (the bulk copy's layout) that nobody sees: their probabilities are zero, but
+// zero times what may lie there need not be.  `threads` threads, thread `at`.
+template <int DP>
+__device__ __forceinline__ void clear_row(char* tile, int rows, int row) {
+#pragma unroll
+    for (int sub = 0; sub < DP / 64; ++sub)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(tile + sub * rows * 128 + row * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+}
+
+// ------------------------------------------------------------------------------------------------ forward
+
+template <int DP> struct Forward {
+    static constexpr int kRowsQ = 128, kRowsK = 128;
+    static constexpr bool kOwnP = DP == 64;          // tensor memory has room for P beside S: the next S can start early
+    static constexpr int kStages = DP == 64 ? 2 : 1;
+    static constexpr int kTileQ = kRowsQ * DP * 2, kTileK = kRowsK * DP * 2;
+    static constexpr int kSmem = 1024 + kTileQ + 2 * kStages * kTileK;
+    static constexpr int kColS = 0, kColP = kOwnP ? 128 : 0, kColO = kOwnP ? 192 : 128, kColumns = 256;
+    static constexpr int kThreads = 192;
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(192, 2)
+attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ CUtensorMap map_q,
+                     const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+    using F = Forward<DP>;
+    extern __shared__ char smem_raw[];
+    char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    char* tile_q = smem;
+    char* tile_k = smem + F::kTileQ;
+    char* tile_v = tile_k + F::kStages * F::kTileK;
+    __shared__ uint64_t bars[6 + 4 * F::kStages];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_gave_up, s_lo[4], s_hi[4];
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t q_full = bar0, s_full = bar0 + 8, s_free = bar0 + 16, p_full = bar0 + 24, pv_done = bar0 + 32, left = bar0 + 40;
+    const uint32_t k_full = bar0 + 48, k_free = k_full + 8 * F::kStages, v_full = k_free + 8 * F::kStages, v_free = v_full + 8 * F::kStages;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    // Longest rows first where the mask is causal.
+    const int heads = P.batch * P.n_q;
+    const int tile = P.causal ? P.q_tiles - 1 - (int)(blockIdx.x / heads) : (int)(blockIdx.x / heads);
+    const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
+
+    if (threadIdx.x == 0) {
+        bar_init(q_full, 1), bar_init(s_full, 1), bar_init(s_free, 128), bar_init(p_full, 128), bar_init(pv_done, 1), bar_init(left, 1);
+        for (int s = 0; s < F::kStages; ++s) bar_init(k_full + 8 * s, 1), bar_init(k_free + 8 * s, 1), bar_init(v_full + 8 * s, 1), bar_init(v_free + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_gave_up = 0;
+    }
+    if (warp == 5) tmem_alloc<F::kColumns>(smem_u32(&s_tmem));
+    int lo = INT_MAX, hi = 0;
+    if (warp < 4) {
+        seen_by(P, b, tile * 128 + threadIdx.x, lo, hi);
+        int l = lo, g = hi;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) l = min(l, __shfl_xor_sync(~0u, l, o)), g = max(g, __shfl_xor_sync(~0u, g, o));
+        if (lane == 0) s_lo[warp] = l, s_hi[warp] = g;
+    }
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = s_tmem;
+    const int min_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), max_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
+    const int first = max_hi ? min_lo / 128 : 0, n = max_hi ? (max_hi + 127) / 128 - first : 0;
+    const Waits W{&s_gave_up, P.fault};
+
+    if (warp == 4) {
+        if (lane == 0 && n) {
+            bar_expect(q_full, F::kTileQ);
+            for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
+            int j = 0;
+            for (; j < n; ++j) {
+                const int s = j % F::kStages, use = j / F::kStages;
+                const int row = (first + j) * 128;
+                if (use && !W.wait(k_free + 8 * s, (use - 1) & 1)) break;
+                bar_expect(k_full + 8 * s, F::kTileK);
+                for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_k) + s * F::kTileK + d * 128 * 128, &map_k, k_full + 8 * s, d * 64, row, hk, b);
+                if (use && !W.wait(v_free + 8 * s, (use - 1) & 1)) break;
+                bar_expect(v_full + 8 * s, F::kTileK);
+                for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_v) + s * F::kTileK + d * 128 * 128, &map_v, v_full + 8 * s, d * 64, row, hk, b);
+            }
+            if (j < n) {  // left early: wait for the copies in flight
+                W.drain(q_full, 0);
+                for (int i = j > F::kStages ? j - F::kStages : 0; i <= j; ++i) {
+                    W.drain(k_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+                    if (i < j) W.drain(v_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+                }
+            }
+        }
+    } else if (warp == 5) {
+        if (lane == 0 && n) {
+            const auto scores = [&](int j) -> bool {
+                const int s = j % F::kStages;
+                if (!W.wait(k_full + 8 * s, (j / F::kStages) & 1)) return false;
+                tc_after_sync();
+                product_ss<T, 128, DP>(tmem + F::kColS, smem_u32(tile_q), 128, smem_u32(tile_k) + s * F::kTileK, 128);
+                mma_commit(k_free + 8 * s);
+                mma_commit(s_full);
+                return true;
+            };
+            bool ok = W.wait(q_full, 0) && scores(0);
+            for (int j = 0; ok && j < n; ++j) {
+                const int s = j % F::kStages;
+                if (F::kOwnP && j + 1 < n) ok = W.wait(s_free, j & 1) && scores(j + 1);
+                ok = ok && W.wait(p_full, j & 1) && W.wait(v_full + 8 * s, (j / F::kStages) & 1);
+                if (!ok) break;
+                tc_after_sync();
+                product_ts<T, DP, 128>(tmem + F::kColO, tmem + F::kColP, smem_u32(tile_v) + s * F::kTileK, j > 0);
+                mma_commit(v_free + 8 * s);
+                mma_commit(pv_done);
+                if (!F::kOwnP && j + 1 < n) ok = scores(j + 1);
+            }
+            if (!ok) {  // products in flight still use tensor memory
+                mma_commit(left);
+                W.drain(left, 0);
+            }
+        }
+    } else {
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        const int i = tile * 128 + threadIdx.x;
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int j = 0; j < n; ++j) {
+            const int key0 = (first + j) * 128;
+            if (!(ok = W.wait_warp(s_full, j & 1))) break;
+            tc_after_sync();
+            uint32_t x[128];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_load32(x + 32 * c, lanes + F::kColS + 32 * c);
+            tmem_wait_loads();
+            if (F::kOwnP) {
+                tc_before_sync();
+                bar_arrive(s_free);
+            }
+            if (!__all_sync(~0u, lo <= key0 && hi >= key0 + 128)) {
+#pragma unroll
+                for (int c = 0; c < 128; ++c)
+                    if (key0 + c < lo || key0 + c >= hi) x[c] = 0xff800000u;
+            }
+            float top = __uint_as_float(x[0]);
+#pragma unroll
+            for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(x[c]));
+            top *= P.scale2;
+            if (__any_sync(~0u, top > m + 8.f)) {
+                const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : fast_exp2(m - to);
+                m = to;
+                l *= f;
+                if (j) {
+                    if (!(ok = W.wait_warp(pv_done, (j - 1) & 1))) break;
+                    tc_after_sync();
+#pragma unroll
+                    for (int c = 0; c < DP / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_load32(o, lanes + F::kColO + 32 * c);
+                        tmem_wait_loads();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_store32(lanes + F::kColO + 32 * c, o);
+                    }
+                }
+            }
+            const float sub = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int c = 0; c < 128; ++c) {
+                const float p = fast_exp2(fmaf(__uint_as_float(x[c]), P.scale2, -sub));
+                l += p;
+                x[c] = __float_as_uint(p);
+            }
+#pragma unroll
+            for (int c = 0; c < 64; ++c) x[c] = pack2<T>(__uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1]));
+            if (F::kOwnP && j && !(ok = W.wait_warp(pv_done, (j - 1) & 1))) break;
+            tmem_store32(lanes + F::kColP, x);
+            tmem_store32(lanes + F::kColP + 32, x + 32);
+            tmem_wait_stores();
+            if (key0 < min_lo || (key0 + 128 > max_hi && max_hi < P.sk)) {
+                const int s = j % F::kStages;
+                if (!(ok = W.wait_warp(v_full + 8 * s, (j / F::kStages) & 1))) break;
+                const int key = key0 + threadIdx.x;
+                if (key < min_lo || key >= max_hi) clear_row<DP>(tile_v + s * F::kTileK, 128, threadIdx.x);
+                fence_async_shared();
+            }
+            tc_before_sync();
+            bar_arrive(p_full);
+        }
+        if (ok && n) {
+            ok = W.wait_warp(pv_done, (n - 1) & 1);
+            tc_after_sync();
+        }
+        if (ok) {
+            const float inv = l > 0.f ? 1.f / l : l;  // a NaN stays one
+#pragma unroll
+            for (int c = 0; c < DP / 32; ++c) {
+                uint32_t o[32];
+                if (n) {
+                    tmem_load32(o, lanes + F::kColO + 32 * c);
+                    tmem_wait_loads();
+                }
+                if (i < P.sq) {
+                    const bool none = hi == 0;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        o[e] = none ? 0u : pack2<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+                    store_row<T>(P.o, b * P.o_stride[0] + i * P.o_stride[1] + h * P.o_stride[2], P.head_dim, o, 32 * c);
+                }
+            }
+            if (i < P.sq) P.lse[((int64_t)b * P.n_q + h) * P.sq + i] = hi == 0 ? -INFINITY : (m + log2f(l)) * kLn2;
+        }
+    }
+    tc_before_sync();
+    __syncthreads();
+    if (warp == 5) tmem_free<F::kColumns>(tmem);
+}
+
+// ------------------------------------------------------------------------------------------------ backward
+
+template <typename T>
+__device__ __forceinline__ const T* row_of(const char* base, const int64_t* stride, int b, int64_t s, int h) {
+    return reinterpret_cast<const T*>(base) + b * stride[0] + s * stride[1] + h * stride[2];
+}
+
+// The share of thread `part` of 8 in the product of two rows.
+template <typename T>
+__device__ __forceinline__ float dot_share(const T* x, const T* y, int head_dim, int part) {
+    float sum = 0.f;
+    for (int c = part * 8; c < head_dim; c += 64) {
+        const uint4 a = *reinterpret_cast<const uint4*>(x + c), b = *reinterpret_cast<const uint4*>(y + c);
+        const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 p = unpack2<T>(as[e]), q = unpack2<T>(bs[e]);
+            sum = fmaf(p.x, q.x, fmaf(p.y, q.y, sum));
+        }
+    }
+    return sum;
+}
+__device__ __forceinline__ float sum_of_8(float v) {
+#pragma unroll
+    for (int s = 4; s; s >>= 1) v += __shfl_xor_sync(~0u, v, s);
+    return v;
+}
+
+// D = dout . o is off by the rounding of o to 16 bits, and ds = p (dp - D) by as much whatever its own size.  Against the sum over
+// many keys that is little; a query with few keys, whose dp and D nearly cancel, would lose half of its digits to it.
+// Its D is formed from sum p dp instead, in 32 bits.
+constexpr int kFewKeys = 16;
+
+// Records of 64 queries of a head, and once per batch row their reach.  Eight threads per query.
+template <typename T>
+__global__ void __launch_bounds__(512) attention_record_kernel(const __grid_constant__ AttentionParams P) {
+    const int rec = blockIdx.x, h = blockIdx.y, b = blockIdx.z, r = threadIdx.x >> 3, part = threadIdx.x & 7;
+    const int i = rec * kRecord + r;
+    __shared__ Reach s_reach[16];
+    float delta = 0.f, lse2 = INFINITY;
+    int lo, hi;
+    seen_by(P, b, i, lo, hi);
+    const bool few = hi && hi - lo <= kFewKeys;
+    if (hi) {
+        lse2 = P.lse[((int64_t)b * P.n_q + h) * P.sq + i] * kLog2e;
+        if (!few) delta = dot_share<T>(row_of<T>(P.o_in, P.o_stride, b, i, h), row_of<T>(P.dout, P.dout_stride, b, i, h), P.head_dim, part);
+    }
+    delta = sum_of_8(delta);
+    if (__any_sync(~0u, few)) {
+        const int n = few ? hi - lo : 0;
+        for (int j = 0; j < kFewKeys; ++j) {
+            float s = 0.f, dp = 0.f;
+            if (j < n) {
+                s = dot_share<T>(row_of<T>(P.q, P.q_stride, b, i, h), row_of<T>(P.k, P.k_stride, b, lo + j, h / P.group), P.head_dim, part);
+                dp = dot_share<T>(row_of<T>(P.dout, P.dout_stride, b, i, h), row_of<T>(P.v, P.v_stride, b, lo + j, h / P.group), P.head_dim, part);
+            }
+            s = sum_of_8(s), dp = sum_of_8(dp);
+            if (j < n) delta = fmaf(fast_exp2(fmaf(s, P.scale2, -lse2)), dp, delta);
+        }
+    }
+    Record* R = P.record + ((int64_t)b * P.n_q + h) * P.records + rec;
+    if (part == 0) {
+        R->lse2[r] = lse2;
+        R->delta[r] = delta;
+        R->lo[r] = lo;
+        R->hi[r] = hi;
+    }
+    if (h == 0) {
+        Reach a{lo, hi, lo, hi ? hi : 0};
+        if (i >= P.sq) a.max_lo = 0, a.min_hi = INT_MAX;  // rows past the end are zeros and need no mask
+#pragma unroll
+        for (int s = 16; s >= 8; s >>= 1) {
+            a.min_lo = min(a.min_lo, __shfl_xor_sync(~0u, a.min_lo, s));
+            a.max_hi = max(a.max_hi, __shfl_xor_sync(~0u, a.max_hi, s));
+            a.max_lo = max(a.max_lo, __shfl_xor_sync(~0u, a.max_lo, s));
+            a.min_hi = min(a.min_hi, __shfl_xor_sync(~0u, a.min_hi, s));
+        }
+        if ((threadIdx.x & 31) == 0) s_reach[threadIdx.x >> 5] = a;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < 16; ++w) {
+                a.min_lo = min(a.min_lo, s_reach[w].min_lo);
+                a.max_hi = max(a.max_hi, s_reach[w].max_hi);
+                a.max_lo = max(a.max_lo, s_reach[w].max_lo);
+                a.min_hi = min(a.min_hi, s_reach[w].min_hi);
+            }
+            P.reach[(int64_t)b * P.records + rec] = a;
+        }
+    }
+}
+
+// dK and dV of 128 keys.  kSlots sets of 4 warps take the query tiles in turn, each with its own S^T and dP^T.
+template <int DP, int kSlots> struct Keys {
+    static constexpr int kTileK = 128 * DP * 2, kTileQ = 64 * DP * 2;
+    static constexpr int kStages = DP == 64 ? 3 : 3;
+    static constexpr int kStageBytes = 2 * kTileQ + 1024;
+    static constexpr int kSmem = 1024 + 2 * kTileK + kStages * kStageBytes;
+    static constexpr int kColDV = kSlots * 128, kColDK = kColDV + DP, kColumns = kColDK + DP <= 256 ? 256 : 512;
+    static constexpr int kThreads = kSlots * 128 + 64;
+    static constexpr int kPerSM = kColumns == 256 ? 2 : 1;
+    static_assert(kColDK + DP <= 512, "tensor memory");
+};
+
+template <typename T, int DP, int kSlots>
+__global__ void __launch_bounds__(Keys<DP, kSlots>::kThreads, Keys<DP, kSlots>::kPerSM)
+attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do) {
+    using F = Keys<DP, kSlots>;
+    extern __shared__ char smem_raw[];
+    char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    char* tile_k = smem;
+    char* tile_v = smem + F::kTileK;
+    char* stages = smem + 2 * F::kTileK;  // each: Q, dO, record
+    __shared__ uint64_t bars[2 + 2 * F::kStages + 2 * kSlots];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_gave_up, s_first, s_end;
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t kv_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kCopyWarp = 4 * kSlots, kMmaWarp = kCopyWarp + 1;
+
+    const int n_kv = P.n_q / P.group, heads = P.batch * n_kv;
+    const int tile = blockIdx.x / heads, bh = blockIdx.x % heads, b = bh / n_kv, hk = bh % n_kv;  // under a causal mask the first keys have the most queries
+    const int key0 = tile * 128;
+
+    if (threadIdx.x == 0) {
+        bar_init(kv_full, 1), bar_init(done, 1);
+        for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
+        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 128);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_gave_up = 0, s_first = INT_MAX, s_end = 0;
+    }
+    if (warp == kMmaWarp) tmem_alloc<F::kColumns>(smem_u32(&s_tmem));
+    __syncthreads();
+    const Reach* reach = P.reach + (int64_t)b * P.records;
+    int begin = INT_MAX, end = 0;
+    for (int r = threadIdx.x; r < P.records; r += F::kThreads) {
+        const Reach a = reach[r];
+        if (a.min_lo < key0 + 128 && a.max_hi > key0) begin = min(begin, r), end = max(end, r + 1);
+    }
+    if (end) atomicMin(&s_first, begin), atomicMax(&s_end, end);
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = s_tmem;
+    const int first = s_first, per_head = s_end ? s_end - first : 0, n = per_head * P.group;
+    const Waits W{&s_gave_up, P.fault};
+
+    if (warp == kCopyWarp) {
+        if (lane == 0 && n) {
+            bar_expect(kv_full, 2 * F::kTileK);
+            for (int d = 0; d < DP / 64; ++d) {
+                tma_load(smem_u32(tile_k) + d * 128 * 128, &map_k, kv_full, d * 64, key0, hk, b);
+                tma_load(smem_u32(tile_v) + d * 128 * 128, &map_v, kv_full, d * 64, key0, hk, b);
+            }
+            int it = 0;
+            for (int g = 0; g < P.group && it < n; ++g) {
+                const int h = hk * P.group + g;
+                const Record* records = P.record + ((int64_t)b * P.n_q + h) * P.records;
+                int r = 0;
+                for (; r < per_head; ++r, ++it) {
+                    const int s = it % F::kStages, use = it / F::kStages;
+                    if (use && !W.wait(free_ + 8 * s, (use - 1) & 1)) break;
+                    const uint32_t at = smem_u32(stages) + s * F::kStageBytes, bar = full + 8 * s;
+                    bar_expect(bar, F::kStageBytes);
+                    for (int d = 0; d < DP / 64; ++d) {
+                        tma_load(at + d * 64 * 128, &map_q, bar, d * 64, (first + r) * 64, h, b);
+                        tma_load(at + F::kTileQ + d * 64 * 128, &map_do, bar, d * 64, (first + r) * 64, h, b);
+                    }
+                    bulk_load(at + 2 * F::kTileQ, records + first + r, 1024, bar);
+                }
+                if (r < per_head) break;
+            }
+            if (it < n) {
+                W.drain(kv_full, 0);
+                for (int i = it > F::kStages ? it - F::kStages : 0; i < it; ++i) W.drain(full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        if (lane == 0 && n) {
+            const auto scores = [&](int it) -> bool {
+                const int s = it % F::kStages;
+                if (!W.wait(full + 8 * s, (it / F::kStages) & 1)) return false;
+                tc_after_sync();
+                const uint32_t q = smem_u32(stages) + s * F::kStageBytes, at = tmem + (it % kSlots) * 128;
+                product_ss<T, 64, DP>(at, smem_u32(tile_k), 128, q, 64);
+                product_ss<T, 64, DP>(at + 64, smem_u32(tile_v), 128, q + F::kTileQ, 64);
+                mma_commit(s_full + 8 * (it % kSlots));
+                return true;
+            };
+            bool ok = W.wait(kv_full, 0);
+            for (int it = 0; ok && it < kSlots && it < n; ++it) ok = scores(it);
+            for (int it = 0; ok && it < n; ++it) {
+                const int s = it % F::kStages, slot = it % kSlots;
+                if (!(ok = W.wait(ds_full + 8 * slot, (it / kSlots) & 1))) break;
+                tc_after_sync();
+                const uint32_t q = smem_u32(stages) + s * F::kStageBytes, at = tmem + slot * 128;
+                product_ts<T, DP, 64>(tmem + F::kColDV, at, q + F::kTileQ, it > 0);
+                product_ts<T, DP, 64>(tmem + F::kColDK, at + 64, q, it > 0);
+                mma_commit(free_ + 8 * s);
+                if (it + kSlots < n) ok = scores(it + kSlots);
+            }
+            mma_commit(done);
+            if (!ok) W.drain(done, 0);
+        }
+    } else {
+        const int slot = warp >> 2, row = threadIdx.x & 127, key = key0 + row;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128;
+        bool ok = true;
+        for (int it = slot; it < n; it += kSlots) {
+            const int s = it % F::kStages, rec = first + it % per_head;
+            const Reach a = reach[rec];
+            if (!(ok = W.wait_warp(full + 8 * s, (it / F::kStages) & 1) && W.wait_warp(s_full + 8 * slot, (it / kSlots) & 1))) break;
+            tc_after_sync();
+            char* stage = stages + s * F::kStageBytes;
+            const Record& R = *reinterpret_cast<const Record*>(stage + 2 * F::kTileQ);
+            uint32_t x[64], y[64];
+            tmem_load32(x, at);
+            tmem_load32(x + 32, at + 32);
+            tmem_load32(y, at + 64);
+            tmem_load32(y + 32, at + 96);
+            tmem_wait_loads();
+            const bool masked = a.max_lo > key0 || a.min_hi < key0 + 128;
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                const float4 lse = *reinterpret_cast<const float4*>(R.lse2 + c), delta = *reinterpret_cast<const float4*>(R.delta + c);
+                const float ls[4] = {lse.x, lse.y, lse.z, lse.w}, de[4] = {delta.x, delta.y, delta.z, delta.w};
+                float p[4], ds[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = fast_exp2(fmaf(__uint_as_float(x[c + e]), P.scale2, -ls[e]));
+                    ds[e] = p[e] * (__uint_as_float(y[c + e]) - de[e]);
+                }
+                if (masked) {
+                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + c), hi = *reinterpret_cast<const int4*>(R.hi + c);
+                    const int los[4] = {lo.x, lo.y, lo.z, lo.w}, his[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (key < los[e] || key >= his[e]) p[e] = ds[e] = 0.f;
+                        if (his[e] - los[e] == 1) ds[e] = 0.f;  // a softmax of one term is constant
+                    }
+                }
+                x[c / 2] = pack2<T>(p[0], p[1]);
+                x[c / 2 + 1] = pack2<T>(p[2], p[3]);
+                y[c / 2] = pack2<T>(ds[0], ds[1]);
+                y[c / 2 + 1] = pack2<T>(ds[2], ds[3]);
+            }
+            tmem_store32(at, x);
+            tmem_store32(at + 64, y);
+            tmem_wait_stores();
+            if (a.max_lo == INT_MAX) {  // a query that sees nothing may hold anything
+                if (row < 64 ? R.hi[row] == 0 : R.hi[row - 64] == 0) clear_row<DP>(stage + (row < 64 ? 0 : F::kTileQ), 64, row & 63);
+                fence_async_shared();
+            }
+            tc_before_sync();
+            bar_arrive(ds_full + 8 * slot);
+        }
+        if (ok && n) ok = W.wait_warp(done, 0);
+        tc_after_sync();
+        if (ok && slot == 0) {
+#pragma unroll
+            for (int what = 0; what < 2; ++what) {
+                const float f = what ? P.scale : 1.f;
+                const int64_t* st = what ? P.dk_stride : P.dv_stride;
+#pragma unroll
+                for (int c = 0; c < DP / 32; ++c) {
+                    uint32_t o[32];
+                    if (n) {
+                        tmem_load32(o, lanes + (what ? F::kColDK : F::kColDV) + 32 * c);
+                        tmem_wait_loads();
+                    }
+                    if (key < P.sk) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = n ? pack2<T>(__uint_as_float(o[2 * e]) * f, __uint_as_float(o[2 * e + 1]) * f) : 0u;
+                        store_row<T>(what ? P.dk : P.dv, b * st[0] + key * st[1] + hk * st[2], P.head_dim, o, 32 * c);
+                    }
+                }
+            }
+        }
+    }
+    tc_before_sync();
+    __syncthreads();
+    if (warp == kMmaWarp) tmem_free<F::kColumns>(tmem);
+}
+
+// dQ of 128 queries.  kSlots sets of 4 warps take the key tiles in turn.
+template <int DP, int kSlots> struct Queries {
+    static constexpr int kTileQ = 128 * DP * 2, kTileK = 64 * DP * 2;
+    static constexpr int kColDQ = kSlots * 128, kColumns = kColDQ + DP <= 256 ? 256 : 512;
+    static constexpr int kPerSM = kColumns == 256 ? 2 : 1;
+    static constexpr int kStages = DP == 64 ? 3 : kPerSM == 2 ? 1 : 4;
+    static constexpr int kSmem = 1024 + 2 * kTileQ + 2 * kStages * kTileK;
+    static constexpr int kThreads = kSlots * 128 + 64;
+    static_assert(kColDQ + DP <= 512, "tensor memory");
+};
+
+template <typename T, int DP, int kSlots>
+__global__ void __launch_bounds__(Queries<DP, kSlots>::kThreads, Queries<DP, kSlots>::kPerSM)
+attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                         const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do) {
+    using F = Queries<DP, kSlots>;
+    extern __shared__ char smem_raw[];
+    char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    char* tile_q = smem;
+    char* tile_do = smem + F::kTileQ;
+    char* stages = smem + 2 * F::kTileQ;  // each: K, V
+    __shared__ uint64_t bars[2 + 2 * F::kStages + 2 * kSlots];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_gave_up, s_lo[4], s_hi[4];
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kCopyWarp = 4 * kSlots, kMmaWarp = kCopyWarp + 1;
+    const int heads = P.batch * P.n_q;
+    const int tile = P.causal ? P.q_tiles - 1 - (int)(blockIdx.x / heads) : (int)(blockIdx.x / heads);
+    const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
+
+    if (threadIdx.x == 0) {
+        bar_init(q_full, 1), bar_init(done, 1);
+        for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
+        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 128);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_gave_up = 0;
+    }
+    if (warp == kMmaWarp) tmem_alloc<F::kColumns>(smem_u32(&s_tmem));
+    const int row = threadIdx.x & 127, i = tile * 128 + row;
+    int lo = INT_MAX, hi = 0;
+    float lse2 = INFINITY, delta = 0.f;
+    if (warp < 4 * kSlots) {
+        if (i < P.sq) {
+            const Record& R = P.record[((int64_t)b * P.n_q + h) * P.records + i / kRecord];
+            lse2 = R.lse2[i % kRecord], delta = R.delta[i % kRecord], lo = R.lo[i % kRecord], hi = R.hi[i % kRecord];
+        }
+        int l = lo, g = hi;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) l = min(l, __shfl_xor_sync(~0u, l, o)), g = max(g, __shfl_xor_sync(~0u, g, o));
+        if (lane == 0 && warp < 4) s_lo[warp] = l, s_hi[warp] = g;
+    }
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = s_tmem;
+    const int min_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), max_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
+    const int first = max_hi ? min_lo / 64 : 0, n = max_hi ? (max_hi + 63) / 64 - first : 0;
+    const Waits W{&s_gave_up, P.fault};
+
+    if (warp == kCopyWarp) {
+        if (lane == 0 && n) {
+            bar_expect(q_full, 2 * F::kTileQ);
+            for (int d = 0; d < DP / 64; ++d) {
+                tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
+                tma_load(smem_u32(tile_do) + d * 128 * 128, &map_do, q_full, d * 64, tile * 128, h, b);
+            }
+            int j = 0;
+            for (; j < n; ++j) {
+                const int s = j % F::kStages, use = j / F::kStages;
+                if (use && !W.wait(free_ + 8 * s, (use - 1) & 1)) break;
+                const uint32_t at = smem_u32(stages) + s * 2 * F::kTileK, bar = full + 8 * s;
+                bar_expect(bar, 2 * F::kTileK);
+                for (int d = 0; d < DP / 64; ++d) {
+                    tma_load(at + d * 64 * 128, &map_k, bar, d * 64, (first + j) * 64, hk, b);
+                    tma_load(at + F::kTileK + d * 64 * 128, &map_v, bar, d * 64, (first + j) * 64, hk, b);
+                }
+            }
+            if (j < n) {
+                W.drain(q_full, 0);
+                for (int k = j > F::kStages ? j - F::kStages : 0; k < j; ++k) W.drain(full + 8 * (k % F::kStages), (k / F::kStages) & 1);
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        if (lane == 0 && n) {
+            const auto scores = [&](int j) -> bool {
+                const int s = j % F::kStages;
+                if (!W.wait(full + 8 * s, (j / F::kStages) & 1)) return false;
+                tc_after_sync();
+                const uint32_t k = smem_u32(stages) + s * 2 * F::kTileK, at = tmem + (j % kSlots) * 128;
+                product_ss<T, 64, DP>(at, smem_u32(tile_q), 128, k, 64);
+                product_ss<T, 64, DP>(at + 64, smem_u32(tile_do), 128, k + F::kTileK, 64);
+                mma_commit(s_full + 8 * (j % kSlots));
+                return true;
+            };
+            bool ok = W.wait(q_full, 0);
+            for (int j = 0; ok && j < kSlots && j < n; ++j) ok = scores(j);
+            for (int j = 0; ok && j < n; ++j) {
+                const int s = j % F::kStages, slot = j % kSlots;
+                if (!(ok = W.wait(ds_full + 8 * slot, (j / kSlots) & 1))) break;
+                tc_after_sync();
+                product_ts<T, DP, 64>(tmem + F::kColDQ, tmem + slot * 128 + 64, smem_u32(stages) + s * 2 * F::kTileK, j > 0);
+                mma_commit(free_ + 8 * s);
+                if (j + kSlots < n) ok = scores(j + kSlots);
+            }
+            mma_commit(done);
+            if (!ok) W.drain(done, 0);
+        }
+    } else {
+        const int slot = warp >> 2;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128;
+        bool ok = true;
+        for (int j = slot; j < n; j += kSlots) {
+            const int s = j % F::kStages, key0 = (first + j) * 64;
+            if (!(ok = W.wait_warp(s_full + 8 * slot, (j / kSlots) & 1))) break;
+            tc_after_sync();
+            uint32_t x[64], y[64];
+            tmem_load32(x, at);
+            tmem_load32(x + 32, at + 32);
+            tmem_load32(y, at + 64);
+            tmem_load32(y + 32, at + 96);
+            tmem_wait_loads();
+            const bool masked = !__all_sync(~0u, lo <= key0 && hi >= key0 + 64);
+#pragma unroll
+            for (int c = 0; c < 64; c += 2) {
+                float ds[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float p = fast_exp2(fmaf(__uint_as_float(x[c + e]), P.scale2, -lse2));
+                    ds[e] = p * (__uint_as_float(y[c + e]) - delta);
+                    if (masked && (key0 + c + e < lo || key0 + c + e >= hi || hi - lo == 1)) ds[e] = 0.f;  // a softmax of one term is constant
+                }
+                y[c / 2] = pack2<T>(ds[0], ds[1]);
+            }
+            tmem_store32(at + 64, y);
+            tmem_wait_stores();
+            if (key0 < min_lo || (key0 + 64 > max_hi && max_hi < P.sk)) {
+                // the copy's writes become visible through its own barrier
+                if (!(ok = W.wait_warp(full + 8 * s, (j / F::kStages) & 1))) break;
+                if (row < 64 && (key0 + row < min_lo || key0 + row >= max_hi)) clear_row<DP>(stages + s * 2 * F::kTileK, 64, row);
+                fence_async_shared();
+            }
+            tc_before_sync();
+            bar_arrive(ds_full + 8 * slot);
+        }
+        if (ok && n) ok = W.wait_warp(done, 0);
+        tc_after_sync();
+        if (ok && slot == 0) {
+#pragma unroll
+            for (int c = 0; c < DP / 32; ++c) {
+                uint32_t o[32];
+                if (n) {
+                    tmem_load32(o, lanes + F::kColDQ + 32 * c);
+                    tmem_wait_loads();
+                }
+                if (i < P.sq) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = hi ? pack2<T>(__uint_as_float(o[2 * e]) * P.scale, __uint_as_float(o[2 * e + 1]) * P.scale) : 0u;
+                    store_row<T>(P.dq, b * P.dq_stride[0] + i * P.dq_stride[1] + h * P.dq_stride[2], P.head_dim, o, 32 * c);
+                }
+            }
+        }
+    }
+    tc_before_sync();
+    __syncthreads();
+    if (warp == kMmaWarp) tmem_free<F::kColumns>(tmem);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                            const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {
+    static Encode f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<Encode>(p);
+    }();
+    return f;
+}
+
+bool usable(const void* p, const int64_t* stride, const int64_t* size, uint32_t d) {
+    if ((uintptr_t)p % 16) return false;
+    for (int i = 0; i < 3; ++i)
+        if (size[i] > 1 && (stride[i] % 8 || stride[i] < d || stride[i] >= (1ll << 38))) return false;
+    return true;
+}
+
+// [batch, s, heads, head_dim] by boxes of `rows` tokens and 64 elements; what lies outside reads as zero.
+int make_map(CUtensorMap* map, const halos_attention_args* a, const void* p, int64_t s, int64_t heads, const int64_t* stride, int rows) {
+    const cuuint64_t dims[4] = {a->head_dim, (cuuint64_t)s, (cuuint64_t)heads, (cuuint64_t)a->batch};
+    const auto bytes = [&](int64_t n, int64_t st) { return (cuuint64_t)(n > 1 ? st * 2 : a->head_dim * 2); };  // of a dimension of 1 it is never used
+    const cuuint64_t strides[3] = {bytes(s, stride[1]), bytes(heads, stride[2]), bytes(a->batch, stride[0])};
+    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, ones[4] = {1, 1, 1, 1};
+    Encode f = encoder();
+    if (!f) return fail(HALOS_ERR_CUDA, "attention: the driver has no tensor maps");
+    const CUresult r = f(map, a->dtype == HALOS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(p), dims, strides, box, ones,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? HALOS_OK : fail(HALOS_ERR_UNSUPPORTED, "attention: a tensor that no tensor map describes");
+}
+
+int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+int check(const halos_attention_args* a, bool back) {
+    if (!a || a->struct_size != sizeof(halos_attention_args)) return fail(HALOS_ERR_INVALID_ARG, "attention: args missing or of another size");
+    if (!is_type(a->dtype)) return fail(HALOS_ERR_INVALID_ARG, "attention: dtype");
+    if (a->dtype == HALOS_F32) return fail(HALOS_ERR_UNSUPPORTED, "attention: 16-bit types only");
+    if (a->batch < 0 || a->sq < 0 || a->sk < 0) return fail(HALOS_ERR_INVALID_ARG, "attention: negative size");
+    if (a->n_q == 0 || a->n_kv == 0 || a->n_q % a->n_kv) return fail(HALOS_ERR_INVALID_ARG, "attention: query heads must be a multiple of key heads");
+    if (a->head_dim == 0 || a->head_dim % 8 || a->head_dim > 128) return fail(HALOS_ERR_UNSUPPORTED, "attention: head_dim must be a multiple of 8, at most 128");
+    if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return fail(HALOS_ERR_INVALID_ARG, "attention: scale must be positive");
+    if (a->sq > (1 << 30) || a->sk > (1 << 30) || a->batch > 65535 || a->n_q > 65535) return fail(HALOS_ERR_UNSUPPORTED, "attention: over 2^30 tokens, 65535 heads or sequences");
+    const int64_t tiles = (a->sq > a->sk ? a->sq : a->sk) / 128 + 1;
+    if (tiles * a->batch * a->n_q > 0x7fffffffll) return fail(HALOS_ERR_UNSUPPORTED, "attention: too many tiles");
+    if (a->batch == 0 || (a->sq == 0 && (!back || a->sk == 0))) return HALOS_OK;
+    if ((a->sq && (!a->q || !a->o || !a->lse)) || (a->sk && (!a->k || !a->v))) return fail(HALOS_ERR_INVALID_ARG, "attention: null pointer");
+    if (back && ((a->sq && (!a->dout || !a->dq)) || (a->sk && (!a->dk || !a->dv)))) return fail(HALOS_ERR_INVALID_ARG, "attention: null pointer");
+    const int64_t q_size[3] = {a->batch, a->sq, a->n_q}, k_size[3] = {a->batch, a->sk, a->n_kv};
+    bool ok = a->sq == 0 || (usable(a->q, a->q_stride, q_size, a->head_dim) && usable(a->o, a->o_stride, q_size, a->head_dim));
+    ok = ok && (a->sk == 0 || (usable(a->k, a->k_stride, k_size, a->head_dim) && usable(a->v, a->v_stride, k_size, a->head_dim)));
+    if (back) {
+        ok = ok && (a->sq == 0 || (usable(a->dout, a->dout_stride, q_size, a->head_dim) && usable(a->dq, a->dq_stride, q_size, a->head_dim)));
+        ok = ok && (a->sk == 0 || (usable(a->dk, a->dk_stride, k_size, a->head_dim) && usable(a->dv, a->dv_stride, k_size, a->head_dim)));
+    }
+    if (!ok) return fail(HALOS_ERR_UNSUPPORTED, "attention: bases and strides must be multiples of 16 bytes and rows apart");
+    return HALOS_OK;
+}
+
+int params(const halos_attention_args* a, AttentionParams& P) {
+    P.sq = (int)a->sq, P.sk = (int)a->sk, P.head_dim = a->head_dim, P.n_q = a->n_q, P.group = a->n_q / a->n_kv, P.batch = (int)a->batch;
+    P.causal = a->causal != 0, P.q_tiles = (P.sq + 127) / 128, P.k_tiles = (P.sk + 127) / 128, P.records = (int)(round_up(a->sq, 128) / kRecord);
+    P.scale = a->scale, P.scale2 = a->scale * kLog2e, P.doc_start = a->doc_start, P.lens = a->lens;
+    P.q = (const char*)a->q, P.k = (const char*)a->k, P.v = (const char*)a->v;
+    P.o_in = P.o = (char*)a->o, P.dout = (const char*)a->dout, P.dq = (char*)a->dq, P.dk = (char*)a->dk, P.dv = (char*)a->dv, P.lse = a->lse;
+    for (int i = 0; i < 3; ++i)
+        P.q_stride[i] = a->q_stride[i], P.k_stride[i] = a->k_stride[i], P.v_stride[i] = a->v_stride[i], P.o_stride[i] = a->o_stride[i], P.dout_stride[i] = a->dout_stride[i], P.dq_stride[i] = a->dq_stride[i], P.dk_stride[i] = a->dk_stride[i], P.dv_stride[i] = a->dv_stride[i];
+    return cuda_status(cudaGetSymbolAddress((void**)&P.fault, g_fault), "attention: fault mark");
+}
+
+template <typename K>
+int allow_smem(K* kernel, int bytes) {
+    return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes), "attention: shared memory");
+}
+
+template <typename T, int DP>
+int forward(const halos_attention_args* a) {
+    using F = Forward<DP>;
+    AttentionParams P{};
+    if (int rc = params(a, P)) return rc;
+    CUtensorMap q, k{}, v{};
+    if (int rc = make_map(&q, a, a->q, a->sq, a->n_q, a->q_stride, 128)) return rc;
+    if (a->sk) {
+        if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, 128)) return rc;
+        if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, 128)) return rc;
+    }
+    if (int rc = allow_smem(attention_fwd_kernel<T, DP>, F::kSmem)) return rc;
+    attention_fwd_kernel<T, DP><<<P.q_tiles * P.batch * P.n_q, F::kThreads, F::kSmem, (cudaStream_t)a->stream>>>(P, q, k, v);
+    return cuda_status(cudaGetLastError(), "attention launch");
+}
+
+uint64_t workspace(const halos_attention_args* a) {
+    const uint64_t records = (uint64_t)(round_up(a->sq, 128) / kRecord);
+    return a->batch * records * (a->n_q * sizeof(Record) + sizeof(Reach));
+}
+
+template <typename T, int DP, int kKeySlots, int kQuerySlots>
+int backward(const halos_attention_args* a) {
+    AttentionParams P{};
+    if (int rc = params(a, P)) return rc;
+    P.record = (Record*)a->workspace;
+    P.reach = (Reach*)(P.record + (int64_t)P.batch * P.n_q * P.records);
+    cudaStream_t st = (cudaStream_t)a->stream;
+    CUtensorMap q{}, d{}, k{}, v{};
+    using K = Keys<DP, kKeySlots>;
+    using Q = Queries<DP, kQuerySlots>;
+    if (int rc = allow_smem(attention_keys_kernel<T, DP, kKeySlots>, K::kSmem)) return rc;
+    if (int rc = allow_smem(attention_queries_kernel<T, DP, kQuerySlots>, Q::kSmem)) return rc;
+    if (P.sq) {
+        attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 512, 0, st>>>(P);
+        if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
+    }
+    if (P.sk) {
+        if (P.sq) {
+            if (int rc = make_map(&q, a, a->q, a->sq, a->n_q, a->q_stride, 64)) return rc;
+            if (int rc = make_map(&d, a, a->dout, a->sq, a->n_q, a->dout_stride, 64)) return rc;
+        }
+        if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, 128)) return rc;
+        if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, 128)) return rc;
+        attention_keys_kernel<T, DP, kKeySlots><<<P.k_tiles * P.batch * (int)a->n_kv, K::kThreads, K::kSmem, st>>>(P, q, k, v, d);
+        if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
+    }
+    if (P.sq) {
+        if (P.sk) {
+            if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, 64)) return rc;
+            if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, 64)) return rc;
+        }
+        if (int rc = make_map(&q, a, a->q, a->sq, a->n_q, a->q_stride, 128)) return rc;
+        if (int rc = make_map(&d, a, a->dout, a->sq, a->n_q, a->dout_stride, 128)) return rc;
+        attention_queries_kernel<T, DP, kQuerySlots><<<P.q_tiles * P.batch * P.n_q, Q::kThreads, Q::kSmem, st>>>(P, q, k, v, d);
+        if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
+    }
+    return HALOS_OK;
+}
+
+}  // namespace
+}  // namespace halos_step
+
+extern "C" int halos_attention_fwd(const halos_attention_args* a) {
+    using namespace halos_step;
+    if (int rc = check(a, false)) return rc;
+    if (a->batch == 0 || a->sq == 0) return HALOS_OK;
+    if (int rc = enter(a->device)) return rc;
+    if (a->dtype == HALOS_BF16) return a->head_dim <= 64 ? forward<__nv_bfloat16, 64>(a) : forward<__nv_bfloat16, 128>(a);
+    return a->head_dim <= 64 ? forward<__half, 64>(a) : forward<__half, 128>(a);
+}
+
+extern "C" int halos_attention_workspace(const halos_attention_args* a, uint64_t* bytes) {
+    using namespace halos_step;
+    if (!a || a->struct_size != sizeof(halos_attention_args) || !bytes || a->batch < 0 || a->sq < 0)
+        return fail(HALOS_ERR_INVALID_ARG, "attention: args missing or of another size");
+    *bytes = workspace(a);
+    return HALOS_OK;
+}
+
+extern "C" int halos_attention_bwd(const halos_attention_args* a) {
+    using namespace halos_step;
+    if (int rc = check(a, true)) return rc;
+    if (a->batch == 0 || (a->sq == 0 && a->sk == 0)) return HALOS_OK;
+    if (workspace(a) && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < workspace(a)))
+        return fail(HALOS_ERR_INVALID_ARG, "attention: workspace missing, unaligned or too small");
+    if (int rc = enter(a->device)) return rc;
+    if (a->dtype == HALOS_BF16) return a->head_dim <= 64 ? backward<__nv_bfloat16, 64, 1, 1>(a) : backward<__nv_bfloat16, 128, 2, 3>(a);
+    return a->head_dim <= 64 ? backward<__half, 64, 1, 1>(a) : backward<__half, 128, 2, 3>(a);
+}
+
+extern "C" int halos_step_fault(int32_t device, int32_t* fault) {
+    using namespace halos_step;
+    if (!fault) return fail(HALOS_ERR_INVALID_ARG, "fault: null pointer");
+    if (int rc = enter(device)) return rc;
+    return cuda_status(cudaMemcpyFromSymbol(fault, g_fault, sizeof(int)), "fault mark");
+}
