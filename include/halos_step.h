@@ -34,7 +34,7 @@ enum { HALOS_F16 = 2 };  /* beside HALOS_F32 and HALOS_BF16 of halos.h */
 
 const char* halos_step_error(void);
 
-/* Device-side waits of the attention kernels are bounded.  One that ran out (it never does unless the GPU lost work)
+/* Device-side waits of these kernels are bounded.  One that ran out (it never does unless the GPU lost work)
  * leaves its outputs undefined and a mark here: *fault = 0 if none has since the library was loaded.  Waits for the device. */
 int halos_step_fault(int32_t device, int32_t* fault);
 

@@ -49,8 +49,6 @@ struct AttentionParams {
     int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3], dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];  // in elements
 };
 
-__device__ int g_fault;
-
 // The keys [lo, hi) that query i of batch row b sees; lo = INT_MAX, hi = 0 if none.
 __device__ __forceinline__ void seen_by(const AttentionParams& P, int b, int i, int& lo, int& hi) {
     lo = INT_MAX, hi = 0;
@@ -813,12 +811,7 @@ int params(const halos_attention_args* a, AttentionParams& P) {
     P.o_in = P.o = (char*)a->o, P.dout = (const char*)a->dout, P.dq = (char*)a->dq, P.dk = (char*)a->dk, P.dv = (char*)a->dv, P.lse = a->lse;
     for (int i = 0; i < 3; ++i)
         P.q_stride[i] = a->q_stride[i], P.k_stride[i] = a->k_stride[i], P.v_stride[i] = a->v_stride[i], P.o_stride[i] = a->o_stride[i], P.dout_stride[i] = a->dout_stride[i], P.dq_stride[i] = a->dq_stride[i], P.dk_stride[i] = a->dk_stride[i], P.dv_stride[i] = a->dv_stride[i];
-    return cuda_status(cudaGetSymbolAddress((void**)&P.fault, g_fault), "attention: fault mark");
-}
-
-template <typename K>
-int allow_smem(K* kernel, int bytes) {
-    return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes), "attention: shared memory");
+    return fault_mark(&P.fault);
 }
 
 template <typename T, int DP>
@@ -910,11 +903,4 @@ extern "C" int halos_attention_bwd(const halos_attention_args* a) {
     if (int rc = enter(a->device)) return rc;
     if (a->dtype == HALOS_BF16) return a->head_dim <= 64 ? backward<__nv_bfloat16, 64, 1, 1>(a) : backward<__nv_bfloat16, 128, 2, 3>(a);
     return a->head_dim <= 64 ? backward<__half, 64, 1, 1>(a) : backward<__half, 128, 2, 3>(a);
-}
-
-extern "C" int halos_step_fault(int32_t device, int32_t* fault) {
-    using namespace halos_step;
-    if (!fault) return fail(HALOS_ERR_INVALID_ARG, "fault: null pointer");
-    if (int rc = enter(device)) return rc;
-    return cuda_status(cudaMemcpyFromSymbol(fault, g_fault, sizeof(int)), "fault mark");
 }

@@ -9,6 +9,7 @@ namespace {
 constexpr int kMaxDevices = 64;
 thread_local char t_error[256] = "";
 std::atomic<int> g_sms[kMaxDevices];
+__device__ int g_fault;
 }  // namespace
 
 int fail(int status, const char* text) {
@@ -34,8 +35,17 @@ int enter(int32_t device) {
     return HALOS_OK;
 }
 
+int fault_mark(int** mark) { return cuda_status(cudaGetSymbolAddress((void**)mark, g_fault), "fault mark"); }
+
 int sm_count(int32_t device) { return g_sms[device].load(std::memory_order_relaxed); }
 
 }  // namespace halos_step
 
 extern "C" const char* halos_step_error(void) { return halos_step::t_error; }
+
+extern "C" int halos_step_fault(int32_t device, int32_t* fault) {
+    using namespace halos_step;
+    if (!fault) return fail(HALOS_ERR_INVALID_ARG, "fault: null pointer");
+    if (int rc = enter(device)) return rc;
+    return cuda_status(cudaMemcpyFromSymbol(fault, g_fault, sizeof(int)), "fault mark");
+}

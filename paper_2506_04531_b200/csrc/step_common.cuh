@@ -13,6 +13,13 @@ int fail(int status, const char* text);                 // sets the thread's err
 int cuda_status(cudaError_t e, const char* where);      // HALOS_OK, or fail(HALOS_ERR_CUDA, ...)
 int enter(int32_t device);                              // makes the device current
 int sm_count(int32_t device);                           // of a device that enter() accepted
+int fault_mark(int** mark);                             // where the current device's kernels say that a wait ran out
+
+constexpr int kSharedPerSM = 228 * 1024;
+template <typename K>
+int allow_smem(K* kernel, int bytes) {
+    return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes), "shared memory");
+}
 
 inline bool is_type(uint32_t t) { return t == HALOS_F32 || t == HALOS_BF16 || t == HALOS_F16; }
 

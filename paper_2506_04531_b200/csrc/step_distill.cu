@@ -7,7 +7,7 @@
 //
 // Statistics are kept online: a thread holds the largest logit it has seen and the two sums relative to it, and
 // rescales them when a larger one comes up, which after the first few vectors is rare.
-#include "step_common.cuh"
+#include "step_tcgen05.cuh"
 
 namespace halos_step {
 namespace {
@@ -283,15 +283,417 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
     }
 }
 
+
+// ------------------------------------------------------------------------------------------------ rows held in registers
+
+// A CTA of kThreads + 32 (a multiple of four warps: registers are given out by that) walks rows.  Its last warp is one or two rows ahead of the others: it has the row copied into shared memory in
+// bulk and works out the teacher's side of it.  The others take the row from there into registers (kVectors of 16 bytes a
+// thread), which frees the buffer for the next copy, and go over the registers twice: once for the statistics, once
+// for the gradient, which they store from there.  So the logits cross HBM once, and copying, exponentials and storing overlap.
+// A wait that runs out is marked and ends every later one at once; the loops and their barriers still run to the end.
+template <int kThreads, int kVectors> struct Held {
+    static constexpr int kWarps = kThreads / 32, kBytes = kThreads * kVectors * 16;
+    static constexpr int kPerSM = kThreads == 32 ? 12 : kThreads == 96 ? 5 : kThreads == 224 ? 2 : 1;
+};
+
+struct Slot {  // what the last warp says of a row beside the entries themselves
+    float plogp, pz, label_z, lse1, lseT, g;
+    int label, ignored, bad, any;
+};
+
+// Splits a row at the 16-byte boundaries: elements [0, head) and [tail, V) singly, `vectors` whole vectors between.
+template <typename T> struct Cut {
+    int head, vectors, tail, singles;
+    __device__ __forceinline__ Cut(const T* z, int V) {
+        constexpr int N = 16 / sizeof(T);
+        head = (int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(T);
+        if (head > V) head = V;
+        vectors = (V - head) / N;
+        tail = head + vectors * N;
+        singles = head + V - tail;
+    }
+    __device__ __forceinline__ int single(int i) const { return i < head ? i : i - head + tail; }
+};
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<uint64_t&>(r))
+        : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+    return r;
+}
+
+// A 32-bit word of a row (one element of 32 bits or two of 16): -infinity throughout, the larger of two, the largest in one.
+template <typename T> __device__ __forceinline__ uint32_t low_word();
+template <> __device__ __forceinline__ uint32_t low_word<float>() { return 0xff800000u; }
+template <> __device__ __forceinline__ uint32_t low_word<__nv_bfloat16>() { return 0xff80ff80u; }
+template <> __device__ __forceinline__ uint32_t low_word<__half>() { return 0xfc00fc00u; }
+template <typename T> __device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t max_words<float>(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+template <> __device__ __forceinline__ uint32_t max_words<__nv_bfloat16>(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <> __device__ __forceinline__ uint32_t max_words<__half>(uint32_t a, uint32_t b) {
+    const __half2 m = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <typename T> __device__ __forceinline__ float max_in_word(uint32_t w) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+    else {
+        const float2 f = unpack2<T>(w);
+        return fmaxf(f.x, f.y);
+    }
+}
+// The pairs of a vector, in order, and back.
+template <typename T> struct Pairs {
+    static constexpr int kCount = sizeof(T) == 4 ? 2 : 4;
+    __device__ static __forceinline__ float2 get(const uint4& v, int i) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        else return unpack2<T>(w[i]);
+    }
+    __device__ static __forceinline__ uint4 join(const float2* f) {
+        if constexpr (sizeof(T) == 4)
+            return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+        else return make_uint4(pack2<T>(f[0].x, f[0].y), pack2<T>(f[1].x, f[1].y), pack2<T>(f[2].x, f[2].y), pack2<T>(f[3].x, f[3].y));
+    }
+};
+
+// The last warp's work on a row: label, teacher's probabilities, logits at their places.
+template <typename T>
+__device__ void describe_row(const DistillParams& P, const T* z, int64_t row, bool back, float* p, float* zk, int* idx, Slot& S) {
+    const int lane = threadIdx.x & 31;
+    int64_t label = 0;
+    int ignored = 0, bad = 0;
+    float label_z = 0.f;
+    if (P.labels) {
+        label = P.labels_64 ? static_cast<const int64_t*>(P.labels)[row] : (int64_t)static_cast<const int32_t*>(P.labels)[row];
+        ignored = label == P.ignore_index;
+        bad = !ignored && (label < 0 || label >= P.vocab);
+        if (lane == 0 && !ignored && !bad) label_z = to_f32<T>(z[label]);
+    }
+    const float invT = 1.f / P.temperature;
+    float top = -INFINITY;
+    for (uint32_t first = 0; first < P.k; first += 128) {
+        int64_t j[4];
+        float t[4], at_z[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t i = first + u * 32 + lane;
+            j[u] = -1, t[u] = 0.f;
+            if (i < P.k) {
+                const int64_t at = row * P.index_stride + i;
+                j[u] = P.index_64 ? static_cast<const int64_t*>(P.index)[at] : (int64_t)static_cast<const int32_t*>(P.index)[at];
+                t[u] = teacher_at(P, row * P.t_stride + i) * invT;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const bool in = j[u] >= 0 && j[u] < P.vocab;
+            if (!in && j[u] != -1) bad = 1;
+            at_z[u] = in && !ignored ? to_f32<T>(z[j[u]]) : 0.f;
+            if (!in) j[u] = -1, t[u] = -INFINITY;
+            top = fmaxf(top, t[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t i = first + u * 32 + lane;
+            if (i < P.k) p[i] = t[u], zk[i] = at_z[u], idx[i] = (int)j[u];
+        }
+    }
+    top = warp_max(top);
+    float sum = 0.f;
+    for (uint32_t i = lane; i < P.k; i += 32)
+        if (p[i] != -INFINITY) sum += fast_exp2((p[i] - top) * kLog2e);
+    sum = warp_sum(sum);
+    const float log_sum = logf(sum);
+    float plogp = 0.f, pz = 0.f;
+    for (uint32_t i = lane; i < P.k; i += 32) {
+        const float t = p[i];
+        float q = 0.f;
+        if (t != -INFINITY) {
+            const float logp = t - top - log_sum;
+            q = fast_exp2(logp * kLog2e);
+            if (q > 0.f) plogp += q * logp, pz += q * zk[i];  // 0 log 0 = 0, whatever the logit there
+        }
+        p[i] = q;
+    }
+    plogp = warp_sum(plogp);
+    pz = warp_sum(pz);
+    bad = __any_sync(~0u, bad);
+    if (lane == 0) {
+        S.plogp = plogp, S.pz = pz, S.any = sum > 0.f, S.label = bad ? -1 : (int)label, S.ignored = ignored, S.bad = bad, S.label_z = label_z;
+        if (P.dloss) S.g = P.dloss[row];
+        if (back) S.lse1 = P.stats[2 * row], S.lseT = P.stats[2 * row + 1];
+    }
+}
+
+// kPower: T = 2^squarings, so exp(z) = exp(z/T)^T.
+template <typename T, bool kPower, int kThreads, int kVectors>
+__global__ void __launch_bounds__(kThreads + 32, Held<kThreads, kVectors>::kPerSM)
+distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int buffers, int mode, int squarings, int* fault) {
+    using H = Held<kThreads, kVectors>;
+    constexpr int N = 16 / sizeof(T), kPairs = Pairs<T>::kCount;
+    extern __shared__ __align__(128) char smem[];  // buffers of a row's whole vectors, then two sets of the teacher's entries
+    __shared__ uint64_t bars[8];                   // full[2], free[2], described[2], used[2]
+    __shared__ Slot slots[2];
+    __shared__ float part[2][3][32];
+    __shared__ int gave_up;
+    const int V = (int)P.vocab, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row_bytes = V / N * 16;
+    char* entries = smem + (size_t)buffers * row_bytes;
+    const uint32_t full = smem_u32(bars), free_ = full + 16, described = full + 32, used = full + 48;
+    const Waits W{&gave_up, fault};
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) bar_init(full + 8 * i, 1), bar_init(free_ + 8 * i, H::kWarps), bar_init(described + 8 * i, 1), bar_init(used + 8 * i, H::kWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        gave_up = 0;
+    }
+    __syncthreads();
+    const bool want_stats = mode != kBackward, want_gradient = mode != kForward;
+
+    if (warp == H::kWarps) {
+        int it = 0;
+        const auto copy = [&](int64_t row, int n) {
+            if (row >= rows) return;
+            const int b = n % buffers;
+            if (n >= buffers) W.wait_warp(free_ + 8 * b, (n / buffers - 1) & 1);
+            if (lane == 0) {
+                const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
+                const Cut<T> c(z, V);
+                if (gave_up || c.vectors == 0) bar_arrive(full + 8 * b);
+                else {
+                    bar_expect(full + 8 * b, c.vectors * 16);
+                    const int piece = ((c.vectors + 3) / 4) * 16;
+                    for (int at = 0; at < c.vectors * 16; at += piece)
+                        bulk_load(smem_u32(smem) + b * row_bytes + at, reinterpret_cast<const char*>(z + c.head) + at, min(piece, c.vectors * 16 - at), full + 8 * b);
+                }
+            }
+        };
+        copy(blockIdx.x, 0);
+        for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, ++it) {
+            copy(row + gridDim.x, it + 1);
+            const int s = it & 1;
+            if (it >= 2) W.wait_warp(used + 8 * s, (it / 2 - 1) & 1);
+            float* p = reinterpret_cast<float*>(entries) + s * 3 * P.k;
+            describe_row<T>(P, reinterpret_cast<const T*>(P.z) + row * P.z_stride, row, mode == kBackward, p, p + P.k, reinterpret_cast<int*>(p + 2 * P.k), slots[s]);
+            __syncwarp();
+            if (lane == 0) bar_arrive(described + 8 * s);
+        }
+        if (gave_up && lane == 0)  // copies in flight still write to shared memory
+            for (int n = it > buffers ? it - buffers : 0; n < it; ++n) W.drain(full + 8 * (n % buffers), (n / buffers) & 1);
+        return;
+    }
+
+    const float c1 = kLog2e, cT = kLog2e / P.temperature;
+    int it = 0;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, ++it) {
+        const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
+        const Cut<T> c(z, V);
+        const int b = it % buffers, s = it & 1;
+        float extra = -INFINITY;
+        if (threadIdx.x < c.singles) extra = to_f32<T>(z[c.single(threadIdx.x)]);
+        W.wait_warp(full + 8 * b, (it / buffers) & 1);
+        uint4 x[kVectors];
+        const uint4* in = reinterpret_cast<const uint4*>(smem + (size_t)b * row_bytes);
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const int v = threadIdx.x + i * kThreads;
+            const uint32_t low = low_word<T>();
+            x[i] = v < c.vectors ? in[v] : make_uint4(low, low, low, low);
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(free_ + 8 * b);
+
+        float lse1, lseT;
+        if (want_stats) {
+            uint32_t top_word = low_word<T>();
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i)
+                if (i * kThreads < c.vectors) top_word = max_words<T>(top_word, max_words<T>(max_words<T>(x[i].x, x[i].y), max_words<T>(x[i].z, x[i].w)));
+            const float m = warp_max(fmaxf(max_in_word<T>(top_word), extra));
+            const float sub = m == -INFINITY ? 0.f : m;
+            // The difference comes before the factor: the type's lowest value times log2(e) would be -infinity.
+            float2 sT = make_float2(0.f, 0.f), s1 = sT;
+            const float2 minus = make_float2(-sub, -sub), cTT = make_float2(cT, cT), c11 = make_float2(c1, c1);
+            const auto both = [&](float2 d, float2& eT, float2& e1) {
+                const float2 a = mul2(d, cTT);
+                eT = make_float2(fast_exp2(a.x), fast_exp2(a.y));
+                if (kPower) {
+                    e1 = eT;
+                    if (squarings > 0) e1 = mul2(e1, e1);
+                    if (squarings > 1) e1 = mul2(e1, e1);
+                } else {
+                    const float2 o = mul2(d, c11);
+                    e1 = make_float2(fast_exp2(o.x), fast_exp2(o.y));
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i)
+                if (i * kThreads < c.vectors)
+#pragma unroll
+                    for (int q = 0; q < kPairs; ++q) {
+                        float2 eT, e1;
+                        both(add2(Pairs<T>::get(x[i], q), minus), eT, e1);
+                        sT = add2(sT, eT), s1 = add2(s1, e1);
+                    }
+            {
+                float2 eT, e1;
+                both(add2(make_float2(extra, -INFINITY), minus), eT, e1);
+                sT = add2(sT, eT), s1 = add2(s1, e1);
+            }
+            const float w1 = warp_sum(s1.x + s1.y), wT = warp_sum(sT.x + sT.y);
+            float M = m, S1 = w1, ST = wT;
+            if (H::kWarps > 1) {
+                if (lane == 0) part[s][0][warp] = m, part[s][1][warp] = w1, part[s][2][warp] = wT;
+                asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+                const float wm = lane < H::kWarps ? part[s][0][lane] : -INFINITY;
+                M = warp_max(wm);
+                const float d = wm == -INFINITY ? 0.f : wm - M;   // a warp with nothing has sums of 0, or a NaN
+                S1 = warp_sum(lane < H::kWarps ? part[s][1][lane] * fast_exp2(d * c1) : 0.f);
+                ST = warp_sum(lane < H::kWarps ? part[s][2][lane] * fast_exp2(d * cT) : 0.f);
+            }
+            lse1 = M + log2f(S1) * kLn2;
+            lseT = M / P.temperature + log2f(ST) * kLn2;
+        }
+        W.wait_warp(described + 8 * s, (it / 2) & 1);
+        const Slot S = slots[s];
+        if (!want_stats) lse1 = S.lse1, lseT = S.lseT;
+        else if (threadIdx.x == 0) {
+            if (P.stats) P.stats[2 * row] = lse1, P.stats[2 * row + 1] = lseT;
+            float loss = 0.f;
+            if (!S.ignored) {
+                if (P.labels) loss += (1.f - P.mix) * (lse1 - S.label_z);
+                if (S.any) loss += P.mix * P.temperature * P.temperature * (S.plogp - S.pz / P.temperature + lseT);
+                if (S.bad) loss = NAN;
+            }
+            P.loss[row] = loss;
+        }
+        if (want_gradient) {
+            // a q1 + b qT; where T = 2^n, q1 = qT^T exp(T lseT - lse1).  An ignored row's gradient is 0 whatever it holds.
+            const float g = S.bad ? NAN : S.g;
+            const float a = P.labels ? g * (1.f - P.mix) : 0.f, bT = S.any ? g * P.mix * P.temperature : 0.f;
+            const float LT = P.temperature * lseT;
+            const float a1 = kPower ? a * fast_exp2((LT - lse1) * kLog2e) : a;
+            const float2 minusT = make_float2(-LT, -LT), minus1 = make_float2(-lse1, -lse1), cTT = make_float2(cT, cT), c11 = make_float2(c1, c1),
+                         aa = make_float2(a1, a1), bb = make_float2(bT, bT);
+            const auto gradient = [&](float2 f) -> float2 {
+                const float2 u = mul2(add2(f, minusT), cTT);
+                const float2 qT = make_float2(fast_exp2(u.x), fast_exp2(u.y));
+                float2 q1;
+                if (kPower) {
+                    q1 = qT;
+                    if (squarings > 0) q1 = mul2(q1, q1);
+                    if (squarings > 1) q1 = mul2(q1, q1);
+                } else {
+                    const float2 o = mul2(add2(f, minus1), c11);
+                    q1 = make_float2(fast_exp2(o.x), fast_exp2(o.y));
+                }
+                return fma2(aa, q1, mul2(bb, qT));
+            };
+            T* dz = reinterpret_cast<T*>(P.dz) + row * P.dz_stride;
+            uint4* out = reinterpret_cast<uint4*>(dz + c.head);
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i) {
+                const int v = threadIdx.x + i * kThreads;
+                if (i * kThreads < c.vectors) {
+                    float2 f[kPairs];
+#pragma unroll
+                    for (int q = 0; q < kPairs; ++q) f[q] = gradient(Pairs<T>::get(x[i], q));
+                    uint4 y = Pairs<T>::join(f);
+                    if (S.ignored) y = make_uint4(0, 0, 0, 0);
+                    if (v < c.vectors) __stcs(out + v, y);
+                }
+            }
+            if (threadIdx.x < c.singles) dz[c.single(threadIdx.x)] = from_f32<T>(S.ignored ? 0.f : gradient(make_float2(extra, extra)).x);
+            // The row's own entries lie in what other threads have written; each is formed once more, whole, and rounded once.
+            if (kThreads > 32) asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+            else __syncwarp();
+            if (!S.ignored) {
+                const float* p = reinterpret_cast<const float*>(entries) + s * 3 * P.k;
+                const float* zk = p + P.k;
+                const int* idx = reinterpret_cast<const int*>(p + 2 * P.k);
+                // four threads to an entry look for its doubles and for the label
+                int there = 0;
+                for (uint32_t first = 0; first < P.k; first += kThreads / 4) {
+                    const uint32_t i = first + threadIdx.x / 4;
+                    const int j = i < P.k ? idx[i] : -1;
+                    float same = 0.f;
+                    if (j >= 0)
+                        for (uint32_t o = threadIdx.x & 3; o < P.k; o += 4) same += idx[o] == j ? p[o] : 0.f;
+                    same += __shfl_xor_sync(~0u, same, 1);
+                    same += __shfl_xor_sync(~0u, same, 2);
+                    if (j >= 0 && (threadIdx.x & 3) == 0) dz[j] = from_f32<T>(gradient(make_float2(zk[i], zk[i])).x - bT * same - (P.labels && j == S.label ? a : 0.f));
+                }
+                if (warp == 0 && P.labels && !S.bad) {
+                    for (uint32_t i = lane; i < P.k; i += 32) there |= idx[i] == S.label;
+                    if (!__any_sync(~0u, there) && lane == 0) dz[S.label] = from_f32<T>(gradient(make_float2(S.label_z, S.label_z)).x - a);
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(used + 8 * s);
+    }
+}
+
+template <typename T, bool kPower, int kThreads, int kVectors>
+int launch_held(const DistillParams& P, int64_t rows, int mode, int squarings, int sms, int* fault, cudaStream_t st) {
+    using H = Held<kThreads, kVectors>;
+    auto* kernel = distill_held_kernel<T, kPower, kThreads, kVectors>;
+    const int row_bytes = (int)(P.vocab * sizeof(T) / 16 * 16), entries = (int)P.k * 24;
+    const int room = (kSharedPerSM / H::kPerSM - 3072 - entries) & ~127;   // beside what the kernel declares itself and 1 KB for the system
+    const int buffers = room >= 2 * row_bytes ? 2 : 1;
+    const int bytes = buffers * row_bytes + entries;
+    if (int rc = allow_smem(kernel, bytes)) return rc;
+    const int64_t most = (int64_t)sms * H::kPerSM;
+    kernel<<<(unsigned)(rows < most ? rows : most), kThreads + 32, bytes, st>>>(P, (int)rows, buffers, mode, squarings, fault);
+    return cuda_status(cudaGetLastError(), "distill launch");
+}
+
+// The smallest CTA whose registers hold the row: many small ones hide each other's latencies, and a row's fixed cost (a
+// reduction, two barriers) falls on fewer threads.
+template <typename T, bool kPower>
+int by_length(const DistillParams& P, int64_t rows, int mode, int squarings, int sms, int* fault, cudaStream_t st) {
+    const int64_t bytes = P.vocab * (int64_t)sizeof(T);
+    if (bytes <= Held<32, 8>::kBytes) return launch_held<T, kPower, 32, 8>(P, rows, mode, squarings, sms, fault, st);
+    if (bytes <= Held<96, 8>::kBytes) return launch_held<T, kPower, 96, 8>(P, rows, mode, squarings, sms, fault, st);
+    if (bytes <= Held<224, 16>::kBytes) return launch_held<T, kPower, 224, 16>(P, rows, mode, squarings, sms, fault, st);
+    return launch_held<T, kPower, 480, 16>(P, rows, mode, squarings, sms, fault, st);
+}
+constexpr int64_t kMostHeld = Held<480, 16>::kBytes;
+
 template <typename T, Mode kMode, int kSquarings>
 int launch(const DistillParams& P, int64_t rows, cudaStream_t st) {
-    if (P.vocab <= 4096) distill_kernel<T, kMode, kSquarings, 128><<<(unsigned)rows, 128, 0, st>>>(P);
-    else distill_kernel<T, kMode, kSquarings, 512><<<(unsigned)rows, 512, 0, st>>>(P);
+    distill_kernel<T, kMode, kSquarings, 512><<<(unsigned)rows, 512, 0, st>>>(P);
     return cuda_status(cudaGetLastError(), "distill launch");
 }
 
 template <typename T, Mode kMode>
-int by_temperature(const DistillParams& P, int64_t rows, cudaStream_t st) {
+int by_temperature(const DistillParams& P, int64_t rows, int32_t device, cudaStream_t st) {
+    // Held rows need the gradient's vectors to lie like the logits', in every row.
+    const auto lies_like = [&] {
+        return (((uintptr_t)P.z ^ (uintptr_t)P.dz) & 15) == 0 && (rows == 1 || (P.z_stride - P.dz_stride) * (int64_t)sizeof(T) % 16 == 0);
+    };
+    if (P.vocab * (int64_t)sizeof(T) <= kMostHeld && (kMode == kForward || lies_like())) {
+        int* fault = nullptr;
+        if (int rc = fault_mark(&fault)) return rc;
+        const int sms = sm_count(device);
+        if (P.temperature == 1.f) return by_length<T, true>(P, rows, kMode, 0, sms, fault, st);
+        if (P.temperature == 2.f) return by_length<T, true>(P, rows, kMode, 1, sms, fault, st);
+        if (P.temperature == 4.f) return by_length<T, true>(P, rows, kMode, 2, sms, fault, st);
+        return by_length<T, false>(P, rows, kMode, 0, sms, fault, st);
+    }
     if (P.temperature == 1.f) return launch<T, kMode, 0>(P, rows, st);
     if (P.temperature == 2.f) return launch<T, kMode, 1>(P, rows, st);
     if (P.temperature == 4.f) return launch<T, kMode, 2>(P, rows, st);
@@ -325,9 +727,9 @@ int distill(const halos_distill_args* a) {
     P.vocab = a->vocab, P.ignore_index = a->ignore_index, P.k = a->k, P.labels_64 = a->labels_64, P.index_64 = a->index_64;
     P.teacher_dtype = a->teacher_dtype, P.temperature = a->temperature, P.mix = a->mix;
     cudaStream_t st = (cudaStream_t)a->stream;
-    if (a->dtype == HALOS_F32) return by_temperature<float, kMode>(P, a->rows, st);
-    if (a->dtype == HALOS_BF16) return by_temperature<__nv_bfloat16, kMode>(P, a->rows, st);
-    return by_temperature<__half, kMode>(P, a->rows, st);
+    if (a->dtype == HALOS_F32) return by_temperature<float, kMode>(P, a->rows, a->device, st);
+    if (a->dtype == HALOS_BF16) return by_temperature<__nv_bfloat16, kMode>(P, a->rows, a->device, st);
+    return by_temperature<__half, kMode>(P, a->rows, a->device, st);
 }
 
 }  // namespace
