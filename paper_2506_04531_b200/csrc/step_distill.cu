@@ -284,16 +284,17 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
 }
 
 
-// ------------------------------------------------------------------------------------------------ rows held in registers
+// ------------------------------------------------------------------------------------------------ rows held in shared memory
 
-// A CTA of kThreads + 32 (a multiple of four warps: registers are given out by that) walks rows.  Its last warp is one or two rows ahead of the others: it has the row copied into shared memory in
-// bulk and works out the teacher's side of it.  The others take the row from there into registers (kVectors of 16 bytes a
-// thread), which frees the buffer for the next copy, and go over the registers twice: once for the statistics, once
-// for the gradient, which they store from there.  So the logits cross HBM once, and copying, exponentials and storing overlap.
+// A CTA of kThreads + 32 walks rows, one held in shared memory at a time, in chunks.  Its last warp copies: as soon as the
+// gradient of a chunk has been formed the next row's chunk is fetched over it, and meanwhile that warp works out the
+// teacher's side of the next row.  The other warps go over the row twice, for the statistics and for the gradient,
+// which they store from registers.  So the logits cross HBM once; several CTAs to an SM fill each other's gaps.
 // A wait that runs out is marked and ends every later one at once; the loops and their barriers still run to the end.
-template <int kThreads, int kVectors> struct Held {
-    static constexpr int kWarps = kThreads / 32, kBytes = kThreads * kVectors * 16;
-    static constexpr int kPerSM = kThreads == 32 ? 12 : kThreads == 96 ? 5 : kThreads == 224 ? 2 : 1;
+template <int kThreads> struct Held {
+    static constexpr int kWarps = kThreads / 32, kUnroll = 4, kChunk = kThreads * kUnroll;  // vectors
+    static constexpr int kPerSM = kThreads == 32 ? 16 : kThreads == 128 ? 6 : kThreads == 256 ? 3 : 1;
+    static constexpr int kMostChunks = 32;
 };
 
 struct Slot {  // what the last warp says of a row beside the entries themselves
@@ -440,23 +441,24 @@ __device__ void describe_row(const DistillParams& P, const T* z, int64_t row, bo
 }
 
 // kPower: T = 2^squarings, so exp(z) = exp(z/T)^T.
-template <typename T, bool kPower, int kThreads, int kVectors>
-__global__ void __launch_bounds__(kThreads + 32, Held<kThreads, kVectors>::kPerSM)
-distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int buffers, int mode, int squarings, int* fault) {
-    using H = Held<kThreads, kVectors>;
-    constexpr int N = 16 / sizeof(T), kPairs = Pairs<T>::kCount;
-    extern __shared__ __align__(128) char smem[];  // buffers of a row's whole vectors, then two sets of the teacher's entries
-    __shared__ uint64_t bars[8];                   // full[2], free[2], described[2], used[2]
+template <typename T, bool kPower, int kThreads>
+__global__ void __launch_bounds__(kThreads + 32, Held<kThreads>::kPerSM)
+distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int squarings, int* fault) {
+    using H = Held<kThreads>;
+    constexpr int N = 16 / sizeof(T), kPairs = Pairs<T>::kCount, U = H::kUnroll;
+    extern __shared__ __align__(128) char smem[];  // a row's whole vectors, then two sets of the teacher's entries
+    __shared__ uint64_t bars[2 * H::kMostChunks + 4];  // full and free of each chunk, described[2], used[2]
     __shared__ Slot slots[2];
     __shared__ float part[2][3][32];
     __shared__ int gave_up;
     const int V = (int)P.vocab, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int row_bytes = V / N * 16;
-    char* entries = smem + (size_t)buffers * row_bytes;
-    const uint32_t full = smem_u32(bars), free_ = full + 16, described = full + 32, used = full + 48;
+    const int row_bytes = V / N * 16, chunks = (V / N + H::kChunk - 1) / H::kChunk;
+    char* entries = smem + row_bytes;
+    const uint32_t full = smem_u32(bars), free_ = full + 8 * H::kMostChunks, described = free_ + 8 * H::kMostChunks, used = described + 16;
     const Waits W{&gave_up, fault};
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) bar_init(full + 8 * i, 1), bar_init(free_ + 8 * i, H::kWarps), bar_init(described + 8 * i, 1), bar_init(used + 8 * i, H::kWarps);
+        for (int i = 0; i < chunks; ++i) bar_init(full + 8 * i, 1), bar_init(free_ + 8 * i, H::kWarps);
+        for (int i = 0; i < 2; ++i) bar_init(described + 8 * i, 1), bar_init(used + 8 * i, H::kWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         gave_up = 0;
     }
@@ -465,104 +467,110 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int buffe
 
     if (warp == H::kWarps) {
         int it = 0;
-        const auto copy = [&](int64_t row, int n) {
-            if (row >= rows) return;
-            const int b = n % buffers;
-            if (n >= buffers) W.wait_warp(free_ + 8 * b, (n / buffers - 1) & 1);
-            if (lane == 0) {
-                const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
-                const Cut<T> c(z, V);
-                if (gave_up || c.vectors == 0) bar_arrive(full + 8 * b);
-                else {
-                    bar_expect(full + 8 * b, c.vectors * 16);
-                    const int piece = ((c.vectors + 3) / 4) * 16;
-                    for (int at = 0; at < c.vectors * 16; at += piece)
-                        bulk_load(smem_u32(smem) + b * row_bytes + at, reinterpret_cast<const char*>(z + c.head) + at, min(piece, c.vectors * 16 - at), full + 8 * b);
+        const auto copy = [&](int64_t row, int n) {  // the n-th row of this CTA
+            const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
+            const Cut<T> c(z, V);
+            for (int i = 0; i < chunks; ++i) {
+                if (n) W.wait_warp(free_ + 8 * i, (n - 1) & 1);
+                const int bytes = min(H::kChunk, c.vectors - i * H::kChunk) * 16;
+                if (lane == 0) {
+                    if (gave_up || bytes <= 0) bar_arrive(full + 8 * i);
+                    else {
+                        bar_expect(full + 8 * i, bytes);
+                        bulk_load(smem_u32(smem) + i * H::kChunk * 16, reinterpret_cast<const char*>(z + c.head) + i * H::kChunk * 16, bytes, full + 8 * i);
+                    }
                 }
             }
         };
         copy(blockIdx.x, 0);
         for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, ++it) {
-            copy(row + gridDim.x, it + 1);
             const int s = it & 1;
             if (it >= 2) W.wait_warp(used + 8 * s, (it / 2 - 1) & 1);
             float* p = reinterpret_cast<float*>(entries) + s * 3 * P.k;
             describe_row<T>(P, reinterpret_cast<const T*>(P.z) + row * P.z_stride, row, mode == kBackward, p, p + P.k, reinterpret_cast<int*>(p + 2 * P.k), slots[s]);
             __syncwarp();
             if (lane == 0) bar_arrive(described + 8 * s);
+            if (row + gridDim.x < rows) copy(row + gridDim.x, it + 1);
         }
         if (gave_up && lane == 0)  // copies in flight still write to shared memory
-            for (int n = it > buffers ? it - buffers : 0; n < it; ++n) W.drain(full + 8 * (n % buffers), (n / buffers) & 1);
+            for (int i = 0; i < chunks; ++i) W.drain(full + 8 * i, (it - 1) & 1);
         return;
     }
 
     const float c1 = kLog2e, cT = kLog2e / P.temperature;
+    const float2 cTT = make_float2(cT, cT), c11 = make_float2(c1, c1);
+    const uint4* held = reinterpret_cast<const uint4*>(smem);
+    // exp2 of d cT, and of d c1 (its power where the temperature allows)
+    const auto both = [&](float2 dT, float2 d1, float2& eT, float2& e1) {
+        const float2 a = mul2(dT, cTT);
+        eT = make_float2(fast_exp2(a.x), fast_exp2(a.y));
+        if (kPower) {
+            e1 = eT;
+            if (squarings > 0) e1 = mul2(e1, e1);
+            if (squarings > 1) e1 = mul2(e1, e1);
+        } else {
+            const float2 o = mul2(d1, c11);
+            e1 = make_float2(fast_exp2(o.x), fast_exp2(o.y));
+        }
+    };
     int it = 0;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, ++it) {
         const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
         const Cut<T> c(z, V);
-        const int b = it % buffers, s = it & 1;
+        const int s = it & 1;
         float extra = -INFINITY;
         if (threadIdx.x < c.singles) extra = to_f32<T>(z[c.single(threadIdx.x)]);
-        W.wait_warp(full + 8 * b, (it / buffers) & 1);
-        uint4 x[kVectors];
-        const uint4* in = reinterpret_cast<const uint4*>(smem + (size_t)b * row_bytes);
-#pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-            const int v = threadIdx.x + i * kThreads;
-            const uint32_t low = low_word<T>();
-            x[i] = v < c.vectors ? in[v] : make_uint4(low, low, low, low);
-        }
-        __syncwarp();
-        if (lane == 0) bar_arrive(free_ + 8 * b);
 
         float lse1, lseT;
         if (want_stats) {
-            uint32_t top_word = low_word<T>();
-#pragma unroll
-            for (int i = 0; i < kVectors; ++i)
-                if (i * kThreads < c.vectors) top_word = max_words<T>(top_word, max_words<T>(max_words<T>(x[i].x, x[i].y), max_words<T>(x[i].z, x[i].w)));
-            const float m = warp_max(fmaxf(max_in_word<T>(top_word), extra));
-            const float sub = m == -INFINITY ? 0.f : m;
+            // A thread's sums are relative to the largest it has seen so far, which after the first few vectors hardly moves.
             // The difference comes before the factor: the type's lowest value times log2(e) would be -infinity.
-            float2 sT = make_float2(0.f, 0.f), s1 = sT;
-            const float2 minus = make_float2(-sub, -sub), cTT = make_float2(cT, cT), c11 = make_float2(c1, c1);
-            const auto both = [&](float2 d, float2& eT, float2& e1) {
-                const float2 a = mul2(d, cTT);
-                eT = make_float2(fast_exp2(a.x), fast_exp2(a.y));
-                if (kPower) {
-                    e1 = eT;
-                    if (squarings > 0) e1 = mul2(e1, e1);
-                    if (squarings > 1) e1 = mul2(e1, e1);
-                } else {
-                    const float2 o = mul2(d, c11);
-                    e1 = make_float2(fast_exp2(o.x), fast_exp2(o.y));
-                }
-            };
-#pragma unroll
-            for (int i = 0; i < kVectors; ++i)
-                if (i * kThreads < c.vectors)
-#pragma unroll
-                    for (int q = 0; q < kPairs; ++q) {
-                        float2 eT, e1;
-                        both(add2(Pairs<T>::get(x[i], q), minus), eT, e1);
-                        sT = add2(sT, eT), s1 = add2(s1, e1);
-                    }
-            {
+            float m = extra;
+            float2 sT = make_float2(0.f, 0.f), s1 = sT, minus = make_float2(m == -INFINITY ? 0.f : -m, m == -INFINITY ? 0.f : -m);
+            const auto add = [&](float2 f) {
+                const float2 d = add2(f, minus);
                 float2 eT, e1;
-                both(add2(make_float2(extra, -INFINITY), minus), eT, e1);
+                both(d, d, eT, e1);
                 sT = add2(sT, eT), s1 = add2(s1, e1);
+            };
+            add(make_float2(extra, -INFINITY));
+            for (int k = 0; k < chunks; ++k) {
+                W.wait_warp(full + 8 * k, it & 1);
+                uint4 x[U];
+                uint32_t top_word = low_word<T>();
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int v = k * H::kChunk + u * kThreads + threadIdx.x;
+                    const uint32_t low = low_word<T>();
+                    x[u] = v < c.vectors ? held[v] : make_uint4(low, low, low, low);
+                    top_word = max_words<T>(top_word, max_words<T>(max_words<T>(x[u].x, x[u].y), max_words<T>(x[u].z, x[u].w)));
+                }
+                const float top = max_in_word<T>(top_word);
+                if (top > m) {
+                    const float fT = m == -INFINITY ? 0.f : fast_exp2((m - top) * cT), f1 = m == -INFINITY ? 0.f : fast_exp2((m - top) * c1);
+                    sT = mul2(sT, make_float2(fT, fT)), s1 = mul2(s1, make_float2(f1, f1));
+                    m = top, minus = make_float2(-m, -m);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int q = 0; q < kPairs; ++q) add(Pairs<T>::get(x[u], q));
+                if (!want_gradient) {
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(free_ + 8 * k);
+                }
             }
-            const float w1 = warp_sum(s1.x + s1.y), wT = warp_sum(sT.x + sT.y);
-            float M = m, S1 = w1, ST = wT;
+            float M = warp_max(m);
+            const float d = m == -INFINITY ? 0.f : m - M;  // who has nothing has sums of 0, or a NaN
+            float S1 = warp_sum((s1.x + s1.y) * fast_exp2(d * c1)), ST = warp_sum((sT.x + sT.y) * fast_exp2(d * cT));
             if (H::kWarps > 1) {
-                if (lane == 0) part[s][0][warp] = m, part[s][1][warp] = w1, part[s][2][warp] = wT;
+                if (lane == 0) part[s][0][warp] = M, part[s][1][warp] = S1, part[s][2][warp] = ST;
                 asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
                 const float wm = lane < H::kWarps ? part[s][0][lane] : -INFINITY;
                 M = warp_max(wm);
-                const float d = wm == -INFINITY ? 0.f : wm - M;   // a warp with nothing has sums of 0, or a NaN
-                S1 = warp_sum(lane < H::kWarps ? part[s][1][lane] * fast_exp2(d * c1) : 0.f);
-                ST = warp_sum(lane < H::kWarps ? part[s][2][lane] * fast_exp2(d * cT) : 0.f);
+                const float e = wm == -INFINITY ? 0.f : wm - M;
+                S1 = warp_sum(lane < H::kWarps ? part[s][1][lane] * fast_exp2(e * c1) : 0.f);
+                ST = warp_sum(lane < H::kWarps ? part[s][2][lane] * fast_exp2(e * cT) : 0.f);
             }
             lse1 = M + log2f(S1) * kLn2;
             lseT = M / P.temperature + log2f(ST) * kLn2;
@@ -586,34 +594,33 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int buffe
             const float a = P.labels ? g * (1.f - P.mix) : 0.f, bT = S.any ? g * P.mix * P.temperature : 0.f;
             const float LT = P.temperature * lseT;
             const float a1 = kPower ? a * fast_exp2((LT - lse1) * kLog2e) : a;
-            const float2 minusT = make_float2(-LT, -LT), minus1 = make_float2(-lse1, -lse1), cTT = make_float2(cT, cT), c11 = make_float2(c1, c1),
-                         aa = make_float2(a1, a1), bb = make_float2(bT, bT);
+            const float2 minusT = make_float2(-LT, -LT), minus1 = make_float2(-lse1, -lse1), aa = make_float2(a1, a1), bb = make_float2(bT, bT);
             const auto gradient = [&](float2 f) -> float2 {
-                const float2 u = mul2(add2(f, minusT), cTT);
-                const float2 qT = make_float2(fast_exp2(u.x), fast_exp2(u.y));
-                float2 q1;
-                if (kPower) {
-                    q1 = qT;
-                    if (squarings > 0) q1 = mul2(q1, q1);
-                    if (squarings > 1) q1 = mul2(q1, q1);
-                } else {
-                    const float2 o = mul2(add2(f, minus1), c11);
-                    q1 = make_float2(fast_exp2(o.x), fast_exp2(o.y));
-                }
+                float2 qT, q1;
+                both(add2(f, minusT), kPower ? f : add2(f, minus1), qT, q1);
                 return fma2(aa, q1, mul2(bb, qT));
             };
             T* dz = reinterpret_cast<T*>(P.dz) + row * P.dz_stride;
             uint4* out = reinterpret_cast<uint4*>(dz + c.head);
+            for (int k = 0; k < chunks; ++k) {
+                if (!want_stats) W.wait_warp(full + 8 * k, it & 1);
+                uint4 x[U];
 #pragma unroll
-            for (int i = 0; i < kVectors; ++i) {
-                const int v = threadIdx.x + i * kThreads;
-                if (i * kThreads < c.vectors) {
-                    float2 f[kPairs];
+                for (int u = 0; u < U; ++u) {
+                    const int v = k * H::kChunk + u * kThreads + threadIdx.x;
+                    if (v < c.vectors) x[u] = held[v];
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(free_ + 8 * k);
 #pragma unroll
-                    for (int q = 0; q < kPairs; ++q) f[q] = gradient(Pairs<T>::get(x[i], q));
-                    uint4 y = Pairs<T>::join(f);
-                    if (S.ignored) y = make_uint4(0, 0, 0, 0);
-                    if (v < c.vectors) __stcs(out + v, y);
+                for (int u = 0; u < U; ++u) {
+                    const int v = k * H::kChunk + u * kThreads + threadIdx.x;
+                    if (v < c.vectors) {
+                        float2 f[kPairs];
+#pragma unroll
+                        for (int q = 0; q < kPairs; ++q) f[q] = gradient(Pairs<T>::get(x[u], q));
+                        __stcs(out + v, S.ignored ? make_uint4(0, 0, 0, 0) : Pairs<T>::join(f));
+                    }
                 }
             }
             if (threadIdx.x < c.singles) dz[c.single(threadIdx.x)] = from_f32<T>(S.ignored ? 0.f : gradient(make_float2(extra, extra)).x);
@@ -647,31 +654,32 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int buffe
     }
 }
 
-template <typename T, bool kPower, int kThreads, int kVectors>
+template <typename T>
+int held_bytes(const DistillParams& P) { return (int)(P.vocab * sizeof(T) / 16 * 16 + P.k * 24); }
+constexpr int kMostHeld = 225 * 1024;  // of 227 KB to a CTA, beside what the kernel declares itself
+
+template <typename T, bool kPower, int kThreads>
 int launch_held(const DistillParams& P, int64_t rows, int mode, int squarings, int sms, int* fault, cudaStream_t st) {
-    using H = Held<kThreads, kVectors>;
-    auto* kernel = distill_held_kernel<T, kPower, kThreads, kVectors>;
-    const int row_bytes = (int)(P.vocab * sizeof(T) / 16 * 16), entries = (int)P.k * 24;
-    const int room = (kSharedPerSM / H::kPerSM - 3072 - entries) & ~127;   // beside what the kernel declares itself and 1 KB for the system
-    const int buffers = room >= 2 * row_bytes ? 2 : 1;
-    const int bytes = buffers * row_bytes + entries;
+    using H = Held<kThreads>;
+    auto* kernel = distill_held_kernel<T, kPower, kThreads>;
+    const int bytes = held_bytes<T>(P);
     if (int rc = allow_smem(kernel, bytes)) return rc;
-    const int64_t most = (int64_t)sms * H::kPerSM;
-    kernel<<<(unsigned)(rows < most ? rows : most), kThreads + 32, bytes, st>>>(P, (int)rows, buffers, mode, squarings, fault);
+    const int fit = kSharedPerSM / (bytes + 3072), per_sm = fit < 1 ? 1 : fit < H::kPerSM ? fit : H::kPerSM;
+    const int64_t most = (int64_t)sms * per_sm;
+    kernel<<<(unsigned)(rows < most ? rows : most), kThreads + 32, bytes, st>>>(P, (int)rows, mode, squarings, fault);
     return cuda_status(cudaGetLastError(), "distill launch");
 }
 
-// The smallest CTA whose registers hold the row: many small ones hide each other's latencies, and a row's fixed cost (a
-// reduction, two barriers) falls on fewer threads.
+// Small CTAs for short rows: many of them hide each other's latencies, and a row's fixed cost (a reduction, two barriers)
+// falls on fewer threads.  From half of an SM's shared memory on there is one CTA to an SM, which then needs all the threads.
 template <typename T, bool kPower>
 int by_length(const DistillParams& P, int64_t rows, int mode, int squarings, int sms, int* fault, cudaStream_t st) {
     const int64_t bytes = P.vocab * (int64_t)sizeof(T);
-    if (bytes <= Held<32, 8>::kBytes) return launch_held<T, kPower, 32, 8>(P, rows, mode, squarings, sms, fault, st);
-    if (bytes <= Held<96, 8>::kBytes) return launch_held<T, kPower, 96, 8>(P, rows, mode, squarings, sms, fault, st);
-    if (bytes <= Held<224, 16>::kBytes) return launch_held<T, kPower, 224, 16>(P, rows, mode, squarings, sms, fault, st);
-    return launch_held<T, kPower, 480, 16>(P, rows, mode, squarings, sms, fault, st);
+    if (bytes <= 4096) return launch_held<T, kPower, 32>(P, rows, mode, squarings, sms, fault, st);
+    if (bytes <= 32768) return launch_held<T, kPower, 128>(P, rows, mode, squarings, sms, fault, st);
+    if (bytes <= 110 * 1024) return launch_held<T, kPower, 256>(P, rows, mode, squarings, sms, fault, st);
+    return launch_held<T, kPower, 512>(P, rows, mode, squarings, sms, fault, st);
 }
-constexpr int64_t kMostHeld = Held<480, 16>::kBytes;
 
 template <typename T, Mode kMode, int kSquarings>
 int launch(const DistillParams& P, int64_t rows, cudaStream_t st) {
@@ -685,7 +693,7 @@ int by_temperature(const DistillParams& P, int64_t rows, int32_t device, cudaStr
     const auto lies_like = [&] {
         return (((uintptr_t)P.z ^ (uintptr_t)P.dz) & 15) == 0 && (rows == 1 || (P.z_stride - P.dz_stride) * (int64_t)sizeof(T) % 16 == 0);
     };
-    if (P.vocab * (int64_t)sizeof(T) <= kMostHeld && (kMode == kForward || lies_like())) {
+    if (P.vocab <= (1 << 20) && held_bytes<T>(P) <= kMostHeld && (kMode == kForward || lies_like())) {
         int* fault = nullptr;
         if (int rc = fault_mark(&fault)) return rc;
         const int sms = sm_count(device);
