@@ -17,6 +17,7 @@
 
 #include <limits.h>
 #include <math.h>
+#include <type_traits>
 
 namespace halos_step {
 namespace {
@@ -25,10 +26,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRecord = 64;   // queries to a record
 
 // What the backward pass knows of 64 queries of a head before it starts.  A query that sees nothing, or is none, has
-// lse2 = infinity: its probabilities are 0.
+// minus_lse2 = -infinity: its probabilities are 0.
 struct Record {
-    float lse2[kRecord];      // log2 of the sum of exponentials
-    float delta[kRecord];     // dout . o
+    float minus_lse2[kRecord];   // - log2 of the sum of exponentials
+    float minus_delta[kRecord];  // - dout . o
     int lo[kRecord], hi[kRecord];
 };
 static_assert(sizeof(Record) == 1024, "one bulk copy");
@@ -84,18 +85,20 @@ __device__ __forceinline__ void clear_row(char* tile, int rows, int row) {
 
 // ------------------------------------------------------------------------------------------------ forward
 
+// Heads of 64: S of 64 keys at a time beside O takes 128 columns of tensor memory, so four CTAs share an SM and fill each other's
+// waits.  Heads of 128: O alone takes 128, two CTAs are left, and S of 128 keys halves how often Q is read from
+// shared memory, which 64 keys would have the product wait for.  The softmax takes 64 keys at a time either way.
 template <int DP> struct Forward {
-    static constexpr int kRowsQ = 128, kRowsK = 128;
-    static constexpr bool kOwnP = DP == 64;          // tensor memory has room for P beside S: the next S can start early
+    static constexpr int kKeys = DP == 64 ? 64 : 128, kHalves = kKeys / 64;
     static constexpr int kStages = DP == 64 ? 2 : 1;
-    static constexpr int kTileQ = kRowsQ * DP * 2, kTileK = kRowsK * DP * 2;
+    static constexpr int kTileQ = 128 * DP * 2, kTileK = kKeys * DP * 2;
     static constexpr int kSmem = 1024 + kTileQ + 2 * kStages * kTileK;
-    static constexpr int kColS = 0, kColP = kOwnP ? 128 : 0, kColO = kOwnP ? 192 : 128, kColumns = 256;
-    static constexpr int kThreads = 192;
+    static constexpr int kColO = kKeys, kColumns = kKeys + DP;   // P lies over S, each 64 keys over their own
+    static constexpr int kPerSM = 512 / kColumns, kThreads = 160;
 };
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(192, 2)
+__global__ void __launch_bounds__(160, Forward<DP>::kPerSM)
 attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ CUtensorMap map_q,
                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using F = Forward<DP>;
@@ -104,12 +107,11 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     char* tile_q = smem;
     char* tile_k = smem + F::kTileQ;
     char* tile_v = tile_k + F::kStages * F::kTileK;
-    __shared__ uint64_t bars[6 + 4 * F::kStages];
+    __shared__ uint64_t bars[3 + 2 * F::kHalves + 2 * F::kStages];
     __shared__ uint32_t s_tmem;
     __shared__ int s_gave_up, s_lo[4], s_hi[4];
-    const uint32_t bar0 = smem_u32(bars);
-    const uint32_t q_full = bar0, s_full = bar0 + 8, s_free = bar0 + 16, p_full = bar0 + 24, pv_done = bar0 + 32, left = bar0 + 40;
-    const uint32_t k_full = bar0 + 48, k_free = k_full + 8 * F::kStages, v_full = k_free + 8 * F::kStages, v_free = v_full + 8 * F::kStages;
+    const uint32_t q_full = smem_u32(bars), s_full = q_full + 8, left = q_full + 16, p_full = q_full + 24, pv_done = p_full + 8 * F::kHalves;
+    const uint32_t k_full = pv_done + 8 * F::kHalves, v_full = k_full + 8 * F::kStages;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // Longest rows first where the mask is causal.
@@ -118,12 +120,13 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
 
     if (threadIdx.x == 0) {
-        bar_init(q_full, 1), bar_init(s_full, 1), bar_init(s_free, 128), bar_init(p_full, 128), bar_init(pv_done, 1), bar_init(left, 1);
-        for (int s = 0; s < F::kStages; ++s) bar_init(k_full + 8 * s, 1), bar_init(k_free + 8 * s, 1), bar_init(v_full + 8 * s, 1), bar_init(v_free + 8 * s, 1);
+        bar_init(q_full, 1), bar_init(s_full, 1), bar_init(left, 1);
+        for (int e = 0; e < F::kHalves; ++e) bar_init(p_full + 8 * e, 128), bar_init(pv_done + 8 * e, 1);
+        for (int s = 0; s < F::kStages; ++s) bar_init(k_full + 8 * s, 1), bar_init(v_full + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_gave_up = 0;
     }
-    if (warp == 5) tmem_alloc<F::kColumns>(smem_u32(&s_tmem));
+    if (warp == 4) tmem_alloc<F::kColumns>(smem_u32(&s_tmem));
     int lo = INT_MAX, hi = 0;
     if (warp < 4) {
         seen_by(P, b, tile * 128 + threadIdx.x, lo, hi);
@@ -137,129 +140,127 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     tc_after_sync();
     const uint32_t tmem = s_tmem;
     const int min_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), max_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
-    const int first = max_hi ? min_lo / 128 : 0, n = max_hi ? (max_hi + 127) / 128 - first : 0;
+    const int first = max_hi ? min_lo / F::kKeys : 0, n = max_hi ? (max_hi + F::kKeys - 1) / F::kKeys - first : 0;
     const Waits W{&s_gave_up, P.fault};
 
     if (warp == 4) {
+        // One thread issues copies and products.  A tile of K may be overwritten when its S is done, one of V when its PV is; both come
+        // long before this thread has anything else to do.
         if (lane == 0 && n) {
-            bar_expect(q_full, F::kTileQ);
-            for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
-            int j = 0;
-            for (; j < n; ++j) {
-                const int s = j % F::kStages, use = j / F::kStages;
-                const int row = (first + j) * 128;
-                if (use && !W.wait(k_free + 8 * s, (use - 1) & 1)) break;
-                bar_expect(k_full + 8 * s, F::kTileK);
-                for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_k) + s * F::kTileK + d * 128 * 128, &map_k, k_full + 8 * s, d * 64, row, hk, b);
-                if (use && !W.wait(v_free + 8 * s, (use - 1) & 1)) break;
-                bar_expect(v_full + 8 * s, F::kTileK);
-                for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_v) + s * F::kTileK + d * 128 * 128, &map_v, v_full + 8 * s, d * 64, row, hk, b);
-            }
-            if (j < n) {  // left early: wait for the copies in flight
-                W.drain(q_full, 0);
-                for (int i = j > F::kStages ? j - F::kStages : 0; i <= j; ++i) {
-                    W.drain(k_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
-                    if (i < j) W.drain(v_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
-                }
-            }
-        }
-    } else if (warp == 5) {
-        if (lane == 0 && n) {
+            const auto load = [&](const CUtensorMap* map, char* tiles, uint32_t bars, int j) {
+                const uint32_t s = j % F::kStages, bar = bars + 8 * s;
+                bar_expect(bar, F::kTileK);
+                for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tiles) + s * F::kTileK + d * F::kKeys * 128, map, bar, d * 64, (first + j) * F::kKeys, hk, b);
+            };
             const auto scores = [&](int j) -> bool {
                 const int s = j % F::kStages;
                 if (!W.wait(k_full + 8 * s, (j / F::kStages) & 1)) return false;
                 tc_after_sync();
-                product_ss<T, 128, DP>(tmem + F::kColS, smem_u32(tile_q), 128, smem_u32(tile_k) + s * F::kTileK, 128);
-                mma_commit(k_free + 8 * s);
+                product_ss<T, F::kKeys, DP>(tmem, smem_u32(tile_q), 128, smem_u32(tile_k) + s * F::kTileK, F::kKeys);
                 mma_commit(s_full);
                 return true;
             };
+            bar_expect(q_full, F::kTileQ);
+            for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
+            int k_loads = 0, v_loads = 0;
+            for (; k_loads < F::kStages && k_loads < n; ++k_loads, ++v_loads) {
+                load(&map_k, tile_k, k_full, k_loads);
+                load(&map_v, tile_v, v_full, v_loads);
+            }
             bool ok = W.wait(q_full, 0) && scores(0);
             for (int j = 0; ok && j < n; ++j) {
                 const int s = j % F::kStages;
-                if (F::kOwnP && j + 1 < n) ok = W.wait(s_free, j & 1) && scores(j + 1);
-                ok = ok && W.wait(p_full, j & 1) && W.wait(v_full + 8 * s, (j / F::kStages) & 1);
-                if (!ok) break;
-                tc_after_sync();
-                product_ts<T, DP, 128>(tmem + F::kColO, tmem + F::kColP, smem_u32(tile_v) + s * F::kTileK, j > 0);
-                mma_commit(v_free + 8 * s);
-                mma_commit(pv_done);
-                if (!F::kOwnP && j + 1 < n) ok = scores(j + 1);
+                if (!(ok = W.wait(s_full, j & 1))) break;
+                if (k_loads < n) load(&map_k, tile_k, k_full, k_loads++);
+                if (!(ok = W.wait(v_full + 8 * s, (j / F::kStages) & 1))) break;
+#pragma unroll
+                for (int e = 0; ok && e < F::kHalves; ++e) {
+                    if (!(ok = W.wait(p_full + 8 * e, j & 1))) break;
+                    tc_after_sync();
+                    product_ts<T, DP, 64, 16>(tmem + F::kColO, tmem + 64 * e, smem_u32(tile_v) + s * F::kTileK + e * 64 * 128, F::kKeys, j > 0 || e > 0);
+                    mma_commit(pv_done + 8 * e);
+                }
+                if (ok && j + 1 < n) ok = scores(j + 1);
+                if (ok && v_loads < n) {
+                    if ((ok = W.wait(pv_done + 8 * (F::kHalves - 1), j & 1))) load(&map_v, tile_v, v_full, v_loads++);
+                }
             }
-            if (!ok) {  // products in flight still use tensor memory
+            if (!ok) {  // leaves early: what is in flight still uses shared and tensor memory
                 mma_commit(left);
                 W.drain(left, 0);
+                W.drain(q_full, 0);
+                for (int i = k_loads > F::kStages ? k_loads - F::kStages : 0; i < k_loads; ++i) W.drain(k_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+                for (int i = v_loads > F::kStages ? v_loads - F::kStages : 0; i < v_loads; ++i) W.drain(v_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
             }
         }
     } else {
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
         const int i = tile * 128 + threadIdx.x;
+        const float2 factor = both(P.scale2);
         float m = -INFINITY, l = 0.f;
         bool ok = true;
-        for (int j = 0; j < n; ++j) {
-            const int key0 = (first + j) * 128;
-            if (!(ok = W.wait_warp(s_full, j & 1))) break;
-            tc_after_sync();
-            uint32_t x[128];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_load32(x + 32 * c, lanes + F::kColS + 32 * c);
-            tmem_wait_loads();
-            if (F::kOwnP) {
-                tc_before_sync();
-                bar_arrive(s_free);
+        for (int half = 0; half < n * F::kHalves; ++half) {
+            const int j = half / F::kHalves, e = half % F::kHalves, key0 = (first + j) * F::kKeys + e * 64;
+            if (e == 0) {
+                if (!(ok = W.wait_warp(s_full, j & 1))) break;
+                tc_after_sync();
             }
-            if (!__all_sync(~0u, lo <= key0 && hi >= key0 + 128)) {
+            uint32_t x[64];
+            tmem_load32(x, lanes + 64 * e);
+            tmem_load32(x + 32, lanes + 64 * e + 32);
+            tmem_wait_loads();
+            if (!__all_sync(~0u, lo <= key0 && hi >= key0 + 64)) {
 #pragma unroll
-                for (int c = 0; c < 128; ++c)
+                for (int c = 0; c < 64; ++c)
                     if (key0 + c < lo || key0 + c >= hi) x[c] = 0xff800000u;
             }
-            float top = __uint_as_float(x[0]);
+            float tops[4];
 #pragma unroll
-            for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(x[c]));
-            top *= P.scale2;
+            for (int c = 0; c < 4; ++c) tops[c] = __uint_as_float(x[c]);
+#pragma unroll
+            for (int c = 4; c < 64; ++c) tops[c & 3] = fmaxf(tops[c & 3], __uint_as_float(x[c]));
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * P.scale2;
             if (__any_sync(~0u, top > m + 8.f)) {
                 const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : fast_exp2(m - to);
                 m = to;
                 l *= f;
-                if (j) {
-                    if (!(ok = W.wait_warp(pv_done, (j - 1) & 1))) break;
+                if (half) {  // every product so far is in O; S of this tile came after those of the tile before
+                    if (!(ok = W.wait_warp(pv_done + 8 * ((half - 1) % F::kHalves), ((half - 1) / F::kHalves) & 1))) break;
                     tc_after_sync();
 #pragma unroll
-                    for (int c = 0; c < DP / 32; ++c) {
-                        uint32_t o[32];
-                        tmem_load32(o, lanes + F::kColO + 32 * c);
+                    for (int c = 0; c < DP / 16; ++c) {
+                        uint32_t o[16];
+                        tmem_load16(o, lanes + F::kColO + 16 * c);
                         tmem_wait_loads();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_store32(lanes + F::kColO + 32 * c, o);
+                        for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * f);
+                        tmem_store16(lanes + F::kColO + 16 * c, o);
                     }
                 }
             }
-            const float sub = m == -INFINITY ? 0.f : m;
+            const float2 minus = both(m == -INFINITY ? 0.f : -m);
+            float2 sums[2] = {both(0.f), both(0.f)};
 #pragma unroll
-            for (int c = 0; c < 128; ++c) {
-                const float p = fast_exp2(fmaf(__uint_as_float(x[c]), P.scale2, -sub));
-                l += p;
-                x[c] = __float_as_uint(p);
+            for (int c = 0; c < 32; ++c) {
+                const float2 p = exp2_both(fma2(make_float2(__uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1])), factor, minus));
+                sums[c & 1] = add2(sums[c & 1], p);
+                x[c] = pack2<T>(p.x, p.y);
             }
-#pragma unroll
-            for (int c = 0; c < 64; ++c) x[c] = pack2<T>(__uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1]));
-            if (F::kOwnP && j && !(ok = W.wait_warp(pv_done, (j - 1) & 1))) break;
-            tmem_store32(lanes + F::kColP, x);
-            tmem_store32(lanes + F::kColP + 32, x + 32);
-            tmem_wait_stores();
-            if (key0 < min_lo || (key0 + 128 > max_hi && max_hi < P.sk)) {
-                const int s = j % F::kStages;
+            tmem_store32(lanes + 64 * e, x);
+            const float2 sum = add2(sums[0], sums[1]);
+            l += sum.x + sum.y;
+            if (key0 < min_lo || (key0 + 64 > max_hi && max_hi < P.sk)) {
+                const int s = j % F::kStages, key = key0 + threadIdx.x;
                 if (!(ok = W.wait_warp(v_full + 8 * s, (j / F::kStages) & 1))) break;
-                const int key = key0 + threadIdx.x;
-                if (key < min_lo || key >= max_hi) clear_row<DP>(tile_v + s * F::kTileK, 128, threadIdx.x);
+                if (threadIdx.x < 64 && (key < min_lo || key >= max_hi)) clear_row<DP>(tile_v + s * F::kTileK, F::kKeys, e * 64 + threadIdx.x);
                 fence_async_shared();
             }
+            tmem_wait_stores();
             tc_before_sync();
-            bar_arrive(p_full);
+            bar_arrive(p_full + 8 * e);
         }
         if (ok && n) {
-            ok = W.wait_warp(pv_done, (n - 1) & 1);
+            ok = W.wait_warp(pv_done + 8 * (F::kHalves - 1), (n - 1) & 1);
             tc_after_sync();
         }
         if (ok) {
@@ -284,7 +285,7 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     }
     tc_before_sync();
     __syncthreads();
-    if (warp == 5) tmem_free<F::kColumns>(tmem);
+    if (warp == 4) tmem_free<F::kColumns>(tmem);
 }
 
 // ------------------------------------------------------------------------------------------------ backward
@@ -349,8 +350,8 @@ __global__ void __launch_bounds__(512) attention_record_kernel(const __grid_cons
     }
     Record* R = P.record + ((int64_t)b * P.n_q + h) * P.records + rec;
     if (part == 0) {
-        R->lse2[r] = lse2;
-        R->delta[r] = delta;
+        R->minus_lse2[r] = -lse2;
+        R->minus_delta[r] = -delta;
         R->lo[r] = lo;
         R->hi[r] = hi;
     }
@@ -378,14 +379,15 @@ __global__ void __launch_bounds__(512) attention_record_kernel(const __grid_cons
     }
 }
 
-// dK and dV of 128 keys.  kSlots sets of 4 warps take the query tiles in turn, each with its own S^T and dP^T.
+// dK and dV of 128 keys.  kSlots sets of 8 warps take the query tiles in turn, each with its own S^T and dP^T; four warps of a set take the
+// first 32 queries, four the others.
 template <int DP, int kSlots> struct Keys {
     static constexpr int kTileK = 128 * DP * 2, kTileQ = 64 * DP * 2;
     static constexpr int kStages = DP == 64 ? 3 : 3;
     static constexpr int kStageBytes = 2 * kTileQ + 1024;
     static constexpr int kSmem = 1024 + 2 * kTileK + kStages * kStageBytes;
     static constexpr int kColDV = kSlots * 128, kColDK = kColDV + DP, kColumns = kColDK + DP <= 256 ? 256 : 512;
-    static constexpr int kThreads = kSlots * 128 + 64;
+    static constexpr int kThreads = kSlots * 256 + 64;
     static constexpr int kPerSM = kColumns == 256 ? 2 : 1;
     static_assert(kColDK + DP <= 512, "tensor memory");
 };
@@ -406,7 +408,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t kv_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kCopyWarp = 4 * kSlots, kMmaWarp = kCopyWarp + 1;
+    constexpr int kCopyWarp = 8 * kSlots, kMmaWarp = kCopyWarp + 1;
 
     const int n_kv = P.n_q / P.group, heads = P.batch * n_kv;
     const int tile = blockIdx.x / heads, bh = blockIdx.x % heads, b = bh / n_kv, hk = bh % n_kv;  // under a causal mask the first keys have the most queries
@@ -415,7 +417,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     if (threadIdx.x == 0) {
         bar_init(kv_full, 1), bar_init(done, 1);
         for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
-        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 128);
+        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 256);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_gave_up = 0, s_first = INT_MAX, s_end = 0;
     }
@@ -484,8 +486,8 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                 if (!(ok = W.wait(ds_full + 8 * slot, (it / kSlots) & 1))) break;
                 tc_after_sync();
                 const uint32_t q = smem_u32(stages) + s * F::kStageBytes, at = tmem + slot * 128;
-                product_ts<T, DP, 64>(tmem + F::kColDV, at, q + F::kTileQ, it > 0);
-                product_ts<T, DP, 64>(tmem + F::kColDK, at + 64, q, it > 0);
+                product_ts<T, DP, 64, 32>(tmem + F::kColDV, at, q + F::kTileQ, 64, it > 0);
+                product_ts<T, DP, 64, 32>(tmem + F::kColDK, at + 64, q, 64, it > 0);
                 mma_commit(free_ + 8 * s);
                 if (it + kSlots < n) ok = scores(it + kSlots);
             }
@@ -493,8 +495,8 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             if (!ok) W.drain(done, 0);
         }
     } else {
-        const int slot = warp >> 2, row = threadIdx.x & 127, key = key0 + row;
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128;
+        const int slot = warp >> 3, part = (warp >> 2) & 1, row = threadIdx.x & 127, key = key0 + row;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128 + part * 32;
         bool ok = true;
         for (int it = slot; it < n; it += kSlots) {
             const int s = it % F::kStages, rec = first + it % per_head;
@@ -503,41 +505,43 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             tc_after_sync();
             char* stage = stages + s * F::kStageBytes;
             const Record& R = *reinterpret_cast<const Record*>(stage + 2 * F::kTileQ);
-            uint32_t x[64], y[64];
+            uint32_t x[32], y[32];
             tmem_load32(x, at);
-            tmem_load32(x + 32, at + 32);
             tmem_load32(y, at + 64);
-            tmem_load32(y + 32, at + 96);
             tmem_wait_loads();
-            const bool masked = a.max_lo > key0 || a.min_hi < key0 + 128;
+            const float2 factor = both(P.scale2);
+            const auto form = [&](int c, auto masked) {  // columns c .. c + 3
+                const float4 ml = *reinterpret_cast<const float4*>(R.minus_lse2 + part * 32 + c), md = *reinterpret_cast<const float4*>(R.minus_delta + part * 32 + c);
+                float2 p[2], ds[2];
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 lse = *reinterpret_cast<const float4*>(R.lse2 + c), delta = *reinterpret_cast<const float4*>(R.delta + c);
-                const float ls[4] = {lse.x, lse.y, lse.z, lse.w}, de[4] = {delta.x, delta.y, delta.z, delta.w};
-                float p[4], ds[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[e] = fast_exp2(fmaf(__uint_as_float(x[c + e]), P.scale2, -ls[e]));
-                    ds[e] = p[e] * (__uint_as_float(y[c + e]) - de[e]);
+                for (int e = 0; e < 2; ++e) {
+                    const float2 s = make_float2(__uint_as_float(x[c + 2 * e]), __uint_as_float(x[c + 2 * e + 1]));
+                    const float2 dp = make_float2(__uint_as_float(y[c + 2 * e]), __uint_as_float(y[c + 2 * e + 1]));
+                    p[e] = exp2_both(fma2(s, factor, e ? make_float2(ml.z, ml.w) : make_float2(ml.x, ml.y)));
+                    ds[e] = mul2(p[e], add2(dp, e ? make_float2(md.z, md.w) : make_float2(md.x, md.y)));
                 }
-                if (masked) {
-                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + c), hi = *reinterpret_cast<const int4*>(R.hi + c);
-                    const int los[4] = {lo.x, lo.y, lo.z, lo.w}, his[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (key < los[e] || key >= his[e]) p[e] = ds[e] = 0.f;
-                        if (his[e] - los[e] == 1) ds[e] = 0.f;  // a softmax of one term is constant
-                    }
+                if constexpr (decltype(masked)::value) {
+                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + part * 32 + c), hi = *reinterpret_cast<const int4*>(R.hi + part * 32 + c);
+                    const auto hide = [&](int l, int h, float& p1, float& ds1) {
+                        if (key < l || key >= h) p1 = ds1 = 0.f;
+                        if (h - l == 1) ds1 = 0.f;  // a softmax of one term is constant
+                    };
+                    hide(lo.x, hi.x, p[0].x, ds[0].x), hide(lo.y, hi.y, p[0].y, ds[0].y), hide(lo.z, hi.z, p[1].x, ds[1].x), hide(lo.w, hi.w, p[1].y, ds[1].y);
                 }
-                x[c / 2] = pack2<T>(p[0], p[1]);
-                x[c / 2 + 1] = pack2<T>(p[2], p[3]);
-                y[c / 2] = pack2<T>(ds[0], ds[1]);
-                y[c / 2 + 1] = pack2<T>(ds[2], ds[3]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) x[c / 2 + e] = pack2<T>(p[e].x, p[e].y), y[c / 2 + e] = pack2<T>(ds[e].x, ds[e].y);
+            };
+            if (a.max_lo > key0 || a.min_hi < key0 + 128) {
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) form(c, std::true_type{});
+            } else {
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) form(c, std::false_type{});
             }
-            tmem_store32(at, x);
-            tmem_store32(at + 64, y);
+            tmem_store16(at, x);
+            tmem_store16(at + 64, y);
             tmem_wait_stores();
-            if (a.max_lo == INT_MAX) {  // a query that sees nothing may hold anything
+            if (a.max_lo == INT_MAX && part == 0) {  // a query that sees nothing may hold anything
                 if (row < 64 ? R.hi[row] == 0 : R.hi[row - 64] == 0) clear_row<DP>(stage + (row < 64 ? 0 : F::kTileQ), 64, row & 63);
                 fence_async_shared();
             }
@@ -546,9 +550,9 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
         }
         if (ok && n) ok = W.wait_warp(done, 0);
         tc_after_sync();
-        if (ok && slot == 0) {
-#pragma unroll
-            for (int what = 0; what < 2; ++what) {
+        if (ok && slot == 0) {  // four warps store dV, four dK
+            {
+                const int what = part;
                 const float f = what ? P.scale : 1.f;
                 const int64_t* st = what ? P.dk_stride : P.dv_stride;
 #pragma unroll
@@ -572,14 +576,14 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     if (warp == kMmaWarp) tmem_free<F::kColumns>(tmem);
 }
 
-// dQ of 128 queries.  kSlots sets of 4 warps take the key tiles in turn.
+// dQ of 128 queries.  kSlots sets of 8 warps take the key tiles in turn, four the first 32 keys of a tile, four the others.
 template <int DP, int kSlots> struct Queries {
     static constexpr int kTileQ = 128 * DP * 2, kTileK = 64 * DP * 2;
     static constexpr int kColDQ = kSlots * 128, kColumns = kColDQ + DP <= 256 ? 256 : 512;
     static constexpr int kPerSM = kColumns == 256 ? 2 : 1;
     static constexpr int kStages = DP == 64 ? 3 : kPerSM == 2 ? 1 : 4;
     static constexpr int kSmem = 1024 + 2 * kTileQ + 2 * kStages * kTileK;
-    static constexpr int kThreads = kSlots * 128 + 64;
+    static constexpr int kThreads = kSlots * 256 + 64;
     static_assert(kColDQ + DP <= 512, "tensor memory");
 };
 
@@ -599,7 +603,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kCopyWarp = 4 * kSlots, kMmaWarp = kCopyWarp + 1;
+    constexpr int kCopyWarp = 8 * kSlots, kMmaWarp = kCopyWarp + 1;
     const int heads = P.batch * P.n_q;
     const int tile = P.causal ? P.q_tiles - 1 - (int)(blockIdx.x / heads) : (int)(blockIdx.x / heads);
     const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
@@ -607,18 +611,18 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     if (threadIdx.x == 0) {
         bar_init(q_full, 1), bar_init(done, 1);
         for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
-        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 128);
+        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 256);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_gave_up = 0;
     }
     if (warp == kMmaWarp) tmem_alloc<F::kColumns>(smem_u32(&s_tmem));
     const int row = threadIdx.x & 127, i = tile * 128 + row;
     int lo = INT_MAX, hi = 0;
-    float lse2 = INFINITY, delta = 0.f;
-    if (warp < 4 * kSlots) {
+    float minus_lse2 = -INFINITY, minus_delta = 0.f;
+    if (warp < 8 * kSlots) {
         if (i < P.sq) {
             const Record& R = P.record[((int64_t)b * P.n_q + h) * P.records + i / kRecord];
-            lse2 = R.lse2[i % kRecord], delta = R.delta[i % kRecord], lo = R.lo[i % kRecord], hi = R.hi[i % kRecord];
+            minus_lse2 = R.minus_lse2[i % kRecord], minus_delta = R.minus_delta[i % kRecord], lo = R.lo[i % kRecord], hi = R.hi[i % kRecord];
         }
         int l = lo, g = hi;
 #pragma unroll
@@ -674,7 +678,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 const int s = j % F::kStages, slot = j % kSlots;
                 if (!(ok = W.wait(ds_full + 8 * slot, (j / kSlots) & 1))) break;
                 tc_after_sync();
-                product_ts<T, DP, 64>(tmem + F::kColDQ, tmem + slot * 128 + 64, smem_u32(stages) + s * 2 * F::kTileK, j > 0);
+                product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + slot * 128 + 64, smem_u32(stages) + s * 2 * F::kTileK, 64, j > 0);
                 mma_commit(free_ + 8 * s);
                 if (j + kSlots < n) ok = scores(j + kSlots);
             }
@@ -682,37 +686,41 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
             if (!ok) W.drain(done, 0);
         }
     } else {
-        const int slot = warp >> 2;
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128;
+        const int slot = warp >> 3, part = (warp >> 2) & 1;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128 + part * 32;
         bool ok = true;
         for (int j = slot; j < n; j += kSlots) {
-            const int s = j % F::kStages, key0 = (first + j) * 64;
+            const int s = j % F::kStages, tile0 = (first + j) * 64, key0 = tile0 + part * 32;
             if (!(ok = W.wait_warp(s_full + 8 * slot, (j / kSlots) & 1))) break;
             tc_after_sync();
-            uint32_t x[64], y[64];
+            uint32_t x[32], y[32];
             tmem_load32(x, at);
-            tmem_load32(x + 32, at + 32);
             tmem_load32(y, at + 64);
-            tmem_load32(y + 32, at + 96);
             tmem_wait_loads();
-            const bool masked = !__all_sync(~0u, lo <= key0 && hi >= key0 + 64);
-#pragma unroll
-            for (int c = 0; c < 64; c += 2) {
-                float ds[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float p = fast_exp2(fmaf(__uint_as_float(x[c + e]), P.scale2, -lse2));
-                    ds[e] = p * (__uint_as_float(y[c + e]) - delta);
-                    if (masked && (key0 + c + e < lo || key0 + c + e >= hi || hi - lo == 1)) ds[e] = 0.f;  // a softmax of one term is constant
+            const float2 factor = both(P.scale2), ml = both(minus_lse2), md = both(minus_delta);
+            const auto form = [&](int c, auto masked) {  // columns c, c + 1
+                const float2 s = make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), dp = make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1]));
+                float2 ds = mul2(exp2_both(fma2(s, factor, ml)), add2(dp, md));
+                if constexpr (decltype(masked)::value) {
+                    const bool one = hi - lo == 1;  // a softmax of one term is constant
+                    if (key0 + c < lo || key0 + c >= hi || one) ds.x = 0.f;
+                    if (key0 + c + 1 < lo || key0 + c + 1 >= hi || one) ds.y = 0.f;
                 }
-                y[c / 2] = pack2<T>(ds[0], ds[1]);
+                y[c / 2] = pack2<T>(ds.x, ds.y);
+            };
+            if (!__all_sync(~0u, lo <= key0 && hi >= key0 + 32)) {
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) form(c, std::true_type{});
+            } else {
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) form(c, std::false_type{});
             }
-            tmem_store32(at + 64, y);
+            tmem_store16(at + 64, y);
             tmem_wait_stores();
-            if (key0 < min_lo || (key0 + 64 > max_hi && max_hi < P.sk)) {
+            if (part == 0 && (tile0 < min_lo || (tile0 + 64 > max_hi && max_hi < P.sk))) {
                 // the copy's writes become visible through its own barrier
                 if (!(ok = W.wait_warp(full + 8 * s, (j / F::kStages) & 1))) break;
-                if (row < 64 && (key0 + row < min_lo || key0 + row >= max_hi)) clear_row<DP>(stages + s * 2 * F::kTileK, 64, row);
+                if (row < 64 && (tile0 + row < min_lo || tile0 + row >= max_hi)) clear_row<DP>(stages + s * 2 * F::kTileK, 64, row);
                 fence_async_shared();
             }
             tc_before_sync();
@@ -722,7 +730,8 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
         tc_after_sync();
         if (ok && slot == 0) {
 #pragma unroll
-            for (int c = 0; c < DP / 32; ++c) {
+            for (int c2 = 0; c2 < DP / 64; ++c2) {
+                const int c = 2 * c2 + part;
                 uint32_t o[32];
                 if (n) {
                     tmem_load32(o, lanes + F::kColDQ + 32 * c);
@@ -822,8 +831,8 @@ int forward(const halos_attention_args* a) {
     CUtensorMap q, k{}, v{};
     if (int rc = make_map(&q, a, a->q, a->sq, a->n_q, a->q_stride, 128)) return rc;
     if (a->sk) {
-        if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, 128)) return rc;
-        if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, 128)) return rc;
+        if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, F::kKeys)) return rc;
+        if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, F::kKeys)) return rc;
     }
     if (int rc = allow_smem(attention_fwd_kernel<T, DP>, F::kSmem)) return rc;
     attention_fwd_kernel<T, DP><<<P.q_tiles * P.batch * P.n_q, F::kThreads, F::kSmem, (cudaStream_t)a->stream>>>(P, q, k, v);
@@ -901,6 +910,6 @@ extern "C" int halos_attention_bwd(const halos_attention_args* a) {
     if (workspace(a) && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < workspace(a)))
         return fail(HALOS_ERR_INVALID_ARG, "attention: workspace missing, unaligned or too small");
     if (int rc = enter(a->device)) return rc;
-    if (a->dtype == HALOS_BF16) return a->head_dim <= 64 ? backward<__nv_bfloat16, 64, 1, 1>(a) : backward<__nv_bfloat16, 128, 2, 3>(a);
-    return a->head_dim <= 64 ? backward<__half, 64, 1, 1>(a) : backward<__half, 128, 2, 3>(a);
+    if (a->dtype == HALOS_BF16) return a->head_dim <= 64 ? backward<__nv_bfloat16, 64, 1, 1>(a) : backward<__nv_bfloat16, 128, 2, 1>(a);
+    return a->head_dim <= 64 ? backward<__half, 64, 1, 1>(a) : backward<__half, 128, 2, 1>(a);
 }

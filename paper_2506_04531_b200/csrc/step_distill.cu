@@ -316,24 +316,6 @@ template <typename T> struct Cut {
     __device__ __forceinline__ int single(int i) const { return i < head ? i : i - head + tail; }
 };
 
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
-    return r;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<uint64_t&>(r))
-        : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
-    return r;
-}
-
 // A 32-bit word of a row (one element of 32 bits or two of 16): -infinity throughout, the larger of two, the largest in one.
 template <typename T> __device__ __forceinline__ uint32_t low_word();
 template <> __device__ __forceinline__ uint32_t low_word<float>() { return 0xff800000u; }
@@ -440,11 +422,12 @@ __device__ void describe_row(const DistillParams& P, const T* z, int64_t row, bo
     }
 }
 
-// kPower: T = 2^squarings, so exp(z) = exp(z/T)^T.
-template <typename T, bool kPower, int kThreads>
+// kSquarings: T = 1, 2, 4 as 0, 1, 2, where exp(z) = exp(z/T)^T; any other T as -1.
+template <typename T, int kSquarings, int kThreads>
 __global__ void __launch_bounds__(kThreads + 32, Held<kThreads>::kPerSM)
-distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int squarings, int* fault) {
+distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int* fault) {
     using H = Held<kThreads>;
+    constexpr bool kPower = kSquarings >= 0;
     constexpr int N = 16 / sizeof(T), kPairs = Pairs<T>::kCount, U = H::kUnroll;
     extern __shared__ __align__(128) char smem[];  // a row's whole vectors, then two sets of the teacher's entries
     __shared__ uint64_t bars[2 * H::kMostChunks + 4];  // full and free of each chunk, described[2], used[2]
@@ -500,17 +483,15 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
     const float c1 = kLog2e, cT = kLog2e / P.temperature;
     const float2 cTT = make_float2(cT, cT), c11 = make_float2(c1, c1);
     const uint4* held = reinterpret_cast<const uint4*>(smem);
-    // exp2 of d cT, and of d c1 (its power where the temperature allows)
-    const auto both = [&](float2 dT, float2 d1, float2& eT, float2& e1) {
-        const float2 a = mul2(dT, cTT);
-        eT = make_float2(fast_exp2(a.x), fast_exp2(a.y));
-        if (kPower) {
+    // exp2 of d cT, and of d c1 (a power of the first where the temperature allows)
+    const auto exponentials = [&](float2 dT, float2 d1, float2& eT, float2& e1) {
+        eT = exp2_both(mul2(dT, cTT));
+        if constexpr (kPower) {
             e1 = eT;
-            if (squarings > 0) e1 = mul2(e1, e1);
-            if (squarings > 1) e1 = mul2(e1, e1);
+#pragma unroll
+            for (int i = 0; i < kSquarings; ++i) e1 = mul2(e1, e1);
         } else {
-            const float2 o = mul2(d1, c11);
-            e1 = make_float2(fast_exp2(o.x), fast_exp2(o.y));
+            e1 = exp2_both(mul2(d1, c11));
         }
     };
     int it = 0;
@@ -530,8 +511,9 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
             const auto add = [&](float2 f) {
                 const float2 d = add2(f, minus);
                 float2 eT, e1;
-                both(d, d, eT, e1);
-                sT = add2(sT, eT), s1 = add2(s1, e1);
+                exponentials(d, d, eT, e1);
+                sT = add2(sT, eT);
+                if (kSquarings != 0) s1 = add2(s1, e1);
             };
             add(make_float2(extra, -INFINITY));
             for (int k = 0; k < chunks; ++k) {
@@ -548,7 +530,7 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
                 const float top = max_in_word<T>(top_word);
                 if (top > m) {
                     const float fT = m == -INFINITY ? 0.f : fast_exp2((m - top) * cT), f1 = m == -INFINITY ? 0.f : fast_exp2((m - top) * c1);
-                    sT = mul2(sT, make_float2(fT, fT)), s1 = mul2(s1, make_float2(f1, f1));
+                    sT = mul2(sT, make_float2(fT, fT)), s1 = mul2(s1, make_float2(f1, f1));  // s1 stays 0 where T = 1
                     m = top, minus = make_float2(-m, -m);
                 }
 #pragma unroll
@@ -560,6 +542,7 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
                     if (lane == 0) bar_arrive(free_ + 8 * k);
                 }
             }
+            if (kSquarings == 0) s1 = sT;
             float M = warp_max(m);
             const float d = m == -INFINITY ? 0.f : m - M;  // who has nothing has sums of 0, or a NaN
             float S1 = warp_sum((s1.x + s1.y) * fast_exp2(d * c1)), ST = warp_sum((sT.x + sT.y) * fast_exp2(d * cT));
@@ -594,11 +577,11 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
             const float a = P.labels ? g * (1.f - P.mix) : 0.f, bT = S.any ? g * P.mix * P.temperature : 0.f;
             const float LT = P.temperature * lseT;
             const float a1 = kPower ? a * fast_exp2((LT - lse1) * kLog2e) : a;
-            const float2 minusT = make_float2(-LT, -LT), minus1 = make_float2(-lse1, -lse1), aa = make_float2(a1, a1), bb = make_float2(bT, bT);
+            const float2 minusT = make_float2(-LT, -LT), minus1 = make_float2(-lse1, -lse1), aa = make_float2(a1, a1), bb = make_float2(bT, bT), ab = add2(aa, bb);
             const auto gradient = [&](float2 f) -> float2 {
                 float2 qT, q1;
-                both(add2(f, minusT), kPower ? f : add2(f, minus1), qT, q1);
-                return fma2(aa, q1, mul2(bb, qT));
+                exponentials(add2(f, minusT), kPower ? f : add2(f, minus1), qT, q1);
+                return kSquarings == 0 ? mul2(ab, qT) : fma2(aa, q1, mul2(bb, qT));
             };
             T* dz = reinterpret_cast<T*>(P.dz) + row * P.dz_stride;
             uint4* out = reinterpret_cast<uint4*>(dz + c.head);
@@ -658,27 +641,27 @@ template <typename T>
 int held_bytes(const DistillParams& P) { return (int)(P.vocab * sizeof(T) / 16 * 16 + P.k * 24); }
 constexpr int kMostHeld = 225 * 1024;  // of 227 KB to a CTA, beside what the kernel declares itself
 
-template <typename T, bool kPower, int kThreads>
-int launch_held(const DistillParams& P, int64_t rows, int mode, int squarings, int sms, int* fault, cudaStream_t st) {
+template <typename T, int kSquarings, int kThreads>
+int launch_held(const DistillParams& P, int64_t rows, int mode, int sms, int* fault, cudaStream_t st) {
     using H = Held<kThreads>;
-    auto* kernel = distill_held_kernel<T, kPower, kThreads>;
+    auto* kernel = distill_held_kernel<T, kSquarings, kThreads>;
     const int bytes = held_bytes<T>(P);
     if (int rc = allow_smem(kernel, bytes)) return rc;
     const int fit = kSharedPerSM / (bytes + 3072), per_sm = fit < 1 ? 1 : fit < H::kPerSM ? fit : H::kPerSM;
     const int64_t most = (int64_t)sms * per_sm;
-    kernel<<<(unsigned)(rows < most ? rows : most), kThreads + 32, bytes, st>>>(P, (int)rows, mode, squarings, fault);
+    kernel<<<(unsigned)(rows < most ? rows : most), kThreads + 32, bytes, st>>>(P, (int)rows, mode, fault);
     return cuda_status(cudaGetLastError(), "distill launch");
 }
 
 // Small CTAs for short rows: many of them hide each other's latencies, and a row's fixed cost (a reduction, two barriers)
 // falls on fewer threads.  From half of an SM's shared memory on there is one CTA to an SM, which then needs all the threads.
-template <typename T, bool kPower>
-int by_length(const DistillParams& P, int64_t rows, int mode, int squarings, int sms, int* fault, cudaStream_t st) {
+template <typename T, int kSquarings>
+int by_length(const DistillParams& P, int64_t rows, int mode, int sms, int* fault, cudaStream_t st) {
     const int64_t bytes = P.vocab * (int64_t)sizeof(T);
-    if (bytes <= 4096) return launch_held<T, kPower, 32>(P, rows, mode, squarings, sms, fault, st);
-    if (bytes <= 32768) return launch_held<T, kPower, 128>(P, rows, mode, squarings, sms, fault, st);
-    if (bytes <= 110 * 1024) return launch_held<T, kPower, 256>(P, rows, mode, squarings, sms, fault, st);
-    return launch_held<T, kPower, 512>(P, rows, mode, squarings, sms, fault, st);
+    if (bytes <= 4096) return launch_held<T, kSquarings, 32>(P, rows, mode, sms, fault, st);
+    if (bytes <= 32768) return launch_held<T, kSquarings, 128>(P, rows, mode, sms, fault, st);
+    if (bytes <= 110 * 1024) return launch_held<T, kSquarings, 256>(P, rows, mode, sms, fault, st);
+    return launch_held<T, kSquarings, 512>(P, rows, mode, sms, fault, st);
 }
 
 template <typename T, Mode kMode, int kSquarings>
@@ -697,10 +680,10 @@ int by_temperature(const DistillParams& P, int64_t rows, int32_t device, cudaStr
         int* fault = nullptr;
         if (int rc = fault_mark(&fault)) return rc;
         const int sms = sm_count(device);
-        if (P.temperature == 1.f) return by_length<T, true>(P, rows, kMode, 0, sms, fault, st);
-        if (P.temperature == 2.f) return by_length<T, true>(P, rows, kMode, 1, sms, fault, st);
-        if (P.temperature == 4.f) return by_length<T, true>(P, rows, kMode, 2, sms, fault, st);
-        return by_length<T, false>(P, rows, kMode, 0, sms, fault, st);
+        if (P.temperature == 1.f) return by_length<T, 0>(P, rows, kMode, sms, fault, st);
+        if (P.temperature == 2.f) return by_length<T, 1>(P, rows, kMode, sms, fault, st);
+        if (P.temperature == 4.f) return by_length<T, 2>(P, rows, kMode, sms, fault, st);
+        return by_length<T, -1>(P, rows, kMode, sms, fault, st);
     }
     if (P.temperature == 1.f) return launch<T, kMode, 0>(P, rows, st);
     if (P.temperature == 2.f) return launch<T, kMode, 1>(P, rows, st);

@@ -89,6 +89,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t* r, uint32_t at) {
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(at));
 }
+__device__ __forceinline__ void tmem_load16(uint32_t* r, uint32_t at) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at));
+}
 __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
@@ -150,18 +158,13 @@ __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, int rows_a, u
         mma_ss(d, operand(a + (k / 4) * rows_a * 128 + (k % 4) * 32, 16), operand(b + (k / 4) * rows_b * 128 + (k % 4) * 32, 16),
                mma_shape<T, 128, N, false>(), k > 0);
 }
-// D[128 x N] (+)= A[128 x K] B[K x N]: A in tensor memory, B's rows along K in shared memory.
-template <typename T, int N, int K>
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, bool add) {
+// D[128 x N] (+)= A[128 x K] B[K x N]: A in tensor memory, 32 summed elements every kApart columns (16: without gaps), B's rows along K
+// in shared memory, sub-tiles of `rows_b` rows.
+template <typename T, int N, int K, int kApart>
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, int rows_b, bool add) {
 #pragma unroll
     for (int k = 0; k < K / 16; ++k)
-        mma_ts(d, a + k * 8, operand(b + k * 2048, K * 128), mma_shape<T, 128, N, true>(), add || k > 0);
-}
-
-__device__ __forceinline__ float fast_exp2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
+        mma_ts(d, a + (k / 2) * kApart + (k % 2) * 8, operand(b + k * 2048, rows_b * 128), mma_shape<T, 128, N, true>(), add || k > 0);
 }
 
 }  // namespace halos_step
