@@ -24,6 +24,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRecord = 64;   // queries to a record
+// Of 64 probabilities relative to a maximum that may be an old one.  Any bound that keeps a single one within 16-bit floats would do.
+constexpr float kMostSum = 1024.f;
 
 // What the backward pass knows of 64 queries of a head before it starts.  A query that sees nothing, or is none, has
 // minus_lse2 = -infinity: its probabilities are 0.
@@ -85,20 +87,22 @@ __device__ __forceinline__ void clear_row(char* tile, int rows, int row) {
 
 // ------------------------------------------------------------------------------------------------ forward
 
-// Heads of 64: S of 64 keys at a time beside O takes 128 columns of tensor memory, so four CTAs share an SM and fill each other's
-// waits.  Heads of 128: O alone takes 128, two CTAs are left, and S of 128 keys halves how often Q is read from
-// shared memory, which 64 keys would have the product wait for.  The softmax takes 64 keys at a time either way.
+// Two CTAs to an SM, each with half of its tensor memory: beside O there is room for S of 64 keys three times (heads of 64) or
+// twice (of 128).  The products run that far ahead, so that the softmax, which is what bounds this kernel (16
+// exponentials per clock), finds its next S done.  P lies over its S.
 template <int DP> struct Forward {
-    static constexpr int kKeys = DP == 64 ? 64 : 128, kHalves = kKeys / 64;
-    static constexpr int kStages = DP == 64 ? 2 : 1;
-    static constexpr int kTileQ = 128 * DP * 2, kTileK = kKeys * DP * 2;
+    static constexpr int kRing = DP == 64 ? 3 : 2;
+    static constexpr int kStages = DP == 64 ? 4 : 2;
+    static constexpr int kTileQ = 128 * DP * 2, kTileK = 64 * DP * 2;
     static constexpr int kSmem = 1024 + kTileQ + 2 * kStages * kTileK;
-    static constexpr int kColO = kKeys, kColumns = kKeys + DP;   // P lies over S, each 64 keys over their own
-    static constexpr int kPerSM = 512 / kColumns, kThreads = 160;
+    static constexpr int kColO = 64 * kRing, kColumns = 256;
+    static constexpr int kThreads = 192;
+    // With one place the wait for PV of a tile could miss that of the next: they would share a barrier.
+    static_assert(kRing > 1 && kColO + DP <= kColumns, "tensor memory");
 };
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(160, Forward<DP>::kPerSM)
+__global__ void __launch_bounds__(192, 2)
 attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ CUtensorMap map_q,
                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using F = Forward<DP>;
@@ -107,11 +111,11 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     char* tile_q = smem;
     char* tile_k = smem + F::kTileQ;
     char* tile_v = tile_k + F::kStages * F::kTileK;
-    __shared__ uint64_t bars[3 + 2 * F::kHalves + 2 * F::kStages];
+    __shared__ uint64_t bars[2 + 3 * F::kRing + 4 * F::kStages];
     __shared__ uint32_t s_tmem;
     __shared__ int s_gave_up, s_lo[4], s_hi[4];
-    const uint32_t q_full = smem_u32(bars), s_full = q_full + 8, left = q_full + 16, p_full = q_full + 24, pv_done = p_full + 8 * F::kHalves;
-    const uint32_t k_full = pv_done + 8 * F::kHalves, v_full = k_full + 8 * F::kStages;
+    const uint32_t q_full = smem_u32(bars), left = q_full + 8, s_full = q_full + 16, p_full = s_full + 8 * F::kRing, pv_done = p_full + 8 * F::kRing;
+    const uint32_t k_full = pv_done + 8 * F::kRing, v_full = k_full + 8 * F::kStages, k_free = v_full + 8 * F::kStages, v_free = k_free + 8 * F::kStages;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // Longest rows first where the mask is causal.
@@ -120,9 +124,9 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
 
     if (threadIdx.x == 0) {
-        bar_init(q_full, 1), bar_init(s_full, 1), bar_init(left, 1);
-        for (int e = 0; e < F::kHalves; ++e) bar_init(p_full + 8 * e, 128), bar_init(pv_done + 8 * e, 1);
-        for (int s = 0; s < F::kStages; ++s) bar_init(k_full + 8 * s, 1), bar_init(v_full + 8 * s, 1);
+        bar_init(q_full, 1), bar_init(left, 1);
+        for (int r = 0; r < F::kRing; ++r) bar_init(s_full + 8 * r, 1), bar_init(p_full + 8 * r, 128), bar_init(pv_done + 8 * r, 1);
+        for (int s = 0; s < F::kStages; ++s) bar_init(k_full + 8 * s, 1), bar_init(v_full + 8 * s, 1), bar_init(k_free + 8 * s, 1), bar_init(v_free + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_gave_up = 0;
     }
@@ -140,57 +144,58 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     tc_after_sync();
     const uint32_t tmem = s_tmem;
     const int min_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), max_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
-    const int first = max_hi ? min_lo / F::kKeys : 0, n = max_hi ? (max_hi + F::kKeys - 1) / F::kKeys - first : 0;
+    const int first = max_hi ? min_lo / 64 : 0, n = max_hi ? (max_hi + 63) / 64 - first : 0;
     const Waits W{&s_gave_up, P.fault};
 
-    if (warp == 4) {
-        // One thread issues copies and products.  A tile of K may be overwritten when its S is done, one of V when its PV is; both come
-        // long before this thread has anything else to do.
+    if (warp == 5) {
         if (lane == 0 && n) {
-            const auto load = [&](const CUtensorMap* map, char* tiles, uint32_t bars, int j) {
-                const uint32_t s = j % F::kStages, bar = bars + 8 * s;
-                bar_expect(bar, F::kTileK);
-                for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tiles) + s * F::kTileK + d * F::kKeys * 128, map, bar, d * 64, (first + j) * F::kKeys, hk, b);
-            };
-            const auto scores = [&](int j) -> bool {
-                const int s = j % F::kStages;
-                if (!W.wait(k_full + 8 * s, (j / F::kStages) & 1)) return false;
-                tc_after_sync();
-                product_ss<T, F::kKeys, DP>(tmem, smem_u32(tile_q), 128, smem_u32(tile_k) + s * F::kTileK, F::kKeys);
-                mma_commit(s_full);
-                return true;
-            };
             bar_expect(q_full, F::kTileQ);
             for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
-            int k_loads = 0, v_loads = 0;
-            for (; k_loads < F::kStages && k_loads < n; ++k_loads, ++v_loads) {
-                load(&map_k, tile_k, k_full, k_loads);
-                load(&map_v, tile_v, v_full, v_loads);
+            const auto load = [&](const CUtensorMap* map, uint32_t tile_at, uint32_t bar, int j) {
+                bar_expect(bar, F::kTileK);
+                for (int d = 0; d < DP / 64; ++d) tma_load(tile_at + d * 64 * 128, map, bar, d * 64, (first + j) * 64, hk, b);
+            };
+            int k_loads = 0, v_loads = 0, s = 0, use = 1;
+            for (int j = 0; j < n; ++j) {
+                if (j >= F::kStages && !W.wait(k_free + 8 * s, use)) break;
+                load(&map_k, smem_u32(tile_k) + s * F::kTileK, k_full + 8 * s, k_loads++);
+                if (j >= F::kStages && !W.wait(v_free + 8 * s, use)) break;
+                load(&map_v, smem_u32(tile_v) + s * F::kTileK, v_full + 8 * s, v_loads++);
+                if (++s == F::kStages) s = 0, use ^= 1;
             }
-            bool ok = W.wait(q_full, 0) && scores(0);
-            for (int j = 0; ok && j < n; ++j) {
-                const int s = j % F::kStages;
-                if (!(ok = W.wait(s_full, j & 1))) break;
-                if (k_loads < n) load(&map_k, tile_k, k_full, k_loads++);
-                if (!(ok = W.wait(v_full + 8 * s, (j / F::kStages) & 1))) break;
-#pragma unroll
-                for (int e = 0; ok && e < F::kHalves; ++e) {
-                    if (!(ok = W.wait(p_full + 8 * e, j & 1))) break;
-                    tc_after_sync();
-                    product_ts<T, DP, 64, 16>(tmem + F::kColO, tmem + 64 * e, smem_u32(tile_v) + s * F::kTileK + e * 64 * 128, F::kKeys, j > 0 || e > 0);
-                    mma_commit(pv_done + 8 * e);
-                }
-                if (ok && j + 1 < n) ok = scores(j + 1);
-                if (ok && v_loads < n) {
-                    if ((ok = W.wait(pv_done + 8 * (F::kHalves - 1), j & 1))) load(&map_v, tile_v, v_full, v_loads++);
-                }
-            }
-            if (!ok) {  // leaves early: what is in flight still uses shared and tensor memory
-                mma_commit(left);
-                W.drain(left, 0);
+            if (v_loads < n) {  // leaves early: the copies in flight still write to shared memory
                 W.drain(q_full, 0);
                 for (int i = k_loads > F::kStages ? k_loads - F::kStages : 0; i < k_loads; ++i) W.drain(k_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
                 for (int i = v_loads > F::kStages ? v_loads - F::kStages : 0; i < v_loads; ++i) W.drain(v_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+            }
+        }
+    } else if (warp == 4) {
+        if (lane == 0 && n) {
+            int ks = 0, k_use = 0, vs = 0, v_use = 0, r = 0, use = 0;  // stage, place in the ring, and how often they came round
+            const auto scores = [&](int place) -> bool {
+                if (!W.wait(k_full + 8 * ks, k_use)) return false;
+                tc_after_sync();
+                product_ss<T, 64, DP, 128, 64>(tmem + 64 * place, smem_u32(tile_q), smem_u32(tile_k) + ks * F::kTileK);
+                mma_commit(s_full + 8 * place);
+                mma_commit(k_free + 8 * ks);
+                if (++ks == F::kStages) ks = 0, k_use ^= 1;
+                return true;
+            };
+            bool ok = W.wait(q_full, 0);
+            for (int j = 0; ok && j < F::kRing && j < n; ++j) ok = scores(j);
+            for (int j = 0; ok && j < n; ++j) {
+                if (!(ok = W.wait(v_full + 8 * vs, v_use) && W.wait(p_full + 8 * r, use))) break;
+                tc_after_sync();
+                product_ts<T, DP, 64, 16>(tmem + F::kColO, tmem + 64 * r, smem_u32(tile_v) + vs * F::kTileK, j > 0);
+                mma_commit(pv_done + 8 * r);
+                mma_commit(v_free + 8 * vs);
+                if (j + F::kRing < n && !(ok = scores(r))) break;
+                if (++vs == F::kStages) vs = 0, v_use ^= 1;
+                if (++r == F::kRing) r = 0, use ^= 1;
+            }
+            if (!ok) {  // leaves early: products in flight still use tensor memory
+                mma_commit(left);
+                W.drain(left, 0);
             }
         }
     } else {
@@ -199,68 +204,90 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
         const float2 factor = both(P.scale2);
         float m = -INFINITY, l = 0.f;
         bool ok = true;
-        for (int half = 0; half < n * F::kHalves; ++half) {
-            const int j = half / F::kHalves, e = half % F::kHalves, key0 = (first + j) * F::kKeys + e * 64;
-            if (e == 0) {
-                if (!(ok = W.wait_warp(s_full, j & 1))) break;
-                tc_after_sync();
-            }
-            uint32_t x[64];
-            tmem_load32(x, lanes + 64 * e);
-            tmem_load32(x + 32, lanes + 64 * e + 32);
-            tmem_wait_loads();
+        int r = 0, use = 0, before = 0, before_use = 0;
+        uint32_t x[64];
+        const auto fetch = [&](uint32_t* to, int from) {
+            tmem_load32(to, lanes + 64 * from);
+            tmem_load32(to + 32, lanes + 64 * from + 32);
+        };
+        for (int j = 0; j < n; ++j) {
+            const int key0 = (first + j) * 64;
+            if (!(ok = W.wait_warp(s_full + 8 * r, use))) break;
+            tc_after_sync();
+            fetch(x, r);
+            tmem_wait_loads32(x);
+            tmem_hold32(x + 32);
             if (!__all_sync(~0u, lo <= key0 && hi >= key0 + 64)) {
 #pragma unroll
                 for (int c = 0; c < 64; ++c)
                     if (key0 + c < lo || key0 + c >= hi) x[c] = 0xff800000u;
             }
-            float tops[4];
+            // The maximum is not looked for as long as the probabilities stay small without: it was right for the first keys,
+            // and where later ones are much larger the sum shows it.
+            const auto move_maximum = [&]() -> bool {
+                float tops[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tops[c] = __uint_as_float(x[c]);
+                for (int c = 0; c < 4; ++c) tops[c] = __uint_as_float(x[c]);
 #pragma unroll
-            for (int c = 4; c < 64; ++c) tops[c & 3] = fmaxf(tops[c & 3], __uint_as_float(x[c]));
-            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * P.scale2;
-            if (__any_sync(~0u, top > m + 8.f)) {
-                const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : fast_exp2(m - to);
+                for (int c = 4; c < 64; ++c) tops[c & 3] = fmaxf(tops[c & 3], __uint_as_float(x[c]));
+                const float to = fmaxf(m, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * P.scale2);
+                const float f = m == -INFINITY ? 0.f : fast_exp2(m - to);
                 m = to;
                 l *= f;
-                if (half) {  // every product so far is in O; S of this tile came after those of the tile before
-                    if (!(ok = W.wait_warp(pv_done + 8 * ((half - 1) % F::kHalves), ((half - 1) / F::kHalves) & 1))) break;
+                if (j) {  // every product so far is in O
+                    if (!W.wait_warp(pv_done + 8 * before, before_use)) return false;
                     tc_after_sync();
 #pragma unroll
                     for (int c = 0; c < DP / 16; ++c) {
                         uint32_t o[16];
                         tmem_load16(o, lanes + F::kColO + 16 * c);
-                        tmem_wait_loads();
+                        tmem_wait_loads16(o);
 #pragma unroll
                         for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * f);
                         tmem_store16(lanes + F::kColO + 16 * c, o);
                     }
+                    tmem_wait_stores();
                 }
-            }
-            const float2 minus = both(m == -INFINITY ? 0.f : -m);
-            float2 sums[2] = {both(0.f), both(0.f)};
+                return true;
+            };
+            if (__any_sync(~0u, m == -INFINITY) && !(ok = move_maximum())) break;
+            float sum;
+            for (;;) {
+                const float2 minus = both(m == -INFINITY ? 0.f : -m);
+                float2 sums[2] = {both(0.f), both(0.f)};
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-                const float2 p = exp2_both(fma2(make_float2(__uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1])), factor, minus));
-                sums[c & 1] = add2(sums[c & 1], p);
-                x[c] = pack2<T>(p.x, p.y);
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t words[16];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        const float2 p = exp2_both(fma2(make_float2(__uint_as_float(x[32 * c + 2 * q]), __uint_as_float(x[32 * c + 2 * q + 1])), factor, minus));
+                        sums[q & 1] = add2(sums[q & 1], p);
+                        words[q] = pack2<T>(p.x, p.y);
+                    }
+                    tmem_store16(lanes + 64 * r + 16 * c, words);
+                }
+                const float2 pair = add2(sums[0], sums[1]);
+                sum = pair.x + pair.y;
+                if (!__any_sync(~0u, sum > kMostSum)) break;
+                tmem_wait_stores();  // before the same places are written again
+                if (!(ok = move_maximum())) break;
             }
-            tmem_store32(lanes + 64 * e, x);
-            const float2 sum = add2(sums[0], sums[1]);
-            l += sum.x + sum.y;
+            if (!ok) break;
+            l += sum;
             if (key0 < min_lo || (key0 + 64 > max_hi && max_hi < P.sk)) {
                 const int s = j % F::kStages, key = key0 + threadIdx.x;
                 if (!(ok = W.wait_warp(v_full + 8 * s, (j / F::kStages) & 1))) break;
-                if (threadIdx.x < 64 && (key < min_lo || key >= max_hi)) clear_row<DP>(tile_v + s * F::kTileK, F::kKeys, e * 64 + threadIdx.x);
+                if (threadIdx.x < 64 && (key < min_lo || key >= max_hi)) clear_row<DP>(tile_v + s * F::kTileK, 64, threadIdx.x);
                 fence_async_shared();
             }
             tmem_wait_stores();
             tc_before_sync();
-            bar_arrive(p_full + 8 * e);
+            bar_arrive(p_full + 8 * r);
+            before = r, before_use = use;
+            if (++r == F::kRing) r = 0, use ^= 1;
         }
         if (ok && n) {
-            ok = W.wait_warp(pv_done + 8 * (F::kHalves - 1), (n - 1) & 1);
+            ok = W.wait_warp(pv_done + 8 * before, before_use);
             tc_after_sync();
         }
         if (ok) {
@@ -270,7 +297,7 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                 uint32_t o[32];
                 if (n) {
                     tmem_load32(o, lanes + F::kColO + 32 * c);
-                    tmem_wait_loads();
+                    tmem_wait_loads32(o);
                 }
                 if (i < P.sq) {
                     const bool none = hi == 0;
@@ -295,11 +322,12 @@ __device__ __forceinline__ const T* row_of(const char* base, const int64_t* stri
     return reinterpret_cast<const T*>(base) + b * stride[0] + s * stride[1] + h * stride[2];
 }
 
-// The share of thread `part` of 8 in the product of two rows.
-template <typename T>
-__device__ __forceinline__ float dot_share(const T* x, const T* y, int head_dim, int part) {
+// The product of two rows, or the share of it that falls to every eighth vector from `first` on.
+template <typename T, int kStep = 1>
+__device__ __forceinline__ float dot(const T* x, const T* y, int head_dim, int first = 0) {
     float sum = 0.f;
-    for (int c = part * 8; c < head_dim; c += 64) {
+#pragma unroll 4
+    for (int c = first * 8; c < head_dim; c += 8 * kStep) {
         const uint4 a = *reinterpret_cast<const uint4*>(x + c), b = *reinterpret_cast<const uint4*>(y + c);
         const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -333,20 +361,18 @@ __global__ void __launch_bounds__(512) attention_record_kernel(const __grid_cons
     const bool few = hi && hi - lo <= kFewKeys;
     if (hi) {
         lse2 = P.lse[((int64_t)b * P.n_q + h) * P.sq + i] * kLog2e;
-        if (!few) delta = dot_share<T>(row_of<T>(P.o_in, P.o_stride, b, i, h), row_of<T>(P.dout, P.dout_stride, b, i, h), P.head_dim, part);
+        if (!few) delta = dot<T, 8>(row_of<T>(P.o_in, P.o_stride, b, i, h), row_of<T>(P.dout, P.dout_stride, b, i, h), P.head_dim, part);
     }
     delta = sum_of_8(delta);
-    if (__any_sync(~0u, few)) {
-        const int n = few ? hi - lo : 0;
-        for (int j = 0; j < kFewKeys; ++j) {
-            float s = 0.f, dp = 0.f;
-            if (j < n) {
-                s = dot_share<T>(row_of<T>(P.q, P.q_stride, b, i, h), row_of<T>(P.k, P.k_stride, b, lo + j, h / P.group), P.head_dim, part);
-                dp = dot_share<T>(row_of<T>(P.dout, P.dout_stride, b, i, h), row_of<T>(P.v, P.v_stride, b, lo + j, h / P.group), P.head_dim, part);
-            }
-            s = sum_of_8(s), dp = sum_of_8(dp);
-            if (j < n) delta = fmaf(fast_exp2(fmaf(s, P.scale2, -lse2)), dp, delta);
+    if (__any_sync(~0u, few)) {  // each of the eight threads takes every eighth key
+        float sum = 0.f;
+        for (int j = lo + part; few && j < hi; j += 8) {
+            const float s = dot<T>(row_of<T>(P.q, P.q_stride, b, i, h), row_of<T>(P.k, P.k_stride, b, j, h / P.group), P.head_dim);
+            const float dp = dot<T>(row_of<T>(P.dout, P.dout_stride, b, i, h), row_of<T>(P.v, P.v_stride, b, j, h / P.group), P.head_dim);
+            sum = fmaf(fast_exp2(fmaf(s, P.scale2, -lse2)), dp, sum);
         }
+        sum = sum_of_8(sum);
+        if (few) delta = sum;
     }
     Record* R = P.record + ((int64_t)b * P.n_q + h) * P.records + rec;
     if (part == 0) {
@@ -383,7 +409,7 @@ __global__ void __launch_bounds__(512) attention_record_kernel(const __grid_cons
 // first 32 queries, four the others.
 template <int DP, int kSlots> struct Keys {
     static constexpr int kTileK = 128 * DP * 2, kTileQ = 64 * DP * 2;
-    static constexpr int kStages = DP == 64 ? 3 : 3;
+    static constexpr int kStages = 3;
     static constexpr int kStageBytes = 2 * kTileQ + 1024;
     static constexpr int kSmem = 1024 + 2 * kTileK + kStages * kStageBytes;
     static constexpr int kColDV = kSlots * 128, kColDK = kColDV + DP, kColumns = kColDK + DP <= 256 ? 256 : 512;
@@ -402,11 +428,12 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     char* tile_k = smem;
     char* tile_v = smem + F::kTileK;
     char* stages = smem + 2 * F::kTileK;  // each: Q, dO, record
-    __shared__ uint64_t bars[2 + 2 * F::kStages + 2 * kSlots];
+    __shared__ uint64_t bars[2 + 2 * F::kStages + 4 * kSlots];
     __shared__ uint32_t s_tmem;
     __shared__ int s_gave_up, s_first, s_end;
     const uint32_t bar0 = smem_u32(bars);
-    const uint32_t kv_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots;
+    const uint32_t kv_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots,
+                   dp_full = ds_full + 8 * kSlots, s_read = dp_full + 8 * kSlots;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int kCopyWarp = 8 * kSlots, kMmaWarp = kCopyWarp + 1;
 
@@ -417,7 +444,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     if (threadIdx.x == 0) {
         bar_init(kv_full, 1), bar_init(done, 1);
         for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
-        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 256);
+        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 256), bar_init(dp_full + 8 * s, 1), bar_init(s_read + 8 * s, 256);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_gave_up = 0, s_first = INT_MAX, s_end = 0;
     }
@@ -469,27 +496,39 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
         }
     } else if (warp == kMmaWarp) {
         if (lane == 0 && n) {
-            const auto scores = [&](int it) -> bool {
-                const int s = it % F::kStages;
-                if (!W.wait(full + 8 * s, (it / F::kStages) & 1)) return false;
+            // stages of the tile whose scores come next, whose dP comes next, and which is being used up
+            int s1 = 0, use1 = 0, s2 = 0, s3 = 0;
+            const auto tile_at = [&](int s) { return smem_u32(stages) + s * F::kStageBytes; };
+            const auto next = [](int& s) { s = s + 1 == F::kStages ? 0 : s + 1; };
+            const auto scores = [&](int slot) -> bool {
+                if (!W.wait(full + 8 * s1, use1)) return false;
                 tc_after_sync();
-                const uint32_t q = smem_u32(stages) + s * F::kStageBytes, at = tmem + (it % kSlots) * 128;
-                product_ss<T, 64, DP>(at, smem_u32(tile_k), 128, q, 64);
-                product_ss<T, 64, DP>(at + 64, smem_u32(tile_v), 128, q + F::kTileQ, 64);
-                mma_commit(s_full + 8 * (it % kSlots));
+                product_ss<T, 64, DP, 128, 64>(tmem + slot * 128, smem_u32(tile_k), tile_at(s1));
+                mma_commit(s_full + 8 * slot);
+                next(s1);
+                use1 ^= s1 == 0;
                 return true;
             };
+            const auto dp = [&](int slot) {
+                product_ss<T, 64, DP, 128, 64>(tmem + slot * 128 + 64, smem_u32(tile_v), tile_at(s2) + F::kTileQ);
+                mma_commit(dp_full + 8 * slot);
+                next(s2);
+            };
             bool ok = W.wait(kv_full, 0);
-            for (int it = 0; ok && it < kSlots && it < n; ++it) ok = scores(it);
+            for (int it = 0; ok && it < kSlots && it < n; ++it)
+                if ((ok = scores(it))) dp(it);
             for (int it = 0; ok && it < n; ++it) {
-                const int s = it % F::kStages, slot = it % kSlots;
-                if (!(ok = W.wait(ds_full + 8 * slot, (it / kSlots) & 1))) break;
+                const int slot = it % kSlots, use = (it / kSlots) & 1;
+                // S of the tile after next in this slot can follow once this one has been read; dP only when P and dS, which lie over it, are used up
+                if (it + kSlots < n && !(ok = W.wait(s_read + 8 * slot, use) && scores(slot))) break;
+                if (!(ok = W.wait(ds_full + 8 * slot, use))) break;
                 tc_after_sync();
-                const uint32_t q = smem_u32(stages) + s * F::kStageBytes, at = tmem + slot * 128;
-                product_ts<T, DP, 64, 32>(tmem + F::kColDV, at, q + F::kTileQ, 64, it > 0);
-                product_ts<T, DP, 64, 32>(tmem + F::kColDK, at + 64, q, 64, it > 0);
-                mma_commit(free_ + 8 * s);
-                if (it + kSlots < n) ok = scores(it + kSlots);
+                const uint32_t q = tile_at(s3), at = tmem + slot * 128 + 64;
+                product_ts<T, DP, 64, 32>(tmem + F::kColDV, at, q + F::kTileQ, it > 0);
+                product_ts<T, DP, 64, 32>(tmem + F::kColDK, at + 16, q, it > 0);
+                mma_commit(free_ + 8 * s3);
+                next(s3);
+                if (it + kSlots < n) dp(slot);
             }
             mma_commit(done);
             if (!ok) W.drain(done, 0);
@@ -498,48 +537,68 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
         const int slot = warp >> 3, part = (warp >> 2) & 1, row = threadIdx.x & 127, key = key0 + row;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128 + part * 32;
         bool ok = true;
+        int s = slot % F::kStages, use = slot / F::kStages, s_use = 0, rec = per_head ? slot % per_head : 0;
         for (int it = slot; it < n; it += kSlots) {
-            const int s = it % F::kStages, rec = first + it % per_head;
-            const Reach a = reach[rec];
-            if (!(ok = W.wait_warp(full + 8 * s, (it / F::kStages) & 1) && W.wait_warp(s_full + 8 * slot, (it / kSlots) & 1))) break;
+            const Reach a = reach[first + rec];
+            if (!(ok = W.wait_warp(full + 8 * s, use) && W.wait_warp(s_full + 8 * slot, s_use))) break;
             tc_after_sync();
             char* stage = stages + s * F::kStageBytes;
             const Record& R = *reinterpret_cast<const Record*>(stage + 2 * F::kTileQ);
             uint32_t x[32], y[32];
             tmem_load32(x, at);
-            tmem_load32(y, at + 64);
-            tmem_wait_loads();
+            tmem_wait_loads32(x);
+            tc_before_sync();
+            bar_arrive(s_read + 8 * slot);
+            const bool masked = a.max_lo > key0 || a.min_hi < key0 + 128;
             const float2 factor = both(P.scale2);
-            const auto form = [&](int c, auto masked) {  // columns c .. c + 3
-                const float4 ml = *reinterpret_cast<const float4*>(R.minus_lse2 + part * 32 + c), md = *reinterpret_cast<const float4*>(R.minus_delta + part * 32 + c);
-                float2 p[2], ds[2];
+            // P first, while the product dP may still be under way
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float2 s = make_float2(__uint_as_float(x[c + 2 * e]), __uint_as_float(x[c + 2 * e + 1]));
-                    const float2 dp = make_float2(__uint_as_float(y[c + 2 * e]), __uint_as_float(y[c + 2 * e + 1]));
-                    p[e] = exp2_both(fma2(s, factor, e ? make_float2(ml.z, ml.w) : make_float2(ml.x, ml.y)));
-                    ds[e] = mul2(p[e], add2(dp, e ? make_float2(md.z, md.w) : make_float2(md.x, md.y)));
-                }
-                if constexpr (decltype(masked)::value) {
-                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + part * 32 + c), hi = *reinterpret_cast<const int4*>(R.hi + part * 32 + c);
-                    const auto hide = [&](int l, int h, float& p1, float& ds1) {
-                        if (key < l || key >= h) p1 = ds1 = 0.f;
-                        if (h - l == 1) ds1 = 0.f;  // a softmax of one term is constant
-                    };
-                    hide(lo.x, hi.x, p[0].x, ds[0].x), hide(lo.y, hi.y, p[0].y, ds[0].y), hide(lo.z, hi.z, p[1].x, ds[1].x), hide(lo.w, hi.w, p[1].y, ds[1].y);
-                }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) x[c / 2 + e] = pack2<T>(p[e].x, p[e].y), y[c / 2 + e] = pack2<T>(ds[e].x, ds[e].y);
-            };
-            if (a.max_lo > key0 || a.min_hi < key0 + 128) {
-#pragma unroll
-                for (int c = 0; c < 32; c += 4) form(c, std::true_type{});
-            } else {
-#pragma unroll
-                for (int c = 0; c < 32; c += 4) form(c, std::false_type{});
+            for (int c = 0; c < 32; c += 4) {
+                const float4 ml = *reinterpret_cast<const float4*>(R.minus_lse2 + part * 32 + c);
+                const float2 p = exp2_both(fma2(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), factor, make_float2(ml.x, ml.y)));
+                const float2 q = exp2_both(fma2(make_float2(__uint_as_float(x[c + 2]), __uint_as_float(x[c + 3])), factor, make_float2(ml.z, ml.w)));
+                x[c] = __float_as_uint(p.x), x[c + 1] = __float_as_uint(p.y), x[c + 2] = __float_as_uint(q.x), x[c + 3] = __float_as_uint(q.y);
             }
-            tmem_store16(at, x);
-            tmem_store16(at + 64, y);
+            if (masked) {
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + part * 32 + c), hi = *reinterpret_cast<const int4*>(R.hi + part * 32 + c);
+                    if (key < lo.x || key >= hi.x) x[c] = 0;
+                    if (key < lo.y || key >= hi.y) x[c + 1] = 0;
+                    if (key < lo.z || key >= hi.z) x[c + 2] = 0;
+                    if (key < lo.w || key >= hi.w) x[c + 3] = 0;
+                }
+            }
+            if (!(ok = W.wait_warp(dp_full + 8 * slot, s_use))) break;
+            tc_after_sync();
+            tmem_load32(y, at + 64);
+            tmem_wait_loads32(y);
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+                const float4 md = *reinterpret_cast<const float4*>(R.minus_delta + part * 32 + c);
+                const float2 d = add2(make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1])), make_float2(md.x, md.y));
+                const float2 e = add2(make_float2(__uint_as_float(y[c + 2]), __uint_as_float(y[c + 3])), make_float2(md.z, md.w));
+                y[c] = __float_as_uint(d.x), y[c + 1] = __float_as_uint(d.y), y[c + 2] = __float_as_uint(e.x), y[c + 3] = __float_as_uint(e.y);
+            }
+            if (masked) {
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + part * 32 + c), hi = *reinterpret_cast<const int4*>(R.hi + part * 32 + c);
+                    const auto hide = [&](int l, int h, uint32_t& d) {  // a softmax of one term is constant
+                        if (key < l || key >= h || h - l == 1) d = 0;
+                    };
+                    hide(lo.x, hi.x, y[c]), hide(lo.y, hi.y, y[c + 1]), hide(lo.z, hi.z, y[c + 2]), hide(lo.w, hi.w, y[c + 3]);
+                }
+            }
+            uint32_t words[32];
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+                const float2 p = make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+                const float2 ds = mul2(p, make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1])));
+                words[c / 2] = pack2<T>(p.x, p.y);
+                words[16 + c / 2] = pack2<T>(ds.x, ds.y);
+            }
+            tmem_store32(at + 64, words);
             tmem_wait_stores();
             if (a.max_lo == INT_MAX && part == 0) {  // a query that sees nothing may hold anything
                 if (row < 64 ? R.hi[row] == 0 : R.hi[row - 64] == 0) clear_row<DP>(stage + (row < 64 ? 0 : F::kTileQ), 64, row & 63);
@@ -547,6 +606,11 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             }
             tc_before_sync();
             bar_arrive(ds_full + 8 * slot);
+            s_use ^= 1;
+            for (int step = 0; step < kSlots; ++step) {
+                if (++s == F::kStages) s = 0, use ^= 1;
+                if (++rec == per_head) rec = 0;
+            }
         }
         if (ok && n) ok = W.wait_warp(done, 0);
         tc_after_sync();
@@ -560,7 +624,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                     uint32_t o[32];
                     if (n) {
                         tmem_load32(o, lanes + (what ? F::kColDK : F::kColDV) + 32 * c);
-                        tmem_wait_loads();
+                        tmem_wait_loads32(o);
                     }
                     if (key < P.sk) {
 #pragma unroll
@@ -576,34 +640,35 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     if (warp == kMmaWarp) tmem_free<F::kColumns>(tmem);
 }
 
-// dQ of 128 queries.  kSlots sets of 8 warps take the key tiles in turn, four the first 32 keys of a tile, four the others.
-template <int DP, int kSlots> struct Queries {
+// dQ of 128 queries, two CTAs to an SM, the keys 64 at a time; four warps take the first 32 keys of a tile, four the others.
+template <int DP> struct Queries {
     static constexpr int kTileQ = 128 * DP * 2, kTileK = 64 * DP * 2;
-    static constexpr int kColDQ = kSlots * 128, kColumns = kColDQ + DP <= 256 ? 256 : 512;
-    static constexpr int kPerSM = kColumns == 256 ? 2 : 1;
-    static constexpr int kStages = DP == 64 ? 3 : kPerSM == 2 ? 1 : 4;
+    static constexpr int kDPs = DP == 64 ? 2 : 1;                 // places for dP, and dS over it, beside one for S
+    static constexpr int kStages = DP == 64 ? 4 : 1;
+    static constexpr int kColDP = 64, kColDQ = 64 + 64 * kDPs, kColumns = 256;
     static constexpr int kSmem = 1024 + 2 * kTileQ + 2 * kStages * kTileK;
-    static constexpr int kThreads = kSlots * 256 + 64;
-    static_assert(kColDQ + DP <= 512, "tensor memory");
+    static constexpr int kThreads = 256 + 64;
+    static_assert(kColDQ + DP <= kColumns, "tensor memory");
 };
 
-template <typename T, int DP, int kSlots>
-__global__ void __launch_bounds__(Queries<DP, kSlots>::kThreads, Queries<DP, kSlots>::kPerSM)
+template <typename T, int DP>
+__global__ void __launch_bounds__(Queries<DP>::kThreads, 2)
 attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                          const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do) {
-    using F = Queries<DP, kSlots>;
+    using F = Queries<DP>;
     extern __shared__ char smem_raw[];
     char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     char* tile_q = smem;
     char* tile_do = smem + F::kTileQ;
     char* stages = smem + 2 * F::kTileQ;  // each: K, V
-    __shared__ uint64_t bars[2 + 2 * F::kStages + 2 * kSlots];
+    __shared__ uint64_t bars[5 + F::kDPs + 2 * F::kStages];
     __shared__ uint32_t s_tmem;
     __shared__ int s_gave_up, s_lo[4], s_hi[4];
     const uint32_t bar0 = smem_u32(bars);
-    const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots;
+    const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8, s_read = s_full + 16,
+                   dp_full = s_full + 24;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kCopyWarp = 8 * kSlots, kMmaWarp = kCopyWarp + 1;
+    constexpr int kCopyWarp = 8, kMmaWarp = kCopyWarp + 1;
     const int heads = P.batch * P.n_q;
     const int tile = P.causal ? P.q_tiles - 1 - (int)(blockIdx.x / heads) : (int)(blockIdx.x / heads);
     const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
@@ -611,7 +676,8 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     if (threadIdx.x == 0) {
         bar_init(q_full, 1), bar_init(done, 1);
         for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
-        for (int s = 0; s < kSlots; ++s) bar_init(s_full + 8 * s, 1), bar_init(ds_full + 8 * s, 256);
+        bar_init(s_full, 1), bar_init(ds_full, 256), bar_init(s_read, 256);
+        for (int s = 0; s < F::kDPs; ++s) bar_init(dp_full + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_gave_up = 0;
     }
@@ -619,7 +685,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     const int row = threadIdx.x & 127, i = tile * 128 + row;
     int lo = INT_MAX, hi = 0;
     float minus_lse2 = -INFINITY, minus_delta = 0.f;
-    if (warp < 8 * kSlots) {
+    if (warp < 8) {
         if (i < P.sq) {
             const Record& R = P.record[((int64_t)b * P.n_q + h) * P.records + i / kRecord];
             minus_lse2 = R.minus_lse2[i % kRecord], minus_delta = R.minus_delta[i % kRecord], lo = R.lo[i % kRecord], hi = R.hi[i % kRecord];
@@ -662,60 +728,78 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
         }
     } else if (warp == kMmaWarp) {
         if (lane == 0 && n) {
+            const auto tile_at = [&](int j) { return smem_u32(stages) + (j % F::kStages) * 2 * F::kTileK; };
             const auto scores = [&](int j) -> bool {
-                const int s = j % F::kStages;
-                if (!W.wait(full + 8 * s, (j / F::kStages) & 1)) return false;
+                if (!W.wait(full + 8 * (j % F::kStages), (j / F::kStages) & 1)) return false;
                 tc_after_sync();
-                const uint32_t k = smem_u32(stages) + s * 2 * F::kTileK, at = tmem + (j % kSlots) * 128;
-                product_ss<T, 64, DP>(at, smem_u32(tile_q), 128, k, 64);
-                product_ss<T, 64, DP>(at + 64, smem_u32(tile_do), 128, k + F::kTileK, 64);
-                mma_commit(s_full + 8 * (j % kSlots));
+                product_ss<T, 64, DP, 128, 64>(tmem, smem_u32(tile_q), tile_at(j));
+                mma_commit(s_full);
                 return true;
             };
-            bool ok = W.wait(q_full, 0);
-            for (int j = 0; ok && j < kSlots && j < n; ++j) ok = scores(j);
+            const auto dp = [&](int j) {
+                product_ss<T, 64, DP, 128, 64>(tmem + F::kColDP + (j % F::kDPs) * 64, smem_u32(tile_do), tile_at(j) + F::kTileK);
+                mma_commit(dp_full + 8 * (j % F::kDPs));
+            };
+            bool ok = W.wait(q_full, 0) && scores(0);
+            if (ok) dp(0);
             for (int j = 0; ok && j < n; ++j) {
-                const int s = j % F::kStages, slot = j % kSlots;
-                if (!(ok = W.wait(ds_full + 8 * slot, (j / kSlots) & 1))) break;
+                // the next S can follow once this one has been read, the next dP too where it has a place of its own
+                if (F::kStages > 1 && j + 1 < n) {
+                    if (!(ok = W.wait(s_read, j & 1) && scores(j + 1))) break;
+                    if (F::kDPs > 1) dp(j + 1);
+                }
+                if (!(ok = W.wait(ds_full, j & 1))) break;
                 tc_after_sync();
-                product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + slot * 128 + 64, smem_u32(stages) + s * 2 * F::kTileK, 64, j > 0);
-                mma_commit(free_ + 8 * s);
-                if (j + kSlots < n) ok = scores(j + kSlots);
+                product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + F::kColDP + (j % F::kDPs) * 64, tile_at(j), j > 0);
+                mma_commit(free_ + 8 * (j % F::kStages));
+                if (j + 1 < n) {
+                    if (F::kStages == 1 && !(ok = scores(j + 1))) break;
+                    if (F::kDPs == 1) dp(j + 1);
+                }
             }
             mma_commit(done);
             if (!ok) W.drain(done, 0);
         }
     } else {
-        const int slot = warp >> 3, part = (warp >> 2) & 1;
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128 + part * 32;
+        const int part = (warp >> 2) & 1;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const float2 factor = both(P.scale2), ml = both(minus_lse2), md = both(minus_delta);
+        const bool one = hi - lo == 1;  // a softmax of one term is constant
         bool ok = true;
-        for (int j = slot; j < n; j += kSlots) {
+        for (int j = 0; j < n; ++j) {
             const int s = j % F::kStages, tile0 = (first + j) * 64, key0 = tile0 + part * 32;
-            if (!(ok = W.wait_warp(s_full + 8 * slot, (j / kSlots) & 1))) break;
+            const uint32_t at_dp = lanes + F::kColDP + (j % F::kDPs) * 64 + part * 32;
+            if (!(ok = W.wait_warp(s_full, j & 1))) break;
             tc_after_sync();
             uint32_t x[32], y[32];
-            tmem_load32(x, at);
-            tmem_load32(y, at + 64);
-            tmem_wait_loads();
-            const float2 factor = both(P.scale2), ml = both(minus_lse2), md = both(minus_delta);
-            const auto form = [&](int c, auto masked) {  // columns c, c + 1
-                const float2 s = make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), dp = make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1]));
-                float2 ds = mul2(exp2_both(fma2(s, factor, ml)), add2(dp, md));
-                if constexpr (decltype(masked)::value) {
-                    const bool one = hi - lo == 1;  // a softmax of one term is constant
-                    if (key0 + c < lo || key0 + c >= hi || one) ds.x = 0.f;
-                    if (key0 + c + 1 < lo || key0 + c + 1 >= hi || one) ds.y = 0.f;
-                }
-                y[c / 2] = pack2<T>(ds.x, ds.y);
-            };
-            if (!__all_sync(~0u, lo <= key0 && hi >= key0 + 32)) {
+            tmem_load32(x, lanes + part * 32);
+            tmem_wait_loads32(x);
+            tc_before_sync();
+            bar_arrive(s_read);
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) form(c, std::true_type{});
-            } else {
-#pragma unroll
-                for (int c = 0; c < 32; c += 2) form(c, std::false_type{});
+            for (int c = 0; c < 32; c += 2) {
+                const float2 p = exp2_both(fma2(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), factor, ml));
+                x[c] = __float_as_uint(p.x), x[c + 1] = __float_as_uint(p.y);
             }
-            tmem_store16(at + 64, y);
+            if (!(ok = W.wait_warp(dp_full + 8 * (j % F::kDPs), (j / F::kDPs) & 1))) break;
+            tc_after_sync();
+            tmem_load32(y, at_dp);
+            tmem_wait_loads32(y);
+            const bool masked = !__all_sync(~0u, lo <= key0 && hi >= key0 + 32);
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+                const float2 ds = mul2(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), add2(make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1])), md));
+                x[c] = __float_as_uint(ds.x), x[c + 1] = __float_as_uint(ds.y);
+            }
+            if (masked) {
+#pragma unroll
+                for (int c = 0; c < 32; ++c)
+                    if (key0 + c < lo || key0 + c >= hi || one) x[c] = 0;
+            }
+            uint32_t words[16];
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) words[c / 2] = pack2<T>(__uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+            tmem_store16(at_dp, words);
             tmem_wait_stores();
             if (part == 0 && (tile0 < min_lo || (tile0 + 64 > max_hi && max_hi < P.sk))) {
                 // the copy's writes become visible through its own barrier
@@ -724,18 +808,18 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 fence_async_shared();
             }
             tc_before_sync();
-            bar_arrive(ds_full + 8 * slot);
+            bar_arrive(ds_full);
         }
         if (ok && n) ok = W.wait_warp(done, 0);
         tc_after_sync();
-        if (ok && slot == 0) {
+        if (ok) {
 #pragma unroll
             for (int c2 = 0; c2 < DP / 64; ++c2) {
                 const int c = 2 * c2 + part;
                 uint32_t o[32];
                 if (n) {
                     tmem_load32(o, lanes + F::kColDQ + 32 * c);
-                    tmem_wait_loads();
+                    tmem_wait_loads32(o);
                 }
                 if (i < P.sq) {
 #pragma unroll
@@ -831,8 +915,8 @@ int forward(const halos_attention_args* a) {
     CUtensorMap q, k{}, v{};
     if (int rc = make_map(&q, a, a->q, a->sq, a->n_q, a->q_stride, 128)) return rc;
     if (a->sk) {
-        if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, F::kKeys)) return rc;
-        if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, F::kKeys)) return rc;
+        if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, 64)) return rc;
+        if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, 64)) return rc;
     }
     if (int rc = allow_smem(attention_fwd_kernel<T, DP>, F::kSmem)) return rc;
     attention_fwd_kernel<T, DP><<<P.q_tiles * P.batch * P.n_q, F::kThreads, F::kSmem, (cudaStream_t)a->stream>>>(P, q, k, v);
@@ -844,7 +928,7 @@ uint64_t workspace(const halos_attention_args* a) {
     return a->batch * records * (a->n_q * sizeof(Record) + sizeof(Reach));
 }
 
-template <typename T, int DP, int kKeySlots, int kQuerySlots>
+template <typename T, int DP, int kKeySlots>
 int backward(const halos_attention_args* a) {
     AttentionParams P{};
     if (int rc = params(a, P)) return rc;
@@ -853,9 +937,9 @@ int backward(const halos_attention_args* a) {
     cudaStream_t st = (cudaStream_t)a->stream;
     CUtensorMap q{}, d{}, k{}, v{};
     using K = Keys<DP, kKeySlots>;
-    using Q = Queries<DP, kQuerySlots>;
+    using Q = Queries<DP>;
     if (int rc = allow_smem(attention_keys_kernel<T, DP, kKeySlots>, K::kSmem)) return rc;
-    if (int rc = allow_smem(attention_queries_kernel<T, DP, kQuerySlots>, Q::kSmem)) return rc;
+    if (int rc = allow_smem(attention_queries_kernel<T, DP>, Q::kSmem)) return rc;
     if (P.sq) {
         attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 512, 0, st>>>(P);
         if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
@@ -877,7 +961,7 @@ int backward(const halos_attention_args* a) {
         }
         if (int rc = make_map(&q, a, a->q, a->sq, a->n_q, a->q_stride, 128)) return rc;
         if (int rc = make_map(&d, a, a->dout, a->sq, a->n_q, a->dout_stride, 128)) return rc;
-        attention_queries_kernel<T, DP, kQuerySlots><<<P.q_tiles * P.batch * P.n_q, Q::kThreads, Q::kSmem, st>>>(P, q, k, v, d);
+        attention_queries_kernel<T, DP><<<P.q_tiles * P.batch * P.n_q, Q::kThreads, Q::kSmem, st>>>(P, q, k, v, d);
         if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
     }
     return HALOS_OK;
@@ -910,6 +994,6 @@ extern "C" int halos_attention_bwd(const halos_attention_args* a) {
     if (workspace(a) && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < workspace(a)))
         return fail(HALOS_ERR_INVALID_ARG, "attention: workspace missing, unaligned or too small");
     if (int rc = enter(a->device)) return rc;
-    if (a->dtype == HALOS_BF16) return a->head_dim <= 64 ? backward<__nv_bfloat16, 64, 1, 1>(a) : backward<__nv_bfloat16, 128, 2, 1>(a);
-    return a->head_dim <= 64 ? backward<__half, 64, 1, 1>(a) : backward<__half, 128, 2, 1>(a);
+    if (a->dtype == HALOS_BF16) return a->head_dim <= 64 ? backward<__nv_bfloat16, 64, 1>(a) : backward<__nv_bfloat16, 128, 2>(a);
+    return a->head_dim <= 64 ? backward<__half, 64, 1>(a) : backward<__half, 128, 2>(a);
 }

@@ -18,11 +18,12 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// Returns at the latest after a millisecond or so, and at once where the phase is over.
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3; selp.b32 %0, 1, 0, p; }"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
     return ok != 0;
 }
 
@@ -32,8 +33,8 @@ constexpr long long kWaitClocks = 2000000000ll;  // about a second
 struct Waits {
     volatile int* gave_up;  // in shared memory
     int* fault;             // in device memory
-    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
-        if (bar_try(bar, parity)) return true;
+    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const { return bar_try(bar, parity) || wait_longer(bar, parity); }
+    __device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity) const {
         const long long began = clock64();
         while (clock64() - began < kWaitClocks) {
             if (bar_try(bar, parity)) return true;
@@ -74,7 +75,18 @@ template <int kColumns> __device__ __forceinline__ void tmem_free(uint32_t tmem)
 }
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The registers of loads in flight go through the wait, so that nothing made of them can come before it.
+#define HALOS_EIGHT(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+__device__ __forceinline__ void tmem_wait_loads16(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : HALOS_EIGHT(r, 0), HALOS_EIGHT(r, 8)::"memory");
+}
+__device__ __forceinline__ void tmem_wait_loads32(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : HALOS_EIGHT(r, 0), HALOS_EIGHT(r, 8), HALOS_EIGHT(r, 16), HALOS_EIGHT(r, 24)::"memory");
+}
+__device__ __forceinline__ void tmem_hold32(uint32_t* r) {  // for further registers of a wait just made
+    asm volatile("" : HALOS_EIGHT(r, 0), HALOS_EIGHT(r, 8), HALOS_EIGHT(r, 16), HALOS_EIGHT(r, 24)::"memory");
+}
+#undef HALOS_EIGHT
 __device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // 32 columns of this warp's 32 lanes: thread = lane, register = column.
@@ -122,10 +134,9 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
 // As a "K-major" operand the 64 columns run along the summed dimension: 8-row blocks are 1024 bytes apart, and a
 // step of 16 summed elements is 32 bytes.  As an "MN-major" operand the rows do: again 1024 bytes between
 // blocks of 8 summed rows, a step of 16 is 2048 bytes, and the next 64 columns lie one sub-tile further.
-constexpr uint64_t kSwizzle128 = (2ull << 61) | (1ull << 46);
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading_bytes) {
-    return ((uint64_t)(addr & 0x3ffff) >> 4) | ((uint64_t)(leading_bytes >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | kSwizzle128;
-}
+constexpr uint32_t kOperandHigh = (2u << 29) | (1u << 14) | (1024 >> 4);
+__device__ __forceinline__ uint32_t operand_low(uint32_t addr, uint32_t leading_bytes) { return ((addr & 0x3ffff) >> 4) | ((leading_bytes >> 4) << 16); }
+__device__ __forceinline__ uint64_t operand(uint32_t low) { return ((uint64_t)kOperandHigh << 32) | low; }
 template <typename T> struct MmaType;
 template <> struct MmaType<__half> { static constexpr uint32_t id = 0; };
 template <> struct MmaType<__nv_bfloat16> { static constexpr uint32_t id = 1; };
@@ -150,21 +161,22 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// D[128 x N] (+)= A[128 x K] B[N x K]^T, both K-major in shared memory; rows_a, rows_b: rows of a sub-tile.
-template <typename T, int N, int K>
-__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, int rows_a, uint32_t b, int rows_b) {
+// D[128 x N] = A[128 x K] B[N x K]^T, both K-major in shared memory, with sub-tiles of kRowsA and kRowsB rows.
+template <typename T, int N, int K, int kRowsA, int kRowsB>
+__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b) {
+    const uint32_t al = operand_low(a, 16), bl = operand_low(b, 16);
 #pragma unroll
     for (int k = 0; k < K / 16; ++k)
-        mma_ss(d, operand(a + (k / 4) * rows_a * 128 + (k % 4) * 32, 16), operand(b + (k / 4) * rows_b * 128 + (k % 4) * 32, 16),
-               mma_shape<T, 128, N, false>(), k > 0);
+        mma_ss(d, operand(al + (k / 4) * kRowsA * 8 + (k % 4) * 2), operand(bl + (k / 4) * kRowsB * 8 + (k % 4) * 2), mma_shape<T, 128, N, false>(), k > 0);
 }
-// D[128 x N] (+)= A[128 x K] B[K x N]: A in tensor memory, 32 summed elements every kApart columns (16: without gaps), B's rows along K
-// in shared memory, sub-tiles of `rows_b` rows.
+// D[128 x N] (+)= A[128 x K] B[K x N]: A in tensor memory, 32 summed elements every kApart columns (16: without gaps), B's K rows
+// in shared memory.
 template <typename T, int N, int K, int kApart>
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, int rows_b, bool add) {
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, bool add) {
+    const uint32_t bl = operand_low(b, K * 128);
 #pragma unroll
     for (int k = 0; k < K / 16; ++k)
-        mma_ts(d, a + (k / 2) * kApart + (k % 2) * 8, operand(b + k * 2048, rows_b * 128), mma_shape<T, 128, N, true>(), add || k > 0);
+        mma_ts(d, a + (k / 2) * kApart + (k % 2) * 8, operand(bl + k * 128), mma_shape<T, 128, N, true>(), add || k > 0);
 }
 
 }  // namespace halos_step
