@@ -97,8 +97,7 @@ template <int DP> struct Forward {
     static constexpr int kSmem = 1024 + kTileQ + 2 * kStages * kTileK;
     static constexpr int kColO = 64 * kRing, kColumns = 256;
     static constexpr int kThreads = 192;
-    // With one place the wait for PV of a tile could miss that of the next: they would share a barrier.
-    static_assert(kRing > 1 && kColO + DP <= kColumns, "tensor memory");
+    static_assert(kColO + DP <= kColumns, "tensor memory");
 };
 
 template <typename T, int DP>
@@ -116,7 +115,7 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     __shared__ int s_gave_up, s_lo[4], s_hi[4];
     const uint32_t q_full = smem_u32(bars), left = q_full + 8, s_full = q_full + 16, p_full = s_full + 8 * F::kRing, pv_done = p_full + 8 * F::kRing;
     const uint32_t k_full = pv_done + 8 * F::kRing, v_full = k_full + 8 * F::kStages, k_free = v_full + 8 * F::kStages, v_free = k_free + 8 * F::kStages;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
 
     // Longest rows first where the mask is causal.
     const int heads = P.batch * P.n_q;
@@ -142,25 +141,28 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = uniform(s_tmem);
     const int min_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), max_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
-    const int first = max_hi ? min_lo / 64 : 0, n = max_hi ? (max_hi + 63) / 64 - first : 0;
+    const int first = uniform(max_hi ? min_lo / 64 : 0), n = uniform(max_hi ? (max_hi + 63) / 64 - first : 0);
     const Waits W{&s_gave_up, P.fault};
 
     if (warp == 5) {
-        if (lane == 0 && n) {
-            bar_expect(q_full, F::kTileQ);
-            for (int d = 0; d < DP / 64; ++d) tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
-            const auto load = [&](const CUtensorMap* map, uint32_t tile_at, uint32_t bar, int j) {
-                bar_expect(bar, F::kTileK);
-                for (int d = 0; d < DP / 64; ++d) tma_load(tile_at + d * 64 * 128, map, bar, d * 64, (first + j) * 64, hk, b);
+        if (n) {
+            const bool issuer = elected();
+            const auto load = [&](const CUtensorMap* map, uint32_t tile_at, uint32_t bar, int row, int head, int rows) {
+                if (!issuer) return;
+                bar_expect(bar, rows * DP * 2);
+                for (int d = 0; d < DP / 64; ++d) tma_load(tile_at + d * rows * 128, map, bar, d * 64, row, head, b);
             };
+            load(&map_q, smem_u32(tile_q), q_full, tile * 128, h, 128);
             int k_loads = 0, v_loads = 0, s = 0, use = 1;
             for (int j = 0; j < n; ++j) {
-                if (j >= F::kStages && !W.wait(k_free + 8 * s, use)) break;
-                load(&map_k, smem_u32(tile_k) + s * F::kTileK, k_full + 8 * s, k_loads++);
-                if (j >= F::kStages && !W.wait(v_free + 8 * s, use)) break;
-                load(&map_v, smem_u32(tile_v) + s * F::kTileK, v_full + 8 * s, v_loads++);
+                if (j >= F::kStages && !W.wait_warp(k_free + 8 * s, use)) break;
+                load(&map_k, smem_u32(tile_k) + s * F::kTileK, k_full + 8 * s, (first + j) * 64, hk, 64);
+                ++k_loads;
+                if (j >= F::kStages && !W.wait_warp(v_free + 8 * s, use)) break;
+                load(&map_v, smem_u32(tile_v) + s * F::kTileK, v_full + 8 * s, (first + j) * 64, hk, 64);
+                ++v_loads;
                 if (++s == F::kStages) s = 0, use ^= 1;
             }
             if (v_loads < n) {  // leaves early: the copies in flight still write to shared memory
@@ -170,31 +172,36 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
             }
         }
     } else if (warp == 4) {
-        if (lane == 0 && n) {
+        if (n) {
+            const bool issuer = elected();
             int ks = 0, k_use = 0, vs = 0, v_use = 0, r = 0, use = 0;  // stage, place in the ring, and how often they came round
             const auto scores = [&](int place) -> bool {
-                if (!W.wait(k_full + 8 * ks, k_use)) return false;
+                if (!W.wait_warp(k_full + 8 * ks, k_use)) return false;
                 tc_after_sync();
-                product_ss<T, 64, DP, 128, 64>(tmem + 64 * place, smem_u32(tile_q), smem_u32(tile_k) + ks * F::kTileK);
-                mma_commit(s_full + 8 * place);
-                mma_commit(k_free + 8 * ks);
+                if (issuer) {
+                    product_ss<T, 64, DP, 128, 64>(tmem + 64 * place, smem_u32(tile_q), smem_u32(tile_k) + ks * F::kTileK);
+                    mma_commit(s_full + 8 * place);
+                    mma_commit(k_free + 8 * ks);
+                }
                 if (++ks == F::kStages) ks = 0, k_use ^= 1;
                 return true;
             };
-            bool ok = W.wait(q_full, 0);
+            bool ok = W.wait_warp(q_full, 0);
             for (int j = 0; ok && j < F::kRing && j < n; ++j) ok = scores(j);
             for (int j = 0; ok && j < n; ++j) {
-                if (!(ok = W.wait(v_full + 8 * vs, v_use) && W.wait(p_full + 8 * r, use))) break;
+                if (!(ok = W.wait_warp(v_full + 8 * vs, v_use) && W.wait_warp(p_full + 8 * r, use))) break;
                 tc_after_sync();
-                product_ts<T, DP, 64, 16>(tmem + F::kColO, tmem + 64 * r, smem_u32(tile_v) + vs * F::kTileK, j > 0);
-                mma_commit(pv_done + 8 * r);
-                mma_commit(v_free + 8 * vs);
+                if (issuer) {
+                    product_ts<T, DP, 64, 16>(tmem + F::kColO, tmem + 64 * r, smem_u32(tile_v) + vs * F::kTileK, j > 0);
+                    mma_commit(pv_done + 8 * r);
+                    mma_commit(v_free + 8 * vs);
+                }
                 if (j + F::kRing < n && !(ok = scores(r))) break;
                 if (++vs == F::kStages) vs = 0, v_use ^= 1;
                 if (++r == F::kRing) r = 0, use ^= 1;
             }
             if (!ok) {  // leaves early: products in flight still use tensor memory
-                mma_commit(left);
+                if (issuer) mma_commit(left);
                 W.drain(left, 0);
             }
         }
@@ -434,7 +441,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t kv_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots,
                    dp_full = ds_full + 8 * kSlots, s_read = dp_full + 8 * kSlots;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5);
     constexpr int kCopyWarp = 8 * kSlots, kMmaWarp = kCopyWarp + 1;
 
     const int n_kv = P.n_q / P.group, heads = P.batch * n_kv;
@@ -460,34 +467,35 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
-    const uint32_t tmem = s_tmem;
-    const int first = s_first, per_head = s_end ? s_end - first : 0, n = per_head * P.group;
+    const uint32_t tmem = uniform(s_tmem);
+    const int first = uniform(s_first), per_head = uniform(s_end ? s_end - first : 0), n = per_head * P.group;
     const Waits W{&s_gave_up, P.fault};
 
     if (warp == kCopyWarp) {
-        if (lane == 0 && n) {
-            bar_expect(kv_full, 2 * F::kTileK);
-            for (int d = 0; d < DP / 64; ++d) {
-                tma_load(smem_u32(tile_k) + d * 128 * 128, &map_k, kv_full, d * 64, key0, hk, b);
-                tma_load(smem_u32(tile_v) + d * 128 * 128, &map_v, kv_full, d * 64, key0, hk, b);
+        if (n) {
+            const bool issuer = elected();
+            if (issuer) {
+                bar_expect(kv_full, 2 * F::kTileK);
+                for (int d = 0; d < DP / 64; ++d) {
+                    tma_load(smem_u32(tile_k) + d * 128 * 128, &map_k, kv_full, d * 64, key0, hk, b);
+                    tma_load(smem_u32(tile_v) + d * 128 * 128, &map_v, kv_full, d * 64, key0, hk, b);
+                }
             }
-            int it = 0;
-            for (int g = 0; g < P.group && it < n; ++g) {
-                const int h = hk * P.group + g;
-                const Record* records = P.record + ((int64_t)b * P.n_q + h) * P.records;
-                int r = 0;
-                for (; r < per_head; ++r, ++it) {
-                    const int s = it % F::kStages, use = it / F::kStages;
-                    if (use && !W.wait(free_ + 8 * s, (use - 1) & 1)) break;
+            int it = 0, s = 0, use = 1, r = 0, h = hk * P.group;
+            const Record* records = P.record + ((int64_t)b * P.n_q + h) * P.records + first;
+            for (; it < n; ++it) {
+                if (it >= F::kStages && !W.wait_warp(free_ + 8 * s, use)) break;
+                if (issuer) {
                     const uint32_t at = smem_u32(stages) + s * F::kStageBytes, bar = full + 8 * s;
                     bar_expect(bar, F::kStageBytes);
                     for (int d = 0; d < DP / 64; ++d) {
                         tma_load(at + d * 64 * 128, &map_q, bar, d * 64, (first + r) * 64, h, b);
                         tma_load(at + F::kTileQ + d * 64 * 128, &map_do, bar, d * 64, (first + r) * 64, h, b);
                     }
-                    bulk_load(at + 2 * F::kTileQ, records + first + r, 1024, bar);
+                    bulk_load(at + 2 * F::kTileQ, records + r, 1024, bar);
                 }
-                if (r < per_head) break;
+                if (++s == F::kStages) s = 0, use ^= 1;
+                if (++r == per_head) r = 0, ++h, records += P.records;
             }
             if (it < n) {
                 W.drain(kv_full, 0);
@@ -495,42 +503,49 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             }
         }
     } else if (warp == kMmaWarp) {
-        if (lane == 0 && n) {
+        if (n) {
+            const bool issuer = elected();
             // stages of the tile whose scores come next, whose dP comes next, and which is being used up
-            int s1 = 0, use1 = 0, s2 = 0, s3 = 0;
+            int s1 = 0, use1 = 0, s2 = 0, s3 = 0, slot = 0, use = 0;
             const auto tile_at = [&](int s) { return smem_u32(stages) + s * F::kStageBytes; };
             const auto next = [](int& s) { s = s + 1 == F::kStages ? 0 : s + 1; };
             const auto scores = [&](int slot) -> bool {
-                if (!W.wait(full + 8 * s1, use1)) return false;
+                if (!W.wait_warp(full + 8 * s1, use1)) return false;
                 tc_after_sync();
-                product_ss<T, 64, DP, 128, 64>(tmem + slot * 128, smem_u32(tile_k), tile_at(s1));
-                mma_commit(s_full + 8 * slot);
+                if (issuer) {
+                    product_ss<T, 64, DP, 128, 64>(tmem + slot * 128, smem_u32(tile_k), tile_at(s1));
+                    mma_commit(s_full + 8 * slot);
+                }
                 next(s1);
                 use1 ^= s1 == 0;
                 return true;
             };
             const auto dp = [&](int slot) {
-                product_ss<T, 64, DP, 128, 64>(tmem + slot * 128 + 64, smem_u32(tile_v), tile_at(s2) + F::kTileQ);
-                mma_commit(dp_full + 8 * slot);
+                if (issuer) {
+                    product_ss<T, 64, DP, 128, 64>(tmem + slot * 128 + 64, smem_u32(tile_v), tile_at(s2) + F::kTileQ);
+                    mma_commit(dp_full + 8 * slot);
+                }
                 next(s2);
             };
-            bool ok = W.wait(kv_full, 0);
+            bool ok = W.wait_warp(kv_full, 0);
             for (int it = 0; ok && it < kSlots && it < n; ++it)
                 if ((ok = scores(it))) dp(it);
             for (int it = 0; ok && it < n; ++it) {
-                const int slot = it % kSlots, use = (it / kSlots) & 1;
-                // S of the tile after next in this slot can follow once this one has been read; dP only when P and dS, which lie over it, are used up
-                if (it + kSlots < n && !(ok = W.wait(s_read + 8 * slot, use) && scores(slot))) break;
-                if (!(ok = W.wait(ds_full + 8 * slot, use))) break;
+                // S of the next tile in this slot can follow once this one has been read; dP only when P and dS, which lie over it, are used up
+                if (it + kSlots < n && !(ok = W.wait_warp(s_read + 8 * slot, use) && scores(slot))) break;
+                if (!(ok = W.wait_warp(ds_full + 8 * slot, use))) break;
                 tc_after_sync();
-                const uint32_t q = tile_at(s3), at = tmem + slot * 128 + 64;
-                product_ts<T, DP, 64, 32>(tmem + F::kColDV, at, q + F::kTileQ, it > 0);
-                product_ts<T, DP, 64, 32>(tmem + F::kColDK, at + 16, q, it > 0);
-                mma_commit(free_ + 8 * s3);
+                if (issuer) {
+                    const uint32_t q = tile_at(s3), at = tmem + slot * 128 + 64;
+                    product_ts<T, DP, 64, 32>(tmem + F::kColDV, at, q + F::kTileQ, it > 0);
+                    product_ts<T, DP, 64, 32>(tmem + F::kColDK, at + 16, q, it > 0);
+                    mma_commit(free_ + 8 * s3);
+                }
                 next(s3);
                 if (it + kSlots < n) dp(slot);
+                if (++slot == kSlots) slot = 0, use ^= 1;
             }
-            mma_commit(done);
+            if (issuer) mma_commit(done);
             if (!ok) W.drain(done, 0);
         }
     } else {
@@ -667,7 +682,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8, s_read = s_full + 16,
                    dp_full = s_full + 24;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int kCopyWarp = 8, kMmaWarp = kCopyWarp + 1;
     const int heads = P.batch * P.n_q;
     const int tile = P.causal ? P.q_tiles - 1 - (int)(blockIdx.x / heads) : (int)(blockIdx.x / heads);
@@ -698,28 +713,33 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = uniform(s_tmem);
     const int min_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), max_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
-    const int first = max_hi ? min_lo / 64 : 0, n = max_hi ? (max_hi + 63) / 64 - first : 0;
+    const int first = uniform(max_hi ? min_lo / 64 : 0), n = uniform(max_hi ? (max_hi + 63) / 64 - first : 0);
     const Waits W{&s_gave_up, P.fault};
 
     if (warp == kCopyWarp) {
-        if (lane == 0 && n) {
-            bar_expect(q_full, 2 * F::kTileQ);
-            for (int d = 0; d < DP / 64; ++d) {
-                tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
-                tma_load(smem_u32(tile_do) + d * 128 * 128, &map_do, q_full, d * 64, tile * 128, h, b);
-            }
-            int j = 0;
-            for (; j < n; ++j) {
-                const int s = j % F::kStages, use = j / F::kStages;
-                if (use && !W.wait(free_ + 8 * s, (use - 1) & 1)) break;
-                const uint32_t at = smem_u32(stages) + s * 2 * F::kTileK, bar = full + 8 * s;
-                bar_expect(bar, 2 * F::kTileK);
+        if (n) {
+            const bool issuer = elected();
+            if (issuer) {
+                bar_expect(q_full, 2 * F::kTileQ);
                 for (int d = 0; d < DP / 64; ++d) {
-                    tma_load(at + d * 64 * 128, &map_k, bar, d * 64, (first + j) * 64, hk, b);
-                    tma_load(at + F::kTileK + d * 64 * 128, &map_v, bar, d * 64, (first + j) * 64, hk, b);
+                    tma_load(smem_u32(tile_q) + d * 128 * 128, &map_q, q_full, d * 64, tile * 128, h, b);
+                    tma_load(smem_u32(tile_do) + d * 128 * 128, &map_do, q_full, d * 64, tile * 128, h, b);
                 }
+            }
+            int j = 0, s = 0, use = 1;
+            for (; j < n; ++j) {
+                if (j >= F::kStages && !W.wait_warp(free_ + 8 * s, use)) break;
+                if (issuer) {
+                    const uint32_t at = smem_u32(stages) + s * 2 * F::kTileK, bar = full + 8 * s;
+                    bar_expect(bar, 2 * F::kTileK);
+                    for (int d = 0; d < DP / 64; ++d) {
+                        tma_load(at + d * 64 * 128, &map_k, bar, d * 64, (first + j) * 64, hk, b);
+                        tma_load(at + F::kTileK + d * 64 * 128, &map_v, bar, d * 64, (first + j) * 64, hk, b);
+                    }
+                }
+                if (++s == F::kStages) s = 0, use ^= 1;
             }
             if (j < n) {
                 W.drain(q_full, 0);
@@ -727,37 +747,50 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
             }
         }
     } else if (warp == kMmaWarp) {
-        if (lane == 0 && n) {
-            const auto tile_at = [&](int j) { return smem_u32(stages) + (j % F::kStages) * 2 * F::kTileK; };
-            const auto scores = [&](int j) -> bool {
-                if (!W.wait(full + 8 * (j % F::kStages), (j / F::kStages) & 1)) return false;
+        if (n) {
+            const bool issuer = elected();
+            int s1 = 0, use1 = 0, s2 = 0, s3 = 0, d2 = 0, d3 = 0;  // stages as for the keys; places of dP
+            const auto tile_at = [&](int s) { return smem_u32(stages) + s * 2 * F::kTileK; };
+            const auto next = [](int& s, int of) { s = s + 1 == of ? 0 : s + 1; };
+            const auto scores = [&]() -> bool {
+                if (!W.wait_warp(full + 8 * s1, use1)) return false;
                 tc_after_sync();
-                product_ss<T, 64, DP, 128, 64>(tmem, smem_u32(tile_q), tile_at(j));
-                mma_commit(s_full);
+                if (issuer) {
+                    product_ss<T, 64, DP, 128, 64>(tmem, smem_u32(tile_q), tile_at(s1));
+                    mma_commit(s_full);
+                }
+                next(s1, F::kStages);
+                use1 ^= s1 == 0;
                 return true;
             };
-            const auto dp = [&](int j) {
-                product_ss<T, 64, DP, 128, 64>(tmem + F::kColDP + (j % F::kDPs) * 64, smem_u32(tile_do), tile_at(j) + F::kTileK);
-                mma_commit(dp_full + 8 * (j % F::kDPs));
+            const auto dp = [&] {
+                if (issuer) {
+                    product_ss<T, 64, DP, 128, 64>(tmem + F::kColDP + d2 * 64, smem_u32(tile_do), tile_at(s2) + F::kTileK);
+                    mma_commit(dp_full + 8 * d2);
+                }
+                next(s2, F::kStages), next(d2, F::kDPs);
             };
-            bool ok = W.wait(q_full, 0) && scores(0);
-            if (ok) dp(0);
+            bool ok = W.wait_warp(q_full, 0) && scores();
+            if (ok) dp();
             for (int j = 0; ok && j < n; ++j) {
                 // the next S can follow once this one has been read, the next dP too where it has a place of its own
                 if (F::kStages > 1 && j + 1 < n) {
-                    if (!(ok = W.wait(s_read, j & 1) && scores(j + 1))) break;
-                    if (F::kDPs > 1) dp(j + 1);
+                    if (!(ok = W.wait_warp(s_read, j & 1) && scores())) break;
+                    if (F::kDPs > 1) dp();
                 }
-                if (!(ok = W.wait(ds_full, j & 1))) break;
+                if (!(ok = W.wait_warp(ds_full, j & 1))) break;
                 tc_after_sync();
-                product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + F::kColDP + (j % F::kDPs) * 64, tile_at(j), j > 0);
-                mma_commit(free_ + 8 * (j % F::kStages));
+                if (issuer) {
+                    product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + F::kColDP + d3 * 64, tile_at(s3), j > 0);
+                    mma_commit(free_ + 8 * s3);
+                }
+                next(s3, F::kStages), next(d3, F::kDPs);
                 if (j + 1 < n) {
-                    if (F::kStages == 1 && !(ok = scores(j + 1))) break;
-                    if (F::kDPs == 1) dp(j + 1);
+                    if (F::kStages == 1 && !(ok = scores())) break;
+                    if (F::kDPs == 1) dp();
                 }
             }
-            mma_commit(done);
+            if (issuer) mma_commit(done);
             if (!ok) W.drain(done, 0);
         }
     } else {

@@ -6,6 +6,16 @@
 
 namespace halos_step {
 
+// ---- warps that act as one ---------------------------------------------------------------------
+// Copies and products are issued by one thread, but the warp goes through the loop together: what it computes is then the same in
+// all lanes, which is where those instructions want their operands.
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.b32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
+}
+template <typename V> __device__ __forceinline__ V uniform(V v) { return __shfl_sync(~0u, v, 0); }
+
 // ---- barriers in shared memory -----------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
