@@ -155,28 +155,24 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                 for (int d = 0; d < DP / 64; ++d) tma_load(tile_at + d * rows * 128, map, bar, d * 64, row, head, b);
             };
             load(&map_q, smem_u32(tile_q), q_full, tile * 128, h, 128);
-            int k_loads = 0, v_loads = 0, s = 0, use = 1;
-            for (int j = 0; j < n; ++j) {
-                if (j >= F::kStages && !W.wait_warp(k_free + 8 * s, use)) break;
+            for (int j = 0, s = 0, use = 1; j < n; ++j) {
+                if (j >= F::kStages) W.wait_warp(k_free + 8 * s, use);
                 load(&map_k, smem_u32(tile_k) + s * F::kTileK, k_full + 8 * s, (first + j) * 64, hk, 64);
-                ++k_loads;
-                if (j >= F::kStages && !W.wait_warp(v_free + 8 * s, use)) break;
+                if (j >= F::kStages) W.wait_warp(v_free + 8 * s, use);
                 load(&map_v, smem_u32(tile_v) + s * F::kTileK, v_full + 8 * s, (first + j) * 64, hk, 64);
-                ++v_loads;
                 if (++s == F::kStages) s = 0, use ^= 1;
             }
-            if (v_loads < n) {  // leaves early: the copies in flight still write to shared memory
+            if (*W.gave_up) {
                 W.drain(q_full, 0);
-                for (int i = k_loads > F::kStages ? k_loads - F::kStages : 0; i < k_loads; ++i) W.drain(k_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
-                for (int i = v_loads > F::kStages ? v_loads - F::kStages : 0; i < v_loads; ++i) W.drain(v_full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+                for (int j = max(0, n - F::kStages); j < n; ++j) W.drain(k_full + 8 * (j % F::kStages), (j / F::kStages) & 1), W.drain(v_full + 8 * (j % F::kStages), (j / F::kStages) & 1);
             }
         }
     } else if (warp == 4) {
         if (n) {
             const bool issuer = elected();
             int ks = 0, k_use = 0, vs = 0, v_use = 0, r = 0, use = 0;  // stage, place in the ring, and how often they came round
-            const auto scores = [&](int place) -> bool {
-                if (!W.wait_warp(k_full + 8 * ks, k_use)) return false;
+            const auto scores = [&](int place) {
+                W.wait_warp(k_full + 8 * ks, k_use);
                 tc_after_sync();
                 if (issuer) {
                     product_ss<T, 64, DP, 128, 64>(tmem + 64 * place, smem_u32(tile_q), smem_u32(tile_k) + ks * F::kTileK);
@@ -184,23 +180,23 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                     mma_commit(k_free + 8 * ks);
                 }
                 if (++ks == F::kStages) ks = 0, k_use ^= 1;
-                return true;
             };
-            bool ok = W.wait_warp(q_full, 0);
-            for (int j = 0; ok && j < F::kRing && j < n; ++j) ok = scores(j);
-            for (int j = 0; ok && j < n; ++j) {
-                if (!(ok = W.wait_warp(v_full + 8 * vs, v_use) && W.wait_warp(p_full + 8 * r, use))) break;
+            W.wait_warp(q_full, 0);
+            for (int j = 0; j < F::kRing && j < n; ++j) scores(j);
+            for (int j = 0; j < n; ++j) {
+                W.wait_warp(v_full + 8 * vs, v_use);
+                W.wait_warp(p_full + 8 * r, use);
                 tc_after_sync();
                 if (issuer) {
                     product_ts<T, DP, 64, 16>(tmem + F::kColO, tmem + 64 * r, smem_u32(tile_v) + vs * F::kTileK, j > 0);
                     mma_commit(pv_done + 8 * r);
                     mma_commit(v_free + 8 * vs);
                 }
-                if (j + F::kRing < n && !(ok = scores(r))) break;
+                if (j + F::kRing < n) scores(r);
                 if (++vs == F::kStages) vs = 0, v_use ^= 1;
                 if (++r == F::kRing) r = 0, use ^= 1;
             }
-            if (!ok) {  // leaves early: products in flight still use tensor memory
+            if (*W.gave_up) {
                 if (issuer) mma_commit(left);
                 W.drain(left, 0);
             }
@@ -210,7 +206,6 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
         const int i = tile * 128 + threadIdx.x;
         const float2 factor = both(P.scale2);
         float m = -INFINITY, l = 0.f;
-        bool ok = true;
         int r = 0, use = 0, before = 0, before_use = 0;
         uint32_t x[64];
         const auto fetch = [&](uint32_t* to, int from) {
@@ -219,7 +214,7 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
         };
         for (int j = 0; j < n; ++j) {
             const int key0 = (first + j) * 64;
-            if (!(ok = W.wait_warp(s_full + 8 * r, use))) break;
+            W.wait_warp(s_full + 8 * r, use);
             tc_after_sync();
             fetch(x, r);
             tmem_wait_loads32(x);
@@ -231,7 +226,7 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
             }
             // The maximum is not looked for as long as the probabilities stay small without: it was right for the first keys,
             // and where later ones are much larger the sum shows it.
-            const auto move_maximum = [&]() -> bool {
+            const auto move_maximum = [&] {
                 float tops[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tops[c] = __uint_as_float(x[c]);
@@ -242,7 +237,7 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                 m = to;
                 l *= f;
                 if (j) {  // every product so far is in O
-                    if (!W.wait_warp(pv_done + 8 * before, before_use)) return false;
+                    W.wait_warp(pv_done + 8 * before, before_use);
                     tc_after_sync();
 #pragma unroll
                     for (int c = 0; c < DP / 16; ++c) {
@@ -255,9 +250,8 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                     }
                     tmem_wait_stores();
                 }
-                return true;
             };
-            if (__any_sync(~0u, m == -INFINITY) && !(ok = move_maximum())) break;
+            if (__any_sync(~0u, m == -INFINITY)) move_maximum();
             float sum;
             for (;;) {
                 const float2 minus = both(m == -INFINITY ? 0.f : -m);
@@ -275,15 +269,14 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                 }
                 const float2 pair = add2(sums[0], sums[1]);
                 sum = pair.x + pair.y;
-                if (!__any_sync(~0u, sum > kMostSum)) break;
+                if (!__any_sync(~0u, sum > kMostSum)) break;  // after the maximum has moved it is 64 at most, or no number
                 tmem_wait_stores();  // before the same places are written again
-                if (!(ok = move_maximum())) break;
+                move_maximum();
             }
-            if (!ok) break;
             l += sum;
             if (key0 < min_lo || (key0 + 64 > max_hi && max_hi < P.sk)) {
                 const int s = j % F::kStages, key = key0 + threadIdx.x;
-                if (!(ok = W.wait_warp(v_full + 8 * s, (j / F::kStages) & 1))) break;
+                W.wait_warp(v_full + 8 * s, (j / F::kStages) & 1);
                 if (threadIdx.x < 64 && (key < min_lo || key >= max_hi)) clear_row<DP>(tile_v + s * F::kTileK, 64, threadIdx.x);
                 fence_async_shared();
             }
@@ -293,11 +286,11 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
             before = r, before_use = use;
             if (++r == F::kRing) r = 0, use ^= 1;
         }
-        if (ok && n) {
-            ok = W.wait_warp(pv_done + 8 * before, before_use);
+        if (n) {
+            W.wait_warp(pv_done + 8 * before, before_use);
             tc_after_sync();
         }
-        if (ok) {
+        {
             const float inv = l > 0.f ? 1.f / l : l;  // a NaN stays one
 #pragma unroll
             for (int c = 0; c < DP / 32; ++c) {
@@ -356,41 +349,54 @@ __device__ __forceinline__ float sum_of_8(float v) {
 // Its D is formed from sum p dp instead, in 32 bits.
 constexpr int kFewKeys = 16;
 
-// Records of 64 queries of a head, and once per batch row their reach.  Eight threads per query.
+// Records of 64 queries of a head, and once per batch row their reach.  Eight threads take four queries, with all their loads in flight at once.
 template <typename T>
-__global__ void __launch_bounds__(512) attention_record_kernel(const __grid_constant__ AttentionParams P) {
-    const int rec = blockIdx.x, h = blockIdx.y, b = blockIdx.z, r = threadIdx.x >> 3, part = threadIdx.x & 7;
-    const int i = rec * kRecord + r;
-    __shared__ Reach s_reach[16];
-    float delta = 0.f, lse2 = INFINITY;
-    int lo, hi;
-    seen_by(P, b, i, lo, hi);
-    const bool few = hi && hi - lo <= kFewKeys;
-    if (hi) {
-        lse2 = P.lse[((int64_t)b * P.n_q + h) * P.sq + i] * kLog2e;
-        if (!few) delta = dot<T, 8>(row_of<T>(P.o_in, P.o_stride, b, i, h), row_of<T>(P.dout, P.dout_stride, b, i, h), P.head_dim, part);
-    }
-    delta = sum_of_8(delta);
-    if (__any_sync(~0u, few)) {  // each of the eight threads takes every eighth key
-        float sum = 0.f;
-        for (int j = lo + part; few && j < hi; j += 8) {
-            const float s = dot<T>(row_of<T>(P.q, P.q_stride, b, i, h), row_of<T>(P.k, P.k_stride, b, j, h / P.group), P.head_dim);
-            const float dp = dot<T>(row_of<T>(P.dout, P.dout_stride, b, i, h), row_of<T>(P.v, P.v_stride, b, j, h / P.group), P.head_dim);
-            sum = fmaf(fast_exp2(fmaf(s, P.scale2, -lse2)), dp, sum);
-        }
-        sum = sum_of_8(sum);
-        if (few) delta = sum;
-    }
+__global__ void __launch_bounds__(128) attention_record_kernel(const __grid_constant__ AttentionParams P) {
+    constexpr int kEach = 4;
+    const int rec = blockIdx.x, h = blockIdx.y, b = blockIdx.z, group = threadIdx.x >> 3, part = threadIdx.x & 7;
+    const int64_t row0 = ((int64_t)b * P.n_q + h) * P.sq;
     Record* R = P.record + ((int64_t)b * P.n_q + h) * P.records + rec;
-    if (part == 0) {
-        R->minus_lse2[r] = -lse2;
-        R->minus_delta[r] = -delta;
-        R->lo[r] = lo;
-        R->hi[r] = hi;
+    __shared__ Reach s_reach[4];
+    float delta[kEach], lse2[kEach];
+    int lo[kEach], hi[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {  // rows that see nothing are read too; what comes of it is not used
+        const int i = rec * kRecord + u * 16 + group;
+        delta[u] = 0.f, lse2[u] = 0.f;
+        if (i < P.sq) {
+            lse2[u] = P.lse[row0 + i] * kLog2e;
+            delta[u] = dot<T, 8>(row_of<T>(P.o_in, P.o_stride, b, i, h), row_of<T>(P.dout, P.dout_stride, b, i, h), P.head_dim, part);
+        }
+        seen_by(P, b, i, lo[u], hi[u]);
+    }
+    Reach a{INT_MAX, 0, 0, INT_MAX};
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const int r = u * 16 + group, i = rec * kRecord + r;
+        float d = sum_of_8(delta[u]);
+        const bool few = hi[u] && hi[u] - lo[u] <= kFewKeys;
+        if (__any_sync(~0u, few)) {  // each of the eight threads takes every eighth key
+            float sum = 0.f;
+            for (int j = lo[u] + part; few && j < hi[u]; j += 8) {
+                const float s = dot<T>(row_of<T>(P.q, P.q_stride, b, i, h), row_of<T>(P.k, P.k_stride, b, j, h / P.group), P.head_dim);
+                const float dp = dot<T>(row_of<T>(P.dout, P.dout_stride, b, i, h), row_of<T>(P.v, P.v_stride, b, j, h / P.group), P.head_dim);
+                sum = fmaf(fast_exp2(fmaf(s, P.scale2, -lse2[u])), dp, sum);
+            }
+            sum = sum_of_8(sum);
+            if (few) d = sum;
+        }
+        if (part == 0) {
+            R->minus_lse2[r] = hi[u] ? -lse2[u] : -INFINITY;
+            R->minus_delta[r] = hi[u] ? -d : 0.f;
+            R->lo[r] = lo[u];
+            R->hi[r] = hi[u];
+        }
+        if (i < P.sq) {  // rows past the end are zeros and need no mask
+            a.min_lo = min(a.min_lo, lo[u]), a.max_hi = max(a.max_hi, hi[u]);
+            a.max_lo = max(a.max_lo, lo[u]), a.min_hi = min(a.min_hi, hi[u]);
+        }
     }
     if (h == 0) {
-        Reach a{lo, hi, lo, hi ? hi : 0};
-        if (i >= P.sq) a.max_lo = 0, a.min_hi = INT_MAX;  // rows past the end are zeros and need no mask
 #pragma unroll
         for (int s = 16; s >= 8; s >>= 1) {
             a.min_lo = min(a.min_lo, __shfl_xor_sync(~0u, a.min_lo, s));
@@ -401,7 +407,7 @@ __global__ void __launch_bounds__(512) attention_record_kernel(const __grid_cons
         if ((threadIdx.x & 31) == 0) s_reach[threadIdx.x >> 5] = a;
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 1; w < 16; ++w) {
+            for (int w = 1; w < 4; ++w) {
                 a.min_lo = min(a.min_lo, s_reach[w].min_lo);
                 a.max_hi = max(a.max_hi, s_reach[w].max_hi);
                 a.max_lo = max(a.max_lo, s_reach[w].max_lo);
@@ -484,7 +490,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             int it = 0, s = 0, use = 1, r = 0, h = hk * P.group;
             const Record* records = P.record + ((int64_t)b * P.n_q + h) * P.records + first;
             for (; it < n; ++it) {
-                if (it >= F::kStages && !W.wait_warp(free_ + 8 * s, use)) break;
+                if (it >= F::kStages) W.wait_warp(free_ + 8 * s, use);
                 if (issuer) {
                     const uint32_t at = smem_u32(stages) + s * F::kStageBytes, bar = full + 8 * s;
                     bar_expect(bar, F::kStageBytes);
@@ -497,9 +503,9 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                 if (++s == F::kStages) s = 0, use ^= 1;
                 if (++r == per_head) r = 0, ++h, records += P.records;
             }
-            if (it < n) {
+            if (*W.gave_up) {
                 W.drain(kv_full, 0);
-                for (int i = it > F::kStages ? it - F::kStages : 0; i < it; ++i) W.drain(full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+                for (int i = max(0, n - F::kStages); i < n; ++i) W.drain(full + 8 * (i % F::kStages), (i / F::kStages) & 1);
             }
         }
     } else if (warp == kMmaWarp) {
@@ -509,8 +515,8 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             int s1 = 0, use1 = 0, s2 = 0, s3 = 0, slot = 0, use = 0;
             const auto tile_at = [&](int s) { return smem_u32(stages) + s * F::kStageBytes; };
             const auto next = [](int& s) { s = s + 1 == F::kStages ? 0 : s + 1; };
-            const auto scores = [&](int slot) -> bool {
-                if (!W.wait_warp(full + 8 * s1, use1)) return false;
+            const auto scores = [&](int slot) {
+                W.wait_warp(full + 8 * s1, use1);
                 tc_after_sync();
                 if (issuer) {
                     product_ss<T, 64, DP, 128, 64>(tmem + slot * 128, smem_u32(tile_k), tile_at(s1));
@@ -518,7 +524,6 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                 }
                 next(s1);
                 use1 ^= s1 == 0;
-                return true;
             };
             const auto dp = [&](int slot) {
                 if (issuer) {
@@ -527,13 +532,15 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                 }
                 next(s2);
             };
-            bool ok = W.wait_warp(kv_full, 0);
-            for (int it = 0; ok && it < kSlots && it < n; ++it)
-                if ((ok = scores(it))) dp(it);
-            for (int it = 0; ok && it < n; ++it) {
+            W.wait_warp(kv_full, 0);
+            for (int it = 0; it < kSlots && it < n; ++it) scores(it), dp(it);
+            for (int it = 0; it < n; ++it) {
                 // S of the next tile in this slot can follow once this one has been read; dP only when P and dS, which lie over it, are used up
-                if (it + kSlots < n && !(ok = W.wait_warp(s_read + 8 * slot, use) && scores(slot))) break;
-                if (!(ok = W.wait_warp(ds_full + 8 * slot, use))) break;
+                if (it + kSlots < n) {
+                    W.wait_warp(s_read + 8 * slot, use);
+                    scores(slot);
+                }
+                W.wait_warp(ds_full + 8 * slot, use);
                 tc_after_sync();
                 if (issuer) {
                     const uint32_t q = tile_at(s3), at = tmem + slot * 128 + 64;
@@ -546,16 +553,16 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                 if (++slot == kSlots) slot = 0, use ^= 1;
             }
             if (issuer) mma_commit(done);
-            if (!ok) W.drain(done, 0);
+            if (*W.gave_up) W.drain(done, 0);
         }
     } else {
         const int slot = warp >> 3, part = (warp >> 2) & 1, row = threadIdx.x & 127, key = key0 + row;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128 + part * 32;
-        bool ok = true;
         int s = slot % F::kStages, use = slot / F::kStages, s_use = 0, rec = per_head ? slot % per_head : 0;
         for (int it = slot; it < n; it += kSlots) {
             const Reach a = reach[first + rec];
-            if (!(ok = W.wait_warp(full + 8 * s, use) && W.wait_warp(s_full + 8 * slot, s_use))) break;
+            W.wait(full + 8 * s, use);
+            W.wait_warp(s_full + 8 * slot, s_use);
             tc_after_sync();
             char* stage = stages + s * F::kStageBytes;
             const Record& R = *reinterpret_cast<const Record*>(stage + 2 * F::kTileQ);
@@ -584,7 +591,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                     if (key < lo.w || key >= hi.w) x[c + 3] = 0;
                 }
             }
-            if (!(ok = W.wait_warp(dp_full + 8 * slot, s_use))) break;
+            W.wait_warp(dp_full + 8 * slot, s_use);
             tc_after_sync();
             tmem_load32(y, at + 64);
             tmem_wait_loads32(y);
@@ -627,9 +634,9 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
                 if (++rec == per_head) rec = 0;
             }
         }
-        if (ok && n) ok = W.wait_warp(done, 0);
+        if (n) W.wait_warp(done, 0);
         tc_after_sync();
-        if (ok && slot == 0) {  // four warps store dV, four dK
+        if (slot == 0) {  // four warps store dV, four dK
             {
                 const int what = part;
                 const float f = what ? P.scale : 1.f;
@@ -730,7 +737,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
             }
             int j = 0, s = 0, use = 1;
             for (; j < n; ++j) {
-                if (j >= F::kStages && !W.wait_warp(free_ + 8 * s, use)) break;
+                if (j >= F::kStages) W.wait_warp(free_ + 8 * s, use);
                 if (issuer) {
                     const uint32_t at = smem_u32(stages) + s * 2 * F::kTileK, bar = full + 8 * s;
                     bar_expect(bar, 2 * F::kTileK);
@@ -741,9 +748,9 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 }
                 if (++s == F::kStages) s = 0, use ^= 1;
             }
-            if (j < n) {
+            if (*W.gave_up) {
                 W.drain(q_full, 0);
-                for (int k = j > F::kStages ? j - F::kStages : 0; k < j; ++k) W.drain(full + 8 * (k % F::kStages), (k / F::kStages) & 1);
+                for (int i = max(0, n - F::kStages); i < n; ++i) W.drain(full + 8 * (i % F::kStages), (i / F::kStages) & 1);
             }
         }
     } else if (warp == kMmaWarp) {
@@ -752,8 +759,8 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
             int s1 = 0, use1 = 0, s2 = 0, s3 = 0, d2 = 0, d3 = 0;  // stages as for the keys; places of dP
             const auto tile_at = [&](int s) { return smem_u32(stages) + s * 2 * F::kTileK; };
             const auto next = [](int& s, int of) { s = s + 1 == of ? 0 : s + 1; };
-            const auto scores = [&]() -> bool {
-                if (!W.wait_warp(full + 8 * s1, use1)) return false;
+            const auto scores = [&] {
+                W.wait_warp(full + 8 * s1, use1);
                 tc_after_sync();
                 if (issuer) {
                     product_ss<T, 64, DP, 128, 64>(tmem, smem_u32(tile_q), tile_at(s1));
@@ -761,7 +768,6 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 }
                 next(s1, F::kStages);
                 use1 ^= s1 == 0;
-                return true;
             };
             const auto dp = [&] {
                 if (issuer) {
@@ -770,15 +776,16 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 }
                 next(s2, F::kStages), next(d2, F::kDPs);
             };
-            bool ok = W.wait_warp(q_full, 0) && scores();
-            if (ok) dp();
-            for (int j = 0; ok && j < n; ++j) {
+            W.wait_warp(q_full, 0);
+            scores(), dp();
+            for (int j = 0; j < n; ++j) {
                 // the next S can follow once this one has been read, the next dP too where it has a place of its own
                 if (F::kStages > 1 && j + 1 < n) {
-                    if (!(ok = W.wait_warp(s_read, j & 1) && scores())) break;
+                    W.wait_warp(s_read, j & 1);
+                    scores();
                     if (F::kDPs > 1) dp();
                 }
-                if (!(ok = W.wait_warp(ds_full, j & 1))) break;
+                W.wait_warp(ds_full, j & 1);
                 tc_after_sync();
                 if (issuer) {
                     product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + F::kColDP + d3 * 64, tile_at(s3), j > 0);
@@ -786,23 +793,22 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 }
                 next(s3, F::kStages), next(d3, F::kDPs);
                 if (j + 1 < n) {
-                    if (F::kStages == 1 && !(ok = scores())) break;
+                    if (F::kStages == 1) scores();
                     if (F::kDPs == 1) dp();
                 }
             }
             if (issuer) mma_commit(done);
-            if (!ok) W.drain(done, 0);
+            if (*W.gave_up) W.drain(done, 0);
         }
     } else {
         const int part = (warp >> 2) & 1;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const float2 factor = both(P.scale2), ml = both(minus_lse2), md = both(minus_delta);
         const bool one = hi - lo == 1;  // a softmax of one term is constant
-        bool ok = true;
         for (int j = 0; j < n; ++j) {
             const int s = j % F::kStages, tile0 = (first + j) * 64, key0 = tile0 + part * 32;
             const uint32_t at_dp = lanes + F::kColDP + (j % F::kDPs) * 64 + part * 32;
-            if (!(ok = W.wait_warp(s_full, j & 1))) break;
+            W.wait_warp(s_full, j & 1);
             tc_after_sync();
             uint32_t x[32], y[32];
             tmem_load32(x, lanes + part * 32);
@@ -814,7 +820,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 const float2 p = exp2_both(fma2(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), factor, ml));
                 x[c] = __float_as_uint(p.x), x[c + 1] = __float_as_uint(p.y);
             }
-            if (!(ok = W.wait_warp(dp_full + 8 * (j % F::kDPs), (j / F::kDPs) & 1))) break;
+            W.wait_warp(dp_full + 8 * (j % F::kDPs), (j / F::kDPs) & 1);
             tc_after_sync();
             tmem_load32(y, at_dp);
             tmem_wait_loads32(y);
@@ -836,16 +842,16 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
             tmem_wait_stores();
             if (part == 0 && (tile0 < min_lo || (tile0 + 64 > max_hi && max_hi < P.sk))) {
                 // the copy's writes become visible through its own barrier
-                if (!(ok = W.wait_warp(full + 8 * s, (j / F::kStages) & 1))) break;
+                W.wait_warp(full + 8 * s, (j / F::kStages) & 1);
                 if (row < 64 && (tile0 + row < min_lo || tile0 + row >= max_hi)) clear_row<DP>(stages + s * 2 * F::kTileK, 64, row);
                 fence_async_shared();
             }
             tc_before_sync();
             bar_arrive(ds_full);
         }
-        if (ok && n) ok = W.wait_warp(done, 0);
+        if (n) W.wait_warp(done, 0);
         tc_after_sync();
-        if (ok) {
+        {
 #pragma unroll
             for (int c2 = 0; c2 < DP / 64; ++c2) {
                 const int c = 2 * c2 + part;
@@ -974,7 +980,7 @@ int backward(const halos_attention_args* a) {
     if (int rc = allow_smem(attention_keys_kernel<T, DP, kKeySlots>, K::kSmem)) return rc;
     if (int rc = allow_smem(attention_queries_kernel<T, DP>, Q::kSmem)) return rc;
     if (P.sq) {
-        attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 512, 0, st>>>(P);
+        attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 128, 0, st>>>(P);
         if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
     }
     if (P.sk) {

@@ -37,27 +37,32 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
-// Waits are bounded: one that runs out marks the CTA (and *fault), and every role of the CTA then leaves its loop,
-// waits for what it has in flight, and goes on to give back its tensor memory.
+// Waits are bounded: one that runs out marks the CTA and *fault, and from then on every wait of the CTA returns at once.  All loops go on
+// to their ends, within their buffers but with whatever is there, and before a CTA ends its copies and products in
+// flight are waited for (again with a bound), so that tensor memory is given back and nothing hangs.
 constexpr long long kWaitClocks = 2000000000ll;  // about a second
 struct Waits {
     volatile int* gave_up;  // in shared memory
     int* fault;             // in device memory
-    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const { return bar_try(bar, parity) || wait_longer(bar, parity); }
-    __device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity) const {
-        const long long began = clock64();
-        while (clock64() - began < kWaitClocks) {
-            if (bar_try(bar, parity)) return true;
-            if (*gave_up) return false;
-        }
-        *gave_up = 1;
-        atomicExch(fault, 1);
-        return false;
+    __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity) const {
+        if (!bar_try(bar, parity)) wait_longer(bar, parity);
     }
-    // For a whole warp, which goes on together or not at all.
-    __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) const { return __all_sync(~0u, wait(bar, parity)); }
-    // For what is in flight when a role leaves early.
-    __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) const {
+    // For a warp whose next instruction is one for all its lanes together.
+    __device__ __forceinline__ void wait_warp(uint32_t bar, uint32_t parity) const {
+        wait(bar, parity);
+        __syncwarp();
+    }
+    __device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity) const {
+        const long long began = clock64();
+        while (!*gave_up) {
+            if (bar_try(bar, parity)) return;
+            if (clock64() - began > kWaitClocks) {
+                *gave_up = 1;
+                atomicExch(fault, 1);
+            }
+        }
+    }
+    __device__ __noinline__ void drain(uint32_t bar, uint32_t parity) const {
         const long long began = clock64();
         while (!bar_try(bar, parity) && clock64() - began < kWaitClocks / 16) {}
     }
