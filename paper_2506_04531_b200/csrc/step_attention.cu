@@ -322,20 +322,21 @@ __device__ __forceinline__ const T* row_of(const char* base, const int64_t* stri
     return reinterpret_cast<const T*>(base) + b * stride[0] + s * stride[1] + h * stride[2];
 }
 
-// The product of two rows, or the share of it that falls to every eighth vector from `first` on.
-template <typename T, int kStep = 1>
-__device__ __forceinline__ float dot(const T* x, const T* y, int head_dim, int first = 0) {
+template <typename T>
+__device__ __forceinline__ float dot8(uint4 a, uint4 b, float sum) {
+    const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float2 p = unpack2<T>(as[e]), q = unpack2<T>(bs[e]);
+        sum = fmaf(p.x, q.x, fmaf(p.y, q.y, sum));
+    }
+    return sum;
+}
+template <typename T>
+__device__ __forceinline__ float dot(const T* x, const T* y, int head_dim) {
     float sum = 0.f;
 #pragma unroll 4
-    for (int c = first * 8; c < head_dim; c += 8 * kStep) {
-        const uint4 a = *reinterpret_cast<const uint4*>(x + c), b = *reinterpret_cast<const uint4*>(y + c);
-        const uint32_t as[4] = {a.x, a.y, a.z, a.w}, bs[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 p = unpack2<T>(as[e]), q = unpack2<T>(bs[e]);
-            sum = fmaf(p.x, q.x, fmaf(p.y, q.y, sum));
-        }
-    }
+    for (int c = 0; c < head_dim; c += 8) sum = dot8<T>(*reinterpret_cast<const uint4*>(x + c), *reinterpret_cast<const uint4*>(y + c), sum);
     return sum;
 }
 __device__ __forceinline__ float sum_of_8(float v) {
@@ -359,21 +360,31 @@ __global__ void __launch_bounds__(128) attention_record_kernel(const __grid_cons
     __shared__ Reach s_reach[4];
     float delta[kEach], lse2[kEach];
     int lo[kEach], hi[kEach];
+    uint4 o[kEach][2], d[kEach][2];
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {  // rows that see nothing are read too; what comes of it is not used
         const int i = rec * kRecord + u * 16 + group;
-        delta[u] = 0.f, lse2[u] = 0.f;
-        if (i < P.sq) {
-            lse2[u] = P.lse[row0 + i] * kLog2e;
-            delta[u] = dot<T, 8>(row_of<T>(P.o_in, P.o_stride, b, i, h), row_of<T>(P.dout, P.dout_stride, b, i, h), P.head_dim, part);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            const int c = part * 8 + v * 64;
+            o[u][v] = d[u][v] = make_uint4(0, 0, 0, 0);
+            if (i < P.sq && c < P.head_dim) {
+                o[u][v] = *reinterpret_cast<const uint4*>(row_of<T>(P.o_in, P.o_stride, b, i, h) + c);
+                d[u][v] = *reinterpret_cast<const uint4*>(row_of<T>(P.dout, P.dout_stride, b, i, h) + c);
+            }
         }
-        seen_by(P, b, i, lo[u], hi[u]);
+        lse2[u] = i < P.sq ? P.lse[row0 + i] * kLog2e : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        seen_by(P, b, rec * kRecord + u * 16 + group, lo[u], hi[u]);
+        delta[u] = dot8<T>(o[u][1], d[u][1], dot8<T>(o[u][0], d[u][0], 0.f));
     }
     Reach a{INT_MAX, 0, 0, INT_MAX};
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
         const int r = u * 16 + group, i = rec * kRecord + r;
-        float d = sum_of_8(delta[u]);
+        float total = sum_of_8(delta[u]);
         const bool few = hi[u] && hi[u] - lo[u] <= kFewKeys;
         if (__any_sync(~0u, few)) {  // each of the eight threads takes every eighth key
             float sum = 0.f;
@@ -383,11 +394,11 @@ __global__ void __launch_bounds__(128) attention_record_kernel(const __grid_cons
                 sum = fmaf(fast_exp2(fmaf(s, P.scale2, -lse2[u])), dp, sum);
             }
             sum = sum_of_8(sum);
-            if (few) d = sum;
+            if (few) total = sum;
         }
         if (part == 0) {
             R->minus_lse2[r] = hi[u] ? -lse2[u] : -INFINITY;
-            R->minus_delta[r] = hi[u] ? -d : 0.f;
+            R->minus_delta[r] = hi[u] ? -total : 0.f;
             R->lo[r] = lo[u];
             R->hi[r] = hi[u];
         }
@@ -447,7 +458,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t kv_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8 * kSlots,
                    dp_full = ds_full + 8 * kSlots, s_read = dp_full + 8 * kSlots;
-    const int warp = uniform((int)threadIdx.x >> 5);
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int kCopyWarp = 8 * kSlots, kMmaWarp = kCopyWarp + 1;
 
     const int n_kv = P.n_q / P.group, heads = P.batch * n_kv;
@@ -566,61 +577,72 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             tc_after_sync();
             char* stage = stages + s * F::kStageBytes;
             const Record& R = *reinterpret_cast<const Record*>(stage + 2 * F::kTileQ);
+            // A thread takes 4 keys by 8 queries: what belongs to a query is then read from shared memory for four keys at once, and shared
+            // memory, which the products read their operands from, is what this loop runs short of.
             uint32_t x[32], y[32];
-            tmem_load32(x, at);
+            tmem_load_16x32(x, at);
+            tmem_load_16x32(x + 16, at + (16 << 16));
             tmem_wait_loads32(x);
             tc_before_sync();
             bar_arrive(s_read + 8 * slot);
+            const int column = part * 32 + 2 * (lane & 3), key_of_lane = key0 + (warp & 3) * 32 + (lane >> 2);
             const bool masked = a.max_lo > key0 || a.min_hi < key0 + 128;
             const float2 factor = both(P.scale2);
             // P first, while the product dP may still be under way
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-                const float4 ml = *reinterpret_cast<const float4*>(R.minus_lse2 + part * 32 + c);
-                const float2 p = exp2_both(fma2(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), factor, make_float2(ml.x, ml.y)));
-                const float2 q = exp2_both(fma2(make_float2(__uint_as_float(x[c + 2]), __uint_as_float(x[c + 3])), factor, make_float2(ml.z, ml.w)));
-                x[c] = __float_as_uint(p.x), x[c + 1] = __float_as_uint(p.y), x[c + 2] = __float_as_uint(q.x), x[c + 3] = __float_as_uint(q.y);
-            }
-            if (masked) {
+            for (int k = 0; k < 4; ++k) {
+                const float2 ml = *reinterpret_cast<const float2*>(R.minus_lse2 + column + 8 * k);
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + part * 32 + c), hi = *reinterpret_cast<const int4*>(R.hi + part * 32 + c);
-                    if (key < lo.x || key >= hi.x) x[c] = 0;
-                    if (key < lo.y || key >= hi.y) x[c + 1] = 0;
-                    if (key < lo.z || key >= hi.z) x[c + 2] = 0;
-                    if (key < lo.w || key >= hi.w) x[c + 3] = 0;
+                for (int i = 0; i < 4; ++i) {  // keys key_of_lane + 8 i
+                    uint32_t* e = x + 16 * (i >> 1) + 4 * k + 2 * (i & 1);
+                    const float2 p = exp2_both(fma2(make_float2(__uint_as_float(e[0]), __uint_as_float(e[1])), factor, ml));
+                    e[0] = __float_as_uint(p.x), e[1] = __float_as_uint(p.y);
                 }
             }
             W.wait_warp(dp_full + 8 * slot, s_use);
             tc_after_sync();
-            tmem_load32(y, at + 64);
+            tmem_load_16x32(y, at + 64);
+            tmem_load_16x32(y + 16, at + 64 + (16 << 16));
             tmem_wait_loads32(y);
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-                const float4 md = *reinterpret_cast<const float4*>(R.minus_delta + part * 32 + c);
-                const float2 d = add2(make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1])), make_float2(md.x, md.y));
-                const float2 e = add2(make_float2(__uint_as_float(y[c + 2]), __uint_as_float(y[c + 3])), make_float2(md.z, md.w));
-                y[c] = __float_as_uint(d.x), y[c + 1] = __float_as_uint(d.y), y[c + 2] = __float_as_uint(e.x), y[c + 3] = __float_as_uint(e.y);
+            for (int k = 0; k < 4; ++k) {
+                const float2 md = *reinterpret_cast<const float2*>(R.minus_delta + column + 8 * k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at_e = 16 * (i >> 1) + 4 * k + 2 * (i & 1);
+                    const float2 ds = mul2(make_float2(__uint_as_float(x[at_e]), __uint_as_float(x[at_e + 1])),
+                                           add2(make_float2(__uint_as_float(y[at_e]), __uint_as_float(y[at_e + 1])), md));
+                    y[at_e] = __float_as_uint(ds.x), y[at_e + 1] = __float_as_uint(ds.y);
+                }
             }
             if (masked) {
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    const int4 lo = *reinterpret_cast<const int4*>(R.lo + part * 32 + c), hi = *reinterpret_cast<const int4*>(R.hi + part * 32 + c);
-                    const auto hide = [&](int l, int h, uint32_t& d) {  // a softmax of one term is constant
-                        if (key < l || key >= h || h - l == 1) d = 0;
-                    };
-                    hide(lo.x, hi.x, y[c]), hide(lo.y, hi.y, y[c + 1]), hide(lo.z, hi.z, y[c + 2]), hide(lo.w, hi.w, y[c + 3]);
+                for (int k = 0; k < 4; ++k) {
+                    const int2 lo = *reinterpret_cast<const int2*>(R.lo + column + 8 * k), hi = *reinterpret_cast<const int2*>(R.hi + column + 8 * k);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int at_e = 16 * (i >> 1) + 4 * k + 2 * (i & 1), key = key_of_lane + 8 * i;
+                        const auto hide = [&](int l, int h, uint32_t& p, uint32_t& ds) {
+                            if (key < l || key >= h) p = ds = 0;
+                            if (h - l == 1) ds = 0;  // a softmax of one term is constant
+                        };
+                        hide(lo.x, hi.x, x[at_e], y[at_e]), hide(lo.y, hi.y, x[at_e + 1], y[at_e + 1]);
+                    }
                 }
             }
-            uint32_t words[32];
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-                const float2 p = make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1]));
-                const float2 ds = mul2(p, make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1])));
-                words[c / 2] = pack2<T>(p.x, p.y);
-                words[16 + c / 2] = pack2<T>(ds.x, ds.y);
+            for (int hh = 0; hh < 2; ++hh) {
+                uint32_t words[16];  // 16 columns of P, then 16 of dS
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int at_e = 16 * hh + 4 * k + 2 * i;
+                        words[2 * k + i] = pack2<T>(__uint_as_float(x[at_e]), __uint_as_float(x[at_e + 1]));
+                        words[8 + 2 * k + i] = pack2<T>(__uint_as_float(y[at_e]), __uint_as_float(y[at_e + 1]));
+                    }
+                tmem_store_16x32(at + 64 + (hh * 16 << 16), words);
             }
-            tmem_store32(at + 64, words);
             tmem_wait_stores();
             if (a.max_lo == INT_MAX && part == 0) {  // a query that sees nothing may hold anything
                 if (row < 64 ? R.hi[row] == 0 : R.hi[row - 64] == 0) clear_row<DP>(stage + (row < 64 ? 0 : F::kTileQ), 64, row & 63);

@@ -142,6 +142,24 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
+// 16 lanes by 32 columns: register 4 k + 2 i + e of a thread = lane t/4 + 8 i, column 8 k + 2 (t % 4) + e.
+__device__ __forceinline__ void tmem_load_16x32(uint32_t* r, uint32_t at) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at));
+}
+// 16 lanes by 32 columns: register 2 k + i of a thread = lane t/4 + 8 i, column 4 k + t % 4.
+__device__ __forceinline__ void tmem_store_16x32(uint32_t at, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
 // ---- matrix products ---------------------------------------------------------------------------
 // Operands in shared memory lie as the bulk copy's 128-byte swizzle leaves them: rows of 64 16-bit elements, blocks of 8
 // rows (1024 bytes), sub-tiles of 64 columns one after another.
