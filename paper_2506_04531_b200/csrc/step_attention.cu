@@ -979,7 +979,8 @@ int forward(const halos_attention_args* a) {
         if (int rc = make_map(&k, a, a->k, a->sk, a->n_kv, a->k_stride, 64)) return rc;
         if (int rc = make_map(&v, a, a->v, a->sk, a->n_kv, a->v_stride, 64)) return rc;
     }
-    if (int rc = allow_smem(attention_fwd_kernel<T, DP>, F::kSmem)) return rc;
+    static Allowed allowed;
+    if (int rc = allow_smem(attention_fwd_kernel<T, DP>, F::kSmem, allowed)) return rc;
     attention_fwd_kernel<T, DP><<<P.q_tiles * P.batch * P.n_q, F::kThreads, F::kSmem, (cudaStream_t)a->stream>>>(P, q, k, v);
     return cuda_status(cudaGetLastError(), "attention launch");
 }
@@ -999,8 +1000,9 @@ int backward(const halos_attention_args* a) {
     CUtensorMap q{}, d{}, k{}, v{};
     using K = Keys<DP, kKeySlots>;
     using Q = Queries<DP>;
-    if (int rc = allow_smem(attention_keys_kernel<T, DP, kKeySlots>, K::kSmem)) return rc;
-    if (int rc = allow_smem(attention_queries_kernel<T, DP>, Q::kSmem)) return rc;
+    static Allowed allowed_keys, allowed_queries;
+    if (int rc = allow_smem(attention_keys_kernel<T, DP, kKeySlots>, K::kSmem, allowed_keys)) return rc;
+    if (int rc = allow_smem(attention_queries_kernel<T, DP>, Q::kSmem, allowed_queries)) return rc;
     if (P.sq) {
         attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 128, 0, st>>>(P);
         if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;

@@ -8,6 +8,7 @@ namespace halos_step {
 namespace {
 constexpr int kMaxDevices = 64;
 thread_local char t_error[256] = "";
+thread_local int t_device = 0;
 std::atomic<int> g_sms[kMaxDevices];
 __device__ int g_fault;
 }  // namespace
@@ -27,6 +28,7 @@ int cuda_status(cudaError_t e, const char* where) {
 int enter(int32_t device) {
     if (device < 0 || device >= kMaxDevices) return fail(HALOS_ERR_INVALID_ARG, "no such device");
     if (int rc = cuda_status(cudaSetDevice(device), "cudaSetDevice (there is no CPU path)")) return rc;
+    t_device = device;
     if (!g_sms[device].load(std::memory_order_relaxed)) {
         int n = 0;
         if (int rc = cuda_status(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device), "multiprocessor count")) return rc;
@@ -35,7 +37,16 @@ int enter(int32_t device) {
     return HALOS_OK;
 }
 
-int fault_mark(int** mark) { return cuda_status(cudaGetSymbolAddress((void**)mark, g_fault), "fault mark"); }
+int fault_mark(int** mark) {
+    static std::atomic<int*> known[kMaxDevices];
+    *mark = known[t_device].load(std::memory_order_relaxed);
+    if (*mark) return HALOS_OK;
+    if (int rc = cuda_status(cudaGetSymbolAddress((void**)mark, g_fault), "fault mark")) return rc;
+    known[t_device].store(*mark, std::memory_order_relaxed);
+    return HALOS_OK;
+}
+
+int current_device() { return t_device; }
 
 int sm_count(int32_t device) { return g_sms[device].load(std::memory_order_relaxed); }
 

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <atomic>
 #include <stdint.h>
 
 namespace halos_step {
@@ -16,9 +17,16 @@ int sm_count(int32_t device);                           // of a device that ente
 int fault_mark(int** mark);                             // where the current device's kernels say that a wait ran out
 
 constexpr int kSharedPerSM = 228 * 1024;
+int current_device();                                   // that enter() was last called with in this thread
+// Lets a kernel have this much dynamic shared memory; each caller keeps what it was last allowed, per device.
+struct Allowed { std::atomic<int> bytes[64]; };
 template <typename K>
-int allow_smem(K* kernel, int bytes) {
-    return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes), "shared memory");
+int allow_smem(K* kernel, int bytes, Allowed& allowed) {
+    std::atomic<int>& had = allowed.bytes[current_device()];
+    if (had.load(std::memory_order_relaxed) >= bytes) return HALOS_OK;
+    if (int rc = cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes), "shared memory")) return rc;
+    had.store(bytes, std::memory_order_relaxed);
+    return HALOS_OK;
 }
 
 inline bool is_type(uint32_t t) { return t == HALOS_F32 || t == HALOS_BF16 || t == HALOS_F16; }

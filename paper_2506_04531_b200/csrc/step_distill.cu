@@ -646,7 +646,8 @@ int launch_held(const DistillParams& P, int64_t rows, int mode, int sms, int* fa
     using H = Held<kThreads>;
     auto* kernel = distill_held_kernel<T, kSquarings, kThreads>;
     const int bytes = held_bytes<T>(P);
-    if (int rc = allow_smem(kernel, bytes)) return rc;
+    static Allowed allowed;
+    if (int rc = allow_smem(kernel, bytes, allowed)) return rc;
     const int fit = kSharedPerSM / (bytes + 3072), per_sm = fit < 1 ? 1 : fit < H::kPerSM ? fit : H::kPerSM;
     const int64_t most = (int64_t)sms * per_sm;
     kernel<<<(unsigned)(rows < most ? rows : most), kThreads + 32, bytes, st>>>(P, (int)rows, mode, fault);

@@ -1,7 +1,8 @@
 // Rotary positions on queries and keys in one launch.
 //
 // Bound by memory: every element is read once and written once, 3 flops each.  What could cost more than that is the
-// sine and cosine, so a thread computes those of its pairs once and takes them through several heads of the token.
+// sine and cosine, so a block forms those of its tokens once, evenly over its threads, and keeps them in shared memory
+// for all heads.
 //
 // Angles.  position * frequency in 32 bits is wrong by 2^-24 of the angle, 0.004 radians at position 65536.  A turn is
 // therefore taken as 2^64: the frequency becomes a 64-bit fraction of a turn, the product with the position wraps
@@ -44,12 +45,40 @@ __device__ __forceinline__ void store_piece(T* p, const float (&f)[N]) {
 }
 
 // A column is two pieces of N neighbouring elements: (x0 of N pairs, x1 of the same pairs) in the half layout, 2N
-// neighbours in the interleaved one and in the copied rest.  U heads are in flight at a time.
+// neighbours in the interleaved one.  The copied rest is cut in two halves of whole pieces, so that neighbouring threads
+// take neighbouring pieces there too.  U heads are in flight at a time.
 template <typename T, int N, bool kInterleaved, int U>
 __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams P) {
+    __shared__ uint64_t turn[128];              // of each pair per position; a whole turn is 2^64
+    __shared__ float2 cos_sin[kThreads * N];    // [token][pair]
+    const int64_t token0 = (int64_t)blockIdx.x * P.tokens_per_block;
+    const uint32_t pairs = P.rot_dim / 2;
+    for (uint32_t p = threadIdx.x; p < pairs; p += kThreads) {
+        double turns = P.freqs[p] * kTurnsPerRadian;
+        turns -= floor(turns);
+        turn[p] = (uint64_t)(turns * 18446744073709551616.0);  // saturates just below a whole turn
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < P.tokens_per_block * pairs; i += kThreads) {
+        const uint32_t sub = i / pairs, p = i - sub * pairs;
+        const int64_t token = token0 + sub;
+        if (token >= P.tokens) break;
+        const int64_t b = token / P.seq, s = token - b * P.seq;
+        int64_t t = P.position_offset + s;
+        if (P.positions) {
+            const int64_t at = b * P.position_stride[0] + s * P.position_stride[1];
+            t = P.positions_64 ? static_cast<const int64_t*>(P.positions)[at] : (int64_t)static_cast<const int32_t*>(P.positions)[at];
+        }
+        const int32_t angle = (int32_t)(((uint64_t)t * turn[p]) >> 32);
+        float sn, c;
+        sincospif((float)angle * 4.656612873077393e-10f, &sn, &c);  // 2^-31 half turns
+        cos_sin[i] = make_float2(c * P.magnitude, sn * (P.inverse ? -P.magnitude : P.magnitude));
+    }
+    __syncthreads();
+
     const uint32_t per_token = P.cols * P.head_groups;
     const uint32_t sub = threadIdx.x / per_token;
-    const int64_t token = (int64_t)blockIdx.x * P.tokens_per_block + sub;
+    const int64_t token = token0 + sub;
     if (sub >= P.tokens_per_block || token >= P.tokens) return;
     const uint32_t r = threadIdx.x - sub * per_token;
     const uint32_t group = r / P.cols, col = r - group * P.cols;
@@ -60,45 +89,33 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
     bool two = true;
     if (rotated) {
         at0 = kInterleaved ? col * 2 * N : col * N;
-        at1 = kInterleaved ? at0 + N : at0 + P.rot_dim / 2;
+        at1 = kInterleaved ? at0 + N : at0 + pairs;
         if (kInterleaved) two = at1 < P.rot_dim;
     } else {
-        at0 = P.rot_dim + (col - P.rot_cols) * 2 * N;
-        at1 = at0 + N;
+        at0 = P.rot_dim + (col - P.rot_cols) * N;
+        at1 = at0 + (P.cols - P.rot_cols) * N;
         two = at1 < P.head_dim;
     }
     float c[N], sn[N];
     if (rotated) {
-        int64_t t = P.position_offset + s;
-        if (P.positions) {
-            const int64_t at = b * P.position_stride[0] + s * P.position_stride[1];
-            t = P.positions_64 ? static_cast<const int64_t*>(P.positions)[at] : (int64_t)static_cast<const int32_t*>(P.positions)[at];
-        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t pair = col * N + i;
-            c[i] = 1.f;
-            sn[i] = 0.f;
-            if (pair < P.rot_dim / 2) {
-                double turns = P.freqs[pair] * kTurnsPerRadian;
-                turns -= floor(turns);
-                const uint64_t step = (uint64_t)(turns * 18446744073709551616.0);  // saturates just below a whole turn
-                const int32_t angle = (int32_t)(((uint64_t)t * step) >> 32);
-                sincospif((float)angle * 4.656612873077393e-10f, &sn[i], &c[i]);   // 2^-31 half turns
-                c[i] *= P.magnitude;
-                sn[i] *= P.inverse ? -P.magnitude : P.magnitude;
-            }
+            const float2 v = pair < pairs ? cos_sin[sub * pairs + pair] : make_float2(1.f, 0.f);
+            c[i] = v.x, sn[i] = v.y;
         }
     }
+    const T* q = reinterpret_cast<const T*>(P.q_in) + b * P.q_in_stride[0] + s * P.q_in_stride[1];
+    const T* k = reinterpret_cast<const T*>(P.k_in) + b * P.k_in_stride[0] + s * P.k_in_stride[1] - P.n_q * P.k_in_stride[2];
+    T* qo = reinterpret_cast<T*>(P.q_out) + b * P.q_out_stride[0] + s * P.q_out_stride[1];
+    T* ko = reinterpret_cast<T*>(P.k_out) + b * P.k_out_stride[0] + s * P.k_out_stride[1] - P.n_q * P.k_out_stride[2];
     for (uint32_t first = group; first < P.heads; first += U * P.head_groups) {
         float x0[U][N], x1[U][N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t h = first + u * P.head_groups;
             if (h < P.heads) {
-                const bool is_q = h < P.n_q;
-                const int64_t* st = is_q ? P.q_in_stride : P.k_in_stride;
-                const T* x = reinterpret_cast<const T*>(is_q ? P.q_in : P.k_in) + b * st[0] + s * st[1] + (int64_t)(is_q ? h : h - P.n_q) * st[2];
+                const T* x = h < P.n_q ? q + h * P.q_in_stride[2] : k + h * P.k_in_stride[2];
                 load_piece<T, N>(x0[u], x + at0);
                 if (two) load_piece<T, N>(x1[u], x + at1);
             }
@@ -107,9 +124,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         for (int u = 0; u < U; ++u) {
             const uint32_t h = first + u * P.head_groups;
             if (h >= P.heads) continue;
-            const bool is_q = h < P.n_q;
-            const int64_t* st = is_q ? P.q_out_stride : P.k_out_stride;
-            T* y = reinterpret_cast<T*>(is_q ? P.q_out : P.k_out) + b * st[0] + s * st[1] + (int64_t)(is_q ? h : h - P.n_q) * st[2];
+            T* y = h < P.n_q ? qo + h * P.q_out_stride[2] : ko + h * P.k_out_stride[2];
             if (rotated) {
                 if (!kInterleaved || N == 1) {
 #pragma unroll
@@ -207,7 +222,7 @@ extern "C" int halos_rope(const halos_rope_args* a) {
     const bool in_place = (!a->n_q || a->q_in == a->q_out) && (!a->n_k || a->k_in == a->k_out);
     P.cols = P.rot_cols + (in_place ? 0 : (a->head_dim - a->rot_dim + 2 * n - 1) / (2 * n));
     if (P.cols == 0) return HALOS_OK;
-    // As few threads per token as still fill the GPU: each then takes its sines through more heads.
+    // As few threads per token as still fill the GPU: their fixed cost then falls on more heads.
     const uint32_t most = kThreads / P.cols < heads ? kThreads / P.cols : heads;
     const int64_t want = ((int64_t)sm_count(a->device) * 1024 + tokens * P.cols - 1) / (tokens * P.cols);
     uint32_t least = (heads + 7) / 8;

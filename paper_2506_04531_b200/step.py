@@ -53,6 +53,9 @@ class DistillArgs(C.Structure):
                 ("dloss", _vp), ("dlogits", _vp), ("dlogits_stride", _i64)]
 
 
+_ROPE_SIZE, _ATTENTION_SIZE, _DISTILL_SIZE = C.sizeof(RopeArgs), C.sizeof(AttentionArgs), C.sizeof(DistillArgs)
+# Small calls are bound by what happens here, so the stream's handle is asked for without building a stream object around it.
+_byref, _raw_stream = C.byref, torch._C._cuda_getCurrentRawStream
 _lib = None
 
 
@@ -75,8 +78,8 @@ def _refuse(text: str):
 
 
 def _call(name: str, args):
-    lib = _library()
-    rc = getattr(lib, name)(C.byref(args))
+    lib = _lib or _library()
+    rc = getattr(lib, name)(_byref(args))
     if rc:
         raise HalosError(rc, lib.halos_step_error().decode())
 
@@ -95,10 +98,10 @@ def _on(x, device, what: str):
         _refuse(f"{what} is on {x.device}, not on {device}")
 
 
-def _begin(args, device):
-    args.struct_size = C.sizeof(args)
+def _begin(args, size: int, device):
+    args.struct_size = size
     args.device = device.index
-    args.stream = torch.cuda.current_stream(device).cuda_stream
+    args.stream = _raw_stream(device.index)
 
 
 def fault(device: Optional[int] = None) -> bool:
@@ -156,29 +159,32 @@ def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", 
     """Rotates the first 2 len(freqs) elements of every head of q and k ([batch, seq, heads, head_dim], any strides that keep a
     head's elements side by side; k may be None) to their positions: int32 or int64 [seq] or [batch, seq], or offset + 0, 1, ...
     inverse: the gradient's way back.  inplace: q and k are overwritten and returned (a view must not overlap itself)."""
+    device, dtype = q.device, q.dtype
     _heads_last(q, "q")
-    _on(q, q.device, "q")
+    _on(q, device, "q")
     a = RopeArgs()
     a.dtype = _dtype(q, "q")
     a.layout = _LAYOUTS.get(layout, 99)
-    a.batch, a.seq, a.n_q, a.head_dim = q.shape
+    a.batch, a.seq, a.n_q, a.head_dim = shape = q.shape
     if k is not None:
         _heads_last(k, "k")
-        _on(k, q.device, "k")
-        if k.dtype != q.dtype or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3]:
+        _on(k, device, "k")
+        k_shape = k.shape
+        if k.dtype != dtype or k_shape[:2] != shape[:2] or k_shape[3] != shape[3]:
             _refuse("q and k must agree in type, batch, seq and head_dim")
-        a.n_k = k.shape[2]
-    _on(freqs, q.device, "freqs")
+        a.n_k = k_shape[2]
+    _on(freqs, device, "freqs")
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
         _refuse("freqs must be a contiguous float64 vector")
     a.rot_dim, a.freqs = 2 * freqs.numel(), freqs.data_ptr()
     if positions is not None:
-        _on(positions, q.device, "positions")
-        if positions.dtype not in (torch.int32, torch.int64):
+        _on(positions, device, "positions")
+        wide = positions.dtype == torch.int64
+        if not wide and positions.dtype != torch.int32:
             _refuse("positions must be int32 or int64")
-        if positions.shape != q.shape[:2] and positions.shape != q.shape[1:2]:
+        if positions.shape != shape[:2] and positions.shape != shape[1:2]:
             _refuse("positions must be [seq] or [batch, seq]")
-        a.positions, a.positions_64 = positions.data_ptr(), positions.dtype == torch.int64
+        a.positions, a.positions_64 = positions.data_ptr(), wide
         st = positions.stride()
         a.position_stride[:] = st if len(st) == 2 else (0, st[0])
     a.position_offset, a.magnitude, a.inverse = offset, magnitude, bool(inverse)
@@ -188,13 +194,13 @@ def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", 
                 _refuse("a broadcast tensor cannot be rotated in place")
         q_out, k_out = q, k
     else:
-        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=q.device), None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
     a.q_in, a.q_out = q.data_ptr(), q_out.data_ptr()
     a.q_in_stride[:], a.q_out_stride[:] = q.stride()[:3], q_out.stride()[:3]
     if k is not None:
         a.k_in, a.k_out = k.data_ptr(), k_out.data_ptr()
         a.k_in_stride[:], a.k_out_stride[:] = k.stride()[:3], k_out.stride()[:3]
-    _begin(a, q.device)
+    _begin(a, _ROPE_SIZE, device)
     _call("halos_rope", a)
     return q_out, k_out
 
@@ -223,26 +229,30 @@ def rotary(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half"
 
 def _aligned(x):
     """x, or a copy of it that bulk copies can address: 16-byte steps, rows apart, elements side by side."""
-    if x.data_ptr() % 16 == 0 and (x.stride(3) == 1 or x.size(3) == 1):
-        if all(n <= 1 or (s % 8 == 0 and s >= x.size(3)) for s, n in zip(x.stride()[:3], x.shape[:3])):
-            return x
+    b, s, h, d = x.shape
+    sb, ss, sh, sd = x.stride()
+    if x.data_ptr() % 16 == 0 and (sd == 1 or d == 1) and (b <= 1 or (sb >= d and sb % 8 == 0)) and (s <= 1 or (ss >= d and ss % 8 == 0)) \
+            and (h <= 1 or (sh >= d and sh % 8 == 0)):
+        return x
     return x.clone(memory_format=torch.contiguous_format)
 
 
 def _attention_args(q, k, v, scale, causal, doc_start, lens):
+    device, dtype = q.device, q.dtype
     for x, what in ((q, "q"), (k, "k"), (v, "v")):
         if x.dim() != 4:
             _refuse(f"{what} must be [batch, seq, heads, head_dim]")
-        _on(x, q.device, what)
-        if x.dtype != q.dtype:
+        _on(x, device, what)
+        if x.dtype != dtype:
             _refuse("q, k and v must be of one type")
-    if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+    q_shape, k_shape = q.shape, k.shape
+    if k_shape != v.shape or k_shape[0] != q_shape[0] or k_shape[3] != q_shape[3]:
         _refuse("k and v must have one shape, and q's batch and head_dim")
     a = AttentionArgs()
     a.dtype, a.causal = _dtype(q, "q"), bool(causal)
-    a.batch, a.sq, a.n_q, a.head_dim = q.shape
-    a.sk, a.n_kv = k.shape[1:3]
-    a.scale = q.shape[3] ** -0.5 if scale is None and q.shape[3] else scale or 0.0
+    a.batch, a.sq, a.n_q, a.head_dim = q_shape
+    a.sk, a.n_kv = k_shape[1:3]
+    a.scale = q_shape[3] ** -0.5 if scale is None and q_shape[3] else scale or 0.0
     if doc_start is not None:
         _on(doc_start, q.device, "doc_start")
         if doc_start.dtype != torch.int32 or doc_start.shape != q.shape[:2] or not doc_start.is_contiguous():
@@ -268,12 +278,12 @@ def attention_forward(q, k, v, *, scale: Optional[float] = None, causal: bool = 
     lse = -infinity.  What lies at or past lens[b] may hold anything.  scale: head_dim^-1/2 unless given."""
     a = _attention_args(q, k, v, scale, causal, doc_start, lens)
     q, k, v = _aligned(q), _aligned(k), _aligned(v)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    o = torch.empty_like(q)
+    lse = q.new_empty((a.batch, a.n_q, a.sq), dtype=torch.float32)
     for n, x in (("q", q), ("k", k), ("v", v), ("o", o)):
         _set(a, n, x)
     a.lse = lse.data_ptr()
-    _begin(a, q.device)
+    _begin(a, _ATTENTION_SIZE, q.device)
     _call("halos_attention_fwd", a)
     return o, lse
 
@@ -289,16 +299,16 @@ def attention_backward(dout, q, k, v, o, lse, *, scale: Optional[float] = None, 
     if lse.dtype != torch.float32 or lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or not lse.is_contiguous():
         _refuse("lse must be contiguous float32 [batch, heads, seq]")
     q, k, v, o, dout = (_aligned(x) for x in (q, k, v, o, dout))
-    dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     for n, x in (("q", q), ("k", k), ("v", v), ("o", o), ("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv)):
         _set(a, n, x)
     a.lse = lse.data_ptr()
     size = _u64(0)
-    a.struct_size = C.sizeof(a)
+    a.struct_size = _ATTENTION_SIZE
     _library().halos_attention_workspace(C.byref(a), C.byref(size))
-    space = torch.empty(size.value, dtype=torch.uint8, device=q.device)
+    space = q.new_empty(size.value, dtype=torch.uint8)
     a.workspace, a.workspace_bytes = space.data_ptr(), size.value
-    _begin(a, q.device)
+    _begin(a, _ATTENTION_SIZE, q.device)
     _call("halos_attention_bwd", a)
     return dq, dk, dv
 
@@ -371,8 +381,7 @@ def _gradient_like(logits, out, a):
         stride = max(vocab, logits.stride(0)) if rows > 1 else vocab
         if stride > vocab + per:  # keep the remainder only
             stride = vocab + (stride - vocab) % per
-        space = torch.empty(first + rows * stride, dtype=logits.dtype, device=logits.device)
-        out = space.as_strided((rows, vocab), (stride, 1), first)
+        out = logits.new_empty(first + rows * stride).as_strided((rows, vocab), (stride, 1), first)
     else:
         _on(out, logits.device, "out")
         if out.shape != logits.shape or out.dtype != logits.dtype or (out.size(1) > 1 and out.stride(1) != 1):
@@ -388,10 +397,10 @@ def distill_forward(logits, labels, teacher_idx, teacher_logits, *, temperature:
     loss = (1 - mix) (-log softmax(z)[label]) + mix T^2 sum p (log p - log softmax(z / T)[idx]); a row whose label is ignore_index
     has loss 0.  labels None: no first term.  stats = log sum exp of z and of z / T, for ``distill_backward``."""
     a = _distill_args(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
-    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
-    stats = torch.empty((logits.shape[0], 2), dtype=torch.float32, device=logits.device)
+    loss = logits.new_empty(a.rows, dtype=torch.float32)
+    stats = logits.new_empty((a.rows, 2), dtype=torch.float32)
     a.loss, a.stats = loss.data_ptr(), stats.data_ptr()
-    _begin(a, logits.device)
+    _begin(a, _DISTILL_SIZE, logits.device)
     _call("halos_distill_fwd", a)
     return loss, stats
 
@@ -405,7 +414,7 @@ def distill_backward(dloss, logits, stats, labels, teacher_idx, teacher_logits, 
         _refuse("stats must be contiguous float32 [rows, 2]")
     a.stats = stats.data_ptr()
     out = _gradient_like(logits, out, a)
-    _begin(a, logits.device)
+    _begin(a, _DISTILL_SIZE, logits.device)
     _call("halos_distill_bwd", a)
     return out
 
@@ -414,10 +423,10 @@ def distill_loss_and_grad(logits, labels, teacher_idx, teacher_logits, dloss, *,
     """(loss, dlogits) in one pass over the logits, for weights dloss [rows] that are known beforehand; out may be the logits."""
     a = _distill_args(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
     a.dloss = _row_weights(dloss, logits)
-    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+    loss = logits.new_empty(a.rows, dtype=torch.float32)
     a.loss = loss.data_ptr()
     out = _gradient_like(logits, out, a)
-    _begin(a, logits.device)
+    _begin(a, _DISTILL_SIZE, logits.device)
     _call("halos_distill_fwd_bwd", a)
     return loss, out
 
