@@ -15,43 +15,82 @@ namespace {
 constexpr int kThreads = 256;
 constexpr double kTurnsPerRadian = 0.15915494309189533577;  // 1 / (2 pi)
 
+struct RopeTensor {                  // q, then k
+    const char* in;
+    char* out;
+    int64_t in_stride[3], out_stride[3];  // in elements
+    uint32_t heads, head_groups;     // threads that share a token's column
+    uint32_t tokens_per_block, blocks;
+};
 struct RopeParams {
-    const char *q_in, *k_in;
-    char *q_out, *k_out;
+    RopeTensor x[2];
     const double* freqs;
     const void* positions;
-    int64_t q_in_stride[3], k_in_stride[3], q_out_stride[3], k_out_stride[3];  // in elements
-    int64_t position_stride[2], position_offset, tokens;
-    uint32_t seq, n_q, heads, head_dim, rot_dim;
+    int64_t position_stride[2], position_offset;
+    uint32_t tokens, seq, head_dim, rot_dim;
     uint32_t rot_cols, cols;         // columns of two pieces per head: rotated ones first, then copied ones
-    uint32_t head_groups;            // threads that share a token's column
-    uint32_t tokens_per_block;
     uint32_t positions_64, inverse;
     float magnitude;
 };
 
+// N neighbouring elements as they lie in memory, in one access and in whole registers.
+template <int kBytes> struct Raw;
+template <> struct Raw<16> { uint4 v; };
+template <> struct Raw<8> { uint2 v; };
+template <> struct Raw<4> { uint32_t v; };
+template <> struct Raw<2> { uint16_t v; };
+__device__ __forceinline__ void words_of(uint32_t (&w)[4], uint4 v) { w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w; }
+__device__ __forceinline__ void words_of(uint32_t (&w)[2], uint2 v) { w[0] = v.x, w[1] = v.y; }
+__device__ __forceinline__ void words_of(uint32_t (&w)[1], uint32_t v) { w[0] = v; }
+__device__ __forceinline__ void words_of(uint32_t (&w)[1], uint16_t v) { w[0] = v; }
+__device__ __forceinline__ void of_words(uint4& v, const uint32_t (&w)[4]) { v = make_uint4(w[0], w[1], w[2], w[3]); }
+__device__ __forceinline__ void of_words(uint2& v, const uint32_t (&w)[2]) { v = make_uint2(w[0], w[1]); }
+__device__ __forceinline__ void of_words(uint32_t& v, const uint32_t (&w)[1]) { v = w[0]; }
+__device__ __forceinline__ void of_words(uint16_t& v, const uint32_t (&w)[1]) { v = (uint16_t)w[0]; }
+
 template <typename T, int N>
-__device__ __forceinline__ void load_piece(float (&f)[N], const T* p) {
-    const Vec<T, N> w = *reinterpret_cast<const Vec<T, N>*>(p);
+__device__ __forceinline__ void widen(float (&f)[N], const Raw<N * sizeof(T)>& r) {
+    uint32_t w[(N * sizeof(T) + 3) / 4];
+    words_of(w, r.v);
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = to_f32<T>(w.v[i]);
+        for (int i = 0; i < N; ++i) f[i] = __uint_as_float(w[i]);
+    } else if constexpr (N == 1) {
+        f[0] = unpack2<T>(w[0]).x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const float2 p = unpack2<T>(w[i]);
+            f[2 * i] = p.x, f[2 * i + 1] = p.y;
+        }
+    }
 }
 template <typename T, int N>
-__device__ __forceinline__ void store_piece(T* p, const float (&f)[N]) {
-    Vec<T, N> w;
+__device__ __forceinline__ Raw<N * sizeof(T)> rounded(const float (&f)[N]) {
+    uint32_t w[(N * sizeof(T) + 3) / 4];
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) w.v[i] = from_f32<T>(f[i]);
-    *reinterpret_cast<Vec<T, N>*>(p) = w;
+        for (int i = 0; i < N; ++i) w[i] = __float_as_uint(f[i]);
+    } else if constexpr (N == 1) {
+        w[0] = pack2<T>(f[0], 0.f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) w[i] = pack2<T>(f[2 * i], f[2 * i + 1]);
+    }
+    Raw<N * sizeof(T)> r;
+    of_words(r.v, w);
+    return r;
 }
 
 // A column is two pieces of N neighbouring elements: (x0 of N pairs, x1 of the same pairs) in the half layout, 2N
 // neighbours in the interleaved one.  The copied rest is cut in two halves of whole pieces, so that neighbouring threads
 // take neighbouring pieces there too.  U heads are in flight at a time.
 template <typename T, int N, bool kInterleaved, int U>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams P) {
-    __shared__ uint64_t turn[128];              // of each pair per position; a whole turn is 2^64
-    __shared__ float2 cos_sin[kThreads * N];    // [token][pair]
-    const int64_t token0 = (int64_t)blockIdx.x * P.tokens_per_block;
+__global__ void __launch_bounds__(kThreads, 4) rope_kernel(const __grid_constant__ RopeParams P) {
+    __shared__ uint64_t turn[128];                       // of each pair per position; a whole turn is 2^64
+    __shared__ __align__(16) float2 cos_sin[kThreads * N];  // [token][pair]
+    const RopeTensor& X = P.x[blockIdx.x >= P.x[0].blocks];
+    const uint32_t token0 = (blockIdx.x >= P.x[0].blocks ? blockIdx.x - P.x[0].blocks : blockIdx.x) * X.tokens_per_block;
     const uint32_t pairs = P.rot_dim / 2;
     for (uint32_t p = threadIdx.x; p < pairs; p += kThreads) {
         double turns = P.freqs[p] * kTurnsPerRadian;
@@ -59,11 +98,10 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         turn[p] = (uint64_t)(turns * 18446744073709551616.0);  // saturates just below a whole turn
     }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < P.tokens_per_block * pairs; i += kThreads) {
-        const uint32_t sub = i / pairs, p = i - sub * pairs;
-        const int64_t token = token0 + sub;
+    for (uint32_t i = threadIdx.x; i < X.tokens_per_block * pairs; i += kThreads) {
+        const uint32_t sub = i / pairs, p = i - sub * pairs, token = token0 + sub;
         if (token >= P.tokens) break;
-        const int64_t b = token / P.seq, s = token - b * P.seq;
+        const uint32_t b = token / P.seq, s = token - b * P.seq;
         int64_t t = P.position_offset + s;
         if (P.positions) {
             const int64_t at = b * P.position_stride[0] + s * P.position_stride[1];
@@ -76,13 +114,10 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
     }
     __syncthreads();
 
-    const uint32_t per_token = P.cols * P.head_groups;
-    const uint32_t sub = threadIdx.x / per_token;
-    const int64_t token = token0 + sub;
-    if (sub >= P.tokens_per_block || token >= P.tokens) return;
-    const uint32_t r = threadIdx.x - sub * per_token;
-    const uint32_t group = r / P.cols, col = r - group * P.cols;
-    const int64_t b = token / P.seq, s = token - b * P.seq;
+    const uint32_t per_token = P.cols * X.head_groups, sub = threadIdx.x / per_token, token = token0 + sub;
+    if (sub >= X.tokens_per_block || token >= P.tokens) return;
+    const uint32_t r = threadIdx.x - sub * per_token, group = r / P.cols, col = r - group * P.cols;
+    const uint32_t b = token / P.seq, s = token - b * P.seq;
 
     const bool rotated = col < P.rot_cols;
     uint32_t at0, at1;
@@ -96,69 +131,59 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         at1 = at0 + (P.cols - P.rot_cols) * N;
         two = at1 < P.head_dim;
     }
-    float c[N], sn[N];
-    if (rotated) {
+    const float2* cs = cos_sin + sub * pairs + col * N;
+    const int64_t in_step = X.in_stride[2] * X.head_groups, out_step = X.out_stride[2] * X.head_groups;
+    const T* x = reinterpret_cast<const T*>(X.in) + b * X.in_stride[0] + s * X.in_stride[1] + group * X.in_stride[2] + at0;
+    T* y = reinterpret_cast<T*>(X.out) + b * X.out_stride[0] + s * X.out_stride[1] + group * X.out_stride[2] + at0;
+    const uint32_t apart = at1 - at0;
+    using Piece = Raw<N * sizeof(T)>;
+    for (uint32_t first = group; first < X.heads; first += U * X.head_groups, x += U * in_step, y += U * out_step) {
+        Piece w0[U], w1[U];  // in flight as they lie in memory; widened one head at a time
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t pair = col * N + i;
-            const float2 v = pair < pairs ? cos_sin[sub * pairs + pair] : make_float2(1.f, 0.f);
-            c[i] = v.x, sn[i] = v.y;
-        }
-    }
-    const T* q = reinterpret_cast<const T*>(P.q_in) + b * P.q_in_stride[0] + s * P.q_in_stride[1];
-    const T* k = reinterpret_cast<const T*>(P.k_in) + b * P.k_in_stride[0] + s * P.k_in_stride[1] - P.n_q * P.k_in_stride[2];
-    T* qo = reinterpret_cast<T*>(P.q_out) + b * P.q_out_stride[0] + s * P.q_out_stride[1];
-    T* ko = reinterpret_cast<T*>(P.k_out) + b * P.k_out_stride[0] + s * P.k_out_stride[1] - P.n_q * P.k_out_stride[2];
-    for (uint32_t first = group; first < P.heads; first += U * P.head_groups) {
-        float x0[U][N], x1[U][N];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t h = first + u * P.head_groups;
-            if (h < P.heads) {
-                const T* x = h < P.n_q ? q + h * P.q_in_stride[2] : k + h * P.k_in_stride[2];
-                load_piece<T, N>(x0[u], x + at0);
-                if (two) load_piece<T, N>(x1[u], x + at1);
+        for (int u = 0; u < U; ++u)
+            if (first + u * X.head_groups < X.heads) {
+                w0[u] = *reinterpret_cast<const Piece*>(x + u * in_step);
+                if (two) w1[u] = *reinterpret_cast<const Piece*>(x + u * in_step + apart);
             }
-        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t h = first + u * P.head_groups;
-            if (h >= P.heads) continue;
-            T* y = h < P.n_q ? qo + h * P.q_out_stride[2] : ko + h * P.k_out_stride[2];
+            if (first + u * X.head_groups >= X.heads) break;
             if (rotated) {
+                float x0[N], x1[N];
+                widen<T, N>(x0, w0[u]);
+                widen<T, N>(x1, w1[u]);  // of no meaning, and not stored, where there is no second piece
                 if (!kInterleaved || N == 1) {
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const float a = x0[u][i], d = x1[u][i];
-                        x0[u][i] = fmaf(a, c[i], -(d * sn[i]));
-                        x1[u][i] = fmaf(d, c[i], a * sn[i]);
+                        const float a = x0[i], d = x1[i];
+                        x0[i] = fmaf(a, cs[i].x, -(d * cs[i].y));
+                        x1[i] = fmaf(d, cs[i].x, a * cs[i].y);
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < N; i += 2) {
                         const int j = i + 1 < N ? i + 1 : i;
-                        const float a = x0[u][i], d = x0[u][j];
-                        x0[u][i] = fmaf(a, c[i / 2], -(d * sn[i / 2]));
-                        x0[u][j] = fmaf(d, c[i / 2], a * sn[i / 2]);
-                        if (two) {
-                            const float e = x1[u][i], g = x1[u][j];
-                            x1[u][i] = fmaf(e, c[N / 2 + i / 2], -(g * sn[N / 2 + i / 2]));
-                            x1[u][j] = fmaf(g, c[N / 2 + i / 2], e * sn[N / 2 + i / 2]);
-                        }
+                        const float a = x0[i], d = x0[j];
+                        x0[i] = fmaf(a, cs[i / 2].x, -(d * cs[i / 2].y));
+                        x0[j] = fmaf(d, cs[i / 2].x, a * cs[i / 2].y);
+                        const float e = x1[i], g = x1[j];
+                        const float2 v = two ? cs[N / 2 + i / 2] : make_float2(1.f, 0.f);
+                        x1[i] = fmaf(e, v.x, -(g * v.y));
+                        x1[j] = fmaf(g, v.x, e * v.y);
                     }
                 }
+                w0[u] = rounded<T, N>(x0);
+                w1[u] = rounded<T, N>(x1);
             }
-            store_piece<T, N>(y + at0, x0[u]);
-            if (two) store_piece<T, N>(y + at1, x1[u]);
+            *reinterpret_cast<Piece*>(y + u * out_step) = w0[u];
+            if (two) *reinterpret_cast<Piece*>(y + u * out_step + apart) = w1[u];
         }
     }
 }
 
 template <typename T, int N, bool I>
 int launch(const RopeParams& P, cudaStream_t st) {
-    const int64_t blocks = (P.tokens + P.tokens_per_block - 1) / P.tokens_per_block;
-    if (blocks > 0x7fffffffll) return fail(HALOS_ERR_UNSUPPORTED, "rope: too many tokens");
-    rope_kernel<T, N, I, (N * sizeof(T) >= 8 ? 4 : 8)><<<(unsigned)blocks, kThreads, 0, st>>>(P);
+    rope_kernel<T, N, I, (N * sizeof(T) >= 8 ? 4 : 8)><<<P.x[0].blocks + P.x[1].blocks, kThreads, 0, st>>>(P);
     return cuda_status(cudaGetLastError(), "rope launch");
 }
 
@@ -191,6 +216,7 @@ extern "C" int halos_rope(const halos_rope_args* a) {
     const int64_t tokens = a->batch * a->seq;
     const uint32_t heads = a->n_q + a->n_k;
     if (tokens == 0 || heads == 0) return HALOS_OK;
+    if (tokens > 0x7fffffffll) return fail(HALOS_ERR_UNSUPPORTED, "rope: over 2^31 - 1 tokens");
     if ((a->n_q && (!a->q_in || !a->q_out)) || (a->n_k && (!a->k_in || !a->k_out)) || (a->rot_dim && !a->freqs))
         return fail(HALOS_ERR_INVALID_ARG, "rope: null pointer");
     const uint32_t size = a->dtype == HALOS_F32 ? 4 : 2;
@@ -210,25 +236,35 @@ extern "C" int halos_rope(const halos_rope_args* a) {
     if (int rc = enter(a->device)) return rc;
 
     RopeParams P{};
-    P.q_in = (const char*)a->q_in, P.k_in = (const char*)a->k_in, P.q_out = (char*)a->q_out, P.k_out = (char*)a->k_out;
+    P.x[0].in = (const char*)a->q_in, P.x[0].out = (char*)a->q_out, P.x[1].in = (const char*)a->k_in, P.x[1].out = (char*)a->k_out;
     P.freqs = a->freqs, P.positions = a->positions;
-    for (int i = 0; i < 3; ++i)
-        P.q_in_stride[i] = a->q_in_stride[i], P.k_in_stride[i] = a->k_in_stride[i], P.q_out_stride[i] = a->q_out_stride[i], P.k_out_stride[i] = a->k_out_stride[i];
+    for (int i = 0; i < 3; ++i) {
+        P.x[0].in_stride[i] = a->q_in_stride[i], P.x[0].out_stride[i] = a->q_out_stride[i];
+        P.x[1].in_stride[i] = a->k_in_stride[i], P.x[1].out_stride[i] = a->k_out_stride[i];
+    }
     P.position_stride[0] = a->position_stride[0], P.position_stride[1] = a->position_stride[1];
     P.position_offset = a->position_offset;
-    P.tokens = tokens, P.seq = (uint32_t)a->seq, P.n_q = a->n_q, P.heads = heads, P.head_dim = a->head_dim, P.rot_dim = a->rot_dim;
+    P.tokens = (uint32_t)tokens, P.seq = (uint32_t)a->seq, P.head_dim = a->head_dim, P.rot_dim = a->rot_dim;
     P.positions_64 = a->positions_64, P.inverse = a->inverse, P.magnitude = a->magnitude;
     P.rot_cols = (a->rot_dim + 2 * n - 1) / (2 * n);
     const bool in_place = (!a->n_q || a->q_in == a->q_out) && (!a->n_k || a->k_in == a->k_out);
     P.cols = P.rot_cols + (in_place ? 0 : (a->head_dim - a->rot_dim + 2 * n - 1) / (2 * n));
     if (P.cols == 0) return HALOS_OK;
     // As few threads per token as still fill the GPU: their fixed cost then falls on more heads.
-    const uint32_t most = kThreads / P.cols < heads ? kThreads / P.cols : heads;
     const int64_t want = ((int64_t)sm_count(a->device) * 1024 + tokens * P.cols - 1) / (tokens * P.cols);
-    uint32_t least = (heads + 7) / 8;
-    if (least > most) least = most;
-    P.head_groups = want > most ? most : want < least ? least : (uint32_t)want;
-    P.tokens_per_block = kThreads / (P.cols * P.head_groups);
+    for (int i = 0; i < 2; ++i) {
+        RopeTensor& X = P.x[i];
+        X.heads = i ? a->n_k : a->n_q;
+        if (!X.heads) continue;
+        const uint32_t most = kThreads / P.cols < X.heads ? kThreads / P.cols : X.heads;
+        uint32_t least = (X.heads + 7) / 8;
+        if (least > most) least = most;
+        X.head_groups = want > most ? most : want < least ? least : (uint32_t)want;
+        X.tokens_per_block = kThreads / (P.cols * X.head_groups);
+        const int64_t blocks = (tokens + X.tokens_per_block - 1) / X.tokens_per_block;
+        if (blocks > 0x3fffffffll) return fail(HALOS_ERR_UNSUPPORTED, "rope: too many tokens");
+        X.blocks = (uint32_t)blocks;
+    }
     cudaStream_t st = (cudaStream_t)a->stream;
     if (a->dtype == HALOS_F32) return by_layout<float>(P, n, a->layout, st);
     if (a->dtype == HALOS_BF16) return by_layout<__nv_bfloat16>(P, n, a->layout, st);
