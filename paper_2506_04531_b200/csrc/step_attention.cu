@@ -705,12 +705,12 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     char* tile_q = smem;
     char* tile_do = smem + F::kTileQ;
     char* stages = smem + 2 * F::kTileQ;  // each: K, V
-    __shared__ uint64_t bars[5 + F::kDPs + 2 * F::kStages];
+    __shared__ uint64_t bars[4 + 2 * F::kDPs + 2 * F::kStages];
     __shared__ uint32_t s_tmem;
     __shared__ int s_gave_up, s_lo[4], s_hi[4];
     const uint32_t bar0 = smem_u32(bars);
-    const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, ds_full = s_full + 8, s_read = s_full + 16,
-                   dp_full = s_full + 24;
+    const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, s_read = s_full + 8,
+                   dp_full = s_full + 16, ds_full = dp_full + 8 * F::kDPs;
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int kCopyWarp = 8, kMmaWarp = kCopyWarp + 1;
     const int heads = P.batch * P.n_q;
@@ -720,8 +720,9 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     if (threadIdx.x == 0) {
         bar_init(q_full, 1), bar_init(done, 1);
         for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
-        bar_init(s_full, 1), bar_init(ds_full, 256), bar_init(s_read, 256);
-        for (int s = 0; s < F::kDPs; ++s) bar_init(dp_full + 8 * s, 1);
+        bar_init(s_full, 1), bar_init(s_read, 256);
+        // A warp may be done with dS of a tile while another is still at the one before: each place has its own count.
+        for (int s = 0; s < F::kDPs; ++s) bar_init(dp_full + 8 * s, 1), bar_init(ds_full + 8 * s, 256);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_gave_up = 0;
     }
@@ -807,7 +808,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                     scores();
                     if (F::kDPs > 1) dp();
                 }
-                W.wait_warp(ds_full, j & 1);
+                W.wait_warp(ds_full + 8 * d3, (j / F::kDPs) & 1);
                 tc_after_sync();
                 if (issuer) {
                     product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + F::kColDP + d3 * 64, tile_at(s3), j > 0);
@@ -869,7 +870,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 fence_async_shared();
             }
             tc_before_sync();
-            bar_arrive(ds_full);
+            bar_arrive(ds_full + 8 * (j % F::kDPs));
         }
         if (n) W.wait_warp(done, 0);
         tc_after_sync();
