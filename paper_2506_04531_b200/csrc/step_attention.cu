@@ -41,6 +41,7 @@ struct Reach { int min_lo, max_hi, max_lo, min_hi; };
 
 struct AttentionParams {
     int sq, sk, head_dim, n_q, group, batch, causal, q_tiles, k_tiles, records;
+    int section;                      // key heads whose tiles are done side by side
     float scale, scale2;              // scale2 = scale log2(e)
     const int32_t *doc_start, *lens;
     const char *q, *k, *v, *o_in, *dout;
@@ -63,6 +64,15 @@ __device__ __forceinline__ void seen_by(const AttentionParams& P, int b, int i, 
     const int h = P.causal ? min(n, t + 1) : n;
     const int l = P.doc_start ? max(P.doc_start[(int64_t)b * P.sq + i], 0) : 0;
     if (l < h) lo = l, hi = h;
+}
+
+// Which tile of which head a CTA takes.  CTAs are numbered so that the longest come first where the mask is causal, and so that the
+// heads whose keys and values are being read at a time fit the L2 cache: sections of heads, within a section tile by tile.
+struct Place { int tile, b, h; };
+__device__ __forceinline__ Place place_of(const AttentionParams& P, int tiles, int heads_per_batch, int section, bool last_first) {
+    const int heads = P.batch * heads_per_batch, whole = section * tiles, sec = blockIdx.x / whole, at = blockIdx.x - sec * whole;
+    const int here = min(section, heads - sec * section), rank = at / here, bh = sec * section + at - rank * here, b = bh / heads_per_batch;
+    return Place{last_first ? tiles - 1 - rank : rank, b, bh - b * heads_per_batch};
 }
 
 template <typename T>
@@ -117,10 +127,8 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
     const uint32_t k_full = pv_done + 8 * F::kRing, v_full = k_full + 8 * F::kStages, k_free = v_full + 8 * F::kStages, v_free = k_free + 8 * F::kStages;
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
 
-    // Longest rows first where the mask is causal.
-    const int heads = P.batch * P.n_q;
-    const int tile = P.causal ? P.q_tiles - 1 - (int)(blockIdx.x / heads) : (int)(blockIdx.x / heads);
-    const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
+    const Place place = place_of(P, P.q_tiles, P.n_q, P.section * P.group, P.causal);
+    const int tile = place.tile, b = place.b, h = place.h, hk = h / P.group;
 
     if (threadIdx.x == 0) {
         bar_init(q_full, 1), bar_init(left, 1);
@@ -339,77 +347,67 @@ __device__ __forceinline__ float dot(const T* x, const T* y, int head_dim) {
     for (int c = 0; c < head_dim; c += 8) sum = dot8<T>(*reinterpret_cast<const uint4*>(x + c), *reinterpret_cast<const uint4*>(y + c), sum);
     return sum;
 }
-__device__ __forceinline__ float sum_of_8(float v) {
-#pragma unroll
-    for (int s = 4; s; s >>= 1) v += __shfl_xor_sync(~0u, v, s);
-    return v;
-}
-
 // D = dout . o is off by the rounding of o to 16 bits, and ds = p (dp - D) by as much whatever its own size.  Against the sum over
 // many keys that is little; a query with few keys, whose dp and D nearly cancel, would lose half of its digits to it.
 // Its D is formed from sum p dp instead, in 32 bits.
 constexpr int kFewKeys = 16;
 
-// Records of 64 queries of a head, and once per batch row their reach.  Eight threads take four queries, with all their loads in flight at once.
+// Records of 64 queries of a head, and once per batch row their reach.  Four threads to a query: with eight most instructions were
+// addresses, with one the loads of a warp lay too far apart.
 template <typename T>
-__global__ void __launch_bounds__(128) attention_record_kernel(const __grid_constant__ AttentionParams P) {
-    constexpr int kEach = 4;
-    const int rec = blockIdx.x, h = blockIdx.y, b = blockIdx.z, group = threadIdx.x >> 3, part = threadIdx.x & 7;
-    const int64_t row0 = ((int64_t)b * P.n_q + h) * P.sq;
+__global__ void __launch_bounds__(4 * kRecord) attention_record_kernel(const __grid_constant__ AttentionParams P) {
+    const int rec = blockIdx.x, h = blockIdx.y, b = blockIdx.z, r = threadIdx.x >> 2, part = threadIdx.x & 3, i = rec * kRecord + r;
     Record* R = P.record + ((int64_t)b * P.n_q + h) * P.records + rec;
-    __shared__ Reach s_reach[4];
-    float delta[kEach], lse2[kEach];
-    int lo[kEach], hi[kEach];
-    uint4 o[kEach][2], d[kEach][2];
+    __shared__ Reach s_reach[8];
+    __shared__ int s_lo[kRecord], s_hi[kRecord];
+    __shared__ float s_lse2[kRecord], s_term[kRecord][kFewKeys + 1];
+    float delta = 0.f, lse2 = 0.f;
+    if (i < P.sq) {  // rows that see nothing are read too; what comes of it is not used
+        const T* o = row_of<T>(P.o_in, P.o_stride, b, i, h) + 8 * part;
+        const T* d = row_of<T>(P.dout, P.dout_stride, b, i, h) + 8 * part;
+        uint4 x[4], y[4];
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {  // rows that see nothing are read too; what comes of it is not used
-        const int i = rec * kRecord + u * 16 + group;
+        for (int c = 0; c < 4; ++c)
+            if (8 * part + 32 * c < P.head_dim) x[c] = *reinterpret_cast<const uint4*>(o + 32 * c), y[c] = *reinterpret_cast<const uint4*>(d + 32 * c);
+        lse2 = P.lse[((int64_t)b * P.n_q + h) * P.sq + i] * kLog2e;
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            const int c = part * 8 + v * 64;
-            o[u][v] = d[u][v] = make_uint4(0, 0, 0, 0);
-            if (i < P.sq && c < P.head_dim) {
-                o[u][v] = *reinterpret_cast<const uint4*>(row_of<T>(P.o_in, P.o_stride, b, i, h) + c);
-                d[u][v] = *reinterpret_cast<const uint4*>(row_of<T>(P.dout, P.dout_stride, b, i, h) + c);
+        for (int c = 0; c < 4; ++c)
+            if (8 * part + 32 * c < P.head_dim) delta = dot8<T>(x[c], y[c], delta);
+    }
+    delta += __shfl_xor_sync(~0u, delta, 1);
+    delta += __shfl_xor_sync(~0u, delta, 2);
+    int lo, hi;
+    seen_by(P, b, i, lo, hi);
+    // The queries with few keys, a thread to a query and a key; the terms are added in the order of the keys.
+    const bool few = hi && hi - lo <= kFewKeys;
+    if (part == 0) s_lse2[r] = lse2, s_lo[r] = lo, s_hi[r] = few ? hi : 0;
+    if (__syncthreads_or(few)) {
+        for (int p = threadIdx.x; p < kRecord * kFewKeys; p += 4 * kRecord) {
+            const int q = p / kFewKeys, k = p % kFewKeys, query = rec * kRecord + q;
+            if (s_lo[q] + k < s_hi[q] && s_hi[q]) {
+                const int j = s_lo[q] + k;
+                const float s = dot<T>(row_of<T>(P.q, P.q_stride, b, query, h), row_of<T>(P.k, P.k_stride, b, j, h / P.group), P.head_dim);
+                const float dp = dot<T>(row_of<T>(P.dout, P.dout_stride, b, query, h), row_of<T>(P.v, P.v_stride, b, j, h / P.group), P.head_dim);
+                s_term[q][k] = fast_exp2(fmaf(s, P.scale2, -s_lse2[q])) * dp;
             }
         }
-        lse2[u] = i < P.sq ? P.lse[row0 + i] * kLog2e : 0.f;
+        __syncthreads();
+        if (few) {
+            delta = 0.f;
+            for (int k = 0; k < hi - lo; ++k) delta += s_term[r][k];
+        }
     }
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        seen_by(P, b, rec * kRecord + u * 16 + group, lo[u], hi[u]);
-        delta[u] = dot8<T>(o[u][1], d[u][1], dot8<T>(o[u][0], d[u][0], 0.f));
-    }
-    Reach a{INT_MAX, 0, 0, INT_MAX};
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const int r = u * 16 + group, i = rec * kRecord + r;
-        float total = sum_of_8(delta[u]);
-        const bool few = hi[u] && hi[u] - lo[u] <= kFewKeys;
-        if (__any_sync(~0u, few)) {  // each of the eight threads takes every eighth key
-            float sum = 0.f;
-            for (int j = lo[u] + part; few && j < hi[u]; j += 8) {
-                const float s = dot<T>(row_of<T>(P.q, P.q_stride, b, i, h), row_of<T>(P.k, P.k_stride, b, j, h / P.group), P.head_dim);
-                const float dp = dot<T>(row_of<T>(P.dout, P.dout_stride, b, i, h), row_of<T>(P.v, P.v_stride, b, j, h / P.group), P.head_dim);
-                sum = fmaf(fast_exp2(fmaf(s, P.scale2, -lse2[u])), dp, sum);
-            }
-            sum = sum_of_8(sum);
-            if (few) total = sum;
-        }
-        if (part == 0) {
-            R->minus_lse2[r] = hi[u] ? -lse2[u] : -INFINITY;
-            R->minus_delta[r] = hi[u] ? -total : 0.f;
-            R->lo[r] = lo[u];
-            R->hi[r] = hi[u];
-        }
-        if (i < P.sq) {  // rows past the end are zeros and need no mask
-            a.min_lo = min(a.min_lo, lo[u]), a.max_hi = max(a.max_hi, hi[u]);
-            a.max_lo = max(a.max_lo, lo[u]), a.min_hi = min(a.min_hi, hi[u]);
-        }
+    if (part == 0) {
+        R->minus_lse2[r] = hi ? -lse2 : -INFINITY;
+        R->minus_delta[r] = hi ? -delta : 0.f;
+        R->lo[r] = lo;
+        R->hi[r] = hi;
     }
     if (h == 0) {
+        Reach a{INT_MAX, 0, 0, INT_MAX};
+        if (i < P.sq) a = Reach{lo, hi, lo, hi};  // rows past the end are zeros and need no mask
 #pragma unroll
-        for (int s = 16; s >= 8; s >>= 1) {
+        for (int s = 16; s >= 4; s >>= 1) {
             a.min_lo = min(a.min_lo, __shfl_xor_sync(~0u, a.min_lo, s));
             a.max_hi = max(a.max_hi, __shfl_xor_sync(~0u, a.max_hi, s));
             a.max_lo = max(a.max_lo, __shfl_xor_sync(~0u, a.max_lo, s));
@@ -418,11 +416,9 @@ __global__ void __launch_bounds__(128) attention_record_kernel(const __grid_cons
         if ((threadIdx.x & 31) == 0) s_reach[threadIdx.x >> 5] = a;
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 1; w < 4; ++w) {
-                a.min_lo = min(a.min_lo, s_reach[w].min_lo);
-                a.max_hi = max(a.max_hi, s_reach[w].max_hi);
-                a.max_lo = max(a.max_lo, s_reach[w].max_lo);
-                a.min_hi = min(a.min_hi, s_reach[w].min_hi);
+            for (int w = 1; w < 8; ++w) {
+                const Reach c = s_reach[w];
+                a = Reach{min(a.min_lo, c.min_lo), max(a.max_hi, c.max_hi), max(a.max_lo, c.max_lo), min(a.min_hi, c.min_hi)};
             }
             P.reach[(int64_t)b * P.records + rec] = a;
         }
@@ -461,8 +457,8 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int kCopyWarp = 8 * kSlots, kMmaWarp = kCopyWarp + 1;
 
-    const int n_kv = P.n_q / P.group, heads = P.batch * n_kv;
-    const int tile = blockIdx.x / heads, bh = blockIdx.x % heads, b = bh / n_kv, hk = bh % n_kv;  // under a causal mask the first keys have the most queries
+    const Place place = place_of(P, P.k_tiles, P.n_q / P.group, P.section, false);  // under a causal mask the first keys have the most queries
+    const int tile = place.tile, b = place.b, hk = place.h;
     const int key0 = tile * 128;
 
     if (threadIdx.x == 0) {
@@ -713,9 +709,8 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                    dp_full = s_full + 16, ds_full = dp_full + 8 * F::kDPs;
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int kCopyWarp = 8, kMmaWarp = kCopyWarp + 1;
-    const int heads = P.batch * P.n_q;
-    const int tile = P.causal ? P.q_tiles - 1 - (int)(blockIdx.x / heads) : (int)(blockIdx.x / heads);
-    const int bh = blockIdx.x % heads, b = bh / P.n_q, h = bh % P.n_q, hk = h / P.group;
+    const Place place = place_of(P, P.q_tiles, P.n_q, P.section * P.group, P.causal);
+    const int tile = place.tile, b = place.b, h = place.h, hk = h / P.group;
 
     if (threadIdx.x == 0) {
         bar_init(q_full, 1), bar_init(done, 1);
@@ -961,6 +956,9 @@ int check(const halos_attention_args* a, bool back) {
 int params(const halos_attention_args* a, AttentionParams& P) {
     P.sq = (int)a->sq, P.sk = (int)a->sk, P.head_dim = a->head_dim, P.n_q = a->n_q, P.group = a->n_q / a->n_kv, P.batch = (int)a->batch;
     P.causal = a->causal != 0, P.q_tiles = (P.sq + 127) / 128, P.k_tiles = (P.sk + 127) / 128, P.records = (int)(round_up(a->sq, 128) / kRecord);
+    // Keys and values of the heads of a section: 40 MB of the 126 MB L2 cache at most, one head at least.
+    const int64_t head_bytes = (a->sk > 0 ? a->sk : 1) * 4 * (a->head_dim <= 64 ? 64 : 128), heads = a->batch * a->n_kv;
+    P.section = (int)(heads < 40000000 / head_bytes ? heads : head_bytes < 40000000 ? 40000000 / head_bytes : 1);
     P.scale = a->scale, P.scale2 = a->scale * kLog2e, P.doc_start = a->doc_start, P.lens = a->lens;
     P.q = (const char*)a->q, P.k = (const char*)a->k, P.v = (const char*)a->v;
     P.o_in = P.o = (char*)a->o, P.dout = (const char*)a->dout, P.dq = (char*)a->dq, P.dk = (char*)a->dk, P.dv = (char*)a->dv, P.lse = a->lse;
@@ -1005,7 +1003,7 @@ int backward(const halos_attention_args* a) {
     if (int rc = allow_smem(attention_keys_kernel<T, DP, kKeySlots>, K::kSmem, allowed_keys)) return rc;
     if (int rc = allow_smem(attention_queries_kernel<T, DP>, Q::kSmem, allowed_queries)) return rc;
     if (P.sq) {
-        attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 128, 0, st>>>(P);
+        attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 4 * kRecord, 0, st>>>(P);
         if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
     }
     if (P.sk) {
