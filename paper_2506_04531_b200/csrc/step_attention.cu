@@ -681,14 +681,22 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
 }
 
 // dQ of 128 queries, two CTAs to an SM, the keys 64 at a time; four warps take the first 32 keys of a tile, four the others.
+// K of a tile is needed from S to dQ, V only for dP: heads of 128, whose tiles fill shared memory to the last KB, have two
+// places for K and one for V.
 template <int DP> struct Queries {
     static constexpr int kTileQ = 128 * DP * 2, kTileK = 64 * DP * 2;
     static constexpr int kDPs = DP == 64 ? 2 : 1;                 // places for dP, and dS over it, beside one for S
-    static constexpr int kStages = DP == 64 ? 4 : 1;
+    static constexpr int kStagesK = DP == 64 ? 4 : 2, kStagesV = DP == 64 ? 4 : 1;
     static constexpr int kColDP = 64, kColDQ = 64 + 64 * kDPs, kColumns = 256;
-    static constexpr int kSmem = 1024 + 2 * kTileQ + 2 * kStages * kTileK;
     static constexpr int kThreads = 256 + 64;
+    struct Control {
+        uint64_t bars[4 + 2 * kDPs + 2 * kStagesK + 2 * kStagesV];
+        uint32_t tmem;
+        int gave_up, lo[4], hi[4];
+    };
+    static constexpr int kTiles = 2 * kTileQ + (kStagesK + kStagesV) * kTileK, kSmem = kTiles + sizeof(Control);
     static_assert(kColDQ + DP <= kColumns, "tensor memory");
+    static_assert(2 * (kSmem + 1024) <= kSharedPerSM, "two CTAs to an SM");
 };
 
 template <typename T, int DP>
@@ -696,17 +704,18 @@ __global__ void __launch_bounds__(Queries<DP>::kThreads, 2)
 attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                          const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do) {
     using F = Queries<DP>;
-    extern __shared__ char smem_raw[];
-    char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    extern __shared__ __align__(1024) char smem[];  // all of it dynamic, so that it begins where the tiles have to
     char* tile_q = smem;
     char* tile_do = smem + F::kTileQ;
-    char* stages = smem + 2 * F::kTileQ;  // each: K, V
-    __shared__ uint64_t bars[4 + 2 * F::kDPs + 2 * F::kStages];
-    __shared__ uint32_t s_tmem;
-    __shared__ int s_gave_up, s_lo[4], s_hi[4];
-    const uint32_t bar0 = smem_u32(bars);
-    const uint32_t q_full = bar0, done = bar0 + 8, full = bar0 + 16, free_ = full + 8 * F::kStages, s_full = free_ + 8 * F::kStages, s_read = s_full + 8,
-                   dp_full = s_full + 16, ds_full = dp_full + 8 * F::kDPs;
+    char* tiles_k = smem + 2 * F::kTileQ;
+    char* tiles_v = tiles_k + F::kStagesK * F::kTileK;
+    typename F::Control& C = *reinterpret_cast<typename F::Control*>(smem + F::kTiles);
+    const uint32_t q_full = smem_u32(C.bars), done = q_full + 8, s_full = q_full + 16, s_read = q_full + 24, dp_full = q_full + 32, ds_full = dp_full + 8 * F::kDPs,
+                   k_full = ds_full + 8 * F::kDPs, k_free = k_full + 8 * F::kStagesK, v_full = k_free + 8 * F::kStagesK, v_free = v_full + 8 * F::kStagesV;
+    if (smem_u32(smem) & 1023) {  // then no tile would lie as its descriptors say
+        if (threadIdx.x == 0) atomicExch(P.fault, 1);
+        return;
+    }
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int kCopyWarp = 8, kMmaWarp = kCopyWarp + 1;
     const Place place = place_of(P, P.q_tiles, P.n_q, P.section * P.group, P.causal);
@@ -714,14 +723,15 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
 
     if (threadIdx.x == 0) {
         bar_init(q_full, 1), bar_init(done, 1);
-        for (int s = 0; s < F::kStages; ++s) bar_init(full + 8 * s, 1), bar_init(free_ + 8 * s, 1);
+        for (int s = 0; s < F::kStagesK; ++s) bar_init(k_full + 8 * s, 1), bar_init(k_free + 8 * s, 1);
+        for (int s = 0; s < F::kStagesV; ++s) bar_init(v_full + 8 * s, 1), bar_init(v_free + 8 * s, 1);
         bar_init(s_full, 1), bar_init(s_read, 256);
         // A warp may be done with dS of a tile while another is still at the one before: each place has its own count.
         for (int s = 0; s < F::kDPs; ++s) bar_init(dp_full + 8 * s, 1), bar_init(ds_full + 8 * s, 256);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        s_gave_up = 0;
+        C.gave_up = 0;
     }
-    if (warp == kMmaWarp) tmem_alloc<F::kColumns>(smem_u32(&s_tmem));
+    if (warp == kMmaWarp) tmem_alloc<F::kColumns>(smem_u32(&C.tmem));
     const int row = threadIdx.x & 127, i = tile * 128 + row;
     int lo = INT_MAX, hi = 0;
     float minus_lse2 = -INFINITY, minus_delta = 0.f;
@@ -733,15 +743,15 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
         int l = lo, g = hi;
 #pragma unroll
         for (int o = 16; o; o >>= 1) l = min(l, __shfl_xor_sync(~0u, l, o)), g = max(g, __shfl_xor_sync(~0u, g, o));
-        if (lane == 0 && warp < 4) s_lo[warp] = l, s_hi[warp] = g;
+        if (lane == 0 && warp < 4) C.lo[warp] = l, C.hi[warp] = g;
     }
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
-    const uint32_t tmem = uniform(s_tmem);
-    const int min_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), max_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
+    const uint32_t tmem = uniform(C.tmem);
+    const int min_lo = min(min(C.lo[0], C.lo[1]), min(C.lo[2], C.lo[3])), max_hi = max(max(C.hi[0], C.hi[1]), max(C.hi[2], C.hi[3]));
     const int first = uniform(max_hi ? min_lo / 64 : 0), n = uniform(max_hi ? (max_hi + 63) / 64 - first : 0);
-    const Waits W{&s_gave_up, P.fault};
+    const Waits W{&C.gave_up, P.fault};
 
     if (warp == kCopyWarp) {
         if (n) {
@@ -753,52 +763,58 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                     tma_load(smem_u32(tile_do) + d * 128 * 128, &map_do, q_full, d * 64, tile * 128, h, b);
                 }
             }
-            int j = 0, s = 0, use = 1;
-            for (; j < n; ++j) {
-                if (j >= F::kStages) W.wait_warp(free_ + 8 * s, use);
-                if (issuer) {
-                    const uint32_t at = smem_u32(stages) + s * 2 * F::kTileK, bar = full + 8 * s;
-                    bar_expect(bar, 2 * F::kTileK);
-                    for (int d = 0; d < DP / 64; ++d) {
-                        tma_load(at + d * 64 * 128, &map_k, bar, d * 64, (first + j) * 64, hk, b);
-                        tma_load(at + F::kTileK + d * 64 * 128, &map_v, bar, d * 64, (first + j) * 64, hk, b);
-                    }
-                }
-                if (++s == F::kStages) s = 0, use ^= 1;
+            int s = 0, use = 1, sv = 0, use_v = 1;
+            const auto load = [&](const CUtensorMap* map, uint32_t at, uint32_t bar, int row) {
+                if (!issuer) return;
+                bar_expect(bar, F::kTileK);
+                for (int d = 0; d < DP / 64; ++d) tma_load(at + d * 64 * 128, map, bar, d * 64, row, hk, b);
+            };
+            for (int j = 0; j < n; ++j) {
+                if (j >= F::kStagesK) W.wait_warp(k_free + 8 * s, use);
+                load(&map_k, smem_u32(tiles_k) + s * F::kTileK, k_full + 8 * s, (first + j) * 64);
+                if (j >= F::kStagesV) W.wait_warp(v_free + 8 * sv, use_v);
+                load(&map_v, smem_u32(tiles_v) + sv * F::kTileK, v_full + 8 * sv, (first + j) * 64);
+                if (++s == F::kStagesK) s = 0, use ^= 1;
+                if (++sv == F::kStagesV) sv = 0, use_v ^= 1;
             }
             if (*W.gave_up) {
                 W.drain(q_full, 0);
-                for (int i = max(0, n - F::kStages); i < n; ++i) W.drain(full + 8 * (i % F::kStages), (i / F::kStages) & 1);
+                for (int i = max(0, n - F::kStagesK); i < n; ++i) W.drain(k_full + 8 * (i % F::kStagesK), (i / F::kStagesK) & 1);
+                for (int i = max(0, n - F::kStagesV); i < n; ++i) W.drain(v_full + 8 * (i % F::kStagesV), (i / F::kStagesV) & 1);
             }
         }
     } else if (warp == kMmaWarp) {
         if (n) {
             const bool issuer = elected();
-            int s1 = 0, use1 = 0, s2 = 0, s3 = 0, d2 = 0, d3 = 0;  // stages as for the keys; places of dP
-            const auto tile_at = [&](int s) { return smem_u32(stages) + s * 2 * F::kTileK; };
+            // places: of K whose scores come next, of V, of K being used up, of dP coming next, of dS being used up
+            int s1 = 0, use1 = 0, s2 = 0, use2 = 0, s3 = 0, d2 = 0, d3 = 0;
             const auto next = [](int& s, int of) { s = s + 1 == of ? 0 : s + 1; };
             const auto scores = [&] {
-                W.wait_warp(full + 8 * s1, use1);
+                W.wait_warp(k_full + 8 * s1, use1);
                 tc_after_sync();
                 if (issuer) {
-                    product_ss<T, 64, DP, 128, 64>(tmem, smem_u32(tile_q), tile_at(s1));
+                    product_ss<T, 64, DP, 128, 64>(tmem, smem_u32(tile_q), smem_u32(tiles_k) + s1 * F::kTileK);
                     mma_commit(s_full);
                 }
-                next(s1, F::kStages);
+                next(s1, F::kStagesK);
                 use1 ^= s1 == 0;
             };
             const auto dp = [&] {
+                W.wait_warp(v_full + 8 * s2, use2);
+                tc_after_sync();
                 if (issuer) {
-                    product_ss<T, 64, DP, 128, 64>(tmem + F::kColDP + d2 * 64, smem_u32(tile_do), tile_at(s2) + F::kTileK);
+                    product_ss<T, 64, DP, 128, 64>(tmem + F::kColDP + d2 * 64, smem_u32(tile_do), smem_u32(tiles_v) + s2 * F::kTileK);
                     mma_commit(dp_full + 8 * d2);
+                    mma_commit(v_free + 8 * s2);
                 }
-                next(s2, F::kStages), next(d2, F::kDPs);
+                next(s2, F::kStagesV), next(d2, F::kDPs);
+                use2 ^= s2 == 0;
             };
             W.wait_warp(q_full, 0);
             scores(), dp();
             for (int j = 0; j < n; ++j) {
                 // the next S can follow once this one has been read, the next dP too where it has a place of its own
-                if (F::kStages > 1 && j + 1 < n) {
+                if (j + 1 < n) {
                     W.wait_warp(s_read, j & 1);
                     scores();
                     if (F::kDPs > 1) dp();
@@ -806,14 +822,11 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                 W.wait_warp(ds_full + 8 * d3, (j / F::kDPs) & 1);
                 tc_after_sync();
                 if (issuer) {
-                    product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + F::kColDP + d3 * 64, tile_at(s3), j > 0);
-                    mma_commit(free_ + 8 * s3);
+                    product_ts<T, DP, 64, 32>(tmem + F::kColDQ, tmem + F::kColDP + d3 * 64, smem_u32(tiles_k) + s3 * F::kTileK, j > 0);
+                    mma_commit(k_free + 8 * s3);
                 }
-                next(s3, F::kStages), next(d3, F::kDPs);
-                if (j + 1 < n) {
-                    if (F::kStages == 1) scores();
-                    if (F::kDPs == 1) dp();
-                }
+                next(s3, F::kStagesK), next(d3, F::kDPs);
+                if (F::kDPs == 1 && j + 1 < n) dp();
             }
             if (issuer) mma_commit(done);
             if (*W.gave_up) W.drain(done, 0);
@@ -824,7 +837,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
         const float2 factor = both(P.scale2), ml = both(minus_lse2), md = both(minus_delta);
         const bool one = hi - lo == 1;  // a softmax of one term is constant
         for (int j = 0; j < n; ++j) {
-            const int s = j % F::kStages, tile0 = (first + j) * 64, key0 = tile0 + part * 32;
+            const int s = j % F::kStagesK, tile0 = (first + j) * 64, key0 = tile0 + part * 32;
             const uint32_t at_dp = lanes + F::kColDP + (j % F::kDPs) * 64 + part * 32;
             W.wait_warp(s_full, j & 1);
             tc_after_sync();
@@ -860,8 +873,8 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
             tmem_wait_stores();
             if (part == 0 && (tile0 < min_lo || (tile0 + 64 > max_hi && max_hi < P.sk))) {
                 // the copy's writes become visible through its own barrier
-                W.wait_warp(full + 8 * s, (j / F::kStages) & 1);
-                if (row < 64 && (tile0 + row < min_lo || tile0 + row >= max_hi)) clear_row<DP>(stages + s * 2 * F::kTileK, 64, row);
+                W.wait_warp(k_full + 8 * s, (j / F::kStagesK) & 1);
+                if (row < 64 && (tile0 + row < min_lo || tile0 + row >= max_hi)) clear_row<DP>(tiles_k + s * F::kTileK, 64, row);
                 fence_async_shared();
             }
             tc_before_sync();

@@ -37,6 +37,14 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.b32 %0, 1, 0, p; }"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+
 // Waits are bounded: one that runs out marks the CTA and *fault, and from then on every wait of the CTA returns at once.  All loops go on
 // to their ends, within their buffers but with whatever is there, and before a CTA ends its copies and products in
 // flight are waited for (again with a bound), so that tensor memory is given back and nothing hangs.
@@ -45,7 +53,7 @@ struct Waits {
     volatile int* gave_up;  // in shared memory
     int* fault;             // in device memory
     __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity) const {
-        if (!bar_try(bar, parity)) wait_longer(bar, parity);
+        if (!bar_test(bar, parity)) wait_longer(bar, parity);
     }
     // For a warp whose next instruction is one for all its lanes together.
     __device__ __forceinline__ void wait_warp(uint32_t bar, uint32_t parity) const {
