@@ -519,15 +519,21 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
             for (int k = 0; k < chunks; ++k) {
                 W.wait_warp(full + 8 * k, it & 1);
                 uint4 x[U];
-                uint32_t top_word = low_word<T>();
+                uint32_t tops[U];
+                const uint4* from = held + k * H::kChunk + threadIdx.x;
+                if ((k + 1) * H::kChunk <= c.vectors) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int v = k * H::kChunk + u * kThreads + threadIdx.x;
+                    for (int u = 0; u < U; ++u) x[u] = from[u * kThreads];
+                } else {
                     const uint32_t low = low_word<T>();
-                    x[u] = v < c.vectors ? held[v] : make_uint4(low, low, low, low);
-                    top_word = max_words<T>(top_word, max_words<T>(max_words<T>(x[u].x, x[u].y), max_words<T>(x[u].z, x[u].w)));
+#pragma unroll
+                    for (int u = 0; u < U; ++u) x[u] = k * H::kChunk + u * kThreads + threadIdx.x < c.vectors ? from[u * kThreads] : make_uint4(low, low, low, low);
                 }
-                const float top = max_in_word<T>(top_word);
+#pragma unroll
+                for (int u = 0; u < U; ++u) tops[u] = max_words<T>(max_words<T>(x[u].x, x[u].y), max_words<T>(x[u].z, x[u].w));
+#pragma unroll
+                for (int u = 1; u < U; ++u) tops[0] = max_words<T>(tops[0], tops[u]);
+                const float top = max_in_word<T>(tops[0]);
                 if (top > m) {
                     const float fT = m == -INFINITY ? 0.f : fast_exp2((m - top) * cT), f1 = m == -INFINITY ? 0.f : fast_exp2((m - top) * c1);
                     sT = mul2(sT, make_float2(fT, fT)), s1 = mul2(s1, make_float2(f1, f1));  // s1 stays 0 where T = 1
@@ -588,22 +594,34 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
             for (int k = 0; k < chunks; ++k) {
                 if (!want_stats) W.wait_warp(full + 8 * k, it & 1);
                 uint4 x[U];
+                const uint4* from = held + k * H::kChunk + threadIdx.x;
+                uint4* to = out + k * H::kChunk + threadIdx.x;
+                const bool whole = (k + 1) * H::kChunk <= c.vectors;
+                const auto inside = [&](int u) { return whole || k * H::kChunk + u * kThreads + threadIdx.x < c.vectors; };
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int v = k * H::kChunk + u * kThreads + threadIdx.x;
-                    if (v < c.vectors) x[u] = held[v];
-                }
+                for (int u = 0; u < U; ++u)
+                    if (inside(u)) x[u] = from[u * kThreads];
                 __syncwarp();
                 if (lane == 0) bar_arrive(free_ + 8 * k);
+                if (S.ignored) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int v = k * H::kChunk + u * kThreads + threadIdx.x;
-                    if (v < c.vectors) {
-                        float2 f[kPairs];
+                    for (int u = 0; u < U; ++u)
+                        if (inside(u)) __stcs(to + u * kThreads, make_uint4(0, 0, 0, 0));
+                    continue;
+                }
+                const auto form = [&](int u) {
+                    float2 f[kPairs];
 #pragma unroll
-                        for (int q = 0; q < kPairs; ++q) f[q] = gradient(Pairs<T>::get(x[u], q));
-                        __stcs(out + v, S.ignored ? make_uint4(0, 0, 0, 0) : Pairs<T>::join(f));
-                    }
+                    for (int q = 0; q < kPairs; ++q) f[q] = gradient(Pairs<T>::get(x[u], q));
+                    __stcs(to + u * kThreads, Pairs<T>::join(f));
+                };
+                if (whole) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) form(u);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (inside(u)) form(u);
                 }
             }
             if (threadIdx.x < c.singles) dz[c.single(threadIdx.x)] = from_f32<T>(S.ignored ? 0.f : gradient(make_float2(extra, extra)).x);
