@@ -85,7 +85,4 @@ __device__ __forceinline__ float fast_exp2(float x) {
 }
 __device__ __forceinline__ float2 exp2_both(float2 x) { return make_float2(fast_exp2(x.x), fast_exp2(x.y)); }
 
-// N elements in one access; the address is a multiple of N elements (16 bytes at most).
-template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T v[N]; };
-
 }  // namespace halos_step

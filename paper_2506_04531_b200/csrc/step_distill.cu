@@ -46,244 +46,6 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// What warp 0 finds out about a row's teacher and label, for everybody.
-struct RowShared {
-    float p[kMaxTeacher], z[kMaxTeacher];   // teacher's probabilities and the row's logits at its entries
-    int32_t idx[kMaxTeacher];
-    float warp_m[32], warp_s1[32], warp_sT[32];
-    float plogp, label_z, pz;               // sum p log p; z at the label; sum p z
-    int64_t label;
-    int ignored, bad, any;                  // label is ignore_index; something points outside; the teacher sent something
-};
-
-template <typename T>
-__device__ void read_teacher(const DistillParams& P, const T* z, int64_t row, RowShared& S) {
-    const int lane = threadIdx.x & 31;
-    int64_t label = 0;
-    int ignored = 0, bad = 0;
-    if (P.labels) {
-        label = P.labels_64 ? static_cast<const int64_t*>(P.labels)[row] : (int64_t)static_cast<const int32_t*>(P.labels)[row];
-        ignored = label == P.ignore_index;
-        bad = !ignored && (label < 0 || label >= P.vocab);
-    }
-    const float invT = 1.f / P.temperature;
-    float top = -INFINITY;
-    for (uint32_t i = lane; i < P.k; i += 32) {
-        const int64_t at = row * P.index_stride + i;
-        const int64_t j = P.index_64 ? static_cast<const int64_t*>(P.index)[at] : (int64_t)static_cast<const int32_t*>(P.index)[at];
-        const bool in = j >= 0 && j < P.vocab;
-        if (!in && j != -1) bad = 1;
-        S.idx[i] = in ? (int32_t)j : -1;
-        S.z[i] = in && !ignored ? to_f32<T>(z[j]) : 0.f;
-        const float t = in ? teacher_at(P, row * P.t_stride + i) * invT : -INFINITY;
-        S.p[i] = t;
-        top = fmaxf(top, t);
-    }
-    top = warp_max(top);
-    float sum = 0.f;
-    for (uint32_t i = lane; i < P.k; i += 32)
-        if (S.p[i] != -INFINITY) sum += exp2f((S.p[i] - top) * kLog2e);
-    sum = warp_sum(sum);
-    const float log_sum = logf(sum);
-    float plogp = 0.f, pz = 0.f;
-    for (uint32_t i = lane; i < P.k; i += 32) {
-        const float t = S.p[i];
-        float p = 0.f;
-        if (t != -INFINITY) {
-            const float logp = t - top - log_sum;
-            p = expf(logp);
-            if (p > 0.f) plogp += p * logp, pz += p * S.z[i];  // 0 log 0 = 0, whatever the logit there
-        }
-        S.p[i] = p;
-    }
-    plogp = warp_sum(plogp);
-    pz = warp_sum(pz);
-    bad = __any_sync(~0u, bad);
-    if (lane == 0) {
-        S.plogp = plogp;
-        S.pz = pz;
-        S.any = sum > 0.f;
-        S.label = label;
-        S.ignored = ignored;
-        S.bad = bad;
-        S.label_z = P.labels && !ignored && !bad ? to_f32<T>(z[label]) : 0.f;
-    }
-}
-
-// x^T for T = 2^n by n squarings
-template <int n> __device__ __forceinline__ float squared(float x) {
-#pragma unroll
-    for (int i = 0; i < n; ++i) x *= x;
-    return x;
-}
-
-// kSquarings: T = 1, 2, 4 as 0, 1, 2; any other T as -1.
-template <int kSquarings>
-struct Online {
-    float m = -INFINITY, s1 = 0.f, sT = 0.f;
-    __device__ __forceinline__ void rescale(float to, float c1, float cT) {
-        const float d = m - to;
-        const float fT = m == -INFINITY ? 0.f : exp2f(d * cT);
-        s1 *= kSquarings >= 0 ? squared<kSquarings < 0 ? 0 : kSquarings>(fT) : (m == -INFINITY ? 0.f : exp2f(d * c1));
-        sT *= fT;
-        m = to;
-    }
-    // The difference comes before the factor: a logit of the type's lowest value times log2(e) would be -infinity, and
-    // -infinity minus itself no number.
-    __device__ __forceinline__ void add(float z, float c1, float cT) {
-        const float d = z - m;
-        const float eT = exp2f(d * cT);
-        sT += eT;
-        s1 += kSquarings >= 0 ? squared<kSquarings < 0 ? 0 : kSquarings>(eT) : exp2f(d * c1);
-    }
-    template <int N> __device__ __forceinline__ void add_vector(const float (&z)[N], float c1, float cT) {
-        float top = z[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) top = fmaxf(top, z[i]);
-        if (top > m) rescale(top, c1, cT);
-        if (m == -INFINITY) {  // nothing but -infinity so far (or a NaN, which has to come through)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (z[i] != z[i]) s1 = sT = z[i];
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) add(z[i], c1, cT);
-    }
-};
-
-template <typename T, Mode kMode, int kSquarings, int kThreads>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant__ DistillParams P) {
-    constexpr int N = 16 / sizeof(T), U = 4;
-    __shared__ RowShared S;
-    const int64_t row = blockIdx.x;
-    const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
-    T* dz = reinterpret_cast<T*>(P.dz) + row * P.dz_stride;
-    const int64_t V = P.vocab;
-    const float c1 = kLog2e, cT = kLog2e / P.temperature;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-    // [0, head) and [head + N vectors, V) singly, the rest in 16-byte vectors
-    int64_t head = (int64_t)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(T);
-    const bool wide = kMode == kForward || ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
-    if (!wide || head > V) head = V;
-    const int64_t vectors = (V - head) / N, tail = head + vectors * N;
-
-    if (warp == 0) read_teacher<T>(P, z, row, S);
-
-    float lse1, lseT;
-    if (kMode == kBackward) {
-        lse1 = P.stats[2 * row];
-        lseT = P.stats[2 * row + 1];
-        __syncthreads();
-    } else {
-        Online<kSquarings> acc;
-        for (int64_t v0 = threadIdx.x; v0 < vectors; v0 += U * kThreads) {
-            Vec<T, N> w[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (v0 + u * kThreads < vectors) w[u] = *reinterpret_cast<const Vec<T, N>*>(z + head + (v0 + u * kThreads) * N);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (v0 + u * kThreads < vectors) {
-                    float f[N];
-#pragma unroll
-                    for (int i = 0; i < N; ++i) f[i] = to_f32<T>(w[u].v[i]);
-                    acc.template add_vector<N>(f, c1, cT);
-                }
-        }
-        for (int64_t j = threadIdx.x; j < head + (V - tail); j += kThreads) {
-            float f[1] = {to_f32<T>(z[j < head ? j : j - head + tail])};
-            acc.template add_vector<1>(f, c1, cT);
-        }
-        const float wm = warp_max(acc.m);
-        acc.rescale(wm, c1, cT);
-        const float w1 = warp_sum(acc.s1), wT = warp_sum(acc.sT);
-        if (lane == 0) S.warp_m[warp] = wm, S.warp_s1[warp] = w1, S.warp_sT[warp] = wT;
-        __syncthreads();
-        float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, S.warp_m[i]);
-        float s1 = 0.f, sT = 0.f;
-#pragma unroll
-        for (int i = 0; i < kThreads / 32; ++i) {
-            const float d = S.warp_m[i] - m;
-            const bool none = S.warp_m[i] == -INFINITY;
-            s1 += none ? S.warp_s1[i] : S.warp_s1[i] * exp2f(d * c1);
-            sT += none ? S.warp_sT[i] : S.warp_sT[i] * exp2f(d * cT);
-        }
-        lse1 = m + log2f(s1) * kLn2;
-        lseT = m / P.temperature + log2f(sT) * kLn2;
-        if (threadIdx.x == 0) {
-            if (P.stats) P.stats[2 * row] = lse1, P.stats[2 * row + 1] = lseT;
-            float loss = 0.f;
-            if (!S.ignored) {
-                if (P.labels) loss += (1.f - P.mix) * (lse1 - S.label_z);
-                if (S.any) loss += P.mix * P.temperature * P.temperature * (S.plogp - S.pz / P.temperature + lseT);
-                if (S.bad) loss = NAN;
-            }
-            P.loss[row] = loss;
-        }
-    }
-    if (kMode == kForward) return;
-
-    // a q1 + b qT, then the rows' own entries
-    const bool ignored = S.ignored;
-    const float g = S.bad ? NAN : P.dloss[row];
-    const float a = P.labels ? g * (1.f - P.mix) : 0.f, b = S.any ? g * P.mix * P.temperature : 0.f;
-    // Where T = 2^n, q1 = qT^T exp(T lseT - lse1).
-    const float ratio = kSquarings > 0 ? exp2f((P.temperature * lseT - lse1) * kLog2e) : 1.f;
-    const float LT = P.temperature * lseT, aR = a * ratio;
-    const auto grad = [&](float x) -> float {
-        if (kSquarings == 0) return (a + b) * exp2f((x - lse1) * c1);
-        const float qT = exp2f((x - LT) * cT);
-        if (kSquarings > 0) return fmaf(aR, squared<kSquarings < 0 ? 0 : kSquarings>(qT), b * qT);
-        return fmaf(a, exp2f((x - lse1) * c1), b * qT);
-    };
-    if (ignored) {
-        for (int64_t v = threadIdx.x; v < vectors; v += kThreads) {
-            Vec<T, N> w;
-#pragma unroll
-            for (int i = 0; i < N; ++i) w.v[i] = from_f32<T>(0.f);
-            *reinterpret_cast<Vec<T, N>*>(dz + head + v * N) = w;
-        }
-        for (int64_t j = threadIdx.x; j < head + (V - tail); j += kThreads) dz[j < head ? j : j - head + tail] = from_f32<T>(0.f);
-        return;
-    }
-    for (int64_t v0 = threadIdx.x; v0 < vectors; v0 += U * kThreads) {
-        Vec<T, N> w[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + u * kThreads < vectors) w[u] = *reinterpret_cast<const Vec<T, N>*>(z + head + (v0 + u * kThreads) * N);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + u * kThreads < vectors) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) w[u].v[i] = from_f32<T>(grad(to_f32<T>(w[u].v[i])));
-                *reinterpret_cast<Vec<T, N>*>(dz + head + (v0 + u * kThreads) * N) = w[u];
-            }
-    }
-    for (int64_t j = threadIdx.x; j < head + (V - tail); j += kThreads) {
-        const int64_t at = j < head ? j : j - head + tail;
-        dz[at] = from_f32<T>(grad(to_f32<T>(z[at])));
-    }
-    __syncthreads();  // the entries below were written above by other threads of this CTA
-    // Each entry is formed once more, whole, from the logit read at the start (dz may lie on z) and rounded once.
-    for (uint32_t i = threadIdx.x; i < P.k; i += kThreads) {
-        const int32_t j = S.idx[i];
-        if (j < 0) continue;
-        float p = 0.f;
-        for (uint32_t o = 0; o < P.k; ++o) p += S.idx[o] == j ? S.p[o] : 0.f;
-        dz[j] = from_f32<T>(grad(S.z[i]) - b * p - (P.labels && j == S.label ? a : 0.f));
-    }
-    if (warp == 0 && P.labels && !S.bad) {
-        int there = 0;
-        for (uint32_t i = lane; i < P.k; i += 32) there |= S.idx[i] == S.label;
-        if (!__any_sync(~0u, there) && lane == 0) dz[S.label] = from_f32<T>(grad(S.label_z) - a);
-    }
-}
-
-
 // ------------------------------------------------------------------------------------------------ rows held in shared memory
 
 // A CTA of kThreads + 32 walks rows, one held in shared memory at a time, in chunks.  Its last warp copies: as soon as the
@@ -423,9 +185,11 @@ __device__ void describe_row(const DistillParams& P, const T* z, int64_t row, bo
 }
 
 // kSquarings: T = 1, 2, 4 as 0, 1, 2, where exp(z) = exp(z/T)^T; any other T as -1.
-template <typename T, int kSquarings, int kThreads>
+// kHeld false: a row that shared memory does not hold is read from global memory both times, the second time from the L2 cache; and
+// a gradient whose rows lie off the logits' 16-byte boundaries is stored by elements.
+template <typename T, int kSquarings, int kThreads, bool kHeld>
 __global__ void __launch_bounds__(kThreads + 32, Held<kThreads>::kPerSM)
-distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int* fault) {
+distill_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int* fault) {
     using H = Held<kThreads>;
     constexpr bool kPower = kSquarings >= 0;
     constexpr int N = 16 / sizeof(T), kPairs = Pairs<T>::kCount, U = H::kUnroll;
@@ -435,12 +199,12 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
     __shared__ float part[2][3][32];
     __shared__ int gave_up;
     const int V = (int)P.vocab, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int row_bytes = V / N * 16, chunks = (V / N + H::kChunk - 1) / H::kChunk;
+    const int row_bytes = kHeld ? V / N * 16 : 0, chunks = (V / N + H::kChunk - 1) / H::kChunk;
     char* entries = smem + row_bytes;
     const uint32_t full = smem_u32(bars), free_ = full + 8 * H::kMostChunks, described = free_ + 8 * H::kMostChunks, used = described + 16;
     const Waits W{&gave_up, fault};
     if (threadIdx.x == 0) {
-        for (int i = 0; i < chunks; ++i) bar_init(full + 8 * i, 1), bar_init(free_ + 8 * i, H::kWarps);
+        for (int i = 0; kHeld && i < chunks; ++i) bar_init(full + 8 * i, 1), bar_init(free_ + 8 * i, H::kWarps);
         for (int i = 0; i < 2; ++i) bar_init(described + 8 * i, 1), bar_init(used + 8 * i, H::kWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         gave_up = 0;
@@ -453,7 +217,7 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
         const auto copy = [&](int64_t row, int n) {  // the n-th row of this CTA
             const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
             const Cut<T> c(z, V);
-            for (int i = 0; i < chunks; ++i) {
+            for (int i = 0; kHeld && i < chunks; ++i) {
                 if (n) W.wait_warp(free_ + 8 * i, (n - 1) & 1);
                 const int bytes = min(H::kChunk, c.vectors - i * H::kChunk) * 16;
                 if (lane == 0) {
@@ -475,14 +239,13 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
             if (lane == 0) bar_arrive(described + 8 * s);
             if (row + gridDim.x < rows) copy(row + gridDim.x, it + 1);
         }
-        if (gave_up && lane == 0)  // copies in flight still write to shared memory
+        if (kHeld && gave_up && lane == 0)  // copies in flight still write to shared memory
             for (int i = 0; i < chunks; ++i) W.drain(full + 8 * i, (it - 1) & 1);
         return;
     }
 
     const float c1 = kLog2e, cT = kLog2e / P.temperature;
     const float2 cTT = make_float2(cT, cT), c11 = make_float2(c1, c1);
-    const uint4* held = reinterpret_cast<const uint4*>(smem);
     // exp2 of d cT, and of d c1 (a power of the first where the temperature allows)
     const auto exponentials = [&](float2 dT, float2 d1, float2& eT, float2& e1) {
         eT = exp2_both(mul2(dT, cTT));
@@ -499,6 +262,7 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
         const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
         const Cut<T> c(z, V);
         const int s = it & 1;
+        const uint4* held = kHeld ? reinterpret_cast<const uint4*>(smem) : reinterpret_cast<const uint4*>(z + c.head);
         float extra = -INFINITY;
         if (threadIdx.x < c.singles) extra = to_f32<T>(z[c.single(threadIdx.x)]);
 
@@ -517,7 +281,7 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
             };
             add(make_float2(extra, -INFINITY));
             for (int k = 0; k < chunks; ++k) {
-                W.wait_warp(full + 8 * k, it & 1);
+                if (kHeld) W.wait_warp(full + 8 * k, it & 1);
                 uint4 x[U];
                 uint32_t tops[U];
                 const uint4* from = held + k * H::kChunk + threadIdx.x;
@@ -543,7 +307,7 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int q = 0; q < kPairs; ++q) add(Pairs<T>::get(x[u], q));
-                if (!want_gradient) {
+                if (kHeld && !want_gradient) {
                     __syncwarp();
                     if (lane == 0) bar_arrive(free_ + 8 * k);
                 }
@@ -592,7 +356,7 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
             T* dz = reinterpret_cast<T*>(P.dz) + row * P.dz_stride;
             uint4* out = reinterpret_cast<uint4*>(dz + c.head);
             for (int k = 0; k < chunks; ++k) {
-                if (!want_stats) W.wait_warp(full + 8 * k, it & 1);
+                if (kHeld && !want_stats) W.wait_warp(full + 8 * k, it & 1);
                 uint4 x[U];
                 const uint4* from = held + k * H::kChunk + threadIdx.x;
                 uint4* to = out + k * H::kChunk + threadIdx.x;
@@ -601,19 +365,30 @@ distill_held_kernel(const __grid_constant__ DistillParams P, int rows, int mode,
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (inside(u)) x[u] = from[u * kThreads];
-                __syncwarp();
-                if (lane == 0) bar_arrive(free_ + 8 * k);
+                if (kHeld) {
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(free_ + 8 * k);
+                }
+                const auto store = [&](int u, uint4 y) {
+                    if (kHeld || ((reinterpret_cast<uintptr_t>(to) & 15) == 0)) {
+                        __stcs(to + u * kThreads, y);
+                    } else {
+                        const T* e = reinterpret_cast<const T*>(&y);
+#pragma unroll
+                        for (int i = 0; i < N; ++i) reinterpret_cast<T*>(to + u * kThreads)[i] = e[i];
+                    }
+                };
                 if (S.ignored) {
 #pragma unroll
                     for (int u = 0; u < U; ++u)
-                        if (inside(u)) __stcs(to + u * kThreads, make_uint4(0, 0, 0, 0));
+                        if (inside(u)) store(u, make_uint4(0, 0, 0, 0));
                     continue;
                 }
                 const auto form = [&](int u) {
                     float2 f[kPairs];
 #pragma unroll
                     for (int q = 0; q < kPairs; ++q) f[q] = gradient(Pairs<T>::get(x[u], q));
-                    __stcs(to + u * kThreads, Pairs<T>::join(f));
+                    store(u, Pairs<T>::join(f));
                 };
                 if (whole) {
 #pragma unroll
@@ -659,11 +434,11 @@ template <typename T>
 int held_bytes(const DistillParams& P) { return (int)(P.vocab * sizeof(T) / 16 * 16 + P.k * 24); }
 constexpr int kMostHeld = 225 * 1024;  // of 227 KB to a CTA, beside what the kernel declares itself
 
-template <typename T, int kSquarings, int kThreads>
-int launch_held(const DistillParams& P, int64_t rows, int mode, int sms, int* fault, cudaStream_t st) {
+template <typename T, int kSquarings, int kThreads, bool kHeld = true>
+int launch_rows(const DistillParams& P, int64_t rows, int mode, int sms, int* fault, cudaStream_t st) {
     using H = Held<kThreads>;
-    auto* kernel = distill_held_kernel<T, kSquarings, kThreads>;
-    const int bytes = held_bytes<T>(P);
+    auto* kernel = distill_kernel<T, kSquarings, kThreads, kHeld>;
+    const int bytes = kHeld ? held_bytes<T>(P) : (int)P.k * 24;
     static Allowed allowed;
     if (int rc = allow_smem(kernel, bytes, allowed)) return rc;
     const int fit = kSharedPerSM / (bytes + 3072), per_sm = fit < 1 ? 1 : fit < H::kPerSM ? fit : H::kPerSM;
@@ -677,37 +452,23 @@ int launch_held(const DistillParams& P, int64_t rows, int mode, int sms, int* fa
 template <typename T, int kSquarings>
 int by_length(const DistillParams& P, int64_t rows, int mode, int sms, int* fault, cudaStream_t st) {
     const int64_t bytes = P.vocab * (int64_t)sizeof(T);
-    if (bytes <= 4096) return launch_held<T, kSquarings, 32>(P, rows, mode, sms, fault, st);
-    if (bytes <= 32768) return launch_held<T, kSquarings, 128>(P, rows, mode, sms, fault, st);
-    if (bytes <= 110 * 1024) return launch_held<T, kSquarings, 256>(P, rows, mode, sms, fault, st);
-    return launch_held<T, kSquarings, 512>(P, rows, mode, sms, fault, st);
+    const bool lies_like = mode == kForward || ((((uintptr_t)P.z ^ (uintptr_t)P.dz) & 15) == 0 && (rows == 1 || (P.z_stride - P.dz_stride) * (int64_t)sizeof(T) % 16 == 0));
+    if (!lies_like || bytes > kMostHeld || held_bytes<T>(P) > kMostHeld) return launch_rows<T, kSquarings, 512, false>(P, rows, mode, sms, fault, st);
+    if (bytes <= 4096) return launch_rows<T, kSquarings, 32>(P, rows, mode, sms, fault, st);
+    if (bytes <= 32768) return launch_rows<T, kSquarings, 128>(P, rows, mode, sms, fault, st);
+    if (bytes <= 110 * 1024) return launch_rows<T, kSquarings, 256>(P, rows, mode, sms, fault, st);
+    return launch_rows<T, kSquarings, 512>(P, rows, mode, sms, fault, st);
 }
 
-template <typename T, Mode kMode, int kSquarings>
-int launch(const DistillParams& P, int64_t rows, cudaStream_t st) {
-    distill_kernel<T, kMode, kSquarings, 512><<<(unsigned)rows, 512, 0, st>>>(P);
-    return cuda_status(cudaGetLastError(), "distill launch");
-}
-
-template <typename T, Mode kMode>
-int by_temperature(const DistillParams& P, int64_t rows, int32_t device, cudaStream_t st) {
-    // Held rows need the gradient's vectors to lie like the logits', in every row.
-    const auto lies_like = [&] {
-        return (((uintptr_t)P.z ^ (uintptr_t)P.dz) & 15) == 0 && (rows == 1 || (P.z_stride - P.dz_stride) * (int64_t)sizeof(T) % 16 == 0);
-    };
-    if (P.vocab <= (1 << 20) && held_bytes<T>(P) <= kMostHeld && (kMode == kForward || lies_like())) {
-        int* fault = nullptr;
-        if (int rc = fault_mark(&fault)) return rc;
-        const int sms = sm_count(device);
-        if (P.temperature == 1.f) return by_length<T, 0>(P, rows, kMode, sms, fault, st);
-        if (P.temperature == 2.f) return by_length<T, 1>(P, rows, kMode, sms, fault, st);
-        if (P.temperature == 4.f) return by_length<T, 2>(P, rows, kMode, sms, fault, st);
-        return by_length<T, -1>(P, rows, kMode, sms, fault, st);
-    }
-    if (P.temperature == 1.f) return launch<T, kMode, 0>(P, rows, st);
-    if (P.temperature == 2.f) return launch<T, kMode, 1>(P, rows, st);
-    if (P.temperature == 4.f) return launch<T, kMode, 2>(P, rows, st);
-    return launch<T, kMode, -1>(P, rows, st);
+template <typename T>
+int by_temperature(const DistillParams& P, int64_t rows, int mode, int32_t device, cudaStream_t st) {
+    int* fault = nullptr;
+    if (int rc = fault_mark(&fault)) return rc;
+    const int sms = sm_count(device);
+    if (P.temperature == 1.f) return by_length<T, 0>(P, rows, mode, sms, fault, st);
+    if (P.temperature == 2.f) return by_length<T, 1>(P, rows, mode, sms, fault, st);
+    if (P.temperature == 4.f) return by_length<T, 2>(P, rows, mode, sms, fault, st);
+    return by_length<T, -1>(P, rows, mode, sms, fault, st);
 }
 
 template <Mode kMode>
@@ -737,9 +498,9 @@ int distill(const halos_distill_args* a) {
     P.vocab = a->vocab, P.ignore_index = a->ignore_index, P.k = a->k, P.labels_64 = a->labels_64, P.index_64 = a->index_64;
     P.teacher_dtype = a->teacher_dtype, P.temperature = a->temperature, P.mix = a->mix;
     cudaStream_t st = (cudaStream_t)a->stream;
-    if (a->dtype == HALOS_F32) return by_temperature<float, kMode>(P, a->rows, a->device, st);
-    if (a->dtype == HALOS_BF16) return by_temperature<__nv_bfloat16, kMode>(P, a->rows, a->device, st);
-    return by_temperature<__half, kMode>(P, a->rows, a->device, st);
+    if (a->dtype == HALOS_F32) return by_temperature<float>(P, a->rows, kMode, a->device, st);
+    if (a->dtype == HALOS_BF16) return by_temperature<__nv_bfloat16>(P, a->rows, kMode, a->device, st);
+    return by_temperature<__half>(P, a->rows, kMode, a->device, st);
 }
 
 }  // namespace

@@ -60,6 +60,14 @@ def test_against_64_bits(n, V, k, temperature, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("temperature", [1.0, 3.0])
+@pytest.mark.parametrize("V,spare", [(130003, 0), (130003, 5), (60000, 0)])
+def test_rows_that_shared_memory_does_not_hold(V, spare, temperature, dtype):
+    z, labels, idx, t, dloss = _case(3, V, 40, dtype, spare=spare)
+    _check(z, labels, idx, t, dloss, temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("mix", [0.0, 1.0])
 @pytest.mark.parametrize("temperature", [1.0, 2.0, 3.0])
 def test_one_term_alone(temperature, mix, dtype):
