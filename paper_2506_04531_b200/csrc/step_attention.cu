@@ -1,8 +1,8 @@
 // Attention and its backward pass on the fifth-generation tensor cores.
 //
 // Forward, one CTA per 128 queries of a head: S = Q K^T into tensor memory, a thread per query takes its row through
-// the online softmax, P goes back into tensor memory as the left operand of O += P V.  The running maximum is only moved
-// (and O rescaled) when it grows by more than 2^8: P stays below 256, which both 16-bit types hold.
+// the online softmax, P goes back into tensor memory as the left operand of O += P V.  The running maximum is moved (and O rescaled)
+// only when the probabilities of a tile add up to more than 2^10 without: a single one stays within both 16-bit types.
 //
 // Backward, two kernels without atomics, so that gradients are the same bits every time:
 //   dK, dV: a CTA keeps 128 keys and walks the queries of its group's heads, 64 at a time.  It works on the transposes,
@@ -13,6 +13,9 @@
 // in memory, its clearing and conversion, and the order of its sums.
 //
 // Roles in a CTA: warps of 4 take the rows (thread = tensor memory lane), one warp issues the bulk copies, one the products.
+//
+// p and ds are rounded to the inputs' type where they become operands (that is what the tensor cores take); every sum,
+// statistic and accumulator is in 32 bits, and each result is rounded once.
 #include "step_tcgen05.cuh"
 
 #include <limits.h>

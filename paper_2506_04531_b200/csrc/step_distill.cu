@@ -55,7 +55,7 @@ __device__ __forceinline__ float warp_sum(float v) {
 // A wait that runs out is marked and ends every later one at once; the loops and their barriers still run to the end.
 template <int kThreads> struct Held {
     static constexpr int kWarps = kThreads / 32, kUnroll = 4, kChunk = kThreads * kUnroll;  // vectors
-    static constexpr int kPerSM = kThreads == 32 ? 16 : kThreads == 128 ? 6 : kThreads == 256 ? 3 : 1;
+    static constexpr int kPerSM = kThreads == 128 ? 6 : kThreads == 256 ? 3 : 1;
     static constexpr int kMostChunks = 32;
 };
 
@@ -184,6 +184,140 @@ __device__ void describe_row(const DistillParams& P, const T* z, int64_t row, bo
     }
 }
 
+// exp2 of d cT, and of d c1 (a power of the first where the temperature allows).
+template <int kSquarings> struct Exponentials {
+    float2 cT, c1;
+    __device__ __forceinline__ explicit Exponentials(float temperature) : cT(both(kLog2e / temperature)), c1(both(kLog2e)) {}
+    __device__ __forceinline__ void operator()(float2 dT, float2 d1, float2& eT, float2& e1) const {
+        eT = exp2_both(mul2(dT, cT));
+        if constexpr (kSquarings >= 0) {
+            e1 = eT;
+#pragma unroll
+            for (int i = 0; i < kSquarings; ++i) e1 = mul2(e1, e1);
+        } else {
+            e1 = exp2_both(mul2(d1, c1));
+        }
+    }
+};
+
+// a q1 + b qT of a row; where T = 2^n, q1 = qT^T exp(T lseT - lse1).
+template <int kSquarings> struct Gradient {
+    const Exponentials<kSquarings>& form;
+    float a, b;
+    float2 minusT, minus1, aa, bb, ab;
+    __device__ __forceinline__ Gradient(const Exponentials<kSquarings>& e, const DistillParams& P, const Slot& S, float lse1, float lseT) : form(e) {
+        const float g = S.bad ? NAN : S.g, LT = P.temperature * lseT;
+        a = P.labels ? g * (1.f - P.mix) : 0.f, b = S.any ? g * P.mix * P.temperature : 0.f;
+        aa = both(kSquarings >= 0 ? a * fast_exp2((LT - lse1) * kLog2e) : a), bb = both(b), ab = add2(aa, bb);
+        minusT = both(-LT), minus1 = both(-lse1);
+    }
+    __device__ __forceinline__ float2 operator()(float2 z) const {
+        float2 qT, q1;
+        form(add2(z, minusT), kSquarings >= 0 ? z : add2(z, minus1), qT, q1);
+        return kSquarings == 0 ? mul2(ab, qT) : fma2(aa, q1, mul2(bb, qT));
+    }
+};
+
+__device__ __forceinline__ void write_loss(const DistillParams& P, int64_t row, const Slot& S, float lse1, float lseT) {
+    if (P.stats) P.stats[2 * row] = lse1, P.stats[2 * row + 1] = lseT;
+    float loss = 0.f;
+    if (!S.ignored) {
+        if (P.labels) loss += (1.f - P.mix) * (lse1 - S.label_z);
+        if (S.any) loss += P.mix * P.temperature * P.temperature * (S.plogp - S.pz / P.temperature + lseT);
+        if (S.bad) loss = NAN;
+    }
+    P.loss[row] = loss;
+}
+
+// The row's own entries (the teacher's and the label) are formed once more, whole, and rounded once, over what is there already.
+// `threads` threads, this one `at`; four to an entry look for its doubles and for the label.
+template <typename T, int kSquarings>
+__device__ __forceinline__ void write_entries(const DistillParams& P, T* dz, const Gradient<kSquarings>& gradient, const Slot& S, const float* p, const float* zk, const int* idx, int at,
+                                              int threads) {
+    for (uint32_t first = 0; first < P.k; first += threads / 4) {
+        const uint32_t i = first + at / 4;
+        const int j = i < P.k ? idx[i] : -1;
+        float same = 0.f;
+        if (j >= 0)
+            for (uint32_t o = at & 3; o < P.k; o += 4) same += idx[o] == j ? p[o] : 0.f;
+        same += __shfl_xor_sync(~0u, same, 1);
+        same += __shfl_xor_sync(~0u, same, 2);
+        if (j >= 0 && (at & 3) == 0) dz[j] = from_f32<T>(gradient(both(zk[i])).x - gradient.b * same - (P.labels && j == S.label ? gradient.a : 0.f));
+    }
+    if (at < 32 && P.labels && !S.bad) {
+        int there = 0;
+        for (uint32_t i = at; i < P.k; i += 32) there |= idx[i] == S.label;
+        if (!__any_sync(~0u, there) && at == 0) dz[S.label] = from_f32<T>(gradient(both(S.label_z)).x - gradient.a);
+    }
+}
+
+// A row to a warp, in registers, for rows of kShort bytes at most: everything that the row needs is asked for at once, and what a
+// CTA per row spends on barriers and on waiting for its teacher falls away.
+constexpr int kShort = 4096, kShortWarps = 4;
+template <typename T, int kSquarings>
+__global__ void __launch_bounds__(32 * kShortWarps) distill_short_kernel(const __grid_constant__ DistillParams P, int rows, int mode) {
+    constexpr int kVectors = kShort / 512, kPairs = Pairs<T>::kCount;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ Slot slots[kShortWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, V = (int)P.vocab;
+    const int64_t row = (int64_t)blockIdx.x * kShortWarps + warp;
+    if (row >= rows) return;
+    const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
+    const Cut<T> c(z, V);
+    const uint4* in = reinterpret_cast<const uint4*>(z + c.head);
+    const uint32_t low = low_word<T>();
+    uint4 x[kVectors];
+#pragma unroll
+    for (int u = 0; u < kVectors; ++u) x[u] = u * 32 + lane < c.vectors ? in[u * 32 + lane] : make_uint4(low, low, low, low);
+    const float extra = lane < c.singles ? to_f32<T>(z[c.single(lane)]) : -INFINITY;
+    float* p = reinterpret_cast<float*>(smem) + warp * 3 * P.k;
+    float* zk = p + P.k;
+    int* idx = reinterpret_cast<int*>(zk + P.k);
+    describe_row<T>(P, z, row, mode == kBackward, p, zk, idx, slots[warp]);
+    __syncwarp();
+    const Slot S = slots[warp];
+    const Exponentials<kSquarings> form(P.temperature);
+    float lse1 = S.lse1, lseT = S.lseT;
+    if (mode != kBackward) {
+        uint32_t top = low;
+#pragma unroll
+        for (int u = 0; u < kVectors; ++u) top = max_words<T>(top, max_words<T>(max_words<T>(x[u].x, x[u].y), max_words<T>(x[u].z, x[u].w)));
+        const float m = warp_max(fmaxf(max_in_word<T>(top), extra));
+        const float2 minus = both(m == -INFINITY ? 0.f : -m);
+        float2 sT = both(0.f), s1 = sT;
+        const auto add = [&](float2 f) {  // the difference before the factor, as above
+            const float2 d = add2(f, minus);
+            float2 eT, e1;
+            form(d, d, eT, e1);
+            sT = add2(sT, eT), s1 = add2(s1, e1);
+        };
+        add(make_float2(extra, -INFINITY));
+#pragma unroll
+        for (int u = 0; u < kVectors; ++u)
+            if (u * 32 < c.vectors)
+#pragma unroll
+                for (int q = 0; q < kPairs; ++q) add(Pairs<T>::get(x[u], q));
+        lse1 = m + log2f(warp_sum(s1.x + s1.y)) * kLn2;
+        lseT = m / P.temperature + log2f(warp_sum(sT.x + sT.y)) * kLn2;
+        if (lane == 0) write_loss(P, row, S, lse1, lseT);
+    }
+    if (mode == kForward) return;
+    const Gradient<kSquarings> gradient(form, P, S, lse1, lseT);
+    T* dz = reinterpret_cast<T*>(P.dz) + row * P.dz_stride;
+    uint4* out = reinterpret_cast<uint4*>(dz + c.head);
+#pragma unroll
+    for (int u = 0; u < kVectors; ++u)
+        if (u * 32 + lane < c.vectors) {
+            float2 f[kPairs];
+#pragma unroll
+            for (int q = 0; q < kPairs; ++q) f[q] = gradient(Pairs<T>::get(x[u], q));
+            out[u * 32 + lane] = S.ignored ? make_uint4(0, 0, 0, 0) : Pairs<T>::join(f);
+        }
+    if (lane < c.singles) dz[c.single(lane)] = from_f32<T>(S.ignored ? 0.f : gradient(both(extra)).x);
+    __syncwarp();  // orders the stores above before those below
+    if (!S.ignored) write_entries<T, kSquarings>(P, dz, gradient, S, p, zk, idx, lane, 32);
+}
+
 // kSquarings: T = 1, 2, 4 as 0, 1, 2, where exp(z) = exp(z/T)^T; any other T as -1.
 // kHeld false: a row that shared memory does not hold is read from global memory both times, the second time from the L2 cache; and
 // a gradient whose rows lie off the logits' 16-byte boundaries is stored by elements.
@@ -191,7 +325,6 @@ template <typename T, int kSquarings, int kThreads, bool kHeld>
 __global__ void __launch_bounds__(kThreads + 32, Held<kThreads>::kPerSM)
 distill_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int* fault) {
     using H = Held<kThreads>;
-    constexpr bool kPower = kSquarings >= 0;
     constexpr int N = 16 / sizeof(T), kPairs = Pairs<T>::kCount, U = H::kUnroll;
     extern __shared__ __align__(128) char smem[];  // a row's whole vectors, then two sets of the teacher's entries
     __shared__ uint64_t bars[2 * H::kMostChunks + 4];  // full and free of each chunk, described[2], used[2]
@@ -245,18 +378,7 @@ distill_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int*
     }
 
     const float c1 = kLog2e, cT = kLog2e / P.temperature;
-    const float2 cTT = make_float2(cT, cT), c11 = make_float2(c1, c1);
-    // exp2 of d cT, and of d c1 (a power of the first where the temperature allows)
-    const auto exponentials = [&](float2 dT, float2 d1, float2& eT, float2& e1) {
-        eT = exp2_both(mul2(dT, cTT));
-        if constexpr (kPower) {
-            e1 = eT;
-#pragma unroll
-            for (int i = 0; i < kSquarings; ++i) e1 = mul2(e1, e1);
-        } else {
-            e1 = exp2_both(mul2(d1, c11));
-        }
-    };
+    const Exponentials<kSquarings> exponentials(P.temperature);
     int it = 0;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, ++it) {
         const T* z = reinterpret_cast<const T*>(P.z) + row * P.z_stride;
@@ -316,7 +438,7 @@ distill_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int*
             float M = warp_max(m);
             const float d = m == -INFINITY ? 0.f : m - M;  // who has nothing has sums of 0, or a NaN
             float S1 = warp_sum((s1.x + s1.y) * fast_exp2(d * c1)), ST = warp_sum((sT.x + sT.y) * fast_exp2(d * cT));
-            if (H::kWarps > 1) {
+            {
                 if (lane == 0) part[s][0][warp] = M, part[s][1][warp] = S1, part[s][2][warp] = ST;
                 asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
                 const float wm = lane < H::kWarps ? part[s][0][lane] : -INFINITY;
@@ -331,28 +453,10 @@ distill_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int*
         W.wait_warp(described + 8 * s, (it / 2) & 1);
         const Slot S = slots[s];
         if (!want_stats) lse1 = S.lse1, lseT = S.lseT;
-        else if (threadIdx.x == 0) {
-            if (P.stats) P.stats[2 * row] = lse1, P.stats[2 * row + 1] = lseT;
-            float loss = 0.f;
-            if (!S.ignored) {
-                if (P.labels) loss += (1.f - P.mix) * (lse1 - S.label_z);
-                if (S.any) loss += P.mix * P.temperature * P.temperature * (S.plogp - S.pz / P.temperature + lseT);
-                if (S.bad) loss = NAN;
-            }
-            P.loss[row] = loss;
-        }
+        else if (threadIdx.x == 0) write_loss(P, row, S, lse1, lseT);
         if (want_gradient) {
-            // a q1 + b qT; where T = 2^n, q1 = qT^T exp(T lseT - lse1).  An ignored row's gradient is 0 whatever it holds.
-            const float g = S.bad ? NAN : S.g;
-            const float a = P.labels ? g * (1.f - P.mix) : 0.f, bT = S.any ? g * P.mix * P.temperature : 0.f;
-            const float LT = P.temperature * lseT;
-            const float a1 = kPower ? a * fast_exp2((LT - lse1) * kLog2e) : a;
-            const float2 minusT = make_float2(-LT, -LT), minus1 = make_float2(-lse1, -lse1), aa = make_float2(a1, a1), bb = make_float2(bT, bT), ab = add2(aa, bb);
-            const auto gradient = [&](float2 f) -> float2 {
-                float2 qT, q1;
-                exponentials(add2(f, minusT), kPower ? f : add2(f, minus1), qT, q1);
-                return kSquarings == 0 ? mul2(ab, qT) : fma2(aa, q1, mul2(bb, qT));
-            };
+            // An ignored row's gradient is 0 whatever it holds.
+            const Gradient<kSquarings> gradient(exponentials, P, S, lse1, lseT);
             T* dz = reinterpret_cast<T*>(P.dz) + row * P.dz_stride;
             uint4* out = reinterpret_cast<uint4*>(dz + c.head);
             for (int k = 0; k < chunks; ++k) {
@@ -400,29 +504,11 @@ distill_kernel(const __grid_constant__ DistillParams P, int rows, int mode, int*
                 }
             }
             if (threadIdx.x < c.singles) dz[c.single(threadIdx.x)] = from_f32<T>(S.ignored ? 0.f : gradient(make_float2(extra, extra)).x);
-            // The row's own entries lie in what other threads have written; each is formed once more, whole, and rounded once.
-            if (kThreads > 32) asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
-            else __syncwarp();
+            // The row's own entries lie in what other threads have written.
+            asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
             if (!S.ignored) {
                 const float* p = reinterpret_cast<const float*>(entries) + s * 3 * P.k;
-                const float* zk = p + P.k;
-                const int* idx = reinterpret_cast<const int*>(p + 2 * P.k);
-                // four threads to an entry look for its doubles and for the label
-                int there = 0;
-                for (uint32_t first = 0; first < P.k; first += kThreads / 4) {
-                    const uint32_t i = first + threadIdx.x / 4;
-                    const int j = i < P.k ? idx[i] : -1;
-                    float same = 0.f;
-                    if (j >= 0)
-                        for (uint32_t o = threadIdx.x & 3; o < P.k; o += 4) same += idx[o] == j ? p[o] : 0.f;
-                    same += __shfl_xor_sync(~0u, same, 1);
-                    same += __shfl_xor_sync(~0u, same, 2);
-                    if (j >= 0 && (threadIdx.x & 3) == 0) dz[j] = from_f32<T>(gradient(make_float2(zk[i], zk[i])).x - bT * same - (P.labels && j == S.label ? a : 0.f));
-                }
-                if (warp == 0 && P.labels && !S.bad) {
-                    for (uint32_t i = lane; i < P.k; i += 32) there |= idx[i] == S.label;
-                    if (!__any_sync(~0u, there) && lane == 0) dz[S.label] = from_f32<T>(gradient(make_float2(S.label_z, S.label_z)).x - a);
-                }
+                write_entries<T, kSquarings>(P, dz, gradient, S, p, p + P.k, reinterpret_cast<const int*>(p + 2 * P.k), threadIdx.x, kThreads);
             }
         }
         __syncwarp();
@@ -447,14 +533,20 @@ int launch_rows(const DistillParams& P, int64_t rows, int mode, int sms, int* fa
     return cuda_status(cudaGetLastError(), "distill launch");
 }
 
-// Small CTAs for short rows: many of them hide each other's latencies, and a row's fixed cost (a reduction, two barriers)
-// falls on fewer threads.  From half of an SM's shared memory on there is one CTA to an SM, which then needs all the threads.
+// Small CTAs (or single warps) for short rows: many of them hide each other's latencies, and a row's fixed cost (a reduction, two
+// barriers) falls on fewer threads.  From half of an SM's shared memory on there is one CTA to an SM, which then needs all the threads.
 template <typename T, int kSquarings>
 int by_length(const DistillParams& P, int64_t rows, int mode, int sms, int* fault, cudaStream_t st) {
     const int64_t bytes = P.vocab * (int64_t)sizeof(T);
     const bool lies_like = mode == kForward || ((((uintptr_t)P.z ^ (uintptr_t)P.dz) & 15) == 0 && (rows == 1 || (P.z_stride - P.dz_stride) * (int64_t)sizeof(T) % 16 == 0));
     if (!lies_like || bytes > kMostHeld || held_bytes<T>(P) > kMostHeld) return launch_rows<T, kSquarings, 512, false>(P, rows, mode, sms, fault, st);
-    if (bytes <= 4096) return launch_rows<T, kSquarings, 32>(P, rows, mode, sms, fault, st);
+    if (bytes <= kShort) {
+        static Allowed allowed;
+        const int shared = kShortWarps * (int)P.k * 12;
+        if (int rc = allow_smem(distill_short_kernel<T, kSquarings>, shared, allowed)) return rc;
+        distill_short_kernel<T, kSquarings><<<(unsigned)((rows + kShortWarps - 1) / kShortWarps), 32 * kShortWarps, shared, st>>>(P, (int)rows, mode);
+        return cuda_status(cudaGetLastError(), "distill launch");
+    }
     if (bytes <= 32768) return launch_rows<T, kSquarings, 128>(P, rows, mode, sms, fault, st);
     if (bytes <= 110 * 1024) return launch_rows<T, kSquarings, 256>(P, rows, mode, sms, fault, st);
     return launch_rows<T, kSquarings, 512>(P, rows, mode, sms, fault, st);
