@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from typing import Optional
 
 import torch
@@ -53,9 +54,26 @@ class DistillArgs(C.Structure):
                 ("dloss", _vp), ("dlogits", _vp), ("dlogits_stride", _i64)]
 
 
-_ROPE_SIZE, _ATTENTION_SIZE, _DISTILL_SIZE = C.sizeof(RopeArgs), C.sizeof(AttentionArgs), C.sizeof(DistillArgs)
-# Small calls are bound by what happens here, so the stream's handle is asked for without building a stream object around it.
-_byref, _raw_stream = C.byref, torch._C._cuda_getCurrentRawStream
+
+def _packer(kind):
+    """A struct's fields as one ``struct.Struct``: small calls are bound by what happens here, and packing all values at once costs a third of
+    setting them one by one.  The kinds have no gaps, so their sizes agree."""
+    codes = {_u32: "I", _i32: "i", _i64: "q", _u64: "Q", _vp: "Q", _f32: "f", _stride3: "3q", _i64 * 2: "2q"}
+    packed = struct.Struct("=" + "".join(codes[f[1]] for f in kind._fields_))
+    assert packed.size == C.sizeof(kind)
+    return packed
+
+
+def _pack(kind, *values) -> bytes:
+    try:
+        return kind.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise HalosError(ERR_INVALID_ARG, f"an argument out of range: {e}") from None
+
+
+_ROPE, _ATTENTION, _DISTILL = _packer(RopeArgs), _packer(AttentionArgs), _packer(DistillArgs)
+# The stream's handle is asked for without building a stream object around it.
+_raw_stream = torch._C._cuda_getCurrentRawStream
 _lib = None
 
 
@@ -65,10 +83,9 @@ def _library():
         lib = load_library()
         lib.halos_step_error.restype = C.c_char_p
         lib.halos_step_fault.argtypes = [_i32, C.POINTER(_i32)]
-        for name, args in (("rope", RopeArgs), ("attention_fwd", AttentionArgs), ("attention_bwd", AttentionArgs), ("distill_fwd", DistillArgs),
-                           ("distill_bwd", DistillArgs), ("distill_fwd_bwd", DistillArgs)):
-            getattr(lib, "halos_" + name).argtypes = [C.POINTER(args)]
-        lib.halos_attention_workspace.argtypes = [C.POINTER(AttentionArgs), C.POINTER(_u64)]
+        for name in ("rope", "attention_fwd", "attention_bwd", "distill_fwd", "distill_bwd", "distill_fwd_bwd"):
+            getattr(lib, "halos_" + name).argtypes = [_vp]
+        lib.halos_attention_workspace.argtypes = [_vp, C.POINTER(_u64)]
         _lib = lib
     return _lib
 
@@ -77,9 +94,9 @@ def _refuse(text: str):
     raise HalosError(ERR_INVALID_ARG, text)
 
 
-def _call(name: str, args):
+def _call(name: str, args: bytes):
     lib = _lib or _library()
-    rc = getattr(lib, name)(_byref(args))
+    rc = getattr(lib, name)(args)
     if rc:
         raise HalosError(rc, lib.halos_step_error().decode())
 
@@ -96,12 +113,6 @@ def _on(x, device, what: str):
         _refuse(f"{what} is not a CUDA tensor (there is no CPU path)")
     if x.device != device:
         _refuse(f"{what} is on {x.device}, not on {device}")
-
-
-def _begin(args, size: int, device):
-    args.struct_size = size
-    args.device = device.index
-    args.stream = _raw_stream(device.index)
 
 
 def fault(device: Optional[int] = None) -> bool:
@@ -162,32 +173,32 @@ def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", 
     device, dtype = q.device, q.dtype
     _heads_last(q, "q")
     _on(q, device, "q")
-    a = RopeArgs()
-    a.dtype = _dtype(q, "q")
-    a.layout = _LAYOUTS.get(layout, 99)
-    a.batch, a.seq, a.n_q, a.head_dim = shape = q.shape
+    kind = _dtype(q, "q")
+    batch, seq, n_q, head_dim = q.shape
+    n_k = 0
     if k is not None:
         _heads_last(k, "k")
         _on(k, device, "k")
-        k_shape = k.shape
-        if k.dtype != dtype or k_shape[:2] != shape[:2] or k_shape[3] != shape[3]:
+        k_batch, k_seq, n_k, k_dim = k.shape
+        if k.dtype != dtype or (k_batch, k_seq, k_dim) != (batch, seq, head_dim):
             _refuse("q and k must agree in type, batch, seq and head_dim")
-        a.n_k = k_shape[2]
     _on(freqs, device, "freqs")
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
         _refuse("freqs must be a contiguous float64 vector")
-    a.rot_dim, a.freqs = 2 * freqs.numel(), freqs.data_ptr()
+    at, wide, st = 0, False, (0, 0)
     if positions is not None:
         _on(positions, device, "positions")
         wide = positions.dtype == torch.int64
         if not wide and positions.dtype != torch.int32:
             _refuse("positions must be int32 or int64")
-        if positions.shape != shape[:2] and positions.shape != shape[1:2]:
-            _refuse("positions must be [seq] or [batch, seq]")
-        a.positions, a.positions_64 = positions.data_ptr(), wide
         st = positions.stride()
-        a.position_stride[:] = st if len(st) == 2 else (0, st[0])
-    a.position_offset, a.magnitude, a.inverse = offset, magnitude, bool(inverse)
+        if positions.shape == (batch, seq):
+            pass
+        elif positions.shape == (seq,):
+            st = (0, st[0])
+        else:
+            _refuse("positions must be [seq] or [batch, seq]")
+        at = positions.data_ptr()
     if inplace:
         for x in (q, k):
             if x is not None and any(s == 0 and n > 1 for s, n in zip(x.stride(), x.shape)):
@@ -195,13 +206,11 @@ def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", 
         q_out, k_out = q, k
     else:
         q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
-    a.q_in, a.q_out = q.data_ptr(), q_out.data_ptr()
-    a.q_in_stride[:], a.q_out_stride[:] = q.stride()[:3], q_out.stride()[:3]
-    if k is not None:
-        a.k_in, a.k_out = k.data_ptr(), k_out.data_ptr()
-        a.k_in_stride[:], a.k_out_stride[:] = k.stride()[:3], k_out.stride()[:3]
-    _begin(a, _ROPE_SIZE, device)
-    _call("halos_rope", a)
+    none = (0, 0, 0)
+    _call("halos_rope", _pack(
+        _ROPE, _ROPE.size, device.index, _raw_stream(device.index), kind, _LAYOUTS.get(layout, 99), bool(inverse), wide, batch, seq, n_q, n_k, head_dim, 2 * freqs.numel(), magnitude, 0,
+        freqs.data_ptr(), at, *st, offset, q.data_ptr(), 0 if k is None else k.data_ptr(), q_out.data_ptr(), 0 if k is None else k_out.data_ptr(),
+        *q.stride()[:3], *(none if k is None else k.stride()[:3]), *q_out.stride()[:3], *(none if k is None else k_out.stride()[:3])))
     return q_out, k_out
 
 
@@ -237,7 +246,8 @@ def _aligned(x):
     return x.clone(memory_format=torch.contiguous_format)
 
 
-def _attention_args(q, k, v, scale, causal, doc_start, lens):
+def _attention_checked(q, k, v, scale, causal, doc_start, lens):
+    """The args' values from dtype to lens, after checks."""
     device, dtype = q.device, q.dtype
     for x, what in ((q, "q"), (k, "k"), (v, "v")):
         if x.dim() != 4:
@@ -245,30 +255,21 @@ def _attention_args(q, k, v, scale, causal, doc_start, lens):
         _on(x, device, what)
         if x.dtype != dtype:
             _refuse("q, k and v must be of one type")
-    q_shape, k_shape = q.shape, k.shape
-    if k_shape != v.shape or k_shape[0] != q_shape[0] or k_shape[3] != q_shape[3]:
+    batch, sq, n_q, head_dim = q.shape
+    k_batch, sk, n_kv, k_dim = k.shape
+    if v.shape != k.shape or k_batch != batch or k_dim != head_dim:
         _refuse("k and v must have one shape, and q's batch and head_dim")
-    a = AttentionArgs()
-    a.dtype, a.causal = _dtype(q, "q"), bool(causal)
-    a.batch, a.sq, a.n_q, a.head_dim = q_shape
-    a.sk, a.n_kv = k_shape[1:3]
-    a.scale = q_shape[3] ** -0.5 if scale is None and q_shape[3] else scale or 0.0
     if doc_start is not None:
-        _on(doc_start, q.device, "doc_start")
-        if doc_start.dtype != torch.int32 or doc_start.shape != q.shape[:2] or not doc_start.is_contiguous():
+        _on(doc_start, device, "doc_start")
+        if doc_start.dtype != torch.int32 or doc_start.shape != (batch, sq) or not doc_start.is_contiguous():
             _refuse("doc_start must be contiguous int32 [batch, seq of q]")
-        a.doc_start = doc_start.data_ptr()
     if lens is not None:
-        _on(lens, q.device, "lens")
-        if lens.dtype != torch.int32 or lens.shape != q.shape[:1] or not lens.is_contiguous():
+        _on(lens, device, "lens")
+        if lens.dtype != torch.int32 or lens.shape != (batch,) or not lens.is_contiguous():
             _refuse("lens must be contiguous int32 [batch]")
-        a.lens = lens.data_ptr()
-    return a
-
-
-def _set(a, name: str, x):
-    setattr(a, name, x.data_ptr())
-    getattr(a, name + "_stride")[:] = x.stride()[:3]
+    if scale is None:
+        scale = head_dim ** -0.5 if head_dim else 0.0
+    return (_dtype(q, "q"), bool(causal), batch, sq, sk, n_q, n_kv, head_dim, scale, 0 if doc_start is None else doc_start.data_ptr(), 0 if lens is None else lens.data_ptr())
 
 
 def attention_forward(q, k, v, *, scale: Optional[float] = None, causal: bool = True, doc_start=None, lens=None):
@@ -276,40 +277,37 @@ def attention_forward(q, k, v, *, scale: Optional[float] = None, causal: bool = 
     shape, lse is float32 [batch, heads, sq].  Query i stands at i + sk - sq; it sees keys from doc_start[b, i] on (int32), before
     lens[b] (int32), and up to its own position if causal.  A query that sees none, or stands at or past lens[b], has o = 0 and
     lse = -infinity.  What lies at or past lens[b] may hold anything.  scale: head_dim^-1/2 unless given."""
-    a = _attention_args(q, k, v, scale, causal, doc_start, lens)
+    values = _attention_checked(q, k, v, scale, causal, doc_start, lens)
     q, k, v = _aligned(q), _aligned(k), _aligned(v)
     o = torch.empty_like(q)
-    lse = q.new_empty((a.batch, a.n_q, a.sq), dtype=torch.float32)
-    for n, x in (("q", q), ("k", k), ("v", v), ("o", o)):
-        _set(a, n, x)
-    a.lse = lse.data_ptr()
-    _begin(a, _ATTENTION_SIZE, q.device)
-    _call("halos_attention_fwd", a)
+    lse = q.new_empty((values[2], values[5], values[3]), dtype=torch.float32)
+    device = q.device.index
+    _call("halos_attention_fwd", _pack(
+        _ATTENTION, _ATTENTION.size, device, _raw_stream(device), *values, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), 0, 0, 0, 0, 0, 0,
+        *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0))
     return o, lse
 
 
 def attention_backward(dout, q, k, v, o, lse, *, scale: Optional[float] = None, causal: bool = True, doc_start=None, lens=None):
     """(dq, dk, dv) from the gradient of o, the forward pass's inputs and what it returned.  Deterministic."""
-    a = _attention_args(q, k, v, scale, causal, doc_start, lens)
+    values = _attention_checked(q, k, v, scale, causal, doc_start, lens)
     for x, what in ((dout, "dout"), (o, "o")):
         _on(x, q.device, what)
         if x.shape != q.shape or x.dtype != q.dtype:
             _refuse(f"{what} must be like q")
     _on(lse, q.device, "lse")
-    if lse.dtype != torch.float32 or lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or not lse.is_contiguous():
+    if lse.dtype != torch.float32 or lse.shape != (values[2], values[5], values[3]) or not lse.is_contiguous():
         _refuse("lse must be contiguous float32 [batch, heads, seq]")
     q, k, v, o, dout = (_aligned(x) for x in (q, k, v, o, dout))
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
-    for n, x in (("q", q), ("k", k), ("v", v), ("o", o), ("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv)):
-        _set(a, n, x)
-    a.lse = lse.data_ptr()
-    size = _u64(0)
-    a.struct_size = _ATTENTION_SIZE
-    _library().halos_attention_workspace(C.byref(a), C.byref(size))
+    device, size = q.device.index, _u64(0)
+    tensors = (q, k, v, o, dout, dq, dk, dv)
+    strides = [s for x in tensors for s in x.stride()[:3]]
+    pointers = [x.data_ptr() for x in (q, k, v, o, lse, dout, dq, dk, dv)]
+    head = (_ATTENTION.size, device, _raw_stream(device), *values, *pointers)
+    (_lib or _library()).halos_attention_workspace(_pack(_ATTENTION, *head, 0, 0, *strides), C.byref(size))
     space = q.new_empty(size.value, dtype=torch.uint8)
-    a.workspace, a.workspace_bytes = space.data_ptr(), size.value
-    _begin(a, _ATTENTION_SIZE, q.device)
-    _call("halos_attention_bwd", a)
+    _call("halos_attention_bwd", _pack(_ATTENTION, *head, space.data_ptr(), size.value, *strides))
     return dq, dk, dv
 
 
@@ -333,35 +331,39 @@ def attention(q, k, v, *, scale: Optional[float] = None, causal: bool = True, do
 
 # ------------------------------------------------------------------------------------------ distillation loss
 
-def _distill_args(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index):
+def _distill_checked(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index):
+    """The args' values from the size to teacher_logits_stride, after checks."""
     if logits.dim() != 2:
         _refuse("logits must be [rows, vocab]")
-    _on(logits, logits.device, "logits")
-    if logits.size(1) > 1 and logits.stride(1) != 1:
+    device = logits.device
+    _on(logits, device, "logits")
+    rows, vocab = logits.shape
+    stride, step_ = logits.stride()
+    if vocab > 1 and step_ != 1:
         _refuse("logits: a row's elements must lie side by side")
-    a = DistillArgs()
-    a.dtype = _dtype(logits, "logits")
-    a.rows, a.vocab = logits.shape
-    a.temperature, a.mix, a.ignore_index = temperature, mix, ignore_index
-    a.logits, a.logits_stride = logits.data_ptr(), logits.stride(0)
+    kind = _dtype(logits, "logits")
+    label_at, labels_64 = 0, False
     if labels is not None:
-        _on(labels, logits.device, "labels")
-        if labels.dtype not in (torch.int32, torch.int64) or labels.shape != logits.shape[:1] or not labels.is_contiguous():
+        _on(labels, device, "labels")
+        labels_64 = labels.dtype == torch.int64
+        if not labels_64 and labels.dtype != torch.int32 or labels.shape != (rows,) or not labels.is_contiguous():
             _refuse("labels must be contiguous int32 or int64 [rows]")
-        a.labels, a.labels_64 = labels.data_ptr(), labels.dtype == torch.int64
+        label_at = labels.data_ptr()
     if (teacher_idx is None) != (teacher_logits is None):
         _refuse("teacher_idx and teacher_logits come together")
+    k, teacher_kind, index_64, index_at, t_at, index_stride, t_stride = 0, 0, False, 0, 0, 0, 0
     if teacher_idx is not None:
         for x, what in ((teacher_idx, "teacher_idx"), (teacher_logits, "teacher_logits")):
-            _on(x, logits.device, what)
-            if x.dim() != 2 or x.shape != teacher_idx.shape or x.shape[0] != logits.shape[0] or (x.size(1) > 1 and x.stride(1) != 1):
+            _on(x, device, what)
+            if x.dim() != 2 or x.shape != teacher_idx.shape or x.size(0) != rows or (x.size(1) > 1 and x.stride(1) != 1):
                 _refuse(f"{what} must be [rows, k], a row's elements side by side")
-        if teacher_idx.dtype not in (torch.int32, torch.int64):
+        index_64 = teacher_idx.dtype == torch.int64
+        if not index_64 and teacher_idx.dtype != torch.int32:
             _refuse("teacher_idx must be int32 or int64")
-        a.teacher_dtype, a.index_64, a.k = _dtype(teacher_logits, "teacher_logits"), teacher_idx.dtype == torch.int64, teacher_idx.shape[1]
-        a.teacher_index, a.teacher_index_stride = teacher_idx.data_ptr(), teacher_idx.stride(0)
-        a.teacher_logits, a.teacher_logits_stride = teacher_logits.data_ptr(), teacher_logits.stride(0)
-    return a
+        teacher_kind, k = _dtype(teacher_logits, "teacher_logits"), teacher_idx.size(1)
+        index_at, index_stride, t_at, t_stride = teacher_idx.data_ptr(), teacher_idx.stride(0), teacher_logits.data_ptr(), teacher_logits.stride(0)
+    return (_DISTILL.size, device.index, _raw_stream(device.index), kind, teacher_kind, labels_64, index_64, rows, vocab, k, temperature, mix, 0, ignore_index, logits.data_ptr(), stride,
+            label_at, index_at, t_at, index_stride, t_stride)
 
 
 def _row_weights(dloss, logits):
@@ -371,7 +373,7 @@ def _row_weights(dloss, logits):
     return dloss.data_ptr()
 
 
-def _gradient_like(logits, out, a):
+def _gradient_like(logits, out):
     """The gradient's tensor: `out`, or one whose rows start at the same offset from a 16-byte boundary as those of the logits
     do, so that both are read and written in whole vectors."""
     if out is None:
@@ -386,7 +388,6 @@ def _gradient_like(logits, out, a):
         _on(out, logits.device, "out")
         if out.shape != logits.shape or out.dtype != logits.dtype or (out.size(1) > 1 and out.stride(1) != 1):
             _refuse("out must be like logits, a row's elements side by side")
-    a.dlogits, a.dlogits_stride = out.data_ptr(), out.stride(0)
     return out
 
 
@@ -396,38 +397,32 @@ def distill_forward(logits, labels, teacher_idx, teacher_logits, *, temperature:
     With p = softmax(teacher_logits / T) over the entries with teacher_idx != -1 ([rows, k], both may be None):
     loss = (1 - mix) (-log softmax(z)[label]) + mix T^2 sum p (log p - log softmax(z / T)[idx]); a row whose label is ignore_index
     has loss 0.  labels None: no first term.  stats = log sum exp of z and of z / T, for ``distill_backward``."""
-    a = _distill_args(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
-    loss = logits.new_empty(a.rows, dtype=torch.float32)
-    stats = logits.new_empty((a.rows, 2), dtype=torch.float32)
-    a.loss, a.stats = loss.data_ptr(), stats.data_ptr()
-    _begin(a, _DISTILL_SIZE, logits.device)
-    _call("halos_distill_fwd", a)
+    values = _distill_checked(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
+    loss = logits.new_empty(values[7], dtype=torch.float32)
+    stats = logits.new_empty((values[7], 2), dtype=torch.float32)
+    _call("halos_distill_fwd", _pack(_DISTILL, *values, loss.data_ptr(), stats.data_ptr(), 0, 0, 0))
     return loss, stats
 
 
 def distill_backward(dloss, logits, stats, labels, teacher_idx, teacher_logits, *, temperature: float = 1.0, mix: float = 0.5, ignore_index: int = -100, out=None):
     """dlogits from dloss [rows] and the forward pass's statistics; out may be the logits themselves."""
-    a = _distill_args(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
-    a.dloss = _row_weights(dloss, logits)
+    values = _distill_checked(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
+    weights = _row_weights(dloss, logits)
     _on(stats, logits.device, "stats")
-    if stats.dtype != torch.float32 or stats.shape != (logits.shape[0], 2) or not stats.is_contiguous():
+    if stats.dtype != torch.float32 or stats.shape != (values[7], 2) or not stats.is_contiguous():
         _refuse("stats must be contiguous float32 [rows, 2]")
-    a.stats = stats.data_ptr()
-    out = _gradient_like(logits, out, a)
-    _begin(a, _DISTILL_SIZE, logits.device)
-    _call("halos_distill_bwd", a)
+    out = _gradient_like(logits, out)
+    _call("halos_distill_bwd", _pack(_DISTILL, *values, 0, stats.data_ptr(), weights, out.data_ptr(), out.stride(0)))
     return out
 
 
 def distill_loss_and_grad(logits, labels, teacher_idx, teacher_logits, dloss, *, temperature: float = 1.0, mix: float = 0.5, ignore_index: int = -100, out=None):
     """(loss, dlogits) in one pass over the logits, for weights dloss [rows] that are known beforehand; out may be the logits."""
-    a = _distill_args(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
-    a.dloss = _row_weights(dloss, logits)
-    loss = logits.new_empty(a.rows, dtype=torch.float32)
-    a.loss = loss.data_ptr()
-    out = _gradient_like(logits, out, a)
-    _begin(a, _DISTILL_SIZE, logits.device)
-    _call("halos_distill_fwd_bwd", a)
+    values = _distill_checked(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
+    weights = _row_weights(dloss, logits)
+    loss = logits.new_empty(values[7], dtype=torch.float32)
+    out = _gradient_like(logits, out)
+    _call("halos_distill_fwd_bwd", _pack(_DISTILL, *values, loss.data_ptr(), 0, weights, out.data_ptr(), out.stride(0)))
     return loss, out
 
 
