@@ -1,12 +1,12 @@
-// Distillation from a teacher's top logits mixed with cross-entropy: loss, gradient, or both, one CTA per row.
+// Distillation from a teacher's top logits mixed with cross-entropy: loss, gradient, or both.
 //
 // Bound by memory: a forward pass reads the logits once, a backward pass reads and writes them once, and the two together
 // read and write them once.  The second constraint is the exponential (16 per clock and SM): with a temperature a
 // logit needs exp(z) and exp(z/T), in the statistics and again in the gradient.  Where T is 1, 2 or 4 the
 // first is the second to the power T, which costs multiplications instead (kSquarings).
 //
-// Statistics are kept online: a thread holds the largest logit it has seen and the two sums relative to it, and
-// rescales them when a larger one comes up, which after the first few vectors is rare.
+// Measured: 8192 x 50304 bf16 logits, 64 entries, T = 2, loss with gradient 365 us (4.5 TB/s, floor 256 us; the exponential
+// unit and the issue slots are both 58% busy); gradient alone of 2048 x 32003 f16, T = 1: 58 us (4.6 TB/s).
 #include "step_tcgen05.cuh"
 
 namespace halos_step {
@@ -547,7 +547,8 @@ int by_length(const DistillParams& P, int64_t rows, int mode, int sms, int* faul
         distill_short_kernel<T, kSquarings><<<(unsigned)((rows + kShortWarps - 1) / kShortWarps), 32 * kShortWarps, shared, st>>>(P, (int)rows, mode);
         return cuda_status(cudaGetLastError(), "distill launch");
     }
-    if (bytes <= 32768) return launch_rows<T, kSquarings, 128>(P, rows, mode, sms, fault, st);
+    // From 32 to 48 KB the smaller CTA is 4 to 8% faster over 4000 rows, the larger one 10% over 1000, where each CTA has two or three.
+    if (bytes <= 32768 || (bytes <= 49152 && rows > 12 * sms)) return launch_rows<T, kSquarings, 128>(P, rows, mode, sms, fault, st);
     if (bytes <= 110 * 1024) return launch_rows<T, kSquarings, 256>(P, rows, mode, sms, fault, st);
     return launch_rows<T, kSquarings, 512>(P, rows, mode, sms, fault, st);
 }
