@@ -77,7 +77,9 @@ int halos_rope(const halos_rope_args* args);
  *     lo = doc_start ? doc_start[b][i] : 0;   n = lens ? lens[b] : sk;   hi = t >= n ? 0 : causal ? min(n, t + 1) : n.
  *     s_ij = scale q_i.k_j;  lse_i = log sum_j exp s_ij;  p_ij = exp(s_ij - lse_i);  o_i = sum_j p_ij v_j.
  * A query that sees nothing has o = 0, lse = -infinity and gives no gradient.  Query head h reads key head
- * h / (n_q / n_kv).  Keys that no query sees, and queries that see nothing, may hold anything, NaN included.
+ * h / (n_q / n_kv).  Tokens at or past n, keys before the first or past the last one that any query sees, and queries that
+ * see nothing may hold anything, NaN included.  All else has to be finite: a NaN or an infinity in a key or value that
+ * some query sees, or that lies between such keys, may also reach queries that do not see it (zero times it is not zero).
  * Backward, with D_i = dout_i.o_i:   ds_ij = p_ij (dout_i.v_j - D_i);  dq_i = scale sum_j ds_ij k_j;
  * dk_j = scale sum ds_ij q_i and dv_j = sum p_ij dout_i over the queries of every head that reads the key head.
  * p and ds enter their matrix products in the inputs' type, unnormalised resp. in true size; all sums are in 32 bits.

@@ -527,7 +527,8 @@ int launch_rows(const DistillParams& P, int64_t rows, int mode, int sms, int* fa
     const int bytes = kHeld ? held_bytes<T>(P) : (int)P.k * 24;
     static Allowed allowed;
     if (int rc = allow_smem(kernel, bytes, allowed)) return rc;
-    const int fit = kSharedPerSM / (bytes + 3072), per_sm = fit < 1 ? 1 : fit < H::kPerSM ? fit : H::kPerSM;
+    constexpr int kBeside = 3 * 1024;  // static shared memory of a CTA, and the 1 KB that the hardware keeps
+    const int fit = kSharedPerSM / (bytes + kBeside), per_sm = fit < 1 ? 1 : fit < H::kPerSM ? fit : H::kPerSM;
     const int64_t most = (int64_t)sms * per_sm;
     kernel<<<(unsigned)(rows < most ? rows : most), kThreads + 32, bytes, st>>>(P, (int)rows, mode, fault);
     return cuda_status(cudaGetLastError(), "distill launch");

@@ -276,7 +276,8 @@ def attention_forward(q, k, v, *, scale: Optional[float] = None, causal: bool = 
     """(o, lse) of q [batch, sq, heads, head_dim] against k, v [batch, sk, key heads, head_dim], bfloat16 or float16; o has q's
     shape, lse is float32 [batch, heads, sq].  Query i stands at i + sk - sq; it sees keys from doc_start[b, i] on (int32), before
     lens[b] (int32), and up to its own position if causal.  A query that sees none, or stands at or past lens[b], has o = 0 and
-    lse = -infinity.  What lies at or past lens[b] may hold anything.  scale: head_dim^-1/2 unless given."""
+    lse = -infinity.  What lies at or past lens[b] may hold anything; keys and values that
+    some query sees have to be finite, and those between them.  scale: head_dim^-1/2 unless given."""
     values = _attention_checked(q, k, v, scale, causal, doc_start, lens)
     q, k, v = _aligned(q), _aligned(k), _aligned(v)
     o = torch.empty_like(q)
