@@ -83,6 +83,8 @@ int halos_rope(const halos_rope_args* args);
  * Backward, with D_i = dout_i.o_i:   ds_ij = p_ij (dout_i.v_j - D_i);  dq_i = scale sum_j ds_ij k_j;
  * dk_j = scale sum ds_ij q_i and dv_j = sum p_ij dout_i over the queries of every head that reads the key head.
  * p and ds enter their matrix products in the inputs' type, unnormalised resp. in true size; all sums are in 32 bits.
+ * scale > 0, and scale log2(e) finite.  Scores are 32-bit sums, and lse one 32-bit number: a p that is formed from it is off by some 2^-23 |lse| of
+ * itself, so that gradients of rows with |lse| in the tens of thousands lose what 16-bit types hold.  o is not formed from it.
  * dtype HALOS_BF16 or HALOS_F16 (HALOS_F32: UNSUPPORTED); head_dim a multiple of 8, <= 128; bases and strides of
  * q, k, v, dout multiples of 16 bytes, of the outputs and of o the same (else UNSUPPORTED). */
 typedef struct halos_attention_args {

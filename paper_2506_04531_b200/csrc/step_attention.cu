@@ -34,6 +34,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRecord = 64;   // queries to a record
 // Of 64 probabilities relative to a maximum that may be an old one.  Any bound that keeps a single one within 16-bit floats would do.
 constexpr float kMostSum = 1024.f;
+// Largest maximum, times scale log2(e), that is rounded to one number and taken off inside the multiply-add: the exponent of the maximum itself
+// is then off by 2^-9 at most. At 2^28 it would be off by 16, and no probability relative to such a number stays small.
+constexpr float kNear = 65536.f;
 
 // What the backward pass knows of 64 queries of a head before it starts.  A query that sees nothing, or is none, has
 // minus_lse2 = -infinity: its probabilities are 0.
@@ -221,9 +224,16 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
         const int i = tile * 128 + threadIdx.x;
         const float2 factor = both(P.scale2);
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f;  // m: of the scores before they are scaled
         int r = 0, use = 0, before = 0, before_use = 0;
         uint32_t x[64];
+        // Probabilities are exp2((x - shift) scale2 - base). Up to kNear shift is 0, which costs one instruction less for each; beyond, the difference
+        // comes before the factor and is exact where it matters, so that no exponent is above 0 once the maximum has moved.
+        const auto reference = [&](float top, float& shift, float& base) {
+            const float scaled = top * P.scale2;
+            const bool near = fabsf(scaled) <= kNear;
+            base = near ? scaled : 0.f, shift = near || top == -INFINITY ? 0.f : top;
+        };
         const auto fetch = [&](uint32_t* to, int from) {
             tmem_load32(to, lanes + 64 * from);
             tmem_load32(to + 32, lanes + 64 * from + 32);
@@ -241,17 +251,24 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                     if (key0 + c < lo || key0 + c >= hi) x[c] = 0xff800000u;
             }
             // The maximum is not looked for as long as the probabilities stay small without: it was right for the first keys,
-            // and where later ones are much larger the sum shows it.
+            // and where later ones are much larger the sum shows it.  Once to a tile: what comes after a move is added up as it is.
+            float2 minus = both(-(m * P.scale2));
             const auto move_maximum = [&] {
                 float tops[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tops[c] = __uint_as_float(x[c]);
 #pragma unroll
                 for (int c = 4; c < 64; ++c) tops[c & 3] = fmaxf(tops[c & 3], __uint_as_float(x[c]));
-                const float to = fmaxf(m, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * P.scale2);
-                const float f = m == -INFINITY ? 0.f : fast_exp2(m - to);
-                m = to;
+                const float to = fmaxf(m, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+                float old_shift, old_base, shift, base;
+                reference(m, old_shift, old_base), reference(to, shift, base);
+                const float f = m == -INFINITY ? 0.f : fast_exp2(fmaf(old_shift - shift, P.scale2, old_base - base));
+                m = to, minus = both(-base);
                 l *= f;
+                if (__any_sync(~0u, shift != 0.f)) {
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) x[c] = __float_as_uint(__uint_as_float(x[c]) - shift);
+                }
                 if (j) {  // every product so far is in O
                     W.wait_warp(pv_done + 8 * before, before_use);
                     tc_after_sync();
@@ -267,10 +284,10 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                     tmem_wait_stores();
                 }
             };
-            if (__any_sync(~0u, m == -INFINITY)) move_maximum();
+            bool moved = __any_sync(~0u, !(fabsf(m * P.scale2) <= kNear));  // none yet, or beyond: always looked for
+            if (moved) move_maximum();
             float sum;
-            for (;;) {
-                const float2 minus = both(m == -INFINITY ? 0.f : -m);
+            for (;;) {  // twice at most
                 float2 sums[2] = {both(0.f), both(0.f)};
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -285,7 +302,8 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                 }
                 const float2 pair = add2(sums[0], sums[1]);
                 sum = pair.x + pair.y;
-                if (!__any_sync(~0u, sum > kMostSum)) break;  // after the maximum has moved it is 64 at most, or no number
+                if (moved || !__any_sync(~0u, sum > kMostSum)) break;
+                moved = true;
                 tmem_wait_stores();  // before the same places are written again
                 move_maximum();
             }
@@ -323,7 +341,9 @@ attention_fwd_kernel(const __grid_constant__ AttentionParams P, const __grid_con
                     store_row<T>(P.o, b * P.o_stride[0] + i * P.o_stride[1] + h * P.o_stride[2], P.head_dim, o, 32 * c);
                 }
             }
-            if (i < P.sq) P.lse[((int64_t)b * P.n_q + h) * P.sq + i] = hi == 0 ? -INFINITY : (m + log2f(l)) * kLn2;
+            float shift, base;
+            reference(m, shift, base);
+            if (i < P.sq) P.lse[((int64_t)b * P.n_q + h) * P.sq + i] = hi == 0 ? -INFINITY : (fmaf(shift, P.scale2, base) + log2f(l)) * kLn2;
         }
     }
     tc_before_sync();
@@ -956,7 +976,7 @@ int check(const halos_attention_args* a, bool back) {
     if (a->batch < 0 || a->sq < 0 || a->sk < 0) return fail(HALOS_ERR_INVALID_ARG, "attention: negative size");
     if (a->n_q == 0 || a->n_kv == 0 || a->n_q % a->n_kv) return fail(HALOS_ERR_INVALID_ARG, "attention: query heads must be a multiple of key heads");
     if (a->head_dim == 0 || a->head_dim % 8 || a->head_dim > 128) return fail(HALOS_ERR_UNSUPPORTED, "attention: head_dim must be a multiple of 8, at most 128");
-    if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return fail(HALOS_ERR_INVALID_ARG, "attention: scale must be positive");
+    if (!(a->scale > 0.f) || !(a->scale * kLog2e < INFINITY)) return fail(HALOS_ERR_INVALID_ARG, "attention: scale must be positive, and finite times log2(e)");
     if (a->sq > (1 << 30) || a->sk > (1 << 30) || a->batch > 65535 || a->n_q > 65535) return fail(HALOS_ERR_UNSUPPORTED, "attention: over 2^30 tokens, 65535 heads or sequences");
     const int64_t tiles = (a->sq > a->sk ? a->sq : a->sk) / 128 + 1;
     if (tiles * a->batch * a->n_q > 0x7fffffffll) return fail(HALOS_ERR_UNSUPPORTED, "attention: too many tiles");
