@@ -170,7 +170,7 @@ __device__ void describe_row(const DistillParams& P, const T* z, int64_t row, bo
         if (t != -INFINITY) {
             const float logp = t - top - log_sum;
             q = fast_exp2(logp * kLog2e);
-            if (q > 0.f) plogp += q * logp, pz += q * zk[i];  // 0 log 0 = 0, whatever the logit there
+            if (!(q == 0.f)) plogp += q * logp, pz += q * zk[i];  // 0 log 0 = 0, whatever the logit there; a NaN stays one
         }
         p[i] = q;
     }
@@ -178,7 +178,7 @@ __device__ void describe_row(const DistillParams& P, const T* z, int64_t row, bo
     pz = warp_sum(pz);
     bad = __any_sync(~0u, bad);
     if (lane == 0) {
-        S.plogp = plogp, S.pz = pz, S.any = sum > 0.f, S.label = bad ? -1 : (int)label, S.ignored = ignored, S.bad = bad, S.label_z = label_z;
+        S.plogp = plogp, S.pz = pz, S.any = !(sum == 0.f), S.label = bad ? -1 : (int)label, S.ignored = ignored, S.bad = bad, S.label_z = label_z;
         if (P.dloss) S.g = P.dloss[row];
         if (back) S.lse1 = P.stats[2 * row], S.lseT = P.stats[2 * row + 1];
     }
