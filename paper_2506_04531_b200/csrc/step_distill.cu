@@ -207,7 +207,7 @@ template <int kSquarings> struct Gradient {
     float2 minusT, minus1, aa, bb, ab;
     __device__ __forceinline__ Gradient(const Exponentials<kSquarings>& e, const DistillParams& P, const Slot& S, float lse1, float lseT) : form(e) {
         const float g = S.bad ? NAN : S.g, LT = P.temperature * lseT;
-        a = P.labels ? g * (1.f - P.mix) : 0.f, b = S.any ? g * P.mix * P.temperature : 0.f;
+        a = P.labels ? g * (1.f - P.mix) : 0.f, b = S.any || S.bad ? g * P.mix * P.temperature : 0.f;
         aa = both(kSquarings >= 0 ? a * fast_exp2((LT - lse1) * kLog2e) : a), bb = both(b), ab = add2(aa, bb);
         minusT = both(-LT), minus1 = both(-lse1);
     }

@@ -65,3 +65,16 @@ def test_entries_of_minus_infinity_are_as_if_they_were_not_there(V):
     for (loss, dz), (loss2, dz2) in zip(_both_ways(z, labels, idx, there, dloss), _both_ways(z, labels, absent, t, dloss)):
         assert torch.equal(loss, loss2) and bool(torch.isfinite(dz).all())
         assert bool(((dz - dz2).abs() <= 2.0 ** -20 * dz2.abs() + 1e-30).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", VOCABS)
+@pytest.mark.parametrize("others", [True, False])
+def test_an_index_outside_the_vocabulary_gives_nan_without_labels_too(others, V, dtype):
+    z, _, idx, t, dloss = _case(3, V, 8, dtype)
+    if not others:                                  # nothing valid beside it
+        idx[1] = -1
+    idx[1, 5] = V
+    for loss, dz in _both_ways(z, None, idx, t, dloss, temperature=2.0):
+        assert torch.isnan(loss).tolist() == [False, True, False]
+        assert bool(torch.isnan(dz[1]).all()) and bool(torch.isfinite(dz[[0, 2]]).all())
