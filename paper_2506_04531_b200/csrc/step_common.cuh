@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <atomic>
+#include <mutex>
 #include <stdint.h>
 
 namespace halos_step {
@@ -18,14 +19,20 @@ int fault_mark(int** mark);                             // where the current dev
 
 constexpr int kSharedPerSM = 228 * 1024;
 int current_device();                                   // that enter() was last called with in this thread
-// Lets a kernel have this much dynamic shared memory; each caller keeps what it was last allowed, per device.
-struct Allowed { std::atomic<int> bytes[64]; };
+// Lets a kernel have this much dynamic shared memory; each caller keeps what it was last allowed, per device.  One thread at a time sets and
+// notes a limit, and it only grows: the limit that holds is never below the one that is noted.
+struct Allowed {
+    std::atomic<int> bytes[64];
+    std::mutex changing;
+};
 template <typename K>
 int allow_smem(K* kernel, int bytes, Allowed& allowed) {
     std::atomic<int>& had = allowed.bytes[current_device()];
+    if (had.load(std::memory_order_acquire) >= bytes) return HALOS_OK;
+    const std::lock_guard<std::mutex> alone(allowed.changing);
     if (had.load(std::memory_order_relaxed) >= bytes) return HALOS_OK;
     if (int rc = cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes), "shared memory")) return rc;
-    had.store(bytes, std::memory_order_relaxed);
+    had.store(bytes, std::memory_order_release);
     return HALOS_OK;
 }
 
