@@ -224,13 +224,13 @@ class _Rotary(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq, dk):
         freqs, positions = ctx.saved_tensors
-        dq, dk = (x if x.stride(3) == 1 else x.contiguous() for x in (dq, dk))
+        dq, dk = (x if x is None or x.stride(3) == 1 else x.contiguous() for x in (dq, dk))  # dk is None where k is
         dq, dk = rope(dq, dk, freqs, positions=positions, inverse=True, **ctx.how)
         return dq, dk, None, None, None, None, None
 
 
 def rotary(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", magnitude: float = 1.0):
-    """``rope`` with autograd."""
+    """``rope`` with autograd; k may be None."""
     return _Rotary.apply(q, k, freqs, positions, offset, layout, magnitude)
 
 

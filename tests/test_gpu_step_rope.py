@@ -144,3 +144,12 @@ def test_refusals(what):
     with pytest.raises(hb.HalosError) as e:
         step.rope(q, k, freqs, **kw)
     assert e.value.status in (hb.ERR_INVALID_ARG, hb.ERR_UNSUPPORTED)
+
+
+def test_gradient_without_keys():
+    q = _x((2, 5, 3, 32), torch.float32, 13).requires_grad_()
+    freqs, w = step.rotary_frequencies(24)[0], _x(q.shape, torch.float32, 14)
+    y, none = step.rotary(q, None, freqs, offset=7)
+    assert none is None
+    (y * w).sum().backward()
+    assert torch.equal(q.grad, step.rope(w, None, freqs, offset=7, inverse=True)[0])

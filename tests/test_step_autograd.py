@@ -1,0 +1,46 @@
+"""What autograd sees of the local step's operators.  The kernels' calls are replaced by plain stand-ins on the host."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2506_04531_b200 import step
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    """Stand-ins with the calls' signatures: a rotation by 90 degrees, uniform attention, and a quadratic loss."""
+    def rope(q, k, freqs, *, inverse=False, **how):
+        sign = -1.0 if inverse else 1.0
+        turned = lambda x: None if x is None else torch.cat([-sign * x[..., 1:2], sign * x[..., :1], x[..., 2:]], -1)  # noqa: E731
+        return turned(q.detach()), turned(None if k is None else k.detach())
+
+    def attention_forward(q, k, v, **how):
+        return v.detach().mean(1, keepdim=True).expand_as(q).contiguous(), q.new_zeros(q.shape[0], q.shape[2], q.shape[1])
+
+    def attention_backward(dout, q, k, v, o, lse, **how):
+        return torch.zeros_like(q), torch.zeros_like(k), dout.mean(1, keepdim=True).expand_as(v).contiguous()
+
+    def distill_forward(z, *rest, **how):
+        return z.detach().pow(2).sum(1) / 2, z.new_zeros(z.shape[0], 2)
+
+    def distill_backward(dloss, z, *rest, **how):
+        return z.detach() * dloss[:, None]
+
+    for f in (rope, attention_forward, attention_backward, distill_forward, distill_backward):
+        monkeypatch.setattr(step, f.__name__, f)
+
+
+def test_rotary_without_keys_has_a_gradient(plain):
+    q = torch.randn(1, 3, 2, 8, requires_grad=True)
+    w = torch.randn(1, 3, 2, 8)
+    y, none = step.rotary(q, None, torch.ones(1, dtype=torch.float64))
+    assert none is None
+    (y * w).sum().backward()
+    assert torch.equal(q.grad, step.rope(w, None, None, inverse=True)[0])
+
+
+def test_rotary_where_only_the_keys_are_used(plain):
+    q, k = torch.randn(1, 3, 2, 8, requires_grad=True), torch.randn(1, 3, 2, 8, requires_grad=True)
+    step.rotary(q, k, torch.ones(1, dtype=torch.float64))[1].sum().backward()
+    assert float(q.grad.abs().sum()) == 0 and torch.equal(k.grad, step.rope(torch.ones_like(k), None, None, inverse=True)[0])
