@@ -10,13 +10,14 @@ allocation, on the current stream of the tensors' device.  There is no CPU path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import struct
 from typing import Optional
 
 import torch
 
-from .binding import BF16, ERR_INVALID_ARG, F32, HalosError, load_library
+from .binding import BF16, ERR_INVALID_ARG, ERR_UNSUPPORTED, F32, HalosError, load_library
 
 F16 = 2
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
@@ -75,6 +76,18 @@ _ROPE, _ATTENTION, _DISTILL = _packer(RopeArgs), _packer(AttentionArgs), _packer
 # The stream's handle is asked for without building a stream object around it.
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _lib = None
+
+
+class _Once(torch.autograd.Function):
+    """Gradients as a function of what they were formed from, for a graph of them (create_graph=True): the kernels have no derivative of
+    their own, and autograd, which does not see them, would take it for zero."""
+    @staticmethod
+    def forward(ctx, form, *inputs):
+        return form(*inputs)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise HalosError(ERR_UNSUPPORTED, "attention and the distillation loss have no second derivative")
 
 
 def _library():
@@ -216,22 +229,20 @@ def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", 
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, freqs, positions, offset, layout, magnitude):
+    def forward(ctx, q, k, freqs, positions, offset, layout, magnitude, inverse):
         ctx.save_for_backward(freqs, positions)
-        ctx.how = dict(offset=offset, layout=layout, magnitude=magnitude)
-        return rope(q, k, freqs, positions=positions, **ctx.how)
+        ctx.how = (offset, layout, magnitude, not inverse)
+        return rope(q, k, freqs, positions=positions, offset=offset, layout=layout, magnitude=magnitude, inverse=inverse)
 
     @staticmethod
     def backward(ctx, dq, dk):
-        freqs, positions = ctx.saved_tensors
         dq, dk = (x if x is None or x.stride(3) == 1 else x.contiguous() for x in (dq, dk))  # dk is None where k is
-        dq, dk = rope(dq, dk, freqs, positions=positions, inverse=True, **ctx.how)
-        return dq, dk, None, None, None, None, None
+        return (*_Rotary.apply(dq, dk, *ctx.saved_tensors, *ctx.how), None, None, None, None, None, None)  # linear: differentiable as often as one likes
 
 
 def rotary(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", magnitude: float = 1.0):
     """``rope`` with autograd; k may be None."""
-    return _Rotary.apply(q, k, freqs, positions, offset, layout, magnitude)
+    return _Rotary.apply(q, k, freqs, positions, offset, layout, magnitude, False)
 
 
 # ------------------------------------------------------------------------------------------ attention
@@ -322,11 +333,13 @@ class _Attention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dout):
-        return (*attention_backward(dout, *ctx.saved_tensors, **ctx.how), None, None, None, None)
+        form = functools.partial(attention_backward, **ctx.how)
+        inputs = (dout, *ctx.saved_tensors)
+        return (*(_Once.apply(form, *inputs) if torch.is_grad_enabled() else form(*inputs)), None, None, None, None)
 
 
 def attention(q, k, v, *, scale: Optional[float] = None, causal: bool = True, doc_start=None, lens=None):
-    """``attention_forward``'s o, with autograd."""
+    """``attention_forward``'s o, with autograd (of first order: a derivative of the gradients is refused)."""
     return _Attention.apply(q, k, v, scale, causal, doc_start, lens)
 
 
@@ -437,10 +450,11 @@ class _Distill(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dloss):
-        logits, *rest = ctx.saved_tensors
-        return (distill_backward(dloss.contiguous(), logits, *rest, **ctx.how), None, None, None, None, None, None)
+        form = functools.partial(distill_backward, **ctx.how)
+        inputs = (dloss.contiguous(), *ctx.saved_tensors)
+        return (_Once.apply(form, *inputs) if torch.is_grad_enabled() else form(*inputs), None, None, None, None, None, None)
 
 
 def distill_loss(logits, labels, teacher_idx=None, teacher_logits=None, *, temperature: float = 1.0, mix: float = 0.5, ignore_index: int = -100):
-    """``distill_forward``'s loss, with autograd for the logits."""
+    """``distill_forward``'s loss, with autograd for the logits (of first order: a derivative of the gradient is refused)."""
     return _Distill.apply(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)

@@ -44,3 +44,45 @@ def test_rotary_where_only_the_keys_are_used(plain):
     q, k = torch.randn(1, 3, 2, 8, requires_grad=True), torch.randn(1, 3, 2, 8, requires_grad=True)
     step.rotary(q, k, torch.ones(1, dtype=torch.float64))[1].sum().backward()
     assert float(q.grad.abs().sum()) == 0 and torch.equal(k.grad, step.rope(torch.ones_like(k), None, None, inverse=True)[0])
+
+
+def test_rotary_twice_differentiated(plain):
+    """Linear in q: the penalty on a gradient sees the way there and back."""
+    q, w = torch.randn(1, 3, 2, 8, requires_grad=True), torch.randn(1, 3, 2, 8)
+    y = step.rotary(q, None, torch.ones(1, dtype=torch.float64))[0]
+    g, = torch.autograd.grad((y.pow(3) * w).sum(), q, create_graph=True)
+    second, = torch.autograd.grad(g.sum(), q)
+    turn = lambda x, inverse=False: step.rope(x, None, None, inverse=inverse)[0]  # noqa: E731
+    want = turn(6 * turn(q) * w * turn(torch.ones_like(q)), True)
+    assert torch.allclose(second, want, atol=1e-5)
+
+
+@pytest.mark.parametrize("last", [True, False])
+def test_a_second_derivative_of_attention_is_refused_and_not_left_out(plain, last):
+    """Where attention comes last, the gradient of its output is a constant: the term that would be dropped is that of q, k and v."""
+    q, k, v = (torch.randn(1, 3, 2, 8, requires_grad=True) for _ in range(3))
+    o = step.attention(q, k, v)
+    grads = torch.autograd.grad(o.sum() if last else o.pow(2).sum(), (q, k, v), create_graph=True)
+    penalty = sum(g.pow(2).sum() for g in grads) + v.pow(2).sum()
+    with pytest.raises(step.HalosError, match="second derivative"):
+        penalty.backward()
+
+
+@pytest.mark.parametrize("last", [True, False])
+def test_a_second_derivative_of_the_loss_is_refused_and_not_left_out(plain, last):
+    z = torch.randn(3, 5, requires_grad=True)
+    loss = step.distill_loss(z, None)
+    g, = torch.autograd.grad(loss.sum() if last else loss.pow(2).sum(), z, create_graph=True)
+    with pytest.raises(step.HalosError, match="second derivative"):
+        (g.pow(2).sum() + z.sum()).backward()
+
+
+def test_first_derivatives_with_a_graph_are_the_same(plain):
+    z = torch.randn(3, 5, requires_grad=True)
+    a, = torch.autograd.grad(step.distill_loss(z, None).sum(), z)
+    b, = torch.autograd.grad(step.distill_loss(z, None).sum(), z, create_graph=True)
+    assert torch.equal(a, b)
+    v = torch.randn(1, 3, 2, 8, requires_grad=True)
+    a, = torch.autograd.grad(step.attention(v.detach(), v.detach(), v).pow(2).sum(), v)
+    b, = torch.autograd.grad(step.attention(v.detach(), v.detach(), v).pow(2).sum(), v, create_graph=True)
+    assert torch.equal(a, b)
