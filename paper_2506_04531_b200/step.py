@@ -326,15 +326,15 @@ def attention_backward(dout, q, k, v, o, lse, *, scale: Optional[float] = None, 
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, scale, causal, doc_start, lens):
-        ctx.how = dict(scale=scale, causal=causal, doc_start=doc_start, lens=lens)
-        o, lse = attention_forward(q, k, v, **ctx.how)
-        ctx.save_for_backward(q, k, v, o, lse)
+        ctx.how = dict(scale=scale, causal=causal)
+        o, lse = attention_forward(q, k, v, doc_start=doc_start, lens=lens, **ctx.how)
+        ctx.save_for_backward(q, k, v, o, lse, doc_start, lens)  # the masks too, so that autograd notices if they are overwritten
         return o
 
     @staticmethod
     def backward(ctx, dout):
-        form = functools.partial(attention_backward, **ctx.how)
-        inputs = (dout, *ctx.saved_tensors)
+        *inputs, doc_start, lens = (dout, *ctx.saved_tensors)
+        form = functools.partial(attention_backward, doc_start=doc_start, lens=lens, **ctx.how)
         return (*(_Once.apply(form, *inputs) if torch.is_grad_enabled() else form(*inputs)), None, None, None, None)
 
 

@@ -86,3 +86,15 @@ def test_first_derivatives_with_a_graph_are_the_same(plain):
     a, = torch.autograd.grad(step.attention(v.detach(), v.detach(), v).pow(2).sum(), v)
     b, = torch.autograd.grad(step.attention(v.detach(), v.detach(), v).pow(2).sum(), v, create_graph=True)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("what", ["doc_start", "lens"])
+def test_a_mask_that_is_overwritten_before_the_backward_pass_is_noticed(plain, what):
+    """A buffer that the next batch's documents are written to."""
+    v = torch.randn(2, 3, 2, 8, requires_grad=True)
+    mask = torch.zeros((2, 3) if what == "doc_start" else (2,), dtype=torch.int32)
+    step.attention(v.detach(), v.detach(), v, **{what: mask}).sum().backward()
+    o = step.attention(v.detach(), v.detach(), v, **{what: mask})
+    mask += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        o.sum().backward()
