@@ -128,6 +128,14 @@ def _on(x, device, what: str):
         _refuse(f"{what} is on {x.device}, not on {device}")
 
 
+def _overwritten(x, what: str):
+    """For a tensor that a kernel is about to write over: refused inside a graph, whose history it would no longer agree with, and noted,
+    so that autograd notices where it had been saved."""
+    if x.requires_grad and torch.is_grad_enabled():
+        _refuse(f"{what} requires a gradient and cannot be overwritten (pass it detached if its history does not matter)")
+    torch.autograd.graph.increment_version(x)
+
+
 def fault(device: Optional[int] = None) -> bool:
     """Whether a bounded wait of an attention kernel has run out on this device; waits for the device."""
     out = _i32(0)
@@ -182,7 +190,7 @@ def _heads_last(x, what: str):
 def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", magnitude: float = 1.0, inverse: bool = False, inplace: bool = False):
     """Rotates the first 2 len(freqs) elements of every head of q and k ([batch, seq, heads, head_dim], any strides that keep a
     head's elements side by side; k may be None) to their positions: int32 or int64 [seq] or [batch, seq], or offset + 0, 1, ...
-    inverse: the gradient's way back.  inplace: q and k are overwritten and returned (a view must not overlap itself)."""
+    inverse: the gradient's way back.  inplace: q and k are overwritten and returned (neither themselves nor one another may they overlap, nor require a gradient)."""
     device, dtype = q.device, q.dtype
     _heads_last(q, "q")
     _on(q, device, "q")
@@ -216,6 +224,9 @@ def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", 
         for x in (q, k):
             if x is not None and any(s == 0 and n > 1 for s, n in zip(x.stride(), x.shape)):
                 _refuse("a broadcast tensor cannot be rotated in place")
+        for x, what in ((q, "q"), (k, "k")):
+            if x is not None:
+                _overwritten(x, what)
         q_out, k_out = q, k
     else:
         q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
@@ -402,6 +413,7 @@ def _gradient_like(logits, out):
         _on(out, logits.device, "out")
         if out.shape != logits.shape or out.dtype != logits.dtype or (out.size(1) > 1 and out.stride(1) != 1):
             _refuse("out must be like logits, a row's elements side by side")
+        _overwritten(out, "out")
     return out
 
 
@@ -419,7 +431,7 @@ def distill_forward(logits, labels, teacher_idx, teacher_logits, *, temperature:
 
 
 def distill_backward(dloss, logits, stats, labels, teacher_idx, teacher_logits, *, temperature: float = 1.0, mix: float = 0.5, ignore_index: int = -100, out=None):
-    """dlogits from dloss [rows] and the forward pass's statistics; out may be the logits themselves."""
+    """dlogits from dloss [rows] and the forward pass's statistics; out may be the logits themselves (detached, if they are in a graph)."""
     values = _distill_checked(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
     weights = _row_weights(dloss, logits)
     _on(stats, logits.device, "stats")
@@ -431,7 +443,8 @@ def distill_backward(dloss, logits, stats, labels, teacher_idx, teacher_logits, 
 
 
 def distill_loss_and_grad(logits, labels, teacher_idx, teacher_logits, dloss, *, temperature: float = 1.0, mix: float = 0.5, ignore_index: int = -100, out=None):
-    """(loss, dlogits) in one pass over the logits, for weights dloss [rows] that are known beforehand; out may be the logits."""
+    """(loss, dlogits) in one pass over the logits, for weights dloss [rows] that are known beforehand; out may be the logits (detached,
+    if they are in a graph)."""
     values = _distill_checked(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
     weights = _row_weights(dloss, logits)
     loss = logits.new_empty(values[7], dtype=torch.float32)
