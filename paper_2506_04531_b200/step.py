@@ -5,7 +5,8 @@
     distill_forward, _backward, distill_loss_and_grad      the loss against labels and a teacher's top logits; distill_loss: with autograd
 
 As in ``binding``, the arithmetic is the CUDA library's; what happens here is checking, marshalling and output
-allocation, on the current stream of the tensors' device.  There is no CPU path.  Errors are ``HalosError``.
+allocation, on the current stream of the tensors' device.  The caller's current device stays what it was.  There is no CPU path.
+Errors are ``HalosError``.
 """
 from __future__ import annotations
 
@@ -75,6 +76,7 @@ def _pack(kind, *values) -> bytes:
 _ROPE, _ATTENTION, _DISTILL = _packer(RopeArgs), _packer(AttentionArgs), _packer(DistillArgs)
 # The stream's handle is asked for without building a stream object around it.
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device, _set_device = torch._C._cuda_getDevice, torch._C._cuda_setDevice
 _lib = None
 
 
@@ -107,9 +109,13 @@ def _refuse(text: str):
     raise HalosError(ERR_INVALID_ARG, text)
 
 
-def _call(name: str, args: bytes):
+def _call(name: str, args: bytes, device: int):
+    """The C calls leave their device current; here the caller's stays."""
     lib = _lib or _library()
+    before = _current_device()
     rc = getattr(lib, name)(args)
+    if before != device:
+        _set_device(before)
     if rc:
         raise HalosError(rc, lib.halos_step_error().decode())
 
@@ -140,7 +146,11 @@ def fault(device: Optional[int] = None) -> bool:
     """Whether a bounded wait of an attention kernel has run out on this device; waits for the device."""
     out = _i32(0)
     lib = _library()
-    rc = lib.halos_step_fault(torch.cuda.current_device() if device is None else int(device), C.byref(out))
+    before = torch.cuda.current_device()
+    device = before if device is None else int(device)
+    rc = lib.halos_step_fault(device, C.byref(out))
+    if before != device:
+        _set_device(before)
     if rc:
         raise HalosError(rc, lib.halos_step_error().decode())
     return bool(out.value)
@@ -234,7 +244,7 @@ def rope(q, k, freqs, *, positions=None, offset: int = 0, layout: str = "half", 
     _call("halos_rope", _pack(
         _ROPE, _ROPE.size, device.index, _raw_stream(device.index), kind, _LAYOUTS.get(layout, 99), bool(inverse), wide, batch, seq, n_q, n_k, head_dim, 2 * freqs.numel(), magnitude, 0,
         freqs.data_ptr(), at, *st, offset, q.data_ptr(), 0 if k is None else k.data_ptr(), q_out.data_ptr(), 0 if k is None else k_out.data_ptr(),
-        *q.stride()[:3], *(none if k is None else k.stride()[:3]), *q_out.stride()[:3], *(none if k is None else k_out.stride()[:3])))
+        *q.stride()[:3], *(none if k is None else k.stride()[:3]), *q_out.stride()[:3], *(none if k is None else k_out.stride()[:3])), device.index)
     return q_out, k_out
 
 
@@ -307,7 +317,7 @@ def attention_forward(q, k, v, *, scale: Optional[float] = None, causal: bool = 
     device = q.device.index
     _call("halos_attention_fwd", _pack(
         _ATTENTION, _ATTENTION.size, device, _raw_stream(device), *values, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), 0, 0, 0, 0, 0, 0,
-        *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0))
+        *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), device)
     return o, lse
 
 
@@ -330,7 +340,7 @@ def attention_backward(dout, q, k, v, o, lse, *, scale: Optional[float] = None, 
     head = (_ATTENTION.size, device, _raw_stream(device), *values, *pointers)
     (_lib or _library()).halos_attention_workspace(_pack(_ATTENTION, *head, 0, 0, *strides), C.byref(size))
     space = q.new_empty(size.value, dtype=torch.uint8)
-    _call("halos_attention_bwd", _pack(_ATTENTION, *head, space.data_ptr(), size.value, *strides))
+    _call("halos_attention_bwd", _pack(_ATTENTION, *head, space.data_ptr(), size.value, *strides), device)
     return dq, dk, dv
 
 
@@ -426,7 +436,7 @@ def distill_forward(logits, labels, teacher_idx, teacher_logits, *, temperature:
     values = _distill_checked(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
     loss = logits.new_empty(values[7], dtype=torch.float32)
     stats = logits.new_empty((values[7], 2), dtype=torch.float32)
-    _call("halos_distill_fwd", _pack(_DISTILL, *values, loss.data_ptr(), stats.data_ptr(), 0, 0, 0))
+    _call("halos_distill_fwd", _pack(_DISTILL, *values, loss.data_ptr(), stats.data_ptr(), 0, 0, 0), values[1])
     return loss, stats
 
 
@@ -438,7 +448,7 @@ def distill_backward(dloss, logits, stats, labels, teacher_idx, teacher_logits, 
     if stats.dtype != torch.float32 or stats.shape != (values[7], 2) or not stats.is_contiguous():
         _refuse("stats must be contiguous float32 [rows, 2]")
     out = _gradient_like(logits, out)
-    _call("halos_distill_bwd", _pack(_DISTILL, *values, 0, stats.data_ptr(), weights, out.data_ptr(), out.stride(0)))
+    _call("halos_distill_bwd", _pack(_DISTILL, *values, 0, stats.data_ptr(), weights, out.data_ptr(), out.stride(0)), values[1])
     return out
 
 
@@ -449,7 +459,7 @@ def distill_loss_and_grad(logits, labels, teacher_idx, teacher_logits, dloss, *,
     weights = _row_weights(dloss, logits)
     loss = logits.new_empty(values[7], dtype=torch.float32)
     out = _gradient_like(logits, out)
-    _call("halos_distill_fwd_bwd", _pack(_DISTILL, *values, loss.data_ptr(), 0, weights, out.data_ptr(), out.stride(0)))
+    _call("halos_distill_fwd_bwd", _pack(_DISTILL, *values, loss.data_ptr(), 0, weights, out.data_ptr(), out.stride(0)), values[1])
     return loss, out
 
 
