@@ -58,5 +58,7 @@ extern "C" int halos_step_fault(int32_t device, int32_t* fault) {
     using namespace halos_step;
     if (!fault) return fail(HALOS_ERR_INVALID_ARG, "fault: null pointer");
     if (int rc = enter(device)) return rc;
+    // A copy alone would not wait for streams that do not synchronise with the default one.
+    if (int rc = cuda_status(cudaDeviceSynchronize(), "fault mark")) return rc;
     return cuda_status(cudaMemcpyFromSymbol(fault, g_fault, sizeof(int)), "fault mark");
 }
