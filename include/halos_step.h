@@ -15,7 +15,8 @@
  *    args->stream (cudaStream_t, NULL = the legacy default stream) and returns without waiting.  Tensors are
  *    borrowed until those kernels have completed in stream order.
  *  - Pointers are device pointers.  Strides are in elements; the innermost dimension is contiguous.
- *  - Nothing is allocated: workspaces are the caller's (halos_attention_workspace says how much).
+ *  - Nothing is allocated but 256 bytes of host memory in the first call: workspaces are the caller's
+ *    (halos_attention_workspace says how much).
  *  - The same inputs give the same bits, call after call: no result depends on the order of atomics.
  *  - Sums, statistics and everything between load and store are held in 32 bits; results are rounded once.
  *  - Status values are those of halos.h; on any other status than HALOS_OK nothing was enqueued (HALOS_ERR_CUDA
@@ -34,8 +35,9 @@ enum { HALOS_F16 = 2 };  /* beside HALOS_F32 and HALOS_BF16 of halos.h */
 
 const char* halos_step_error(void);
 
-/* Device-side waits of these kernels are bounded.  One that ran out (it never does unless the GPU lost work)
- * leaves its outputs undefined and a mark here: *fault = 0 if none has since the library was loaded.  Waits for the device. */
+/* Device-side waits of these kernels are bounded.  One that ran out (it never does unless the GPU lost work, or kept a kernel from
+ * running for a second) leaves its outputs undefined and a mark, and every later call on that device returns HALOS_ERR_CUDA
+ * until the mark has been asked for here: *fault = 0 if there was none, and there is none afterwards.  Waits for the device. */
 int halos_step_fault(int32_t device, int32_t* fault);
 
 /* ------------------------------------------------------------------ rotary positions ----------- */

@@ -741,7 +741,7 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     const uint32_t q_full = smem_u32(C.bars), done = q_full + 8, s_full = q_full + 16, s_read = q_full + 24, dp_full = q_full + 32, ds_full = dp_full + 8 * F::kDPs,
                    k_full = ds_full + 8 * F::kDPs, k_free = k_full + 8 * F::kStagesK, v_full = k_free + 8 * F::kStagesK, v_free = v_full + 8 * F::kStagesV;
     if (smem_u32(smem) & 1023) {  // then no tile would lie as its descriptors say
-        if (threadIdx.x == 0) atomicExch(P.fault, 1);
+        if (threadIdx.x == 0) say_fault(P.fault);
         return;
     }
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;

@@ -2,6 +2,7 @@
 #include "step_common.cuh"
 
 #include <atomic>
+#include <mutex>
 #include <stdio.h>
 
 namespace halos_step {
@@ -10,7 +11,33 @@ constexpr int kMaxDevices = 64;
 thread_local char t_error[256] = "";
 thread_local int t_device = 0;
 std::atomic<int> g_sms[kMaxDevices];
-__device__ int g_fault;
+// A word for each device, in host memory that kernels write to: every call looks at it without asking the device.  Never given back.
+std::atomic<volatile int*> g_marks;
+std::mutex g_making_marks;
+
+int marks(volatile int** at) {
+    *at = g_marks.load(std::memory_order_acquire);
+    if (*at) return HALOS_OK;
+    const std::lock_guard<std::mutex> alone(g_making_marks);
+    *at = g_marks.load(std::memory_order_relaxed);
+    if (*at) return HALOS_OK;
+    // The first call may come while its stream is being captured, which an allocation has no part in.
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    if (int rc = cuda_status(cudaThreadExchangeStreamCaptureMode(&mode), "fault marks")) return rc;
+    int* made = nullptr;
+    const cudaError_t e = cudaHostAlloc((void**)&made, kMaxDevices * sizeof(int), cudaHostAllocPortable | cudaHostAllocMapped);
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
+    if (int rc = cuda_status(e, "fault marks")) return rc;
+    for (int i = 0; i < kMaxDevices; ++i) made[i] = 0;
+    *at = made;
+    g_marks.store(made, std::memory_order_release);
+    return HALOS_OK;
+}
+
+int make_current(int32_t device) {
+    if (device < 0 || device >= kMaxDevices) return fail(HALOS_ERR_INVALID_ARG, "no such device");
+    return cuda_status(cudaSetDevice(device), "cudaSetDevice (there is no CPU path)");
+}
 }  // namespace
 
 int fail(int status, const char* text) {
@@ -26,23 +53,23 @@ int cuda_status(cudaError_t e, const char* where) {
 }
 
 int enter(int32_t device) {
-    if (device < 0 || device >= kMaxDevices) return fail(HALOS_ERR_INVALID_ARG, "no such device");
-    if (int rc = cuda_status(cudaSetDevice(device), "cudaSetDevice (there is no CPU path)")) return rc;
+    if (int rc = make_current(device)) return rc;
     t_device = device;
     if (!g_sms[device].load(std::memory_order_relaxed)) {
         int n = 0;
         if (int rc = cuda_status(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device), "multiprocessor count")) return rc;
         g_sms[device].store(n, std::memory_order_relaxed);
     }
+    volatile int* at = nullptr;
+    if (int rc = marks(&at)) return rc;
+    if (at[device]) return fail(HALOS_ERR_CUDA, "a bounded wait of an earlier call on this device ran out: what that call returned is undefined (halos_step_fault clears the mark)");
     return HALOS_OK;
 }
 
 int fault_mark(int** mark) {
-    static std::atomic<int*> known[kMaxDevices];
-    *mark = known[t_device].load(std::memory_order_relaxed);
-    if (*mark) return HALOS_OK;
-    if (int rc = cuda_status(cudaGetSymbolAddress((void**)mark, g_fault), "fault mark")) return rc;
-    known[t_device].store(*mark, std::memory_order_relaxed);
+    volatile int* at = nullptr;
+    if (int rc = marks(&at)) return rc;
+    *mark = const_cast<int*>(at) + t_device;  // one address on the host and on every device
     return HALOS_OK;
 }
 
@@ -57,8 +84,10 @@ extern "C" const char* halos_step_error(void) { return halos_step::t_error; }
 extern "C" int halos_step_fault(int32_t device, int32_t* fault) {
     using namespace halos_step;
     if (!fault) return fail(HALOS_ERR_INVALID_ARG, "fault: null pointer");
-    if (int rc = enter(device)) return rc;
-    // A copy alone would not wait for streams that do not synchronise with the default one.
+    if (int rc = make_current(device)) return rc;
+    volatile int* at = nullptr;
+    if (int rc = marks(&at)) return rc;
     if (int rc = cuda_status(cudaDeviceSynchronize(), "fault mark")) return rc;
-    return cuda_status(cudaMemcpyFromSymbol(fault, g_fault, sizeof(int)), "fault mark");
+    *fault = at[device], at[device] = 0;
+    return HALOS_OK;
 }

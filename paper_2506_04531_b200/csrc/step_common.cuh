@@ -13,9 +13,9 @@ namespace halos_step {
 
 int fail(int status, const char* text);                 // sets the thread's error text, returns status
 int cuda_status(cudaError_t e, const char* where);      // HALOS_OK, or fail(HALOS_ERR_CUDA, ...)
-int enter(int32_t device);                              // makes the device current
+int enter(int32_t device);                              // makes the device current; fails where a wait has run out on it
 int sm_count(int32_t device);                           // of a device that enter() accepted
-int fault_mark(int** mark);                             // where the current device's kernels say that a wait ran out
+int fault_mark(int** mark);                             // where the current device's kernels say that a wait ran out: host memory
 
 constexpr int kSharedPerSM = 228 * 1024;
 int current_device();                                   // that enter() was last called with in this thread
@@ -35,6 +35,8 @@ int allow_smem(K* kernel, int bytes, Allowed& allowed) {
     had.store(bytes, std::memory_order_release);
     return HALOS_OK;
 }
+
+__device__ __forceinline__ void say_fault(int* mark) { *const_cast<volatile int*>(mark) = 1; }
 
 inline bool is_type(uint32_t t) { return t == HALOS_F32 || t == HALOS_BF16 || t == HALOS_F16; }
 

@@ -51,7 +51,7 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
 constexpr long long kWaitClocks = 2000000000ll;  // about a second
 struct Waits {
     volatile int* gave_up;  // in shared memory
-    int* fault;             // in device memory
+    int* fault;             // in host memory
     __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity) const {
         if (!bar_test(bar, parity)) wait_longer(bar, parity);
     }
@@ -66,7 +66,7 @@ struct Waits {
             if (bar_try(bar, parity)) return;
             if (clock64() - began > kWaitClocks) {
                 *gave_up = 1;
-                atomicExch(fault, 1);
+                say_fault(fault);
             }
         }
     }

@@ -143,7 +143,8 @@ def _overwritten(x, what: str):
 
 
 def fault(device: Optional[int] = None) -> bool:
-    """Whether a bounded wait of an attention kernel has run out on this device; waits for the device."""
+    """Whether a bounded wait of a kernel has run out on this device since this was last asked; waits for the device.  Until it is asked, the
+    calls that follow such a wait raise HalosError: what some call before them returned is undefined."""
     out = _i32(0)
     lib = _library()
     before = torch.cuda.current_device()
