@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import math
+from fractions import Fraction
 
 import pytest
 import torch
@@ -153,3 +154,22 @@ def test_gradient_without_keys():
     assert none is None
     (y * w).sum().backward()
     assert torch.equal(q.grad, step.rope(w, None, freqs, offset=7, inverse=True)[0])
+
+
+# 2 pi to 60 digits: what a 64-bit float leaves out of it is 10^-4 of a turn at position 2^40
+TWO_PI = Fraction(6283185307179586476925286766559005768394338798750211641949889, 10 ** 60)
+
+
+@pytest.mark.parametrize("base", [0, 10 ** 6 + 3, 2 ** 31 - 40, -2 ** 31, 2 ** 36 + 1, 2 ** 40 + 12345, -2 ** 44])
+def test_angles_against_exact_ones(base):
+    """Ones and zeros, so that cosine and sine of the angles come back as they are."""
+    freqs, seq = step.rotary_frequencies(64, scaling="linear", factor=3.0)[0], 33
+    q = torch.zeros((1, seq, 1, 64), device="cuda")
+    q[..., :32] = 1.0
+    y = step.rope(q, None, freqs, offset=base)[0][0, :, 0].double().cpu()
+    turns = [[float(Fraction(w) * (base + s) / TWO_PI % 1) for w in freqs.tolist()] for s in range(seq)]
+    angle = torch.tensor(turns, dtype=torch.float64) * (2 * math.pi)
+    # the angle: 2^-31 of a turn, 2^-62 more for each position, 2^-25 half turns of rounding; sine and cosine 2 ulp, rounded once more
+    bound = (2.0 ** -31 + 2.0 ** -62 * abs(base)) * 2 * math.pi + 2.0 ** -25 * math.pi + 3 * 2.0 ** -24
+    assert float((y[:, :32] - angle.cos()).abs().max()) <= bound
+    assert float((y[:, 32:] - angle.sin()).abs().max()) <= bound
