@@ -18,7 +18,8 @@
  *  - Nothing is allocated but 256 bytes of host memory in the first call: workspaces are the caller's
  *    (halos_attention_workspace says how much).
  *  - The same inputs give the same bits, call after call: no result depends on the order of atomics.
- *  - Sums, statistics and everything between load and store are held in 32 bits; results are rounded once.
+ *  - Sums, statistics and everything between load and store are held in 32 bits, and results are rounded once, except that attention rounds p
+ *    and ds to the inputs' type where they enter matrix products, and forms D from the o that was returned.
  *  - Status values are those of halos.h; on any other status than HALOS_OK nothing was enqueued (HALOS_ERR_CUDA
  *    excepted).  halos_step_error() is the calling thread's last error as text.
  */
@@ -84,7 +85,8 @@ int halos_rope(const halos_rope_args* args);
  * some query sees, or that lies between such keys, may also reach queries that do not see it (zero times it is not zero).
  * Backward, with D_i = dout_i.o_i:   ds_ij = p_ij (dout_i.v_j - D_i);  dq_i = scale sum_j ds_ij k_j;
  * dk_j = scale sum ds_ij q_i and dv_j = sum p_ij dout_i over the queries of every head that reads the key head.
- * p and ds enter their matrix products in the inputs' type, unnormalised resp. in true size; all sums are in 32 bits.
+ * p and ds enter their matrix products in the inputs' type; all sums are in 32 bits.  Backward with HALOS_F16 they are taken times powers of two,
+ * ds by the lengths of dout and v, so that gradients follow dout over its whole range, a loss scale included.
  * scale > 0, and scale log2(e) finite.  Scores are 32-bit sums, and lse one 32-bit number: a p that is formed from it is off by some 2^-23 |lse| of
  * itself, so that gradients of rows with |lse| in the tens of thousands lose what 16-bit types hold.  o is not formed from it.
  * dtype HALOS_BF16 or HALOS_F16 (HALOS_F32: UNSUPPORTED); head_dim a multiple of 8, <= 128; bases and strides of

@@ -19,8 +19,8 @@
 // exponential unit is busy 74%; a quarter of a CTA's time is its beginning and end, which the other CTA only partly
 // fills.  dK, dV: 1.1 us for 64 queries, bound by the products (63%); dQ: 0.76 us for 64 keys.
 //
-// p and ds are rounded to the inputs' type where they become operands (that is what the tensor cores take); every sum,
-// statistic and accumulator is in 32 bits, and each result is rounded once.
+// p and ds are rounded to the inputs' type where they become operands (that is what the tensor cores take), and D comes from an o that was rounded
+// to it (the forward pass returns no other); every sum, statistic and accumulator is in 32 bits, and each result is rounded once.
 #include "step_tcgen05.cuh"
 
 #include <limits.h>
@@ -49,6 +49,25 @@ static_assert(sizeof(Record) == 1024, "one bulk copy");
 // The keys that a batch row's 64 queries see, in four numbers: some of them see [min_lo, max_hi), all of them see
 // [max_lo, min_hi).  max_lo = INT_MAX: one of them sees nothing.
 struct Reach { int min_lo, max_hi, max_lo, min_hi; };
+// Largest squared lengths of dout of the queries and of v of the keys that take part, as bits of non-negative floats.
+struct Lengths { uint32_t dout, v; };
+
+// Floats with 5 bits of exponent hold neither a small p (under 2^-14 they lose digits) nor a ds of any size: it is as small as p times
+// dout, and may be as large as the loss scale that dout carries. There p is taken 2^kRaised times and ds kSteps times (a power of two that
+// goes by the lengths of dout and v, |ds| <= 2 |dout| |v|), and what they add up to is divided again.  The lengths take a kernel of their own, 8 us
+// of 440 (8197 tokens, 16/4 heads of 128).  bfloat16 has the exponents of 32-bit floats.
+constexpr int kRaised = 10;
+template <typename T> constexpr bool kNarrow = std::is_same<T, __half>::value;
+template <typename T> __host__ __device__ constexpr float raised() { return kNarrow<T> ? (float)(1 << kRaised) : 1.f; }
+// The power of two by which ds is taken: 2 |dout| |v| times it is 2^15 at most, of 65504.
+template <typename T>
+__device__ __forceinline__ float ds_steps(const Lengths* lengths) {
+    if constexpr (!kNarrow<T>) return 1.f;
+    const float square = __uint_as_float(lengths->dout) * __uint_as_float(lengths->v);
+    if (!(square > 0.f)) return 1.f;                                   // then ds is 0
+    const int e = (int)(__float_as_uint(square) >> 23) - 127;          // square < 2^(e + 1), so the product of the lengths < 2^((e + 2) >> 1)
+    return __uint_as_float((uint32_t)(14 - ((e + 2) >> 1) + 127) << 23);
+}
 
 struct AttentionParams {
     int sq, sk, head_dim, n_q, group, batch, causal, q_tiles, k_tiles, records;
@@ -60,6 +79,8 @@ struct AttentionParams {
     float* lse;
     Record* record;                   // [batch, n_q, records]
     Reach* reach;                     // [batch, records]
+    Lengths* lengths;                 // [batch, key heads], for kNarrow types
+    float* dout_square;               // [batch, n_q, records], for kNarrow types: of a record's queries
     int* fault;
     int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3], dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];  // in elements
 };
@@ -388,8 +409,8 @@ __global__ void __launch_bounds__(4 * kRecord) attention_record_kernel(const __g
     Record* R = P.record + ((int64_t)b * P.n_q + h) * P.records + rec;
     __shared__ Reach s_reach[8];
     __shared__ int s_lo[kRecord], s_hi[kRecord];
-    __shared__ float s_lse2[kRecord], s_term[kRecord][kFewKeys + 1];
-    float delta = 0.f, lse2 = 0.f;
+    __shared__ float s_lse2[kRecord], s_term[kRecord][kFewKeys + 1], s_square[8];
+    float delta = 0.f, lse2 = 0.f, square = 0.f;
     if (i < P.sq) {  // rows that see nothing are read too; what comes of it is not used
         const T* o = row_of<T>(P.o_in, P.o_stride, b, i, h) + 8 * part;
         const T* d = row_of<T>(P.dout, P.dout_stride, b, i, h) + 8 * part;
@@ -400,12 +421,23 @@ __global__ void __launch_bounds__(4 * kRecord) attention_record_kernel(const __g
         lse2 = P.lse[((int64_t)b * P.n_q + h) * P.sq + i] * kLog2e;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            if (8 * part + 32 * c < P.head_dim) delta = dot8<T>(x[c], y[c], delta);
+            if (8 * part + 32 * c < P.head_dim) {
+                delta = dot8<T>(x[c], y[c], delta);
+                if (kNarrow<T>) square = dot8<T>(y[c], y[c], square);
+            }
     }
     delta += __shfl_xor_sync(~0u, delta, 1);
     delta += __shfl_xor_sync(~0u, delta, 2);
     int lo, hi;
     seen_by(P, b, i, lo, hi);
+    if constexpr (kNarrow<T>) {
+        square += __shfl_xor_sync(~0u, square, 1);
+        square += __shfl_xor_sync(~0u, square, 2);
+        if (hi == 0) square = 0.f;
+#pragma unroll
+        for (int o = 16; o >= 4; o >>= 1) square = fmaxf(square, __shfl_xor_sync(~0u, square, o));
+        if ((threadIdx.x & 31) == 0) s_square[threadIdx.x >> 5] = square;
+    }
     // The queries with few keys, a thread to a query and a key; the terms are added in the order of the keys.
     const bool few = hi && hi - lo <= kFewKeys;
     if (part == 0) s_lse2[r] = lse2, s_lo[r] = lo, s_hi[r] = few ? hi : 0;
@@ -426,10 +458,15 @@ __global__ void __launch_bounds__(4 * kRecord) attention_record_kernel(const __g
         }
     }
     if (part == 0) {
-        R->minus_lse2[r] = hi ? -lse2 : -INFINITY;
+        R->minus_lse2[r] = hi ? (kNarrow<T> ? kRaised - lse2 : -lse2) : -INFINITY;
         R->minus_delta[r] = hi ? -delta : 0.f;
         R->lo[r] = lo;
         R->hi[r] = hi;
+    }
+    if (kNarrow<T> && threadIdx.x == 0) {  // written before the barrier that all threads have gone through
+        for (int w = 1; w < 8; ++w) square = fmaxf(square, s_square[w]);
+        P.dout_square[((int64_t)b * P.n_q + h) * P.records + rec] = square;
+        if (rec == 0 && h % P.group == 0) P.lengths[(int64_t)b * (P.n_q / P.group) + h / P.group] = Lengths{0, 0};
     }
     if (h == 0) {
         Reach a{INT_MAX, 0, 0, INT_MAX};
@@ -450,6 +487,60 @@ __global__ void __launch_bounds__(4 * kRecord) attention_record_kernel(const __g
             }
             P.reach[(int64_t)b * P.records + rec] = a;
         }
+    }
+}
+
+// The lengths that ds_steps goes by: a block takes its share of a key head's keys, eight threads to a key, and of its heads' records.  The
+// first keys are under way while the block finds out which of them some query sees.
+constexpr int kLengthsThreads = 256, kLengthsKeys = kLengthsThreads / 8, kLengthsAhead = 4;
+template <typename T>
+__global__ void __launch_bounds__(kLengthsThreads) attention_lengths_kernel(const __grid_constant__ AttentionParams P) {
+    const int hk = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31, part = threadIdx.x & 7;
+    __shared__ int s_lo, s_hi;
+    __shared__ uint32_t s_v, s_d;
+    if (threadIdx.x == 0) s_lo = INT_MAX, s_hi = 0, s_v = s_d = 0;
+    __syncthreads();
+    float v = 0.f, d = 0.f;
+    bool known = false;
+    const int64_t apart = (int64_t)gridDim.x * kLengthsKeys;
+    for (int64_t first = (int64_t)blockIdx.x * kLengthsKeys + (threadIdx.x >> 3), done = 0; done < P.sk; done += apart * kLengthsAhead, first += apart * kLengthsAhead) {
+        uint4 w[kLengthsAhead][2];
+#pragma unroll
+        for (int u = 0; u < kLengthsAhead; ++u)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int64_t j = first + u * apart;
+                w[u][c] = make_uint4(0, 0, 0, 0);
+                if (j < P.sk && 8 * part + 64 * c < P.head_dim) w[u][c] = *reinterpret_cast<const uint4*>(row_of<T>(P.v, P.v_stride, b, j, hk) + 8 * part + 64 * c);
+            }
+        if (!known) {
+            int lo = INT_MAX, hi = 0;
+            for (int r = threadIdx.x; r < P.records; r += kLengthsThreads) {
+                const Reach a = P.reach[(int64_t)b * P.records + r];
+                lo = min(lo, a.min_lo), hi = max(hi, a.max_hi);
+            }
+            if (hi) atomicMin(&s_lo, lo), atomicMax(&s_hi, hi);
+            __syncthreads();
+            known = true;
+        }
+#pragma unroll
+        for (int u = 0; u < kLengthsAhead; ++u) {
+            const int64_t j = first + u * apart;
+            float square = dot8<T>(w[u][1], w[u][1], dot8<T>(w[u][0], w[u][0], 0.f));
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) square += __shfl_xor_sync(~0u, square, o);
+            if (j >= s_lo && j < s_hi) v = fmaxf(v, square);
+        }
+    }
+    for (int64_t r = (int64_t)blockIdx.x * kLengthsThreads + threadIdx.x; r < (int64_t)P.group * P.records; r += (int64_t)gridDim.x * kLengthsThreads)
+        d = fmaxf(d, P.dout_square[((int64_t)b * P.n_q + hk * P.group) * P.records + r]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o)), d = fmaxf(d, __shfl_xor_sync(~0u, d, o));
+    if (lane == 0) atomicMax(&s_v, __float_as_uint(v)), atomicMax(&s_d, __float_as_uint(d));
+    __syncthreads();
+    if (threadIdx.x == 0) {  // a maximum does not depend on the order
+        Lengths& L = P.lengths[(int64_t)b * (P.n_q / P.group) + hk];
+        atomicMax(&L.v, s_v), atomicMax(&L.dout, s_d);
     }
 }
 
@@ -594,6 +685,8 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
         const int slot = warp >> 3, part = (warp >> 2) & 1, row = threadIdx.x & 127, key = key0 + row;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), at = lanes + slot * 128 + part * 32;
         int s = slot % F::kStages, use = slot / F::kStages, s_use = 0, rec = per_head ? slot % per_head : 0;
+        const float steps = n ? ds_steps<T>(P.lengths + (int64_t)b * (P.n_q / P.group) + hk) : 1.f;
+        const float2 step = both(steps / raised<T>());
         for (int it = slot; it < n; it += kSlots) {
             const Reach a = reach[first + rec];
             W.wait(full + 8 * s, use);
@@ -630,12 +723,13 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
             tmem_wait_loads32(y);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float2 md = *reinterpret_cast<const float2*>(R.minus_delta + column + 8 * k);
+                float2 md = *reinterpret_cast<const float2*>(R.minus_delta + column + 8 * k);
+                if (kNarrow<T>) md = mul2(md, step);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int at_e = 16 * (i >> 1) + 4 * k + 2 * (i & 1);
-                    const float2 ds = mul2(make_float2(__uint_as_float(x[at_e]), __uint_as_float(x[at_e + 1])),
-                                           add2(make_float2(__uint_as_float(y[at_e]), __uint_as_float(y[at_e + 1])), md));
+                    const float2 dp = make_float2(__uint_as_float(y[at_e]), __uint_as_float(y[at_e + 1]));
+                    const float2 ds = mul2(make_float2(__uint_as_float(x[at_e]), __uint_as_float(x[at_e + 1])), kNarrow<T> ? fma2(dp, step, md) : add2(dp, md));
                     y[at_e] = __float_as_uint(ds.x), y[at_e + 1] = __float_as_uint(ds.y);
                 }
             }
@@ -685,7 +779,7 @@ attention_keys_kernel(const __grid_constant__ AttentionParams P, const __grid_co
         if (slot == 0) {  // four warps store dV, four dK
             {
                 const int what = part;
-                const float f = what ? P.scale : 1.f;
+                const float f = what ? P.scale / steps : 1.f / raised<T>();
                 const int64_t* st = what ? P.dk_stride : P.dv_stride;
 #pragma unroll
                 for (int c = 0; c < DP / 32; ++c) {
@@ -862,7 +956,8 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
     } else {
         const int part = (warp >> 2) & 1;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const float2 factor = both(P.scale2), ml = both(minus_lse2), md = both(minus_delta);
+        const float steps = n ? ds_steps<T>(P.lengths + (int64_t)b * (P.n_q / P.group) + hk) : 1.f;
+        const float2 factor = both(P.scale2), ml = both(minus_lse2), step = both(steps / raised<T>()), md = both(minus_delta * step.x);
         const bool one = hi - lo == 1;  // a softmax of one term is constant
         for (int j = 0; j < n; ++j) {
             const int s = j % F::kStagesK, tile0 = (first + j) * 64, key0 = tile0 + part * 32;
@@ -886,7 +981,8 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
             const bool masked = !__all_sync(~0u, lo <= key0 && hi >= key0 + 32);
 #pragma unroll
             for (int c = 0; c < 32; c += 2) {
-                const float2 ds = mul2(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), add2(make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1])), md));
+                const float2 dp = make_float2(__uint_as_float(y[c]), __uint_as_float(y[c + 1]));
+                const float2 ds = mul2(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), kNarrow<T> ? fma2(dp, step, md) : add2(dp, md));
                 x[c] = __float_as_uint(ds.x), x[c + 1] = __float_as_uint(ds.y);
             }
             if (masked) {
@@ -920,8 +1016,9 @@ attention_queries_kernel(const __grid_constant__ AttentionParams P, const __grid
                     tmem_wait_loads32(o);
                 }
                 if (i < P.sq) {
+                    const float f = P.scale / steps;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = hi ? pack2<T>(__uint_as_float(o[2 * e]) * P.scale, __uint_as_float(o[2 * e + 1]) * P.scale) : 0u;
+                    for (int e = 0; e < 16; ++e) o[e] = hi ? pack2<T>(__uint_as_float(o[2 * e]) * f, __uint_as_float(o[2 * e + 1]) * f) : 0u;
                     store_row<T>(P.dq, b * P.dq_stride[0] + i * P.dq_stride[1] + h * P.dq_stride[2], P.head_dim, o, 32 * c);
                 }
             }
@@ -1027,7 +1124,9 @@ int forward(const halos_attention_args* a) {
 
 uint64_t workspace(const halos_attention_args* a) {
     const uint64_t records = (uint64_t)(round_up(a->sq, 128) / kRecord);
-    return a->batch * records * (a->n_q * sizeof(Record) + sizeof(Reach));
+    uint64_t bytes = a->batch * records * (a->n_q * sizeof(Record) + sizeof(Reach));
+    if (a->dtype == HALOS_F16) bytes += a->batch * (a->n_kv * sizeof(Lengths) + a->n_q * records * sizeof(float));
+    return bytes;
 }
 
 template <typename T, int DP, int kKeySlots>
@@ -1036,6 +1135,8 @@ int backward(const halos_attention_args* a) {
     if (int rc = params(a, P)) return rc;
     P.record = (Record*)a->workspace;
     P.reach = (Reach*)(P.record + (int64_t)P.batch * P.n_q * P.records);
+    P.lengths = (Lengths*)(P.reach + (int64_t)P.batch * P.records);
+    P.dout_square = (float*)(P.lengths + (int64_t)P.batch * a->n_kv);
     cudaStream_t st = (cudaStream_t)a->stream;
     CUtensorMap q{}, d{}, k{}, v{};
     using K = Keys<DP, kKeySlots>;
@@ -1046,6 +1147,14 @@ int backward(const halos_attention_args* a) {
     if (P.sq) {
         attention_record_kernel<T><<<dim3(P.records, P.n_q, P.batch), 4 * kRecord, 0, st>>>(P);
         if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
+    }
+    if constexpr (kNarrow<T>) {
+        if (P.sq && P.sk) {
+            // Four blocks to an SM over all heads at most: each goes over the reaches of its batch row once.
+            const int64_t heads = (int64_t)P.batch * a->n_kv, most = (P.sk + kLengthsKeys - 1) / kLengthsKeys, want = (4 * (int64_t)sm_count(a->device) + heads - 1) / heads;
+            attention_lengths_kernel<T><<<dim3((unsigned)(most < want ? most : want), a->n_kv, P.batch), kLengthsThreads, 0, st>>>(P);
+            if (int rc = cuda_status(cudaGetLastError(), "attention launch")) return rc;
+        }
     }
     if (P.sk) {
         if (P.sq) {

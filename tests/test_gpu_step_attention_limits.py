@@ -90,3 +90,56 @@ def test_a_scale_that_overflows_is_refused():
     with pytest.raises(hb.HalosError) as e:
         step.attention_forward(q, q, q, scale=3e38)
     assert e.value.status == hb.ERR_INVALID_ARG
+
+
+def _gradients(q, k, v, dout, **mask):
+    o, lse = step.attention_forward(q, k, v, **mask)
+    return step.attention_backward(dout, q, k, v, o, lse, **mask)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("s,causal", [(2048, False), (300, True), (40, True)])
+@pytest.mark.parametrize("power", [-16, -14, -10, -6, 6, 10, 12])
+def test_gradients_follow_the_size_of_dout_in_float16(power, s, causal, d):
+    """dout 2^power times gives gradients 2^power times, but for their own rounding: nothing on the way is too small or too large for the type."""
+    q, k, v = (_x((1, s, 2, d), F16, i, 0.5 if i < 2 else 1.0) for i in range(3))
+    dout = (_x((1, s, 2, d), torch.float32, 3).clamp(-4, 4) * 16).round().div(16).to(F16)   # multiples of 2^-4: exact at every power here
+    one = _gradients(q, k, v, dout, causal=causal)
+    other = _gradients(q, k, v, dout * 2.0 ** power, causal=causal)
+    for a, b in zip(one, other):
+        want = a.double() * 2.0 ** power
+        off = 2 * so.U[F16] * want.abs() + 2.0 ** -25 * (1 + 2.0 ** power)
+        fits = want.abs() < 65000
+        assert bool(((b.double() - want).abs() <= off)[fits].all())
+
+
+@pytest.mark.parametrize("size", [2.0 ** -10, 30.0, 2000.0])
+def test_gradients_follow_the_size_of_the_values_in_float16(size):
+    q, k, v, dout = (_x((1, 260, 4, 64), F16, i) for i in range(4))
+    dout, v = dout * 2.0 ** -4, v[:, :, :2] * size
+    want = so.attention(q, k[:, :, :2], v, dout, scale=0.125, causal=True)
+    for name, got in zip(("dq", "dk", "dv"), _gradients(q, k[:, :, :2], v, dout)):
+        assert bool(((got.double() - want[name]).abs() <= want[name + "_bound"]).all()), name
+
+
+@pytest.mark.parametrize("garbage", [float("nan"), float("inf"), -60000.0])
+def test_what_nobody_sees_does_not_weigh_on_the_gradients_in_float16(garbage):
+    """Past the ends of sequences and before the first document: the same bits as with zeros there."""
+    s, lens = 270, torch.tensor([270, 0, 65, 130], dtype=torch.int32, device="cuda")
+    starts = torch.zeros((4, s), dtype=torch.int32, device="cuda")
+    starts[3] = 70
+    q, k, v, dout = (_x((4, s, 4, 64), F16, i) for i in range(4))
+    k, v = k[:, :, :2].contiguous(), v[:, :, :2].contiguous()
+    place = torch.arange(s, device="cuda")[None]
+    unseen = (place >= lens[:, None]) | (place < starts[:, :1])
+    fill = lambda x: [t.masked_fill(unseen[:, :, None, None], x) for t in (q, k, v, dout)]  # noqa: E731
+    clean, dirty = (_gradients(*fill(x), doc_start=starts, lens=lens) for x in (0.0, garbage))
+    assert all(torch.equal(a, b) and bool(torch.isfinite(b).all()) for a, b in zip(clean, dirty))
+
+
+def test_no_gradient_at_all_in_float16():
+    q, k, v = (_x((1, 100, 2, 64), F16, i) for i in range(3))
+    for dout, values in ((torch.zeros_like(q), v), (q, torch.zeros_like(v))):
+        dq, dk, dv = _gradients(q, k, values, dout)
+        assert float(dq.abs().sum()) == float(dk.abs().sum()) == 0
+        assert bool(torch.isfinite(dv).all()) and (float(dv.abs().sum()) > 0) == bool(dout.any())
