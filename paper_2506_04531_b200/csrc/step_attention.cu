@@ -53,7 +53,7 @@ struct Reach { int min_lo, max_hi, max_lo, min_hi; };
 struct Lengths { uint32_t dout, v; };
 
 // Floats with 5 bits of exponent hold neither a small p (under 2^-14 they lose digits) nor a ds of any size: it is as small as p times
-// dout, and may be as large as the loss scale that dout carries. There p is taken 2^kRaised times and ds kSteps times (a power of two that
+// dout, and may be as large as the loss scale that dout carries. There p is taken 2^kRaised times and ds ds_steps times (a power of two that
 // goes by the lengths of dout and v, |ds| <= 2 |dout| |v|), and what they add up to is divided again.  The lengths take a kernel of their own, 8 us
 // of 440 (8197 tokens, 16/4 heads of 128).  bfloat16 has the exponents of 32-bit floats.
 constexpr int kRaised = 10;

@@ -584,6 +584,8 @@ int distill(const halos_distill_args* a) {
     if ((uintptr_t)a->logits % size || (kMode != kForward && (uintptr_t)a->dlogits % size))
         return fail(HALOS_ERR_INVALID_ARG, "distill: tensor not aligned to its elements");
     if (kMode != kForward && a->rows > 1 && a->dlogits_stride < a->vocab) return fail(HALOS_ERR_INVALID_ARG, "distill: rows of dlogits overlap");
+    if (kMode != kForward && a->rows > 1 && a->dlogits == a->logits && a->dlogits_stride != a->logits_stride)
+        return fail(HALOS_ERR_INVALID_ARG, "distill: over the logits themselves dlogits must have their stride");
     if (int rc = enter(a->device)) return rc;
     DistillParams P{};
     P.z = (const char*)a->logits, P.dz = (char*)a->dlogits, P.labels = a->labels, P.index = a->teacher_index, P.t = (const char*)a->teacher_logits;

@@ -225,6 +225,11 @@ extern "C" int halos_rope(const halos_rope_args* a) {
     if (tokens > 0x7fffffffll) return fail(HALOS_ERR_UNSUPPORTED, "rope: over 2^31 - 1 tokens");
     if ((a->n_q && (!a->q_in || !a->q_out)) || (a->n_k && (!a->k_in || !a->k_out)) || (a->rot_dim && !a->freqs))
         return fail(HALOS_ERR_INVALID_ARG, "rope: null pointer");
+    const int64_t q_size[3] = {a->batch, a->seq, a->n_q}, k_size[3] = {a->batch, a->seq, a->n_k};
+    for (int i = 0; i < 3; ++i)
+        if ((a->n_q && a->q_in == a->q_out && q_size[i] > 1 && a->q_in_stride[i] != a->q_out_stride[i]) ||
+            (a->n_k && a->k_in == a->k_out && k_size[i] > 1 && a->k_in_stride[i] != a->k_out_stride[i]))
+            return fail(HALOS_ERR_INVALID_ARG, "rope: in place the strides must be the same");
     const uint32_t size = a->dtype == HALOS_F32 ? 4 : 2;
     // Widest access (16 bytes) that divides the head, the pairs and every address.
     uint64_t all = a->head_dim | (a->layout == HALOS_ROPE_HALF ? a->rot_dim / 2 : a->rot_dim);

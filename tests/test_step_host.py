@@ -133,3 +133,22 @@ def test_without_a_device_valid_calls_fail_with_a_cuda_error(lib):
     from paper_2506_04531_b200 import binding, step
     assert lib.halos_attention_fwd(C.byref(_attention(step))) == binding.ERR_CUDA
     assert b"no CPU path" in lib.halos_step_error()
+
+
+def test_writing_over_the_input_with_other_strides_is_refused(lib):
+    """The rows that are written would be others than those that are still to be read."""
+    from paper_2506_04531_b200 import binding, step
+    d = step.DistillArgs()
+    d.struct_size, d.rows, d.vocab, d.temperature, d.mix = C.sizeof(d), 4, 100, 1.0, 0.5
+    d.logits = d.labels = d.loss = d.stats = d.dloss = d.dlogits = 4096
+    d.logits_stride, d.dlogits_stride = 108, 100
+    for call in (lib.halos_distill_fwd_bwd, lib.halos_distill_bwd):
+        assert call(C.byref(d)) == binding.ERR_INVALID_ARG and b"stride" in lib.halos_step_error()
+    for which in "qk":
+        r = step.RopeArgs()
+        r.struct_size, r.dtype, r.batch, r.seq, r.n_q, r.n_k, r.head_dim, r.rot_dim = C.sizeof(r), 1, 1, 2, 2, 2, 64, 16
+        r.freqs, r.q_in, r.k_in, r.q_out, r.k_out = 4096, 8192, 16384, 8192, 16384
+        for n in ("q_in", "k_in", "q_out", "k_out"):
+            getattr(r, n + "_stride")[:] = (256, 128, 64)
+        getattr(r, which + "_out_stride")[:] = (256, 192, 64)
+        assert lib.halos_rope(C.byref(r)) == binding.ERR_INVALID_ARG and b"strides" in lib.halos_step_error()
