@@ -114,7 +114,7 @@ typedef struct halos_attention_args {
 } halos_attention_args;
 int halos_attention_fwd(const halos_attention_args* args);
 int halos_attention_bwd(const halos_attention_args* args);
-/* Bytes of workspace that halos_attention_bwd needs for these sizes (halos_attention_fwd needs none). */
+/* Bytes of workspace that halos_attention_bwd needs for these sizes and this dtype (halos_attention_fwd needs none). */
 int halos_attention_workspace(const halos_attention_args* args, uint64_t* bytes);
 
 /* ------------------------------------------------------------------ distillation loss ----------- */
@@ -126,8 +126,10 @@ int halos_attention_workspace(const halos_attention_args* args, uint64_t* bytes)
  *     dz_j = dloss [ (1 - m) (q1_j - [j = y]) + m T (qT_j - p_j) ]
  * labels NULL: no first term; k = 0 (or no entry there): no second.  A row with label == ignore_index has loss 0 and
  * gradient 0 whatever its logits hold.  Another label, or teacher index, outside the vocabulary makes that row's
- * loss and gradient NaN.  Of two entries with the same index both count.  Logits of -infinity or of the type's lowest value
- * are probability 0 and get the gradient that follows. */
+ * loss and gradient NaN, and a teacher logit that is NaN or +infinity its loss and, at the teacher's entries, its gradient.  Of two
+ * entries with the same index both count.  Logits of -infinity or of the type's lowest value are probability 0 beside others and get the
+ * gradient that follows.  The statistics are one 32-bit number each, so a probability is off by some 2^-23 |lse| of itself, and
+ * a row of nothing but the lowest value of a type with 8 bits of exponent has probability 1 in every place. */
 typedef struct halos_distill_args {
     uint32_t struct_size;
     int32_t device;
@@ -147,7 +149,7 @@ typedef struct halos_distill_args {
     const void* teacher_logits;
     int64_t teacher_index_stride, teacher_logits_stride;
     float* loss;                    /* [rows]; fwd, fwd_bwd */
-    float* stats;                   /* [rows, 2] = log sum exp z, log sum exp z/T; written by fwd, read by bwd */
+    float* stats;                   /* [rows, 2] = log sum exp z, log sum exp z/T; written by fwd (by fwd_bwd if not NULL), read by bwd */
     const float* dloss;             /* [rows]; bwd, fwd_bwd */
     void* dlogits;                  /* may equal logits (same stride); bwd, fwd_bwd */
     int64_t dlogits_stride;

@@ -14,8 +14,8 @@
 //
 // Roles in a CTA: warps of 4 take the rows (thread = tensor memory lane), one warp issues the bulk copies, one the products.
 //
-// Measured, causal, 2048 tokens, bf16: 16 x 12 heads of 64 forward 203 us (510 TFLOP/s of visible pairs), backward 570 us (450);
-// 4 x 16 heads of 128 forward 98 us (700).  Under way, a tile of 64 keys takes 0.76 us in each of an SM's two CTAs, of which the
+// Measured, causal, 2048 tokens, bf16: 16 x 12 heads of 64 forward 196 us (525 TFLOP/s of visible pairs), backward 568 us (454);
+// 4 x 16 heads of 128 forward 97 us (708).  Under way, a tile of 64 keys takes 0.76 us in each of an SM's two CTAs, of which the
 // exponential unit is busy 74%; a quarter of a CTA's time is its beginning and end, which the other CTA only partly
 // fills.  dK, dV: 1.1 us for 64 queries, bound by the products (63%); dQ: 0.76 us for 64 keys.
 //

@@ -5,7 +5,7 @@
 // logit needs exp(z) and exp(z/T), in the statistics and again in the gradient.  Where T is 1, 2 or 4 the
 // first is the second to the power T, which costs multiplications instead (kSquarings).
 //
-// Measured: 8192 x 50304 bf16 logits, 64 entries, T = 2, loss with gradient 365 us (4.5 TB/s, floor 256 us; the exponential
+// Measured: 8192 x 50304 bf16 logits, 64 entries, T = 2, loss with gradient 352 to 365 us (4.7 to 4.5 TB/s, floor 256 us; the exponential
 // unit and the issue slots are both 58% busy); gradient alone of 2048 x 32003 f16, T = 1: 58 us (4.6 TB/s).
 #include "step_tcgen05.cuh"
 
