@@ -8,6 +8,9 @@
  *   halos_attention_fwd/bwd  masked attention; the backward pass recomputes the probabilities
  *   halos_distill_*          cross-entropy mixed with distillation from a teacher's top logits (K pairs per token
  *                            are what a slow link can carry of the global model's opinion), and its gradient
+ *   halos_embedding_fwd/bwd  rows of a table by tokens, scaled; the gradient by sorted tokens
+ *   halos_rms_norm_fwd/bwd   root-mean-square norm with the residual's addition, in 8 bits with scales if asked for; its gradient
+ *   halos_grad_norm, halos_clip_grads, halos_sgd_step      the norm of many gradients at once, clipping by it, and the step
  *
  * Conventions
  *  - No context is needed.  Every call takes one args struct, whose first field is its size (checked), checks it
@@ -16,7 +19,7 @@
  *    borrowed until those kernels have completed in stream order.
  *  - Pointers are device pointers.  Strides are in elements; the innermost dimension is contiguous.
  *  - Nothing is allocated but 256 bytes of host memory in the first call: workspaces are the caller's
- *    (halos_attention_workspace says how much).
+ *    (halos_*_workspace say how much).
  *  - The same inputs give the same bits, call after call: no result depends on the order of atomics.
  *  - Sums, statistics and everything between load and store are held in 32 bits, and results are rounded once, except that attention rounds p
  *    and ds to the inputs' type where they enter matrix products, and forms D from the o that was returned.
@@ -158,6 +161,112 @@ int halos_distill_fwd(const halos_distill_args* args);
 int halos_distill_bwd(const halos_distill_args* args);
 /* Both in one pass over the logits, for a caller that knows dloss beforehand (1 / tokens, a weight per token). */
 int halos_distill_fwd_bwd(const halos_distill_args* args);
+
+/* ------------------------------------------------------------------ embedding ----------- */
+
+/* fwd:  out[t][c] = scale weight[token[t]][c];   bwd:  dweight[v][c] = scale sum of dout[t][c] over the t with token[t] = v, and 0 where there
+ * is none; accumulate: that is added to what dweight holds, and rows that no token names are not touched.
+ * A token outside [0, vocab) gives a row of NaN and takes no part in the gradient.  dtype is that of out and dout, weight_dtype that of weight
+ * and dweight, any pair of the three.  Products and sums are in 32 bits, the sums of a row in a fixed order, and each result is rounded once. */
+typedef struct halos_embedding_args {
+    uint32_t struct_size;
+    int32_t device;
+    void* stream;
+    uint32_t dtype, weight_dtype;
+    uint32_t tokens_64;             /* int64, else int32 */
+    uint32_t accumulate;
+    int64_t tokens, vocab;          /* tokens <= 2^31 - 1, 0 < vocab < 2^31 - 1 */
+    uint32_t dim;                   /* > 0 */
+    float scale;
+    const void* token;              /* [tokens] */
+    const void* weight;             /* [vocab, dim]; fwd */
+    int64_t weight_stride;          /* between rows, here and below */
+    void* out;                      /* [tokens, dim]; fwd */
+    int64_t out_stride;
+    const void* dout;               /* [tokens, dim]; bwd, from here on */
+    int64_t dout_stride;
+    void* dweight;                  /* [vocab, dim] */
+    int64_t dweight_stride;
+    void* workspace;                /* 16-byte aligned, halos_embedding_workspace bytes */
+    uint64_t workspace_bytes;
+} halos_embedding_args;
+int halos_embedding_fwd(const halos_embedding_args* args);
+int halos_embedding_bwd(const halos_embedding_args* args);
+/* Bytes of workspace that halos_embedding_bwd needs for these sizes (halos_embedding_fwd needs none). */
+int halos_embedding_workspace(const halos_embedding_args* args, uint64_t* bytes);
+
+/* ------------------------------------------------------------------ root-mean-square norm ----------- */
+
+/* For every row of dim elements, with s = x + residual (x, without one) in 32 bits:
+ *     rstd = 1 / sqrt(mean of s^2 + eps);  y = s rstd weight;  summed = s, rounded to dtype (written if there is a residual).
+ * quantized: y is written in 8 bits (4 of exponent, 3 of mantissa, largest 448) as the nearest to y / scale, and scales has for every `group`
+ * neighbouring elements of a row (the last of a row may be fewer; group = 0: the whole row)  scale = max(max |y| / 448, 2^-126).
+ * Rows of any size, those whose squares 32 bits do not hold included, give what the formula does: 1 / 0 is infinity, a NaN makes its row NaN, an
+ * infinity its own place and the rest 0.
+ * bwd, from s as it was rounded (x, without a residual), rstd, dy and dsummed (the gradient of summed, or NULL), with u = s rstd and g = dy weight:
+ *     dx = rstd (g - u mean of g u) + dsummed,  which is the gradient of x and of residual;   dweight = sum over rows of dy u.
+ * The sums of dweight are in 32 bits and a fixed order, and each result is rounded once.
+ * Rows are those of three outer sizes (1 where there are fewer) with strides of their own; the elements of a row lie side by side. */
+typedef struct halos_rms_norm_args {
+    uint32_t struct_size;
+    int32_t device;
+    void* stream;
+    uint32_t dtype, weight_dtype;   /* of weight and dweight */
+    uint32_t quantized;
+    uint32_t group;                 /* 0, 32, 64 or 128; quantized */
+    int64_t size[3];                /* product <= 2^31 - 1 */
+    uint32_t dim;                   /* 0 < dim < 2^30 */
+    float eps;                      /* >= 0, finite */
+    const void* x;                  /* fwd */
+    const void* residual;           /* fwd, or NULL */
+    void* summed;                   /* written by fwd if there is a residual, read by bwd */
+    void* y;                        /* fwd */
+    float* scales;                  /* [rows, groups of a row] contiguous; fwd, quantized */
+    float* rstd;                    /* [rows] contiguous; written by fwd, read by bwd */
+    const void* weight;             /* [dim] */
+    const void* dy;                 /* bwd, from here on */
+    const void* dsummed;            /* or NULL */
+    void* dx;
+    void* dweight;                  /* [dim] */
+    void* workspace;                /* 16-byte aligned, halos_rms_norm_workspace bytes */
+    uint64_t workspace_bytes;
+    int64_t x_stride[3], residual_stride[3], summed_stride[3], y_stride[3], dy_stride[3], dsummed_stride[3], dx_stride[3];
+} halos_rms_norm_args;
+int halos_rms_norm_fwd(const halos_rms_norm_args* args);
+int halos_rms_norm_bwd(const halos_rms_norm_args* args);
+/* Bytes of workspace that halos_rms_norm_bwd needs for these sizes (halos_rms_norm_fwd needs none). */
+int halos_rms_norm_workspace(const halos_rms_norm_args* args, uint64_t* bytes);
+
+/* ------------------------------------------------------------------ gradients ----------- */
+
+/* n = sqrt(sum of the squares of every element of every gradient), f = n > max_norm ? max_norm / n : 1  (n, f in 64 bits; a NaN n has f = 1)
+ *     halos_grad_norm    *norm = n
+ *     halos_clip_grads   *norm = n;  out_i = f grad_i;  out_i may be grad_i
+ *     halos_sgd_step     out_i = out_i - rate f grad_i;  *norm = n where norm is not NULL.  norm NULL: no norm is formed, f = 1
+ * Each element is rounded once, to its type.  Squares are added up in groups of eight in 32 bits where that holds them, else and from there on in
+ * 64 bits, in a fixed order.  In place and with f = 1 nothing is written.  Tensors are dense runs of numel elements of any type each; those that
+ * are written may overlap neither one another nor another gradient.  The arrays are read before the call returns. */
+typedef struct halos_grads_args {
+    uint32_t struct_size;
+    int32_t device;
+    void* stream;
+    uint64_t count;
+    const void* const* grads;       /* [count] device pointers, in host memory as the other arrays */
+    void* const* outs;              /* [count]; clip, step */
+    const int64_t* numel;           /* [count] */
+    const uint8_t* grad_dtypes;     /* [count] */
+    const uint8_t* out_dtypes;      /* [count]; clip, step */
+    float max_norm;                 /* >= 0; clip, and step with a norm */
+    float rate;                     /* finite; step */
+    float* norm;                    /* device */
+    void* workspace;                /* 16-byte aligned, halos_grads_workspace bytes; none is needed without a norm */
+    uint64_t workspace_bytes;
+} halos_grads_args;
+int halos_grad_norm(const halos_grads_args* args);
+int halos_clip_grads(const halos_grads_args* args);
+int halos_sgd_step(const halos_grads_args* args);
+/* Bytes of workspace for `count` tensors on this device. */
+int halos_grads_workspace(const halos_grads_args* args, uint64_t* bytes);
 
 #ifdef __cplusplus
 }

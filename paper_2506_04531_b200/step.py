@@ -3,6 +3,9 @@
     rope, rotary                      rotary positions (rotary: with autograd)
     attention_forward, _backward      masked attention and its gradients; attention: with autograd
     distill_forward, _backward, distill_loss_and_grad      the loss against labels and a teacher's top logits; distill_loss: with autograd
+    embedding_forward, _backward      rows of a table by tokens, scaled, and the table's gradient; embedding: with autograd
+    rms_norm_forward, _quantized, _backward      root-mean-square norm with the residual's addition; rms_norm: with autograd
+    grad_norm, clip_grads, sgd_step   the norm of many gradients at once, clipping by it, and a step of plain descent
 
 As in ``binding``, the arithmetic is the CUDA library's; what happens here is checking, marshalling and output
 allocation, on the current stream of the tensors' device.  The caller's current device stays what it was.  There is no CPU path.
@@ -26,7 +29,9 @@ _LAYOUTS = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 EXPORTED = ("halos_step_error", "halos_step_fault", "halos_rope", "halos_attention_fwd", "halos_attention_bwd",
-            "halos_attention_workspace", "halos_distill_fwd", "halos_distill_bwd", "halos_distill_fwd_bwd")
+            "halos_attention_workspace", "halos_distill_fwd", "halos_distill_bwd", "halos_distill_fwd_bwd",
+            "halos_embedding_fwd", "halos_embedding_bwd", "halos_embedding_workspace", "halos_rms_norm_fwd", "halos_rms_norm_bwd",
+            "halos_rms_norm_workspace", "halos_grad_norm", "halos_clip_grads", "halos_sgd_step", "halos_grads_workspace")
 
 _u32, _i32, _i64, _u64, _vp, _f32 = C.c_uint32, C.c_int32, C.c_int64, C.c_uint64, C.c_void_p, C.c_float
 _stride3 = _i64 * 3
@@ -56,6 +61,26 @@ class DistillArgs(C.Structure):
                 ("dloss", _vp), ("dlogits", _vp), ("dlogits_stride", _i64)]
 
 
+class EmbeddingArgs(C.Structure):
+    _fields_ = [("struct_size", _u32), ("device", _i32), ("stream", _vp), ("dtype", _u32), ("weight_dtype", _u32), ("tokens_64", _u32),
+                ("accumulate", _u32), ("tokens", _i64), ("vocab", _i64), ("dim", _u32), ("scale", _f32), ("token", _vp), ("weight", _vp),
+                ("weight_stride", _i64), ("out", _vp), ("out_stride", _i64), ("dout", _vp), ("dout_stride", _i64), ("dweight", _vp),
+                ("dweight_stride", _i64), ("workspace", _vp), ("workspace_bytes", _u64)]
+
+
+class RmsNormArgs(C.Structure):
+    _fields_ = [("struct_size", _u32), ("device", _i32), ("stream", _vp), ("dtype", _u32), ("weight_dtype", _u32), ("quantized", _u32),
+                ("group", _u32), ("size", _stride3), ("dim", _u32), ("eps", _f32), ("x", _vp), ("residual", _vp), ("summed", _vp), ("y", _vp),
+                ("scales", _vp), ("rstd", _vp), ("weight", _vp), ("dy", _vp), ("dsummed", _vp), ("dx", _vp), ("dweight", _vp),
+                ("workspace", _vp), ("workspace_bytes", _u64)] + \
+               [(n + "_stride", _stride3) for n in ("x", "residual", "summed", "y", "dy", "dsummed", "dx")]
+
+
+class GradsArgs(C.Structure):
+    _fields_ = [("struct_size", _u32), ("device", _i32), ("stream", _vp), ("count", _u64), ("grads", _vp), ("outs", _vp), ("numel", _vp),
+                ("grad_dtypes", _vp), ("out_dtypes", _vp), ("max_norm", _f32), ("rate", _f32), ("norm", _vp), ("workspace", _vp),
+                ("workspace_bytes", _u64)]
+
 
 def _packer(kind):
     """A struct's fields as one ``struct.Struct``: small calls are bound by what happens here, and packing all values at once costs a third of
@@ -74,6 +99,7 @@ def _pack(kind, *values) -> bytes:
 
 
 _ROPE, _ATTENTION, _DISTILL = _packer(RopeArgs), _packer(AttentionArgs), _packer(DistillArgs)
+_EMBEDDING, _RMS_NORM, _GRADS = _packer(EmbeddingArgs), _packer(RmsNormArgs), _packer(GradsArgs)
 # The stream's handle is asked for without building a stream object around it.
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _current_device, _set_device = torch._C._cuda_getDevice, torch._C._cuda_setDevice
@@ -89,7 +115,7 @@ class _Once(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *grads):
-        raise HalosError(ERR_UNSUPPORTED, "attention and the distillation loss have no second derivative")
+        raise HalosError(ERR_UNSUPPORTED, "attention, the distillation loss and norms have no second derivative")
 
 
 def _library():
@@ -98,9 +124,11 @@ def _library():
         lib = load_library()
         lib.halos_step_error.restype = C.c_char_p
         lib.halos_step_fault.argtypes = [_i32, C.POINTER(_i32)]
-        for name in ("rope", "attention_fwd", "attention_bwd", "distill_fwd", "distill_bwd", "distill_fwd_bwd"):
+        for name in ("rope", "attention_fwd", "attention_bwd", "distill_fwd", "distill_bwd", "distill_fwd_bwd", "embedding_fwd", "embedding_bwd",
+                     "rms_norm_fwd", "rms_norm_bwd", "grad_norm", "clip_grads", "sgd_step"):
             getattr(lib, "halos_" + name).argtypes = [_vp]
-        lib.halos_attention_workspace.argtypes = [_vp, C.POINTER(_u64)]
+        for name in ("attention", "embedding", "rms_norm", "grads"):
+            getattr(lib, f"halos_{name}_workspace").argtypes = [_vp, C.POINTER(_u64)]
         _lib = lib
     return _lib
 
@@ -132,6 +160,18 @@ def _on(x, device, what: str):
         _refuse(f"{what} is not a CUDA tensor (there is no CPU path)")
     if x.device != device:
         _refuse(f"{what} is on {x.device}, not on {device}")
+
+
+def _workspace(name: str, args: bytes, device: int) -> int:
+    """Bytes of workspace; the C calls leave their device current, here the caller's stays."""
+    lib = _lib or _library()
+    size, before = _u64(0), _current_device()
+    rc = getattr(lib, name)(args, C.byref(size))
+    if before != device:
+        _set_device(before)
+    if rc:
+        raise HalosError(rc, lib.halos_step_error().decode())
+    return size.value
 
 
 def _overwritten(x, what: str):
@@ -482,3 +522,301 @@ class _Distill(torch.autograd.Function):
 def distill_loss(logits, labels, teacher_idx=None, teacher_logits=None, *, temperature: float = 1.0, mix: float = 0.5, ignore_index: int = -100):
     """``distill_forward``'s loss, with autograd for the logits (of first order: a derivative of the gradient is refused)."""
     return _Distill.apply(logits, labels, teacher_idx, teacher_logits, temperature, mix, ignore_index)
+
+
+# ------------------------------------------------------------------------------------------ embedding
+
+def _as_rows(x, dim: int):
+    """x, or a copy of it, as a matrix of rows whose elements lie side by side."""
+    if x.dim() != 2:
+        x = x.reshape(-1, dim)
+    return x if x.stride(1) == 1 or dim == 1 else x.contiguous()
+
+
+def _tokens_checked(tokens, device):
+    _on(tokens, device, "tokens")
+    wide = tokens.dtype == torch.int64
+    if not wide and tokens.dtype != torch.int32:
+        _refuse("tokens must be int32 or int64")
+    return tokens if tokens.is_contiguous() else tokens.contiguous(), wide
+
+
+def embedding_forward(weight, tokens, *, scale: float = 1.0, dtype=None):
+    """scale times the rows of weight [vocab, dim] (any distance apart) that tokens (int32 or int64, any shape) name, as [*tokens.shape, dim] of
+    dtype (float32, bfloat16 or float16; weight's unless given).  A token outside the vocabulary gives a row of NaN."""
+    if weight.dim() != 2:
+        _refuse("weight must be [vocab, dim]")
+    device = weight.device
+    _on(weight, device, "weight")
+    vocab, dim = weight.shape
+    if weight.stride(1) != 1 and dim > 1:
+        _refuse("weight: a row's elements must lie side by side")
+    tokens, wide = _tokens_checked(tokens, device)
+    out = torch.empty((*tokens.shape, dim), dtype=dtype or weight.dtype, device=device)
+    _call("halos_embedding_fwd", _pack(
+        _EMBEDDING, _EMBEDDING.size, device.index, _raw_stream(device.index), _dtype(out, "dtype"), _dtype(weight, "weight"), wide, 0, tokens.numel(), vocab, dim, scale,
+        tokens.data_ptr(), weight.data_ptr(), weight.stride(0), out.data_ptr(), dim, 0, 0, 0, 0, 0, 0), device.index)
+    return out
+
+
+def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False):
+    """The gradient [vocab, dim] of the table from that of the rows, dout [*tokens.shape, dim]: for every token scale times the sum of dout where it
+    stands, in a fixed order, 0 where it does not.  Of dtype (dout's unless given), or written to out (rows any distance apart, detached if it is in a graph);
+    accumulate: added to what out holds, whose other rows are not touched.  Tokens outside the vocabulary take no part."""
+    device = dout.device
+    _on(dout, device, "dout")
+    if dout.dim() < 1 or dout.shape[:-1] != tokens.shape:
+        _refuse("dout must be [*tokens.shape, dim]")
+    tokens, wide = _tokens_checked(tokens, device)
+    dim = dout.size(-1)
+    rows = _as_rows(dout, dim) if dim else dout
+    if out is None:
+        if accumulate:
+            _refuse("accumulate needs out")
+        out = torch.empty((vocab, dim), dtype=dtype or dout.dtype, device=device)
+    else:
+        _on(out, device, "out")
+        if out.shape != (vocab, dim) or (dtype is not None and out.dtype != dtype) or (out.stride(1) != 1 and dim > 1) or (vocab > 1 and out.stride(0) < dim):
+            _refuse("out must be [vocab, dim] of dtype, a row's elements side by side and rows apart")
+        _overwritten(out, "out")
+    index = device.index
+    head = (_EMBEDDING.size, index, _raw_stream(index), _dtype(dout, "dout"), _dtype(out, "dtype"), wide, bool(accumulate), tokens.numel(), vocab, dim, scale,
+            tokens.data_ptr(), 0, 0, 0, 0, rows.data_ptr(), rows.stride(0), out.data_ptr(), out.stride(0))
+    size = _workspace("halos_embedding_workspace", _pack(_EMBEDDING, *head, 0, 0), index)
+    space = torch.empty(size, dtype=torch.uint8, device=device)
+    _call("halos_embedding_bwd", _pack(_EMBEDDING, *head, space.data_ptr(), size), index)
+    return out
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, weight, tokens, scale, dtype):
+        ctx.save_for_backward(tokens)
+        ctx.how = (weight.size(0), scale, weight.dtype)
+        return embedding_forward(weight, tokens, scale=scale, dtype=dtype)
+
+    @staticmethod
+    def backward(ctx, dout):
+        return _EmbeddingBack.apply(dout, *ctx.saved_tensors, *ctx.how), None, None, None
+
+
+class _EmbeddingBack(torch.autograd.Function):
+    """Linear, as the embedding is: differentiable as often as one likes."""
+    @staticmethod
+    def forward(ctx, dout, tokens, vocab, scale, dtype):
+        ctx.save_for_backward(tokens)
+        ctx.how = (scale, dout.dtype)
+        return embedding_backward(dout, tokens, vocab, scale=scale, dtype=dtype)
+
+    @staticmethod
+    def backward(ctx, dweight):
+        return _Embedding.apply(dweight if dweight.stride(1) == 1 else dweight.contiguous(), *ctx.saved_tensors, *ctx.how), None, None, None, None
+
+
+def embedding(weight, tokens, *, scale: float = 1.0, dtype=None):
+    """``embedding_forward`` with autograd; the gradient is of weight's type."""
+    return _Embedding.apply(weight, tokens, scale, dtype)
+
+
+# ------------------------------------------------------------------------------------------ root-mean-square norm
+
+def _outer(x, shape):
+    """x [*shape, dim], or a copy of it, with three outer sizes, and their strides."""
+    if x.stride(-1) != 1 and x.size(-1) > 1:
+        x = x.contiguous()
+    n = len(shape)
+    if n > 3:
+        x = x.reshape(-1, x.size(-1))
+        n = 1
+    return x, (0,) * (3 - n) + x.stride()[:-1]
+
+
+def _sizes(shape):
+    return (1,) * (3 - len(shape)) + tuple(shape) if len(shape) <= 3 else (1, 1, math.prod(shape))
+
+
+def _norm_weight(weight, x):
+    if x.dim() < 1:
+        _refuse("rows must have a last dimension")
+    _on(weight, x.device, "weight")
+    if weight.shape != x.shape[-1:] or not weight.is_contiguous():
+        _refuse("weight must be a contiguous vector as long as a row")
+    return _dtype(weight, "weight")
+
+
+def _like(a, b, what: str):
+    _on(a, b.device, what)
+    if a.shape != b.shape or a.dtype != b.dtype:
+        _refuse(f"{what} must be of the same shape and type")
+
+
+def _rms_norm(x, weight, residual, eps, quantized, group):
+    device, shape, dim = x.device, x.shape[:-1], x.shape[-1] if x.dim() else 0
+    _on(x, device, "x")
+    kind, weight_kind = _dtype(x, "x"), _norm_weight(weight, x)
+    x3, x_stride = _outer(x, shape)
+    none, summed, r3, r_stride, s_stride = (0, 0, 0), x, None, (0, 0, 0), (0, 0, 0)
+    if residual is not None:
+        _like(residual, x, "residual")
+        r3, r_stride = _outer(residual, shape)
+        summed = torch.empty(x.shape, dtype=x.dtype, device=device)
+        s_stride = _outer(summed, shape)[1]
+    y = torch.empty(x.shape, dtype=torch.float8_e4m3fn if quantized else x.dtype, device=device)
+    y_stride = _outer(y, shape)[1]
+    rstd = torch.empty(shape, dtype=torch.float32, device=device)
+    scales = torch.empty((*shape, -(-dim // (group or dim or 1))), dtype=torch.float32, device=device) if quantized else None
+    _call("halos_rms_norm_fwd", _pack(
+        _RMS_NORM, _RMS_NORM.size, device.index, _raw_stream(device.index), kind, weight_kind, quantized, group, *_sizes(shape), dim, eps, x3.data_ptr(),
+        0 if r3 is None else r3.data_ptr(), 0 if r3 is None else summed.data_ptr(), y.data_ptr(), 0 if scales is None else scales.data_ptr(), rstd.data_ptr(),
+        weight.data_ptr(), 0, 0, 0, 0, 0, 0, *x_stride, *r_stride, *s_stride, *y_stride, *none, *none, *none), device.index)
+    return y, scales, summed, rstd
+
+
+def rms_norm_forward(x, weight, *, residual=None, eps: float = 1e-5):
+    """(y, summed, rstd) of the rows of x [..., dim] (float32, bfloat16 or float16; any strides that keep a row's elements side by side): with s = x +
+    residual in 32 bits, rstd = 1 / sqrt(mean of s^2 + eps) in float32 [...], y = s rstd weight, and summed = s rounded to x's type (x itself without
+    a residual), which the next residual is.  weight [dim] may be of another type."""
+    y, _, summed, rstd = _rms_norm(x, weight, residual, eps, False, 0)
+    return y, summed, rstd
+
+
+def rms_norm_quantized(x, weight, *, residual=None, eps: float = 1e-5, group: int = 0):
+    """(q, scales, summed, rstd): ``rms_norm_forward`` with y in 8 bits (float8_e4m3fn), q scales being nearest to y.  scales [..., n] in float32 has one value for
+    every group (32, 64 or 128) of a row's elements, or one for the row (0): the largest of them over 448."""
+    return _rms_norm(x, weight, residual, eps, True, group)
+
+
+def rms_norm_backward(dy, summed, weight, rstd, *, dsummed=None):
+    """(dx, dweight) from the gradient of y, what the forward pass returned, and the gradient of summed.  dx is the gradient of x and of the
+    residual; dweight is of weight's type.  Deterministic."""
+    device, shape, dim = dy.device, dy.shape[:-1], dy.shape[-1] if dy.dim() else 0
+    _on(dy, device, "dy")
+    kind, weight_kind = _dtype(dy, "dy"), _norm_weight(weight, dy)
+    _like(summed, dy, "summed")
+    _on(rstd, device, "rstd")
+    if rstd.dtype != torch.float32 or rstd.shape != shape or not rstd.is_contiguous():
+        _refuse("rstd must be contiguous float32 [...]")
+    dy3, dy_stride = _outer(dy, shape)
+    s3, s_stride = _outer(summed, shape)
+    d3, d_stride, none = None, (0, 0, 0), (0, 0, 0)
+    if dsummed is not None:
+        _like(dsummed, dy, "dsummed")
+        d3, d_stride = _outer(dsummed, shape)
+    dx, dweight = torch.empty(dy.shape, dtype=dy.dtype, device=device), torch.empty_like(weight)
+    dx_stride, index = _outer(dx, shape)[1], device.index
+    head = (_RMS_NORM.size, index, _raw_stream(index), kind, weight_kind, 0, 0, *_sizes(shape), dim, 0.0, 0, 0, s3.data_ptr(), 0, 0, rstd.data_ptr(), weight.data_ptr(),
+            dy3.data_ptr(), 0 if d3 is None else d3.data_ptr(), dx.data_ptr(), dweight.data_ptr())
+    strides = (*none, *none, *s_stride, *none, *dy_stride, *d_stride, *dx_stride)
+    size = _workspace("halos_rms_norm_workspace", _pack(_RMS_NORM, *head, 0, 0, *strides), index)
+    space = torch.empty(size, dtype=torch.uint8, device=device)
+    _call("halos_rms_norm_bwd", _pack(_RMS_NORM, *head, space.data_ptr(), size, *strides), index)
+    return dx, dweight
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        y, summed, rstd = rms_norm_forward(x, weight, residual=residual, eps=eps)
+        ctx.save_for_backward(summed, weight, rstd)
+        ctx.added = residual is not None
+        ctx.set_materialize_grads(False)
+        return (y, summed) if ctx.added else y
+
+    @staticmethod
+    def backward(ctx, dy, dsummed=None):
+        if dy is None:                   # nobody used the norm: the sum's gradient goes through
+            return dsummed, None, dsummed if ctx.added else None, None
+        form = lambda dy, summed, weight, rstd, dsummed: rms_norm_backward(dy, summed, weight, rstd, dsummed=dsummed)  # noqa: E731
+        inputs = (dy, *ctx.saved_tensors, dsummed)
+        dx, dweight = _Once.apply(form, *inputs) if torch.is_grad_enabled() else form(*inputs)
+        return dx, dweight, dx if ctx.added else None, None
+
+
+def rms_norm(x, weight, *, residual=None, eps: float = 1e-5):
+    """``rms_norm_forward``'s y, or (y, summed) with a residual, with autograd (of first order: a derivative of the gradients is refused)."""
+    return _RmsNorm.apply(x, weight, residual, eps)
+
+
+# ------------------------------------------------------------------------------------------ gradients
+
+def _dense(x) -> bool:
+    """Whether x's elements fill a run of memory, in whatever order."""
+    return x.is_contiguous() or x.permute(sorted(range(x.dim()), key=lambda i: (x.stride(i), x.size(i)), reverse=True)).is_contiguous()
+
+
+def _listed(tensors, what: str):
+    tensors = list(tensors)
+    if not tensors or not all(isinstance(x, torch.Tensor) for x in tensors):
+        _refuse(f"{what} must be one tensor or more")
+    return tensors
+
+
+def _grads_call(name: str, grads, outs, max_norm: float, rate: float, norm):
+    device = grads[0].device
+    both = grads if outs is None else grads + outs
+    for x in both:
+        if x.device != device or not x.is_cuda:
+            _on(x, device, "a tensor")
+    kinds = [_DTYPES.get(x.dtype) for x in both]
+    if None in kinds:
+        _dtype(both[kinds.index(None)], "a tensor")
+    if outs is None:
+        grads = [x if _dense(x) else x.contiguous() for x in grads]
+    else:
+        for x in outs:
+            if not _dense(x):
+                _refuse("a tensor that is written must fill a run of memory")
+        # elements side by side in the one are to be so in the other
+        grads = [g if (g.is_contiguous() and o.is_contiguous()) or (g.stride() == o.stride() and g.shape == o.shape) else torch.empty_like(o, dtype=g.dtype).copy_(g) for g, o in zip(grads, outs)]
+        for x in outs:
+            _overwritten(x, "a tensor that is written")
+    n, index = len(grads), device.index
+    at = lambda values: (C.c_uint64 * n)(*values)  # noqa: E731
+    g_at, sizes, g_kinds = at([x.data_ptr() for x in grads]), at([x.numel() for x in grads]), bytes(kinds[:n])
+    o_at, o_kinds = (None, None) if outs is None else (at([x.data_ptr() for x in outs]), bytes(kinds[n:]))
+    head = (_GRADS.size, index, _raw_stream(index), n, C.addressof(g_at), 0 if o_at is None else C.addressof(o_at), C.addressof(sizes), _address(g_kinds), 0 if o_at is None else _address(o_kinds),
+            max_norm, rate, 0 if norm is None else norm.data_ptr())
+    if norm is None:
+        space, size = None, 0
+    else:
+        size = _workspace("halos_grads_workspace", _pack(_GRADS, *head, 0, 0), index)
+        space = torch.empty(size, dtype=torch.uint8, device=device)
+    _call(name, _pack(_GRADS, *head, 0 if space is None else space.data_ptr(), size), index)
+    return norm
+
+
+def _address(data: bytes) -> int:
+    return C.cast(C.c_char_p(data), _vp).value
+
+
+def _scalar(grads):
+    return torch.empty((), dtype=torch.float32, device=grads[0].device)
+
+
+def grad_norm(grads):
+    """The root of the sum of the squares of every element of `grads` (tensors of float32, bfloat16 and float16, any strides), a float32 scalar on their
+    device.  Formed so that neither large nor small gradients leave what 32 bits hold on the way, in a fixed order."""
+    grads = _listed(grads, "grads")
+    return _grads_call("halos_grad_norm", grads, None, 0.0, 0.0, _scalar(grads))
+
+
+def clip_grads(grads, max_norm: float, *, out=None):
+    """``grad_norm``, and where it is above max_norm the gradients times max_norm / norm: in place, or to the tensors of out (one for each, of the same
+    sizes and any of the types).  A norm that is NaN leaves them as they are."""
+    grads = _listed(grads, "grads")
+    outs = grads if out is None else _paired(_listed(out, "out"), grads)
+    return _grads_call("halos_clip_grads", grads, outs, max_norm, 0.0, _scalar(grads))
+
+
+def sgd_step(params, grads, rate: float, *, max_norm: Optional[float] = None):
+    """params -= rate grads, the gradients clipped to max_norm as by ``clip_grads`` if it is given (they themselves stay as they are).  Returns their norm, or
+    None without max_norm.  The parameters may be of other types than the gradients, and detached if they are in a graph."""
+    grads = _listed(grads, "grads")
+    params = _paired(_listed(params, "params"), grads)
+    return _grads_call("halos_sgd_step", grads, params, 0.0 if max_norm is None else max_norm, rate, None if max_norm is None else _scalar(grads))
+
+
+def _paired(tensors, grads):
+    if len(tensors) != len(grads) or any(x.shape != g.shape for x, g in zip(tensors, grads)):
+        _refuse("there must be one tensor for each gradient, of its shape")
+    return tensors
