@@ -23,8 +23,8 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 TARGETS = {
     "halos": dict(out=PKG / "libhalos_b200.so",
                   src=[PKG / "csrc" / f for f in ("halos.cu", "halos_noalloc.cu", "step_common.cu", "step_rope.cu", "step_attention.cu",
-                                                  "step_distill.cu", "step_embedding.cu", "step_norm.cu", "step_grads.cu")],
-                  deps=[PKG / "csrc" / "halos_kernels.cuh", PKG / "csrc" / "step_common.cuh", PKG / "csrc" / "step_tcgen05.cuh", PKG / "csrc" / "step_vector.cuh",
+                                                  "step_distill.cu", "step_embedding.cu", "step_norm.cu", "step_norm_back.cu", "step_grads.cu")],
+                  deps=[PKG / "csrc" / "halos_kernels.cuh", PKG / "csrc" / "step_common.cuh", PKG / "csrc" / "step_tcgen05.cuh", PKG / "csrc" / "step_vector.cuh", PKG / "csrc" / "step_norm.cuh",
                         INCLUDE / "halos.h", INCLUDE / "halos_step.h"]),
     "inputs": dict(out=PKG / "inputs" / "libhalos_inputs.so", src=[PKG / "inputs" / "csrc" / "synth_inputs.cu"],
                    deps=[]),

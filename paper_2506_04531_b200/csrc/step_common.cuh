@@ -36,6 +36,18 @@ int allow_smem(K* kernel, int bytes, Allowed& allowed) {
     return HALOS_OK;
 }
 
+// A kernel that may be started while the one before it in the stream still runs, and what it does before it touches what that one leaves: nothing
+// of this waits for anything but that kernel's end.
+template <typename... P, typename... A>
+int launch_after(void (*kernel)(P...), dim3 grid, uint32_t threads, size_t shared, cudaStream_t st, const char* where, const A&... args) {
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization, early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid, config.blockDim = dim3(threads), config.dynamicSmemBytes = shared, config.stream = st, config.attrs = &early, config.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&config, kernel, args...), where);
+}
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ void say_fault(int* mark) { *const_cast<volatile int*>(mark) = 1; }
 
 inline bool is_type(uint32_t t) { return t == HALOS_F32 || t == HALOS_BF16 || t == HALOS_F16; }

@@ -92,6 +92,26 @@ __device__ __forceinline__ Words<T, N> narrow(const float (&v)[N]) {
     return r;
 }
 
+// The same by pairs, for operations on two 32-bit floats at once.
+template <typename T, int N>
+__device__ __forceinline__ void widen(const Words<T, N>& r, float2 (&v)[N / 2]) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        if constexpr (sizeof(T) == 4) v[i] = make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
+        else v[i] = unpack2<T>(r.w[i]);
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ Words<T, N> narrow(const float2 (&v)[N / 2]) {
+    Words<T, N> r;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        if constexpr (sizeof(T) == 4) r.w[2 * i] = __float_as_uint(v[i].x), r.w[2 * i + 1] = __float_as_uint(v[i].y);
+        else r.w[i] = pack2<T>(v[i].x, v[i].y);
+    }
+    return r;
+}
+
 inline uint32_t size_of(uint32_t type) { return type == HALOS_F32 ? 4 : 2; }
 
 }  // namespace halos_step
