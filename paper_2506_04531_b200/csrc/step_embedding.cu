@@ -6,6 +6,7 @@
 // token, however frequent, waits for one warp.
 #include "step_vector.cuh"
 
+#include <atomic>
 #include <math.h>
 #include <type_traits>
 
@@ -13,7 +14,6 @@ namespace halos_step {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 32;             // sorted places to a warp
 constexpr int kMostBits = 9;           // of a radix pass
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 
@@ -26,8 +26,10 @@ struct EmbedParams {
     uint32_t *key[2], *place[2];       // [tokens] each: sorted so far, and where they stood
     uint32_t *counts;                  // [bins, sort blocks]
     uint32_t *met;                     // a bit for each token of the vocabulary
-    float *head, *tail;                // [chunks, dim]: sums of places that go on from the chunk before, or into the next
-    uint32_t chunks, sort_blocks, span;
+    float *head, *tail;                // [CTAs, dim]: sums of places that go on from the CTA before, or into the next
+    uint32_t *arrived;                 // [CTAs, slabs]: how many have left their part of what begins in this one
+    uint32_t chunk, slabs, jobs;       // places to a warp; runs of 256 columns; CTAs times slabs
+    uint32_t sort_blocks, span;
 };
 
 // The token at place t; vocab where it is none.
@@ -36,14 +38,37 @@ __device__ __forceinline__ uint32_t token_at(const EmbedParams& P, uint32_t t) {
     return v < 0 || v >= (int64_t)P.vocab ? P.vocab : (uint32_t)v;
 }
 
-template <typename A, typename W>
+constexpr int kSlab = 256, kWarps = kThreads / 32;             // columns of a warp, eight to a lane
+
+// A warp takes `AT_ONCE` tokens and 256 columns, with all loads under way before the first of them is used.
+template <typename A, typename W, int V, int AT_ONCE>
 __global__ void __launch_bounds__(kThreads) embedding_kernel(const __grid_constant__ EmbedParams P) {
-    const uint32_t t = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-    if (t >= P.tokens) return;
-    const uint32_t v = token_at(P, t);
-    A* out = reinterpret_cast<A*>(P.out) + t * P.out_stride;
-    const W* row = reinterpret_cast<const W*>(P.weight) + v * P.weight_stride;
-    for (uint32_t c = threadIdx.x % 32; c < P.dim; c += 32) out[c] = from_f32<A>(v == P.vocab ? NAN : P.scale * to_f32<W>(row[c]));
+    constexpr int J = kSlab / 32 / V;
+    const uint32_t slab = blockIdx.x % P.slabs, first = (blockIdx.x / P.slabs * kWarps + threadIdx.x / 32) * AT_ONCE, lane = threadIdx.x % 32;
+    if (first >= P.tokens) return;
+    const auto column = [&](int j) { return slab * kSlab + (j * 32 + lane) * V; };
+    uint32_t token[AT_ONCE];
+    Words<W, V> w[AT_ONCE][J];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) token[i] = first + i < P.tokens ? token_at(P, first + i) : P.vocab;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            w[i][j] = token[i] < P.vocab && column(j) < P.dim ? load_words<W, V>(reinterpret_cast<const W*>(P.weight) + token[i] * P.weight_stride + column(j)) : no_words<W, V>();
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+        if (first + i >= P.tokens) break;
+        A* out = reinterpret_cast<A*>(P.out) + (first + i) * P.out_stride;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            float v[V];
+            widen<W, V>(w[i][j], v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = token[i] < P.vocab ? P.scale * v[e] : NAN;
+            if (column(j) < P.dim) store_words<A, V>(out + column(j), narrow<A, V>(v));
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ sort
@@ -114,11 +139,154 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const __g
     }
 }
 
+// ------------------------------------------------------------------------------------------------ sort of up to 65536 places
+
+// One cluster of CTAs sorts in its shared memory, a pass to a digit: threads rank their places within their warp, CTAs scan their warps' counts and exchange totals
+// through the cluster, and places move to where they belong.  All other CTAs of the launch meanwhile write zeros to the rows that no token names, which
+// they find out by going through the tokens themselves: the sort leaves the memory idle, and needs no other kernel's result.
+constexpr int kMostInCluster = 8, kMostItems = 8;
+constexpr uint32_t kMostClustered = kMostInCluster * kMostItems * kSortThreads;
+constexpr uint32_t kMetWords = 4096;                         // of the vocabulary that a CTA looks at at a time
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_meet() { asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t address_in(const void* shared, uint32_t rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(shared)), "r"(rank));
+    return a;
+}
+
+// Writes zeros to a row wherever it begins.
+template <typename W>
+__device__ __forceinline__ void clear_row(W* row, uint32_t dim, uint32_t lane, uint32_t lanes) {
+    constexpr uint32_t kPer = 16 / sizeof(W);
+    const uint32_t head = min(dim, (uint32_t)((16 - (uintptr_t)row % 16) % 16 / sizeof(W))), whole = (dim - head) / kPer, rest = head + whole * kPer;
+    for (uint32_t c = lane; c < head; c += lanes) row[c] = from_f32<W>(0.f);
+    for (uint32_t v = lane; v < whole; v += lanes) reinterpret_cast<uint4*>(row + head)[v] = make_uint4(0, 0, 0, 0);
+    for (uint32_t c = rest + lane; c < dim; c += lanes) row[c] = from_f32<W>(0.f);
+}
+
+template <typename W>
+__device__ __forceinline__ void clear_rows_not_met(const EmbedParams& P, uint32_t mine, uint32_t many, uint32_t* s_met) {
+    const uint32_t words = (P.vocab + 31) / 32, warp = threadIdx.x / 32;
+    // short rows take part of a warp each
+    uint32_t lanes = 32;
+    while (lanes > 1 && lanes * 16 / 2 >= P.dim * sizeof(W)) lanes /= 2;
+    const uint32_t lane = threadIdx.x % lanes, sub = threadIdx.x % 32 / lanes;
+    for (uint32_t first = 0; (uint64_t)first * many + mine < words; first += kMetWords) {       // word i of this CTA is word i * many + mine of all
+        for (uint32_t i = threadIdx.x; i < kMetWords; i += kSortThreads) s_met[i] = 0;
+        __syncthreads();
+#pragma unroll 4
+        for (uint32_t t = threadIdx.x; t < P.tokens; t += kSortThreads) {
+            const uint32_t v = token_at(P, t), word = v / 32, i = word / many;
+            if (v < P.vocab && word - i * many == mine && i - first < kMetWords) atomicOr(&s_met[i - first], 1u << v % 32);
+        }
+        __syncthreads();
+        for (uint32_t i = warp; i < kMetWords; i += kSortWarps) {
+            const uint64_t word = (uint64_t)(first + i) * many + mine;
+            if (word >= words) break;
+            const uint32_t met = s_met[i];
+            for (uint32_t r = sub; r < 32; r += 32 / lanes) {
+                const uint32_t v = (uint32_t)word * 32 + r;
+                if (v < P.vocab && !(met >> r & 1)) clear_row(reinterpret_cast<W*>(P.dweight) + v * P.dweight_stride, P.dim, lane, lanes);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+__global__ void __launch_bounds__(kSortThreads, 1) embedding_sort_kernel(const __grid_constant__ EmbedParams P, int passes, int bits_of_all, int items, int in_cluster, uint32_t weight_type) {
+    extern __shared__ __align__(16) uint64_t s_item[];         // [items * kSortThreads]: key << 32 | place
+    __shared__ uint16_t s_count[kSortWarps][1 << kMostBits];
+    __shared__ uint32_t s_total[1 << kMostBits], s_base[1 << kMostBits], s_warp[kSortWarps];
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if ((int)blockIdx.x >= in_cluster) {
+        uint32_t* s_met = reinterpret_cast<uint32_t*>(&s_count[0][0]);
+        const uint32_t mine = blockIdx.x - in_cluster, many = gridDim.x - in_cluster;
+        if (weight_type == HALOS_F32) clear_rows_not_met<float>(P, mine, many, s_met);
+        else clear_rows_not_met<__half>(P, mine, many, s_met);   // zero is the same in both
+        return;
+    }
+    const uint32_t rank = cluster_rank(), span = items * kSortThreads, span_bits = 31 - __clz(span);
+    for (uint32_t i = rank * kSortThreads + threadIdx.x; i < P.jobs; i += in_cluster * kSortThreads) P.arrived[i] = 0;
+    int shift = 0;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int bits = (bits_of_all - shift + passes - pass - 1) / (passes - pass);
+        const uint32_t bins = 1u << bits;
+        uint64_t item[kMostItems];
+        uint32_t at[kMostItems];
+#pragma unroll
+        for (int k = 0; k < kMostItems; ++k)
+            if (k < items) {
+                const uint32_t local = (warp * items + k) * 32 + lane, t = rank * span + local;
+                item[k] = t >= P.tokens ? ~0ull : pass ? s_item[local] : (uint64_t)token_at(P, t) << 32 | t;
+            }
+        for (uint32_t i = threadIdx.x; i < sizeof s_count / 4; i += kSortThreads) reinterpret_cast<uint32_t*>(&s_count[0][0])[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kMostItems; ++k)
+            if (k < items) {
+                const bool here = rank * span + (warp * items + k) * 32 + lane < P.tokens;
+                const uint32_t digit = (uint32_t)(item[k] >> 32) >> shift & (bins - 1);
+                const uint32_t same = __match_any_sync(~0u, here ? digit : bins), before = __popc(same & ((1u << lane) - 1));
+                const uint32_t had = here ? s_count[warp][digit] : 0;
+                __syncwarp();
+                if (here && before == 0) s_count[warp][digit] = (uint16_t)(had + __popc(same));
+                __syncwarp();
+                at[k] = had + before;
+            }
+        __syncthreads();
+        if (threadIdx.x < bins) {
+            uint32_t sum = 0;
+#pragma unroll 8
+            for (int w = 0; w < kSortWarps; ++w) {
+                const uint32_t n = s_count[w][threadIdx.x];
+                s_count[w][threadIdx.x] = (uint16_t)sum;
+                sum += n;
+            }
+            s_total[threadIdx.x] = sum;
+        }
+        cluster_meet();                                        // totals are there, and every place is in registers
+        uint32_t total = 0, before = 0;
+        if (threadIdx.x < bins)
+            for (uint32_t c = 0; c < (uint32_t)in_cluster; ++c) {
+                uint32_t n;
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(address_in(&s_total[threadIdx.x], c)) : "memory");
+                total += n;
+                if (c < rank) before += n;
+            }
+        uint32_t upto = total;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t n = __shfl_up_sync(~0u, upto, o);
+            if (lane >= o) upto += n;
+        }
+        if (lane == 31) s_warp[warp] = upto;
+        __syncthreads();
+        for (uint32_t w = 0; w < warp; ++w) upto += s_warp[w];
+        if (threadIdx.x < bins) s_base[threadIdx.x] = upto - total + before;
+        __syncthreads();
+        const bool last = pass + 1 == passes;
+#pragma unroll
+        for (int k = 0; k < kMostItems; ++k)
+            if (k < items && rank * span + (warp * items + k) * 32 + lane < P.tokens) {
+                const uint32_t digit = (uint32_t)(item[k] >> 32) >> shift & (bins - 1), to = s_base[digit] + s_count[warp][digit] + at[k];
+                if (last) P.key[0][to] = (uint32_t)(item[k] >> 32), P.place[0][to] = (uint32_t)item[k];
+                else asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(address_in(&s_item[to & (span - 1)], to >> span_bits)), "l"(item[k]) : "memory");
+            }
+        cluster_meet();                                        // places have moved, totals have been read
+        shift += bits;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ sums
 
-// Where V columns of T begin that a lane takes, for slab s; V divides the row.
 template <typename W, int V>
-__device__ __forceinline__ void write_row(const EmbedParams& P, uint32_t v, uint32_t c, const float (&sum)[V]) {
+__device__ __forceinline__ void write_part(const EmbedParams& P, uint32_t v, uint32_t c, const float* sum) {
     W* to = reinterpret_cast<W*>(P.dweight) + v * P.dweight_stride + c;
     float r[V];
     if (P.accumulate) {
@@ -132,79 +300,166 @@ __device__ __forceinline__ void write_row(const EmbedParams& P, uint32_t v, uint
     store_words<W, V>(to, narrow<W, V>(r));
 }
 
-template <int V>
-__device__ __forceinline__ void write_floats(float* to, const float (&v)[V]) { store_words<float, V>(to, narrow<float, V>(v)); }
-
+// A CTA takes 8 `chunk` neighbouring places in the sorted order and 256 columns, a warp `chunk` of the places (32 at most).  A token whose places lie in one warp's
+// chunk is written there.  What goes on from warp to warp is joined in shared memory; what goes on from CTA to CTA is left in memory, and the CTA that
+// comes last, whichever it is, adds up the parts, in their order.
 template <typename A, typename W, int V>
-__global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_constant__ EmbedParams P, const uint32_t* key, const uint32_t* place, uint32_t slabs) {
-    const uint32_t job = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, lane = threadIdx.x % 32, chunk = job / slabs, c = ((job - chunk * slabs) * 32 + lane) * V;
-    if (chunk >= P.chunks) return;
-    const uint32_t from = chunk * kChunk, n = min((uint32_t)kChunk, P.tokens - from);
+__global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_constant__ EmbedParams P, const uint32_t* key, const uint32_t* place) {
+    constexpr int J = kSlab / 32 / V, kAhead = V == 1 || (sizeof(A) == 4 && V >= 4) ? 4 : 8;
+    __shared__ float s_head[kWarps][kSlab], s_tail[kWarps][kSlab];
+    __shared__ uint32_t s_through[kWarps], s_last, s_ends;
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, slab = blockIdx.x % P.slabs, block = blockIdx.x / P.slabs;
+    const uint32_t span = P.chunk * kWarps, cta_from = block * span, from = min(P.tokens, cta_from + warp * P.chunk), n = min(P.chunk, P.tokens - from), blocks = P.jobs / P.slabs;
+    const auto column = [&](int j) { return slab * kSlab + (j * 32 + lane) * V; };
+    after_previous();
     const uint32_t my_key = lane < n ? key[from + lane] : P.vocab, my_place = lane < n ? place[from + lane] : 0;
-    const uint32_t key_before = from ? key[from - 1] : P.vocab, key_after = from + n < P.tokens ? key[from + n] : P.vocab;
-    const bool mine = c < P.dim;
-    float sum[V];
+    const uint32_t key_before = from && n ? key[from - 1] : P.vocab, key_after = from + n < P.tokens ? key[from + n] : P.vocab;
+    float sum[J][V];
+    const auto clear = [&] {
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] = 0.f;
-    constexpr int kAhead = 8;
-    bool began_before = __shfl_sync(~0u, my_key, 0) == key_before;
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[j][e] = 0.f;
+    };
+    const auto keep = [&](float* s) {                           // [256], in the columns' order
+#pragma unroll
+        for (int j = 0; j < J; ++j) store_words<float, V>(s + (j * 32 + lane) * V, narrow<float, V>(sum[j]));
+    };
+    const auto add = [&](const float* s) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            float v[V];
+            widen<float, V>(load_words<float, V>(s + (j * 32 + lane) * V), v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[j][e] += v[e];
+        }
+    };
+    const auto write = [&](uint32_t k) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (column(j) < P.dim) write_part<W, V>(P, k, column(j), sum[j]);
+    };
+    clear();
+    bool began_before = n && __shfl_sync(~0u, my_key, 0) == key_before && key_before < P.vocab;
+    bool through = false, tail = false;
     for (uint32_t i0 = 0; i0 < n; i0 += kAhead) {
-        Words<A, V> w[kAhead];
+        Words<A, V> w[kAhead][J];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const uint32_t k = __shfl_sync(~0u, my_key, i0 + i), t = __shfl_sync(~0u, my_place, i0 + i);
-            w[i] = mine && k < P.vocab ? load_words<A, V>(reinterpret_cast<const A*>(P.dout) + t * P.dout_stride + c) : no_words<A, V>();
+            const A* row = reinterpret_cast<const A*>(P.dout) + t * P.dout_stride;
+#pragma unroll
+            for (int j = 0; j < J; ++j) w[i][j] = column(j) < P.dim && i0 + i < n && k < P.vocab ? load_words<A, V>(row + column(j)) : no_words<A, V>();
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const uint32_t at = i0 + i;
             if (at >= n) break;
             const uint32_t k = __shfl_sync(~0u, my_key, at), next = at + 1 < n ? __shfl_sync(~0u, my_key, at + 1) : key_after;
-            if (k >= P.vocab) break;                    // no tokens: they come last
-            float v[V];
-            widen<A, V>(w[i], v);
+            if (k >= P.vocab) break;                            // no tokens: they come last
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] += v[e];
-            const bool ends = at + 1 == n;
-            if (next != k || ends) {
-                if (mine) {
-                    if (began_before) write_floats<V>(P.head + (int64_t)chunk * P.dim + c, sum);
-                    else if (next == k) write_floats<V>(P.tail + (int64_t)chunk * P.dim + c, sum);
-                    else write_row<W, V>(P, k, c, sum);
-                }
+            for (int j = 0; j < J; ++j) {
+                float v[V];
+                widen<A, V>(w[i][j], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[j][e] += v[e];
+            }
+            if (next != k || at + 1 == n) {
+                if (began_before) keep(s_head[warp]), through = next == k;
+                else if (next == k) keep(s_tail[warp]), tail = true;
+                else write(k);
                 began_before = false;
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] = 0.f;
+                clear();
             }
         }
     }
-}
-
-// The tokens whose places go on from one chunk into the next: the chunk where they begin adds up.
-template <typename W, int V>
-__global__ void __launch_bounds__(kThreads) embedding_join_kernel(const __grid_constant__ EmbedParams P, const uint32_t* key, uint32_t slabs) {
-    const uint32_t job = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, lane = threadIdx.x % 32, chunk = job / slabs, c = ((job - chunk * slabs) * 32 + lane) * V;
-    if (chunk + 1 >= P.chunks) return;
-    const uint32_t from = chunk * kChunk, k = key[from + kChunk - 1];
-    if (k >= P.vocab || key[from + kChunk] != k || (from && key[from] == k && key[from - 1] == k)) return;
-    if (c >= P.dim) return;
-    float sum[V];
-    widen<float, V>(load_words<float, V>(P.tail + (int64_t)chunk * P.dim + c), sum);
-    for (uint32_t i = chunk + 1; i < P.chunks && key[i * kChunk] == k; ++i) {
-        float v[V];
-        widen<float, V>(load_words<float, V>(P.head + (int64_t)i * P.dim + c), v);
+    if (lane == 0) s_through[warp] = through;
+    __syncthreads();
+    // From warp to warp.  The run that comes from the CTA before is warp 0's, any other that of the warp where it begins.
+    const uint32_t cta_end = min(P.tokens, cta_from + span);
+    const bool comes = cta_from && key[cta_from] == key[cta_from - 1] && key[cta_from] < P.vocab;
+    const bool goes = cta_end < P.tokens && key[cta_end] == key[cta_end - 1] && key[cta_end] < P.vocab;
+    if (warp == 0 && comes) {
+        clear(), add(s_head[0]);
+        for (uint32_t w = 0; s_through[w] && w + 1 < kWarps; ) add(s_head[++w]);
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] += v[e];
+        for (int j = 0; j < J; ++j)
+            if (column(j) < P.dim) store_words<float, V>(P.head + (int64_t)block * P.dim + column(j), narrow<float, V>(sum[j]));
     }
-    write_row<W, V>(P, k, c, sum);
+    if (tail) {
+        clear(), add(s_tail[warp]);
+        uint32_t w = warp + 1;
+        for (; w < kWarps; ++w) {
+            add(s_head[w]);
+            if (!s_through[w]) break;
+        }
+        if (w < kWarps) write(__shfl_sync(~0u, my_key, n - 1));
+        else {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (column(j) < P.dim) store_words<float, V>(P.tail + (int64_t)block * P.dim + column(j), narrow<float, V>(sum[j]));
+        }
+    }
+    if (!comes && !goes) return;
+    // From CTA to CTA: up to two runs, or one that goes all the way through.
+    __syncthreads();
+    const bool one = comes && goes && key[cta_from] == key[cta_end];
+    for (int r = 0; r < 2; ++r) {
+        if (r == 0 ? !comes : !goes || one) continue;
+        const uint32_t k = r == 0 ? key[cta_from] : key[cta_end];
+        if (warp == 0) {
+            uint32_t begins = block, ends = block;
+            if (r == 0)
+                for (bool more = true; more;) {                 // CTAs before this whose last place is k's
+                    const bool is = lane < begins && key[(begins - lane) * span - 1] == k;
+                    const uint32_t run = __ffs(~__ballot_sync(~0u, is)) - 1u;   // 2^32 - 1 where all are
+                    begins -= run < 32 ? run : 32, more = run >= 32;
+                }
+            if (r == 1 || one)
+                for (bool more = true; more;) {                 // CTAs behind it whose first place is k's
+                    const uint32_t i = ends + 1 + lane;
+                    const bool is = i < blocks && key[i * span] == k;
+                    const uint32_t run = __ffs(~__ballot_sync(~0u, is)) - 1u;
+                    ends += run < 32 ? run : 32, more = run >= 32;
+                }
+            if (lane == 0) {
+                __threadfence();
+                s_last = atomicAdd(&P.arrived[begins * P.slabs + slab], 1u) == ends - begins ? begins + 1 : 0;
+                s_ends = ends;
+                __threadfence();
+            }
+        }
+        __syncthreads();
+        const uint32_t begins = s_last - 1, ends = s_ends;
+        if (s_last) {                                           // parts begins .. ends, in eight runs of neighbours
+            const uint32_t parts = ends - begins + 1, per = (parts + kWarps - 1) / kWarps, lo = min(parts, warp * per), hi = min(parts, lo + per);
+            clear();
+#pragma unroll 4
+            for (uint32_t i = lo; i < hi; ++i) {
+                const float* part = (i ? P.head : P.tail) + (int64_t)(begins + i) * P.dim;
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    if (column(j) < P.dim) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) sum[j][e] += __ldcg(part + column(j) + e);
+                    }
+            }
+            keep(s_head[warp]);
+            __syncthreads();
+            if (warp == 0) {
+                for (uint32_t w = 1; w < kWarps && w * per < parts; ++w) add(s_head[w]);
+                write(k);
+            }
+        }
+        __syncthreads();
+    }
 }
 
-template <typename W, int V>
+template <typename W>
 __global__ void __launch_bounds__(kThreads) embedding_zero_kernel(const __grid_constant__ EmbedParams P) {
-    const uint32_t v = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+    const uint32_t v = blockIdx.x * kWarps + threadIdx.x / 32;
     if (v >= P.vocab || (P.tokens && P.met[v / 32] >> v % 32 & 1)) return;
-    W* row = reinterpret_cast<W*>(P.dweight) + v * P.dweight_stride;
-    for (uint32_t c = threadIdx.x % 32 * V; c < P.dim; c += 32 * V) store_words<W, V>(row + c, no_words<W, V>());
+    clear_row(reinterpret_cast<W*>(P.dweight) + v * P.dweight_stride, P.dim, threadIdx.x % 32, 32);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -217,9 +472,26 @@ int check(const halos_embedding_args* a) {
     return HALOS_OK;
 }
 
+// Widest access of 16 bytes at most that divides rows of these two tensors and every address; 32-bit tensors may take two of them.
+uint32_t width_of(uint32_t dim, const void* a, int64_t a_stride, uint32_t a_size, const void* b, int64_t b_stride, uint32_t b_size) {
+    const auto fits = [&](const void* p, int64_t stride, uint32_t size, uint32_t n) { return ((uintptr_t)p | (uint64_t)stride * size) % (n * size < 16 ? n * size : 16) == 0; };
+    uint32_t v = 8;
+    while (v > 1 && (dim % v || !fits(a, a_stride, a_size, v) || !fits(b, b_stride, b_size, v))) v /= 2;
+    return v;
+}
+template <typename F>
+int by_width(uint32_t v, F f) {
+    switch (v) {
+        case 8: return f(std::integral_constant<int, 8>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 2: return f(std::integral_constant<int, 2>());
+        default: return f(std::integral_constant<int, 1>());
+    }
+}
+
 struct Sizes {
-    uint32_t bits, passes, blocks, span, chunks;
-    uint64_t arrays, counts, met, sums, all;   // bytes
+    uint32_t bits, passes, blocks, span, chunk, slabs, ctas;
+    uint64_t arrays, counts, met, arrived, sums, all;   // bytes
 };
 uint64_t rounded_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 Sizes sizes_of(const halos_embedding_args* a, int32_t device) {
@@ -231,13 +503,30 @@ Sizes sizes_of(const halos_embedding_args* a, int32_t device) {
     if (s.blocks > most) s.blocks = (uint32_t)most;
     if (s.blocks == 0) s.blocks = 1;
     s.span = (uint32_t)rounded_up((a->tokens + s.blocks - 1) / s.blocks, kSortThreads);
-    s.chunks = (uint32_t)((a->tokens + kChunk - 1) / kChunk);
+    s.slabs = (a->dim + kSlab - 1) / kSlab;
+    // 32 places to a warp, or as few as give every SM two CTAs.
+    s.chunk = 32;
+    while (s.chunk > 4 && (uint64_t)a->tokens * s.slabs < most * 2 * kWarps * s.chunk) s.chunk /= 2;
+    s.ctas = (uint32_t)((a->tokens + s.chunk * kWarps - 1) / (s.chunk * kWarps));
     s.arrays = rounded_up((uint64_t)a->tokens * 4, 16);
     s.counts = ((uint64_t)s.blocks << kMostBits) * 4;
     s.met = rounded_up(((uint64_t)a->vocab + 31) / 32 * 4, 16);
-    s.sums = rounded_up((uint64_t)s.chunks * a->dim * 4, 16);
-    s.all = 4 * s.arrays + s.counts + s.met + 2 * s.sums;
+    s.arrived = rounded_up((uint64_t)s.ctas * s.slabs * 4, 16);
+    s.sums = rounded_up((uint64_t)s.ctas * a->dim * 4, 16);
+    s.all = 4 * s.arrays + s.counts + s.met + s.arrived + 2 * s.sums;
     return s;
+}
+
+// How many clusters of the sort's kernel the device runs at the same time: asked for once for each size of a cluster.  Shared memory goes by that size, too,
+// but leaves room for one CTA to an SM whatever it is.
+int clusters_at_once(int32_t device, const cudaLaunchConfig_t& config, uint32_t in_cluster, int* clusters) {
+    static std::atomic<int> known[64][kMostInCluster + 1];
+    *clusters = known[device][in_cluster].load(std::memory_order_relaxed);
+    if (*clusters) return HALOS_OK;
+    if (int rc = cuda_status(cudaOccupancyMaxActiveClusters(clusters, embedding_sort_kernel, &config), "embedding clusters")) return rc;
+    if (*clusters < 1) *clusters = 1;
+    known[device][in_cluster].store(*clusters, std::memory_order_relaxed);
+    return HALOS_OK;
 }
 
 template <typename F>
@@ -261,11 +550,20 @@ extern "C" int halos_embedding_fwd(const halos_embedding_args* a) {
     EmbedParams P{};
     P.weight = (const char*)a->weight, P.out = (char*)a->out, P.token = (const char*)a->token, P.weight_stride = a->weight_stride, P.out_stride = a->out_stride;
     P.tokens = (uint32_t)a->tokens, P.vocab = (uint32_t)a->vocab, P.dim = a->dim, P.tokens_64 = a->tokens_64, P.scale = a->scale;
+    P.slabs = (P.dim + kSlab - 1) / kSlab;
     cudaStream_t st = (cudaStream_t)a->stream;
-    return by_type(a->dtype, [&](auto x) {
-        return by_type(a->weight_dtype, [&](auto w) {
-            embedding_kernel<decltype(x), decltype(w)><<<(P.tokens + kThreads / 32 - 1) / (kThreads / 32), kThreads, 0, st>>>(P);
-            return cuda_status(cudaGetLastError(), "embedding launch");
+    // Four tokens to a warp, or one where that gives no SM eight warps.
+    const bool few = (uint64_t)P.tokens * P.slabs < (uint64_t)sm_count(a->device) * 32;
+    const uint64_t jobs = ((uint64_t)P.tokens + kWarps * (few ? 1 : 4) - 1) / (kWarps * (few ? 1 : 4)) * P.slabs;
+    if (jobs > 0x7fffffffull) return fail(HALOS_ERR_UNSUPPORTED, "embedding: too many rows");
+    return by_width(width_of(P.dim, a->weight, a->weight_stride, size_of(a->weight_dtype), a->out, a->out_stride, size_of(a->dtype)), [&](auto n) {
+        return by_type(a->dtype, [&](auto x) {
+            return by_type(a->weight_dtype, [&](auto w) {
+                constexpr int V = decltype(n)::value;
+                if (few) embedding_kernel<decltype(x), decltype(w), V, 1><<<(unsigned)jobs, kThreads, 0, st>>>(P);
+                else embedding_kernel<decltype(x), decltype(w), V, 4><<<(unsigned)jobs, kThreads, 0, st>>>(P);
+                return cuda_status(cudaGetLastError(), "embedding launch");
+            });
         });
     });
 }
@@ -296,28 +594,34 @@ extern "C" int halos_embedding_bwd(const halos_embedding_args* a) {
     for (int i = 0; i < 2; ++i) P.key[i] = (uint32_t*)at, at += s.arrays, P.place[i] = (uint32_t*)at, at += s.arrays;
     P.counts = (uint32_t*)at, at += s.counts;
     P.met = (uint32_t*)at, at += s.met;
+    P.arrived = (uint32_t*)at, at += s.arrived;
     P.head = (float*)at, at += s.sums;
     P.tail = (float*)at;
-    P.chunks = s.chunks, P.sort_blocks = s.blocks, P.span = s.span;
+    if ((uint64_t)s.ctas * s.slabs > 0x7fffffffull) return fail(HALOS_ERR_UNSUPPORTED, "embedding: too many sums");
+    P.chunk = s.chunk, P.slabs = s.slabs, P.jobs = s.ctas * s.slabs, P.sort_blocks = s.blocks, P.span = s.span;
     cudaStream_t st = (cudaStream_t)a->stream;
-    // Widest access of 16 bytes at most that divides the rows and every address.
-    uint32_t v = 8;
-    const auto divides = [&](uint32_t n) {
-        const auto fits = [&](const void* p, int64_t stride, uint32_t bytes) { return ((uintptr_t)p | (uint64_t)stride * bytes) % (n * bytes < 16 ? n * bytes : 16) == 0; };
-        return a->dim % n == 0 && n * size <= 16 && fits(a->dweight, a->dweight_stride, wsize) && (!a->tokens || fits(a->dout, a->dout_stride, size));
-    };
-    while (v > 1 && !divides(v)) v /= 2;
-    const auto by_width = [&](auto f) -> int {
-        switch (v) {
-            case 8: return f(std::integral_constant<int, 8>());
-            case 4: return f(std::integral_constant<int, 4>());
-            case 2: return f(std::integral_constant<int, 2>());
-            default: return f(std::integral_constant<int, 1>());
+    const uint32_t width = width_of(P.dim, a->dweight, a->dweight_stride, wsize, P.tokens ? a->dout : a->dweight, P.tokens ? a->dout_stride : a->dweight_stride, P.tokens ? size : wsize);
+    int sorted = 0;                                    // which of the two arrays holds the sorted places
+    if (P.tokens && P.tokens <= kMostClustered) {
+        uint32_t in_cluster = 1, items = 1;
+        while (in_cluster < kMostInCluster && in_cluster * kSortThreads < P.tokens) in_cluster *= 2;
+        while (in_cluster * items * kSortThreads < P.tokens) items *= 2;
+        const uint32_t shared = items * kSortThreads * 8;
+        static Allowed allowed;
+        if (int rc = allow_smem(embedding_sort_kernel, (int)shared, allowed)) return rc;
+        cudaLaunchAttribute cluster{};
+        cluster.id = cudaLaunchAttributeClusterDimension, cluster.val.clusterDim.x = in_cluster, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+        cudaLaunchConfig_t config{};
+        config.gridDim = in_cluster, config.blockDim = kSortThreads, config.dynamicSmemBytes = shared, config.stream = st, config.attrs = &cluster, config.numAttrs = 1;
+        if (!P.accumulate) {                           // as many more as run at the same time; a word of 32 rows to each at least
+            int clusters = 0;
+            if (int rc = clusters_at_once(a->device, config, in_cluster, &clusters)) return rc;
+            const uint32_t words = (P.vocab + 31) / 32, wanted = 1 + (words + in_cluster - 1) / in_cluster;
+            config.gridDim = in_cluster * (clusters < 2 ? 2 : (uint32_t)clusters < wanted ? (uint32_t)clusters : wanted);
         }
-    };
-    if ((uint64_t)P.chunks * ((P.dim + 32 * v - 1) / (32 * v)) > 0xffffff00ull) return fail(HALOS_ERR_UNSUPPORTED, "embedding: too many sums");
-    if (P.tokens) {
-        if (int rc = cuda_status(cudaMemsetAsync(P.met, 0, s.met, st), "embedding workspace")) return rc;
+        if (int rc = cuda_status(cudaLaunchKernelEx(&config, embedding_sort_kernel, P, (int)s.passes, (int)s.bits, (int)items, (int)in_cluster, a->weight_dtype), "embedding launch")) return rc;
+    } else if (P.tokens) {
+        if (int rc = cuda_status(cudaMemsetAsync(P.met, 0, s.met + s.arrived, st), "embedding workspace")) return rc;
         for (uint32_t pass = 0, shift = 0; pass < s.passes; ++pass) {
             const int bits = (int)((s.bits - shift + s.passes - pass - 1) / (s.passes - pass));
             embedding_count_kernel<<<P.sort_blocks, kSortThreads, 0, st>>>(P, (int)pass, (int)shift, bits);
@@ -325,25 +629,19 @@ extern "C" int halos_embedding_bwd(const halos_embedding_args* a) {
             if (int rc = cuda_status(cudaGetLastError(), "embedding launch")) return rc;
             shift += bits;
         }
+        sorted = s.passes & 1;
     }
     return by_type(a->weight_dtype, [&](auto wt) -> int {
         using W = decltype(wt);
-        return by_width([&](auto n) -> int {
-            constexpr int V = decltype(n)::value;
-            const uint32_t slabs = (P.dim + 32 * V - 1) / (32 * V), per = kThreads / 32;
-            if (!P.accumulate) embedding_zero_kernel<W, V><<<(P.vocab + per - 1) / per, kThreads, 0, st>>>(P);
-            if (!P.tokens) return cuda_status(cudaGetLastError(), "embedding launch");
-            const uint64_t jobs = (uint64_t)P.chunks * slabs;
-            const uint32_t* key = P.key[s.passes & 1];
-            const uint32_t* place = P.place[s.passes & 1];
-            const unsigned grid = (unsigned)((jobs + per - 1) / per);
-            const int rc = by_type(a->dtype, [&](auto x) {
-                if constexpr (V * sizeof(x) <= 16) embedding_sum_kernel<decltype(x), W, V><<<grid, kThreads, 0, st>>>(P, key, place, slabs);
-                return cuda_status(cudaGetLastError(), "embedding launch");
+        if (!P.accumulate && (!P.tokens || P.tokens > kMostClustered)) {
+            embedding_zero_kernel<W><<<(P.vocab + kWarps - 1) / kWarps, kThreads, 0, st>>>(P);
+            if (int rc = cuda_status(cudaGetLastError(), "embedding launch")) return rc;
+        }
+        if (!P.tokens) return HALOS_OK;
+        return by_width(width, [&](auto n) {
+            return by_type(a->dtype, [&](auto x) {
+                return launch_after(embedding_sum_kernel<decltype(x), W, decltype(n)::value>, P.jobs, kThreads, 0, st, "embedding launch", P, (const uint32_t*)P.key[sorted], (const uint32_t*)P.place[sorted]);
             });
-            if (rc) return rc;
-            embedding_join_kernel<W, V><<<grid, kThreads, 0, st>>>(P, key, slabs);
-            return cuda_status(cudaGetLastError(), "embedding launch");
         });
     });
 }

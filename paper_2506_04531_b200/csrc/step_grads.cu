@@ -17,6 +17,7 @@ namespace halos_step {
 namespace {
 
 constexpr int kThreads = 256, kResident = 4;        // CTAs to an SM
+constexpr int kWaves = 4;                           // of CTAs, at most: partial sums have an end
 constexpr uint32_t kChunkBytes = 32768;             // of gradients
 constexpr int kMostPieces = 960;                    // what a launch's 32764 bytes of arguments hold
 enum Mode { kClip, kStep };
@@ -30,7 +31,7 @@ struct Piece {
 };
 template <int N>
 struct Table {
-    uint32_t pieces, chunks;
+    uint32_t pieces, chunks, run;                   // run: chunks to a CTA
     const double* partial;                          // of the norm; NULL: the factor is 1
     uint32_t partials;
     float max_norm, rate;
@@ -105,7 +106,8 @@ __device__ __forceinline__ double squares_of_chunk(const T* x, int n) {
 template <int N>
 __global__ void __launch_bounds__(kThreads, kResident) grads_squares_kernel(const __grid_constant__ Table<N> t, double* partial) {
     double sum = 0.0;
-    for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const uint32_t end = min(t.chunks, (blockIdx.x + 1) * t.run);
+    for (uint32_t c = blockIdx.x * t.run; c < end; ++c) {
         const Piece& p = t.piece[piece_of(t, c)];
         const uint32_t size = p.in_type == HALOS_F32 ? 4 : 2;
         const int64_t at = (int64_t)(c - p.first) * (kChunkBytes / size), left = p.n - at;
@@ -125,6 +127,7 @@ __device__ __forceinline__ double norm_of(const double* partial, uint32_t n) {
 }
 
 __global__ void __launch_bounds__(kThreads) grads_norm_kernel(const double* partial, uint32_t n, float* norm) {
+    after_previous();
     const double d = norm_of(partial, n);
     if (threadIdx.x == 0) *norm = (float)d;
 }
@@ -180,13 +183,15 @@ __device__ __forceinline__ void apply_by_out(const Piece& p, int64_t at, int n, 
 template <Mode M, int N>
 __global__ void __launch_bounds__(kThreads, kResident) grads_apply_kernel(const __grid_constant__ Table<N> t) {
     double f = 1.0;
+    after_previous();
     if (t.partial) {
         const double n = norm_of(t.partial, t.partials);
         if (n > (double)t.max_norm) f = (double)t.max_norm / n;
         if (t.norm && blockIdx.x == 0 && threadIdx.x == 0) *t.norm = (float)n;
     }
     const float factor = M == kStep ? (float)((double)t.rate * f) : (float)f;
-    for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const uint32_t end = min(t.chunks, (blockIdx.x + 1) * t.run);
+    for (uint32_t c = blockIdx.x * t.run; c < end; ++c) {
         const uint32_t chunk = t.chunks - 1 - c;
         const Piece& p = t.piece[piece_of(t, chunk)];
         if (M == kClip && p.in == p.out && factor == 1.f) continue;
@@ -243,7 +248,7 @@ int check(const halos_grads_args* a, bool outs, bool norm) {
     return HALOS_OK;
 }
 
-uint64_t grid_limit(int32_t device) { return (uint64_t)sm_count(device) * kResident; }
+uint64_t grid_limit(int32_t device) { return (uint64_t)sm_count(device) * kResident * kWaves; }
 
 // Calls `launch` with tables of as many tensors as fit one; the number of CTAs goes by the chunks and is `limit` at most.
 template <int N, typename F>
@@ -263,8 +268,9 @@ int in_tables(const halos_grads_args* a, bool outs, uint64_t limit, F launch) {
             chunks += here;
         }
         t.chunks = (uint32_t)chunks;
+        t.run = (uint32_t)((chunks + limit - 1) / limit);
         if (t.pieces)
-            if (int rc = launch(t, (unsigned)(chunks < limit ? chunks : limit))) return rc;
+            if (int rc = launch(t, (unsigned)((chunks + t.run - 1) / t.run))) return rc;
         if (i == a->count) return HALOS_OK;
     }
 }
@@ -305,15 +311,12 @@ int run(const halos_grads_args* a, bool apply, Mode mode) {
             if (int rc = in_tables<N>(a, true, limit, [&](Table<N>& t, unsigned grid) {
                     t.partial = with_norm ? partial : nullptr, t.partials = partials, t.max_norm = a->max_norm, t.rate = a->rate;
                     t.norm = first ? a->norm : nullptr, first = false;
-                    if (mode == kStep) grads_apply_kernel<kStep, N><<<grid, kThreads, 0, st>>>(t);
-                    else grads_apply_kernel<kClip, N><<<grid, kThreads, 0, st>>>(t);
-                    return cuda_status(cudaGetLastError(), "gradient launch");
+                    return launch_after(mode == kStep ? grads_apply_kernel<kStep, N> : grads_apply_kernel<kClip, N>, grid, kThreads, 0, st, "gradient launch", t);
                 }))
                 return rc;
         }
         if (with_norm && first) {  // nobody has written the norm
-            grads_norm_kernel<<<1, kThreads, 0, st>>>(partial, partials, a->norm);
-            return cuda_status(cudaGetLastError(), "gradient norm launch");
+            return launch_after(grads_norm_kernel, 1, kThreads, 0, st, "gradient norm launch", (const double*)partial, partials, a->norm);
         }
         return HALOS_OK;
     });

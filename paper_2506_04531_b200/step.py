@@ -13,9 +13,11 @@ Errors are ``HalosError``.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import math
+import operator
 import struct
 from typing import Optional
 
@@ -526,6 +528,9 @@ def distill_loss(logits, labels, teacher_idx=None, teacher_logits=None, *, tempe
 
 # ------------------------------------------------------------------------------------------ embedding
 
+_STREAM = struct.Struct("=IiQ")              # what every args struct begins with: its size, device and stream
+
+
 def _as_rows(x, dim: int):
     """x, or a copy of it, as a matrix of rows whose elements lie side by side."""
     if x.dim() != 2:
@@ -541,6 +546,12 @@ def _tokens_checked(tokens, device):
     return tokens if tokens.is_contiguous() else tokens.contiguous(), wide
 
 
+@functools.lru_cache(maxsize=256)
+def _embedding_workspace(device: int, dtype: int, weight_dtype: int, tokens: int, vocab: int, dim: int) -> int:
+    """Goes by sizes alone, so that they are asked for once."""
+    return _workspace("halos_embedding_workspace", _pack(_EMBEDDING, _EMBEDDING.size, device, 0, dtype, weight_dtype, 0, 0, tokens, vocab, dim, 1.0, *(0,) * 11), device)
+
+
 def embedding_forward(weight, tokens, *, scale: float = 1.0, dtype=None):
     """scale times the rows of weight [vocab, dim] (any distance apart) that tokens (int32 or int64, any shape) name, as [*tokens.shape, dim] of
     dtype (float32, bfloat16 or float16; weight's unless given).  A token outside the vocabulary gives a row of NaN."""
@@ -549,13 +560,19 @@ def embedding_forward(weight, tokens, *, scale: float = 1.0, dtype=None):
     device = weight.device
     _on(weight, device, "weight")
     vocab, dim = weight.shape
-    if weight.stride(1) != 1 and dim > 1:
+    stride, step_ = weight.stride()
+    if step_ != 1 and dim > 1:
         _refuse("weight: a row's elements must lie side by side")
     tokens, wide = _tokens_checked(tokens, device)
-    out = torch.empty((*tokens.shape, dim), dtype=dtype or weight.dtype, device=device)
+    kind = _dtype(weight, "weight")
+    out_kind = kind if dtype is None else _DTYPES.get(dtype)
+    if out_kind is None:
+        _refuse(f"dtype: {dtype} is not float32, bfloat16 or float16")
+    out = weight.new_empty((*tokens.shape, dim), dtype=dtype)
+    index = device.index
     _call("halos_embedding_fwd", _pack(
-        _EMBEDDING, _EMBEDDING.size, device.index, _raw_stream(device.index), _dtype(out, "dtype"), _dtype(weight, "weight"), wide, 0, tokens.numel(), vocab, dim, scale,
-        tokens.data_ptr(), weight.data_ptr(), weight.stride(0), out.data_ptr(), dim, 0, 0, 0, 0, 0, 0), device.index)
+        _EMBEDDING, _EMBEDDING.size, index, _raw_stream(index), out_kind, kind, wide, 0, tokens.numel(), vocab, dim, scale,
+        tokens.data_ptr(), weight.data_ptr(), stride, out.data_ptr(), dim, 0, 0, 0, 0, 0, 0), index)
     return out
 
 
@@ -565,26 +582,29 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
     accumulate: added to what out holds, whose other rows are not touched.  Tokens outside the vocabulary take no part."""
     device = dout.device
     _on(dout, device, "dout")
-    if dout.dim() < 1 or dout.shape[:-1] != tokens.shape:
+    shape = dout.shape
+    if not shape or shape[:-1] != tokens.shape:
         _refuse("dout must be [*tokens.shape, dim]")
     tokens, wide = _tokens_checked(tokens, device)
-    dim = dout.size(-1)
+    dim = shape[-1]
     rows = _as_rows(dout, dim) if dim else dout
     if out is None:
         if accumulate:
             _refuse("accumulate needs out")
-        out = torch.empty((vocab, dim), dtype=dtype or dout.dtype, device=device)
+        if vocab < 0 or (dtype is not None and dtype not in _DTYPES):
+            _refuse("vocab must be positive and dtype float32, bfloat16 or float16")
+        out = dout.new_empty((vocab, dim), dtype=dtype)
     else:
         _on(out, device, "out")
         if out.shape != (vocab, dim) or (dtype is not None and out.dtype != dtype) or (out.stride(1) != 1 and dim > 1) or (vocab > 1 and out.stride(0) < dim):
             _refuse("out must be [vocab, dim] of dtype, a row's elements side by side and rows apart")
         _overwritten(out, "out")
-    index = device.index
-    head = (_EMBEDDING.size, index, _raw_stream(index), _dtype(dout, "dout"), _dtype(out, "dtype"), wide, bool(accumulate), tokens.numel(), vocab, dim, scale,
-            tokens.data_ptr(), 0, 0, 0, 0, rows.data_ptr(), rows.stride(0), out.data_ptr(), out.stride(0))
-    size = _workspace("halos_embedding_workspace", _pack(_EMBEDDING, *head, 0, 0), index)
-    space = torch.empty(size, dtype=torch.uint8, device=device)
-    _call("halos_embedding_bwd", _pack(_EMBEDDING, *head, space.data_ptr(), size), index)
+    index, count, kind, out_kind = device.index, tokens.numel(), _dtype(dout, "dout"), _dtype(out, "out")
+    size = _embedding_workspace(index, kind, out_kind, count, vocab, dim)
+    space = dout.new_empty(size, dtype=torch.uint8)
+    _call("halos_embedding_bwd", _pack(
+        _EMBEDDING, _EMBEDDING.size, index, _raw_stream(index), kind, out_kind, wide, bool(accumulate), count, vocab, dim, scale,
+        tokens.data_ptr(), 0, 0, 0, 0, rows.data_ptr(), rows.stride(0), out.data_ptr(), out.stride(0), space.data_ptr(), size), index)
     return out
 
 
@@ -620,26 +640,44 @@ def embedding(weight, tokens, *, scale: float = 1.0, dtype=None):
 
 # ------------------------------------------------------------------------------------------ root-mean-square norm
 
-def _outer(x, shape):
-    """x [*shape, dim], or a copy of it, with three outer sizes, and their strides."""
+_NORM_POINTERS, _NORM_STRIDES = struct.Struct("=13Q"), struct.Struct("=21q")
+_NORM_LAYOUT = struct.Struct("=IIII3qIf")
+
+
+def _side_by_side(x):
+    """x, or a copy of it whose rows' elements lie side by side; more than three outer sizes as one."""
     if x.stride(-1) != 1 and x.size(-1) > 1:
         x = x.contiguous()
-    n = len(shape)
-    if n > 3:
-        x = x.reshape(-1, x.size(-1))
-        n = 1
-    return x, (0,) * (3 - n) + x.stride()[:-1]
+    return x if x.dim() <= 4 else x.reshape(-1, x.size(-1))
 
 
-def _sizes(shape):
-    return (1,) * (3 - len(shape)) + tuple(shape) if len(shape) <= 3 else (1, 1, math.prod(shape))
+@functools.lru_cache(maxsize=256)
+def _norm_layout(shape, strides, kind: int, weight_kind: int, quantized: bool, group: int, eps: float):
+    """The args' part that goes by sizes and strides alone (those of x, residual, summed, y, dy, dsummed, dx without the innermost; None: not there, or
+    contiguous where True), the bytes before the pointers and those behind them."""
+    dim, outer = shape[-1], shape[:-1]
+    size = (1,) * (3 - len(outer)) + tuple(outer) if len(outer) <= 3 else (1, 1, math.prod(outer))
+    plain = (size[1] * size[2] * dim, size[2] * dim, dim)
+    every = []
+    for s in strides:
+        every += plain if s is True else (0, 0, 0) if s is None else (0,) * (3 - len(s)) + s
+    try:
+        return _NORM_LAYOUT.pack(kind, weight_kind, quantized, group, *size, dim, eps), _NORM_STRIDES.pack(*every)
+    except (struct.error, OverflowError) as e:
+        raise HalosError(ERR_INVALID_ARG, f"an argument out of range: {e}") from None
 
 
-def _norm_weight(weight, x):
-    if x.dim() < 1:
-        _refuse("rows must have a last dimension")
-    _on(weight, x.device, "weight")
-    if weight.shape != x.shape[-1:] or not weight.is_contiguous():
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(device: int, shape, kind: int, weight_kind: int) -> int:
+    """Goes by sizes alone, so that they are asked for once."""
+    layout, strides = _norm_layout(shape, (None,) * 7, kind, weight_kind, False, 0, 0.0)
+    return _workspace("halos_rms_norm_workspace", _STREAM.pack(_RMS_NORM.size, device, 0) + layout + _NORM_POINTERS.pack(*(0,) * 13) + strides, device)
+
+
+def _norm_weight(weight, x, device):
+    if weight.device != device:
+        _on(weight, device, "weight")
+    if weight.dim() != 1 or weight.size(0) != x.size(-1) or not weight.is_contiguous():
         _refuse("weight must be a contiguous vector as long as a row")
     return _dtype(weight, "weight")
 
@@ -651,24 +689,25 @@ def _like(a, b, what: str):
 
 
 def _rms_norm(x, weight, residual, eps, quantized, group):
-    device, shape, dim = x.device, x.shape[:-1], x.shape[-1] if x.dim() else 0
+    device, shape = x.device, x.shape
     _on(x, device, "x")
-    kind, weight_kind = _dtype(x, "x"), _norm_weight(weight, x)
-    x3, x_stride = _outer(x, shape)
-    none, summed, r3, r_stride, s_stride = (0, 0, 0), x, None, (0, 0, 0), (0, 0, 0)
+    if not shape:
+        _refuse("rows must have a last dimension")
+    kind, weight_kind = _dtype(x, "x"), _norm_weight(weight, x, device)
+    x3, summed, at_r, at_s, r_stride, s_stride = _side_by_side(x), x, 0, 0, None, None
     if residual is not None:
         _like(residual, x, "residual")
-        r3, r_stride = _outer(residual, shape)
-        summed = torch.empty(x.shape, dtype=x.dtype, device=device)
-        s_stride = _outer(summed, shape)[1]
-    y = torch.empty(x.shape, dtype=torch.float8_e4m3fn if quantized else x.dtype, device=device)
-    y_stride = _outer(y, shape)[1]
-    rstd = torch.empty(shape, dtype=torch.float32, device=device)
-    scales = torch.empty((*shape, -(-dim // (group or dim or 1))), dtype=torch.float32, device=device) if quantized else None
-    _call("halos_rms_norm_fwd", _pack(
-        _RMS_NORM, _RMS_NORM.size, device.index, _raw_stream(device.index), kind, weight_kind, quantized, group, *_sizes(shape), dim, eps, x3.data_ptr(),
-        0 if r3 is None else r3.data_ptr(), 0 if r3 is None else summed.data_ptr(), y.data_ptr(), 0 if scales is None else scales.data_ptr(), rstd.data_ptr(),
-        weight.data_ptr(), 0, 0, 0, 0, 0, 0, *x_stride, *r_stride, *s_stride, *y_stride, *none, *none, *none), device.index)
+        r3 = _side_by_side(residual)
+        summed = x.new_empty(shape)
+        at_r, at_s, r_stride, s_stride = r3.data_ptr(), summed.data_ptr(), r3.stride()[:-1], True
+    layout, strides = _norm_layout(shape, (x3.stride()[:-1], r_stride, s_stride, True, None, None, None), kind, weight_kind, quantized, group, eps)
+    y, rstd, scales, at_scales = x.new_empty(shape, dtype=torch.float8_e4m3fn if quantized else None), x.new_empty(shape[:-1], dtype=torch.float32), None, 0
+    if quantized:
+        scales = x.new_empty((*shape[:-1], -(-shape[-1] // (group or shape[-1] or 1))), dtype=torch.float32)
+        at_scales = scales.data_ptr()
+    index = device.index
+    _call("halos_rms_norm_fwd", b"".join((_STREAM.pack(_RMS_NORM.size, index, _raw_stream(index)), layout, _NORM_POINTERS.pack(
+        x3.data_ptr(), at_r, at_s, y.data_ptr(), at_scales, rstd.data_ptr(), weight.data_ptr(), 0, 0, 0, 0, 0, 0), strides)), index)
     return y, scales, summed, rstd
 
 
@@ -689,27 +728,26 @@ def rms_norm_quantized(x, weight, *, residual=None, eps: float = 1e-5, group: in
 def rms_norm_backward(dy, summed, weight, rstd, *, dsummed=None):
     """(dx, dweight) from the gradient of y, what the forward pass returned, and the gradient of summed.  dx is the gradient of x and of the
     residual; dweight is of weight's type.  Deterministic."""
-    device, shape, dim = dy.device, dy.shape[:-1], dy.shape[-1] if dy.dim() else 0
+    device, shape = dy.device, dy.shape
     _on(dy, device, "dy")
-    kind, weight_kind = _dtype(dy, "dy"), _norm_weight(weight, dy)
+    if not shape:
+        _refuse("rows must have a last dimension")
+    kind, weight_kind = _dtype(dy, "dy"), _norm_weight(weight, dy, device)
     _like(summed, dy, "summed")
     _on(rstd, device, "rstd")
-    if rstd.dtype != torch.float32 or rstd.shape != shape or not rstd.is_contiguous():
+    if rstd.dtype != torch.float32 or rstd.shape != shape[:-1] or not rstd.is_contiguous():
         _refuse("rstd must be contiguous float32 [...]")
-    dy3, dy_stride = _outer(dy, shape)
-    s3, s_stride = _outer(summed, shape)
-    d3, d_stride, none = None, (0, 0, 0), (0, 0, 0)
+    dy3, s3, at_d, d_stride = _side_by_side(dy), _side_by_side(summed), 0, None
     if dsummed is not None:
         _like(dsummed, dy, "dsummed")
-        d3, d_stride = _outer(dsummed, shape)
-    dx, dweight = torch.empty(dy.shape, dtype=dy.dtype, device=device), torch.empty_like(weight)
-    dx_stride, index = _outer(dx, shape)[1], device.index
-    head = (_RMS_NORM.size, index, _raw_stream(index), kind, weight_kind, 0, 0, *_sizes(shape), dim, 0.0, 0, 0, s3.data_ptr(), 0, 0, rstd.data_ptr(), weight.data_ptr(),
-            dy3.data_ptr(), 0 if d3 is None else d3.data_ptr(), dx.data_ptr(), dweight.data_ptr())
-    strides = (*none, *none, *s_stride, *none, *dy_stride, *d_stride, *dx_stride)
-    size = _workspace("halos_rms_norm_workspace", _pack(_RMS_NORM, *head, 0, 0, *strides), index)
-    space = torch.empty(size, dtype=torch.uint8, device=device)
-    _call("halos_rms_norm_bwd", _pack(_RMS_NORM, *head, space.data_ptr(), size, *strides), index)
+        d3 = _side_by_side(dsummed)
+        at_d, d_stride = d3.data_ptr(), d3.stride()[:-1]
+    index = device.index
+    layout, strides = _norm_layout(shape, (None, None, s3.stride()[:-1], None, dy3.stride()[:-1], d_stride, True), kind, weight_kind, False, 0, 0.0)
+    size = _norm_workspace(index, shape, kind, weight_kind)
+    dx, dweight, space = dy.new_empty(shape), weight.new_empty(shape[-1:]), dy.new_empty(size, dtype=torch.uint8)
+    _call("halos_rms_norm_bwd", b"".join((_STREAM.pack(_RMS_NORM.size, index, _raw_stream(index)), layout, _NORM_POINTERS.pack(
+        0, 0, s3.data_ptr(), 0, 0, rstd.data_ptr(), weight.data_ptr(), dy3.data_ptr(), at_d, dx.data_ptr(), dweight.data_ptr(), space.data_ptr(), size), strides)), index)
     return dx, dweight
 
 
@@ -739,6 +777,10 @@ def rms_norm(x, weight, *, residual=None, eps: float = 1e-5):
 
 # ------------------------------------------------------------------------------------------ gradients
 
+# Many small tensors are bound by what is asked of each: attributes by map, whose loop is not Python's.
+_DTYPE_OF, _SHAPE_OF, _REQUIRES = operator.attrgetter("dtype"), operator.attrgetter("shape"), operator.attrgetter("requires_grad")
+
+
 def _dense(x) -> bool:
     """Whether x's elements fill a run of memory, in whatever order."""
     return x.is_contiguous() or x.permute(sorted(range(x.dim()), key=lambda i: (x.stride(i), x.size(i)), reverse=True)).is_contiguous()
@@ -746,58 +788,70 @@ def _dense(x) -> bool:
 
 def _listed(tensors, what: str):
     tensors = list(tensors)
-    if not tensors or not all(isinstance(x, torch.Tensor) for x in tensors):
+    if not tensors or not all([issubclass(kind, torch.Tensor) for kind in set(map(type, tensors))]):
         _refuse(f"{what} must be one tensor or more")
     return tensors
 
 
-def _grads_call(name: str, grads, outs, max_norm: float, rate: float, norm):
+@functools.lru_cache(maxsize=256)
+def _grads_workspace(device: int, count: int) -> int:
+    """Goes by the number of tensors alone, so that it is asked for once."""
+    return _workspace("halos_grads_workspace", _pack(_GRADS, _GRADS.size, device, 0, count, *(0,) * 5, 0.0, 0.0, 0, 0, 0), device)
+
+
+def _words(values):
+    """An array of 64-bit values, and where it lies."""
+    words = array.array("Q", values)
+    return words, words.buffer_info()[0]
+
+
+def _grads_call(name: str, grads, outs, max_norm: float, rate: float, with_norm: bool):
     device = grads[0].device
-    both = grads if outs is None else grads + outs
-    for x in both:
-        if x.device != device or not x.is_cuda:
+    index = device.index if grads[0].is_cuda else -1
+    both = grads if outs is None or outs is grads else grads + outs
+    if index < 0 or set(map(torch.Tensor.get_device, both)) != {index}:
+        for x in both:
             _on(x, device, "a tensor")
-    kinds = [_DTYPES.get(x.dtype) for x in both]
-    if None in kinds:
-        _dtype(both[kinds.index(None)], "a tensor")
-    if outs is None:
-        grads = [x if _dense(x) else x.contiguous() for x in grads]
-    else:
-        for x in outs:
-            if not _dense(x):
+    kinds = [_DTYPES.get(kind, 255) for kind in map(_DTYPE_OF, both)]
+    if 255 in kinds:
+        _dtype(both[kinds.index(255)], "a tensor")
+    in_place = outs is grads
+    if not all(map(torch.Tensor.is_contiguous, both)):
+        if outs is None:
+            grads = [x if _dense(x) else x.contiguous() for x in grads]
+        else:
+            if not all([_dense(x) for x in outs]):
                 _refuse("a tensor that is written must fill a run of memory")
-        # elements side by side in the one are to be so in the other
-        grads = [g if (g.is_contiguous() and o.is_contiguous()) or (g.stride() == o.stride() and g.shape == o.shape) else torch.empty_like(o, dtype=g.dtype).copy_(g) for g, o in zip(grads, outs)]
-        for x in outs:
-            _overwritten(x, "a tensor that is written")
-    n, index = len(grads), device.index
-    at = lambda values: (C.c_uint64 * n)(*values)  # noqa: E731
-    g_at, sizes, g_kinds = at([x.data_ptr() for x in grads]), at([x.numel() for x in grads]), bytes(kinds[:n])
-    o_at, o_kinds = (None, None) if outs is None else (at([x.data_ptr() for x in outs]), bytes(kinds[n:]))
-    head = (_GRADS.size, index, _raw_stream(index), n, C.addressof(g_at), 0 if o_at is None else C.addressof(o_at), C.addressof(sizes), _address(g_kinds), 0 if o_at is None else _address(o_kinds),
-            max_norm, rate, 0 if norm is None else norm.data_ptr())
-    if norm is None:
-        space, size = None, 0
-    else:
-        size = _workspace("halos_grads_workspace", _pack(_GRADS, *head, 0, 0), index)
-        space = torch.empty(size, dtype=torch.uint8, device=device)
-    _call(name, _pack(_GRADS, *head, 0 if space is None else space.data_ptr(), size), index)
+            if not in_place:  # elements side by side in the one are to be so in the other
+                grads = [g if (g.is_contiguous() and o.is_contiguous()) or (g.stride() == o.stride()) else torch.empty_like(o, dtype=g.dtype).copy_(g) for g, o in zip(grads, outs)]
+    if outs is not None:
+        if torch.is_grad_enabled() and any(map(_REQUIRES, outs)):
+            _overwritten(next(x for x in outs if x.requires_grad), "a tensor that is written")
+        torch.autograd.graph.increment_version(outs)
+    n = len(grads)
+    g_words, g_at = _words(map(torch.Tensor.data_ptr, grads))
+    sizes, sizes_at = _words(map(torch.Tensor.numel, grads))
+    g_kinds = bytes(kinds[:n])
+    kinds_at = o_kinds_at = C.cast(C.c_char_p(g_kinds), _vp).value
+    o_at, norm, space, size = 0, None, 0, 0
+    if in_place:
+        o_at = g_at
+    elif outs is not None:
+        o_kinds = bytes(kinds[n:])
+        (o_words, o_at), o_kinds_at = _words(map(torch.Tensor.data_ptr, outs)), C.cast(C.c_char_p(o_kinds), _vp).value
+    if with_norm:
+        norm, size = grads[0].new_empty((), dtype=torch.float32), _grads_workspace(index, n)
+        space = grads[0].new_empty(size, dtype=torch.uint8)
+    _call(name, _pack(_GRADS, _GRADS.size, index, _raw_stream(index), n, g_at, o_at, sizes_at, kinds_at, o_kinds_at, max_norm, rate,
+                      norm.data_ptr() if with_norm else 0, space.data_ptr() if with_norm else 0, size), index)
     return norm
-
-
-def _address(data: bytes) -> int:
-    return C.cast(C.c_char_p(data), _vp).value
-
-
-def _scalar(grads):
-    return torch.empty((), dtype=torch.float32, device=grads[0].device)
 
 
 def grad_norm(grads):
     """The root of the sum of the squares of every element of `grads` (tensors of float32, bfloat16 and float16, any strides), a float32 scalar on their
     device.  Formed so that neither large nor small gradients leave what 32 bits hold on the way, in a fixed order."""
     grads = _listed(grads, "grads")
-    return _grads_call("halos_grad_norm", grads, None, 0.0, 0.0, _scalar(grads))
+    return _grads_call("halos_grad_norm", grads, None, 0.0, 0.0, True)
 
 
 def clip_grads(grads, max_norm: float, *, out=None):
@@ -805,7 +859,7 @@ def clip_grads(grads, max_norm: float, *, out=None):
     sizes and any of the types).  A norm that is NaN leaves them as they are."""
     grads = _listed(grads, "grads")
     outs = grads if out is None else _paired(_listed(out, "out"), grads)
-    return _grads_call("halos_clip_grads", grads, outs, max_norm, 0.0, _scalar(grads))
+    return _grads_call("halos_clip_grads", grads, outs, max_norm, 0.0, True)
 
 
 def sgd_step(params, grads, rate: float, *, max_norm: Optional[float] = None):
@@ -813,10 +867,10 @@ def sgd_step(params, grads, rate: float, *, max_norm: Optional[float] = None):
     None without max_norm.  The parameters may be of other types than the gradients, and detached if they are in a graph."""
     grads = _listed(grads, "grads")
     params = _paired(_listed(params, "params"), grads)
-    return _grads_call("halos_sgd_step", grads, params, 0.0 if max_norm is None else max_norm, rate, None if max_norm is None else _scalar(grads))
+    return _grads_call("halos_sgd_step", grads, params, 0.0 if max_norm is None else max_norm, rate, max_norm is not None)
 
 
 def _paired(tensors, grads):
-    if len(tensors) != len(grads) or any(x.shape != g.shape for x, g in zip(tensors, grads)):
+    if len(tensors) != len(grads) or list(map(_SHAPE_OF, tensors)) != list(map(_SHAPE_OF, grads)):
         _refuse("there must be one tensor for each gradient, of its shape")
     return tensors
