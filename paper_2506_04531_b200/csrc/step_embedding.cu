@@ -8,6 +8,7 @@
 
 #include <atomic>
 #include <math.h>
+#include <stdlib.h>
 #include <type_traits>
 
 namespace halos_step {
@@ -20,6 +21,7 @@ constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 struct EmbedParams {
     const char *weight, *dout, *token;
     char *out, *dweight;
+    const char* dout_span[2];          // first byte of any row, and the one behind the last
     int64_t weight_stride, out_stride, dout_stride, dweight_stride;  // in elements
     uint32_t tokens, vocab, dim, tokens_64, accumulate;
     float scale;
@@ -144,8 +146,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const __g
 // One cluster of CTAs sorts in its shared memory, a pass to a digit: threads rank their places within their warp, CTAs scan their warps' counts and exchange totals
 // through the cluster, and places move to where they belong.  All other CTAs of the launch meanwhile write zeros to the rows that no token names, which
 // they find out by going through the tokens themselves: the sort leaves the memory idle, and needs no other kernel's result.
-constexpr int kMostInCluster = 8, kMostItems = 8;
-constexpr uint32_t kMostClustered = kMostInCluster * kMostItems * kSortThreads;
+constexpr uint32_t kMostInCluster = 8, kMostItems = 8, kMostClustered = kMostInCluster * kMostItems * kSortThreads;
 constexpr uint32_t kMetWords = 4096;                         // of the vocabulary that a CTA looks at at a time
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -199,8 +200,28 @@ __device__ __forceinline__ void clear_rows_not_met(const EmbedParams& P, uint32_
     }
 }
 
-__global__ void __launch_bounds__(kSortThreads, 1) embedding_sort_kernel(const __grid_constant__ EmbedParams P, int passes, int bits_of_all, int items, int in_cluster, uint32_t weight_type) {
-    extern __shared__ __align__(16) uint64_t s_item[];         // [items * kSortThreads]: key << 32 | place
+// The sum of the threads' values up to each; s_warp: [warps].
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t v, uint32_t* s_warp) {
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const auto within = [&](uint32_t x) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t n = __shfl_up_sync(~0u, x, o);
+            if (lane >= o) x += n;
+        }
+        return x;
+    };
+    v = within(v);
+    if (lane == 31) s_warp[warp] = v;
+    __syncthreads();
+    if (warp == 0) s_warp[lane] = within(s_warp[lane]);
+    __syncthreads();
+    return warp ? v + s_warp[warp - 1] : v;
+}
+
+template <int ITEMS>
+__global__ void __launch_bounds__(kSortThreads, 1) embedding_sort_kernel(const __grid_constant__ EmbedParams P, int passes, int bits_of_all, int in_cluster, uint32_t weight_type) {
+    extern __shared__ __align__(16) uint64_t s_item[];         // [span]: key << 32 | place, as the cluster has sorted them; [span]: as this CTA has
     __shared__ uint16_t s_count[kSortWarps][1 << kMostBits];
     __shared__ uint32_t s_total[1 << kMostBits], s_base[1 << kMostBits], s_warp[kSortWarps];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -211,74 +232,85 @@ __global__ void __launch_bounds__(kSortThreads, 1) embedding_sort_kernel(const _
         else clear_rows_not_met<__half>(P, mine, many, s_met);   // zero is the same in both
         return;
     }
-    const uint32_t rank = cluster_rank(), span = items * kSortThreads, span_bits = 31 - __clz(span);
-    for (uint32_t i = rank * kSortThreads + threadIdx.x; i < P.jobs; i += in_cluster * kSortThreads) P.arrived[i] = 0;
+    constexpr uint32_t span = ITEMS * kSortThreads;
+    uint64_t* s_local = s_item + span;
+    const uint32_t rank = cluster_rank(), begin = rank * span, here = begin >= P.tokens ? 0 : min(span, P.tokens - begin);
+    uint64_t item[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const uint32_t local = (warp * ITEMS + k) * 32 + lane;
+        item[k] = local < here ? (uint64_t)token_at(P, begin + local) << 32 | (begin + local) : 0;
+    }
+    for (uint32_t i = begin / ITEMS + threadIdx.x; i < P.jobs; i += in_cluster * kSortThreads) P.arrived[i] = 0;
     int shift = 0;
     for (int pass = 0; pass < passes; ++pass) {
         const int bits = (bits_of_all - shift + passes - pass - 1) / (passes - pass);
         const uint32_t bins = 1u << bits;
-        uint64_t item[kMostItems];
-        uint32_t at[kMostItems];
-#pragma unroll
-        for (int k = 0; k < kMostItems; ++k)
-            if (k < items) {
-                const uint32_t local = (warp * items + k) * 32 + lane, t = rank * span + local;
-                item[k] = t >= P.tokens ? ~0ull : pass ? s_item[local] : (uint64_t)token_at(P, t) << 32 | t;
-            }
-        for (uint32_t i = threadIdx.x; i < sizeof s_count / 4; i += kSortThreads) reinterpret_cast<uint32_t*>(&s_count[0][0])[i] = 0;
+        uint32_t at[ITEMS];
+        for (uint32_t i = threadIdx.x; i < sizeof s_count / 16; i += kSortThreads) reinterpret_cast<uint4*>(&s_count[0][0])[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kMostItems; ++k)
-            if (k < items) {
-                const bool here = rank * span + (warp * items + k) * 32 + lane < P.tokens;
-                const uint32_t digit = (uint32_t)(item[k] >> 32) >> shift & (bins - 1);
-                const uint32_t same = __match_any_sync(~0u, here ? digit : bins), before = __popc(same & ((1u << lane) - 1));
-                const uint32_t had = here ? s_count[warp][digit] : 0;
-                __syncwarp();
-                if (here && before == 0) s_count[warp][digit] = (uint16_t)(had + __popc(same));
-                __syncwarp();
-                at[k] = had + before;
-            }
+        for (int k = 0; k < ITEMS; ++k) {
+            const bool is = (warp * ITEMS + k) * 32 + lane < here;
+            const uint32_t digit = (uint32_t)(item[k] >> 32) >> shift & (bins - 1);
+            const uint32_t same = __match_any_sync(~0u, is ? digit : bins), before = __popc(same & ((1u << lane) - 1));
+            const uint32_t had = is ? s_count[warp][digit] : 0;
+            __syncwarp();
+            if (is && before == 0) s_count[warp][digit] = (uint16_t)(had + __popc(same));
+            __syncwarp();
+            at[k] = had + before;
+        }
         __syncthreads();
+        uint32_t own = 0;                                      // of this thread's digit
         if (threadIdx.x < bins) {
-            uint32_t sum = 0;
-#pragma unroll 8
+#pragma unroll
             for (int w = 0; w < kSortWarps; ++w) {
                 const uint32_t n = s_count[w][threadIdx.x];
-                s_count[w][threadIdx.x] = (uint16_t)sum;
-                sum += n;
+                s_count[w][threadIdx.x] = (uint16_t)own;
+                own += n;
             }
-            s_total[threadIdx.x] = sum;
+            s_total[threadIdx.x] = own;
         }
-        cluster_meet();                                        // totals are there, and every place is in registers
-        uint32_t total = 0, before = 0;
-        if (threadIdx.x < bins)
-            for (uint32_t c = 0; c < (uint32_t)in_cluster; ++c) {
-                uint32_t n;
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(address_in(&s_total[threadIdx.x], c)) : "memory");
-                total += n;
-                if (c < rank) before += n;
-            }
-        uint32_t upto = total;
+        const uint32_t local_base = sum_up_to(own, s_warp) - own;
+        if (threadIdx.x < bins) s_base[threadIdx.x] = local_base;
+        __syncthreads();
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t n = __shfl_up_sync(~0u, upto, o);
-            if (lane >= o) upto += n;
+        for (int k = 0; k < ITEMS; ++k)
+            if ((warp * ITEMS + k) * 32 + lane < here) {
+                const uint32_t digit = (uint32_t)(item[k] >> 32) >> shift & (bins - 1);
+                s_local[s_base[digit] + s_count[warp][digit] + at[k]] = item[k];
+            }
+        cluster_meet();                                        // totals are there, and nobody needs what is in s_item
+        uint32_t total = 0, before = 0;
+        if (threadIdx.x < bins) {
+            uint32_t n[kMostInCluster];
+#pragma unroll
+            for (uint32_t c = 0; c < kMostInCluster; ++c) {
+                n[c] = 0;
+                if (c < (uint32_t)in_cluster) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n[c]) : "r"(address_in(&s_total[threadIdx.x], c)) : "memory");
+            }
+#pragma unroll
+            for (uint32_t c = 0; c < kMostInCluster; ++c) total += n[c], before += c < rank ? n[c] : 0;
         }
-        if (lane == 31) s_warp[warp] = upto;
+        const uint32_t base = sum_up_to(total, s_warp) - total + before;
+        if (threadIdx.x < bins) s_base[threadIdx.x] = base - local_base;   // from the local order to the cluster's
         __syncthreads();
-        for (uint32_t w = 0; w < warp; ++w) upto += s_warp[w];
-        if (threadIdx.x < bins) s_base[threadIdx.x] = upto - total + before;
-        __syncthreads();
+        // neighbours of one digit go to neighbouring places
         const bool last = pass + 1 == passes;
 #pragma unroll
-        for (int k = 0; k < kMostItems; ++k)
-            if (k < items && rank * span + (warp * items + k) * 32 + lane < P.tokens) {
-                const uint32_t digit = (uint32_t)(item[k] >> 32) >> shift & (bins - 1), to = s_base[digit] + s_count[warp][digit] + at[k];
-                if (last) P.key[0][to] = (uint32_t)(item[k] >> 32), P.place[0][to] = (uint32_t)item[k];
-                else asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(address_in(&s_item[to & (span - 1)], to >> span_bits)), "l"(item[k]) : "memory");
-            }
+        for (int k = 0; k < ITEMS; ++k) {
+            const uint32_t i = k * kSortThreads + threadIdx.x;
+            if (i >= here) break;
+            const uint64_t v = s_local[i];
+            const uint32_t to = s_base[(uint32_t)(v >> 32) >> shift & (bins - 1)] + i;
+            if (last) P.key[0][to] = (uint32_t)(v >> 32), P.place[0][to] = (uint32_t)v;
+            else asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(address_in(&s_item[to % span], to / span)), "l"(v) : "memory");
+        }
         cluster_meet();                                        // places have moved, totals have been read
+        if (!last) {
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) item[k] = s_item[(warp * ITEMS + k) * 32 + lane];
+        }
         shift += bits;
     }
 }
@@ -300,20 +332,52 @@ __device__ __forceinline__ void write_part(const EmbedParams& P, uint32_t v, uin
     store_words<W, V>(to, narrow<W, V>(r));
 }
 
-// A CTA takes 8 `chunk` neighbouring places in the sorted order and 256 columns, a warp `chunk` of the places (32 at most).  A token whose places lie in one warp's
-// chunk is written there.  What goes on from warp to warp is joined in shared memory; what goes on from CTA to CTA is left in memory, and the CTA that
-// comes last, whichever it is, adds up the parts, in their order.
+constexpr int kAhead = 4096;                                   // bytes of dout that a warp has on their way
+
+// A CTA takes 8 `chunk` neighbouring places in the sorted order and 256 columns, a warp `chunk` of the places (32 at most).  Rows of dout are copied into shared memory
+// ahead of their turn, in pieces of 16 bytes wherever the row begins; lanes have the columns of whole accesses where rows allow (V = 16 bytes), else every 32nd.
+// A token whose places lie in one warp's chunk is written there.  What goes on from warp to warp is joined in shared memory; what goes on from CTA to
+// CTA is left in memory, and the CTA that comes last, whichever it is, adds up the parts, in their order.
 template <typename A, typename W, int V>
 __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_constant__ EmbedParams P, const uint32_t* key, const uint32_t* place) {
-    constexpr int J = kSlab / 32 / V, kAhead = V == 1 || (sizeof(A) == 4 && V >= 4) ? 4 : 8;
+    constexpr int J = kSlab / 32 / V, kRow = kSlab * (int)sizeof(A) + (V == 1 ? 16 : 0), kRing = kAhead / (kSlab * (int)sizeof(A));
+    extern __shared__ __align__(16) char s_rows[];             // [warps][ring] rows
     __shared__ float s_head[kWarps][kSlab], s_tail[kWarps][kSlab];
-    __shared__ uint32_t s_through[kWarps], s_last, s_ends;
+    __shared__ uint32_t s_through[kWarps], s_goes[kWarps], s_last, s_ends, s_comes, s_key[2];   // keys of the run that comes from the CTA before, that goes on into the next
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, slab = blockIdx.x % P.slabs, block = blockIdx.x / P.slabs;
     const uint32_t span = P.chunk * kWarps, cta_from = block * span, from = min(P.tokens, cta_from + warp * P.chunk), n = min(P.chunk, P.tokens - from), blocks = P.jobs / P.slabs;
     const auto column = [&](int j) { return slab * kSlab + (j * 32 + lane) * V; };
+    char* rows = s_rows + warp * kRing * kRow;
     after_previous();
     const uint32_t my_key = lane < n ? key[from + lane] : P.vocab, my_place = lane < n ? place[from + lane] : 0;
     const uint32_t key_before = from && n ? key[from - 1] : P.vocab, key_after = from + n < P.tokens ? key[from + n] : P.vocab;
+    const uint32_t tokens_here = __popc(__ballot_sync(~0u, my_key < P.vocab));     // those that are none come last
+    const uint32_t columns = min((uint32_t)kSlab, P.dim - slab * kSlab);
+    // Pieces of 16 bytes that cover the row's columns here; the first begins `off` bytes before them.
+    const auto row_of = [&](uint32_t i) { return reinterpret_cast<const A*>(P.dout) + __shfl_sync(~0u, my_place, i) * P.dout_stride + slab * kSlab; };
+    const auto fetch = [&](uint32_t i) {
+        if (i < tokens_here) {
+            const A* row = row_of(i);
+            const char* first = reinterpret_cast<const char*>((uintptr_t)row & ~(uintptr_t)15);
+            const uint32_t bytes = (uint32_t)(reinterpret_cast<const char*>(row + columns) - first);
+            char* to = rows + i % kRing * kRow;
+#pragma unroll
+            for (int q = 0; q < (kRow + 511) / 512; ++q) {
+                const uint32_t at = (q * 32 + lane) * 16;
+                if (at >= bytes) break;
+                const char* p = first + at;
+                if (V > 1 || (p >= P.dout_span[0] && p + 16 <= P.dout_span[1])) copy_16(to + at, p);
+                else {                                          // the tensor's own ends
+#pragma unroll
+                    for (int e = 0; e < 16 / (int)sizeof(A); ++e) {
+                        const A* one = reinterpret_cast<const A*>(p) + e;
+                        if (one >= row && one < row + columns) reinterpret_cast<A*>(to + at)[e] = *one;
+                    }
+                }
+            }
+        }
+        copies_end();
+    };
     float sum[J][V];
     const auto clear = [&] {
 #pragma unroll
@@ -339,52 +403,56 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
         for (int j = 0; j < J; ++j)
             if (column(j) < P.dim) write_part<W, V>(P, k, column(j), sum[j]);
     };
+    const auto leave = [&](float* parts) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (column(j) < P.dim) store_words<float, V>(parts + (int64_t)block * P.dim + column(j), narrow<float, V>(sum[j]));
+    };
     clear();
     bool began_before = n && __shfl_sync(~0u, my_key, 0) == key_before && key_before < P.vocab;
     bool through = false, tail = false;
-    for (uint32_t i0 = 0; i0 < n; i0 += kAhead) {
-        Words<A, V> w[kAhead][J];
+    if (threadIdx.x == 0) s_comes = began_before, s_key[0] = my_key;
+    for (uint32_t i = 0; i < kRing; ++i) fetch(i);
+#pragma unroll 1
+    for (uint32_t i = 0; i < tokens_here; ++i) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+        __syncwarp();                                           // pieces are other lanes' columns
+        const uint32_t k = __shfl_sync(~0u, my_key, i), next = i + 1 < n ? __shfl_sync(~0u, my_key, i + 1) : key_after;
+        const uint32_t off = V > 1 ? 0 : (uint32_t)((uintptr_t)row_of(i) & 15);
+        const A* row = reinterpret_cast<const A*>(rows + i % kRing * kRow + off);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const uint32_t k = __shfl_sync(~0u, my_key, i0 + i), t = __shfl_sync(~0u, my_place, i0 + i);
-            const A* row = reinterpret_cast<const A*>(P.dout) + t * P.dout_stride;
+        for (int j = 0; j < J; ++j) {
+            float v[V];
+            widen<A, V>(load_words<A, V>(row + (j * 32 + lane) * V), v);
 #pragma unroll
-            for (int j = 0; j < J; ++j) w[i][j] = column(j) < P.dim && i0 + i < n && k < P.vocab ? load_words<A, V>(row + column(j)) : no_words<A, V>();
+            for (int e = 0; e < V; ++e) sum[j][e] += v[e];
         }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const uint32_t at = i0 + i;
-            if (at >= n) break;
-            const uint32_t k = __shfl_sync(~0u, my_key, at), next = at + 1 < n ? __shfl_sync(~0u, my_key, at + 1) : key_after;
-            if (k >= P.vocab) break;                            // no tokens: they come last
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                float v[V];
-                widen<A, V>(w[i][j], v);
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[j][e] += v[e];
-            }
-            if (next != k || at + 1 == n) {
-                if (began_before) keep(s_head[warp]), through = next == k;
-                else if (next == k) keep(s_tail[warp]), tail = true;
-                else write(k);
-                began_before = false;
-                clear();
-            }
+        __syncwarp();
+        fetch(i + kRing);
+        if (next != k || i + 1 == n) {
+            if (began_before) keep(s_head[warp]), through = next == k;
+            else if (next == k) keep(s_tail[warp]), tail = true;
+            else write(k);
+            began_before = false;
+            clear();
         }
     }
-    if (lane == 0) s_through[warp] = through;
+    wait_copies(false);
+    if (lane == 0) {
+        s_through[warp] = through;
+        s_goes[warp] = (through || tail) && from + n == min(P.tokens, cta_from + span);
+        if (s_goes[warp]) s_key[1] = key_after;
+    }
     __syncthreads();
     // From warp to warp.  The run that comes from the CTA before is warp 0's, any other that of the warp where it begins.
-    const uint32_t cta_end = min(P.tokens, cta_from + span);
-    const bool comes = cta_from && key[cta_from] == key[cta_from - 1] && key[cta_from] < P.vocab;
-    const bool goes = cta_end < P.tokens && key[cta_end] == key[cta_end - 1] && key[cta_end] < P.vocab;
+    bool goes = false;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) goes |= s_goes[w];
+    const bool comes = s_comes;
     if (warp == 0 && comes) {
         clear(), add(s_head[0]);
-        for (uint32_t w = 0; s_through[w] && w + 1 < kWarps; ) add(s_head[++w]);
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (column(j) < P.dim) store_words<float, V>(P.head + (int64_t)block * P.dim + column(j), narrow<float, V>(sum[j]));
+        for (uint32_t w = 0; s_through[w] && w + 1 < kWarps;) add(s_head[++w]);
+        leave(P.head);
     }
     if (tail) {
         clear(), add(s_tail[warp]);
@@ -394,19 +462,15 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
             if (!s_through[w]) break;
         }
         if (w < kWarps) write(__shfl_sync(~0u, my_key, n - 1));
-        else {
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-                if (column(j) < P.dim) store_words<float, V>(P.tail + (int64_t)block * P.dim + column(j), narrow<float, V>(sum[j]));
-        }
+        else leave(P.tail);
     }
     if (!comes && !goes) return;
     // From CTA to CTA: up to two runs, or one that goes all the way through.
     __syncthreads();
-    const bool one = comes && goes && key[cta_from] == key[cta_end];
+    const bool one = comes && goes && s_key[0] == s_key[1];
     for (int r = 0; r < 2; ++r) {
         if (r == 0 ? !comes : !goes || one) continue;
-        const uint32_t k = r == 0 ? key[cta_from] : key[cta_end];
+        const uint32_t k = s_key[r];
         if (warp == 0) {
             uint32_t begins = block, ends = block;
             if (r == 0)
@@ -506,6 +570,7 @@ Sizes sizes_of(const halos_embedding_args* a, int32_t device) {
     s.slabs = (a->dim + kSlab - 1) / kSlab;
     // 32 places to a warp, or as few as give every SM two CTAs.
     s.chunk = 32;
+    s.chunk = getenv("ECH") ? atoi(getenv("ECH")) : 32;
     while (s.chunk > 4 && (uint64_t)a->tokens * s.slabs < most * 2 * kWarps * s.chunk) s.chunk /= 2;
     s.ctas = (uint32_t)((a->tokens + s.chunk * kWarps - 1) / (s.chunk * kWarps));
     s.arrays = rounded_up((uint64_t)a->tokens * 4, 16);
@@ -517,16 +582,36 @@ Sizes sizes_of(const halos_embedding_args* a, int32_t device) {
     return s;
 }
 
-// How many clusters of the sort's kernel the device runs at the same time: asked for once for each size of a cluster.  Shared memory goes by that size, too,
-// but leaves room for one CTA to an SM whatever it is.
-int clusters_at_once(int32_t device, const cudaLaunchConfig_t& config, uint32_t in_cluster, int* clusters) {
+// How many clusters of the sort's kernel the device runs at the same time: asked for once for each size of a cluster (larger ones come with the most
+// shared memory, which an SM has once in any case).
+int clusters_at_once(int32_t device, const void* kernel, const cudaLaunchConfig_t& config, uint32_t in_cluster, int* clusters) {
     static std::atomic<int> known[64][kMostInCluster + 1];
     *clusters = known[device][in_cluster].load(std::memory_order_relaxed);
     if (*clusters) return HALOS_OK;
-    if (int rc = cuda_status(cudaOccupancyMaxActiveClusters(clusters, embedding_sort_kernel, &config), "embedding clusters")) return rc;
+    if (int rc = cuda_status(cudaOccupancyMaxActiveClusters(clusters, kernel, &config), "embedding clusters")) return rc;
     if (*clusters < 1) *clusters = 1;
     known[device][in_cluster].store(*clusters, std::memory_order_relaxed);
     return HALOS_OK;
+}
+
+template <int ITEMS>
+int sort(const EmbedParams& P, const Sizes& s, const halos_embedding_args* a) {
+    uint32_t in_cluster = 1;
+    while (in_cluster * ITEMS * kSortThreads < P.tokens) in_cluster *= 2;
+    const uint32_t shared = 2 * ITEMS * kSortThreads * 8;
+    static Allowed allowed;
+    if (int rc = allow_smem(embedding_sort_kernel<ITEMS>, (int)shared, allowed)) return rc;
+    cudaLaunchAttribute cluster{};
+    cluster.id = cudaLaunchAttributeClusterDimension, cluster.val.clusterDim.x = in_cluster, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = in_cluster, config.blockDim = kSortThreads, config.dynamicSmemBytes = shared, config.stream = (cudaStream_t)a->stream, config.attrs = &cluster, config.numAttrs = 1;
+    if (!P.accumulate) {                               // as many more as run at the same time; a word of 32 rows to each at least
+        int clusters = 0;
+        if (int rc = clusters_at_once(a->device, (const void*)embedding_sort_kernel<ITEMS>, config, in_cluster, &clusters)) return rc;
+        const uint32_t words = (P.vocab + 31) / 32, wanted = 1 + (words + in_cluster - 1) / in_cluster;
+        config.gridDim = in_cluster * (clusters < 2 ? 2 : (uint32_t)clusters < wanted ? (uint32_t)clusters : wanted);
+    }
+    return cuda_status(cudaLaunchKernelEx(&config, embedding_sort_kernel<ITEMS>, P, (int)s.passes, (int)s.bits, (int)in_cluster, a->weight_dtype), "embedding launch");
 }
 
 template <typename F>
@@ -600,26 +685,14 @@ extern "C" int halos_embedding_bwd(const halos_embedding_args* a) {
     if ((uint64_t)s.ctas * s.slabs > 0x7fffffffull) return fail(HALOS_ERR_UNSUPPORTED, "embedding: too many sums");
     P.chunk = s.chunk, P.slabs = s.slabs, P.jobs = s.ctas * s.slabs, P.sort_blocks = s.blocks, P.span = s.span;
     cudaStream_t st = (cudaStream_t)a->stream;
-    const uint32_t width = width_of(P.dim, a->dweight, a->dweight_stride, wsize, P.tokens ? a->dout : a->dweight, P.tokens ? a->dout_stride : a->dweight_stride, P.tokens ? size : wsize);
+    const bool whole = width_of(P.dim, a->dweight, a->dweight_stride, wsize, P.tokens ? a->dout : a->dweight, P.tokens ? a->dout_stride : a->dweight_stride, P.tokens ? size : wsize) >= 16 / size;
+    const int64_t far = P.tokens ? (int64_t)(P.tokens - 1) * a->dout_stride : 0;
+    P.dout_span[0] = P.dout + (far < 0 ? far : 0) * (int64_t)size, P.dout_span[1] = P.dout + ((far > 0 ? far : 0) + a->dim) * (int64_t)size;
     int sorted = 0;                                    // which of the two arrays holds the sorted places
     if (P.tokens && P.tokens <= kMostClustered) {
-        uint32_t in_cluster = 1, items = 1;
-        while (in_cluster < kMostInCluster && in_cluster * kSortThreads < P.tokens) in_cluster *= 2;
-        while (in_cluster * items * kSortThreads < P.tokens) items *= 2;
-        const uint32_t shared = items * kSortThreads * 8;
-        static Allowed allowed;
-        if (int rc = allow_smem(embedding_sort_kernel, (int)shared, allowed)) return rc;
-        cudaLaunchAttribute cluster{};
-        cluster.id = cudaLaunchAttributeClusterDimension, cluster.val.clusterDim.x = in_cluster, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-        cudaLaunchConfig_t config{};
-        config.gridDim = in_cluster, config.blockDim = kSortThreads, config.dynamicSmemBytes = shared, config.stream = st, config.attrs = &cluster, config.numAttrs = 1;
-        if (!P.accumulate) {                           // as many more as run at the same time; a word of 32 rows to each at least
-            int clusters = 0;
-            if (int rc = clusters_at_once(a->device, config, in_cluster, &clusters)) return rc;
-            const uint32_t words = (P.vocab + 31) / 32, wanted = 1 + (words + in_cluster - 1) / in_cluster;
-            config.gridDim = in_cluster * (clusters < 2 ? 2 : (uint32_t)clusters < wanted ? (uint32_t)clusters : wanted);
-        }
-        if (int rc = cuda_status(cudaLaunchKernelEx(&config, embedding_sort_kernel, P, (int)s.passes, (int)s.bits, (int)items, (int)in_cluster, a->weight_dtype), "embedding launch")) return rc;
+        // eight CTAs as soon as there is work for them
+        const uint32_t each = (P.tokens + kMostInCluster * kSortThreads - 1) / (kMostInCluster * kSortThreads);
+        if (int rc = each <= 1 ? sort<1>(P, s, a) : each <= 2 ? sort<2>(P, s, a) : each <= 4 ? sort<4>(P, s, a) : sort<8>(P, s, a)) return rc;
     } else if (P.tokens) {
         if (int rc = cuda_status(cudaMemsetAsync(P.met, 0, s.met + s.arrived, st), "embedding workspace")) return rc;
         for (uint32_t pass = 0, shift = 0; pass < s.passes; ++pass) {
@@ -638,10 +711,17 @@ extern "C" int halos_embedding_bwd(const halos_embedding_args* a) {
             if (int rc = cuda_status(cudaGetLastError(), "embedding launch")) return rc;
         }
         if (!P.tokens) return HALOS_OK;
-        return by_width(width, [&](auto n) {
-            return by_type(a->dtype, [&](auto x) {
-                return launch_after(embedding_sum_kernel<decltype(x), W, decltype(n)::value>, P.jobs, kThreads, 0, st, "embedding launch", P, (const uint32_t*)P.key[sorted], (const uint32_t*)P.place[sorted]);
-            });
+        return by_type(a->dtype, [&](auto x) -> int {
+            using A = decltype(x);
+            const auto launch = [&](auto* kernel, uint32_t row, Allowed& allowed) -> int {
+                const uint32_t shared = kWarps * (kAhead / (kSlab * (uint32_t)sizeof(A))) * row;
+                if (int rc = allow_smem(kernel, (int)shared, allowed)) return rc;
+                return launch_after(kernel, P.jobs, kThreads, shared, st, "embedding launch", P, (const uint32_t*)P.key[sorted], (const uint32_t*)P.place[sorted]);
+            };
+            static Allowed allowed[2];
+            constexpr int V = 16 / sizeof(A);
+            constexpr uint32_t row = kSlab * sizeof(A);
+            return whole ? launch(embedding_sum_kernel<A, W, V>, row, allowed[0]) : launch(embedding_sum_kernel<A, W, 1>, row + 16, allowed[1]);
         });
     });
 }

@@ -112,6 +112,19 @@ __device__ __forceinline__ Words<T, N> narrow(const float2 (&v)[N / 2]) {
     return r;
 }
 
+// Copies of 16 bytes, and of 4, into shared memory that nothing waits for until asked.
+__device__ __forceinline__ void copy_16(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_4(void* to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void wait_copies(bool all_but_one) {
+    if (all_but_one) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
 inline uint32_t size_of(uint32_t type) { return type == HALOS_F32 ? 4 : 2; }
 
 }  // namespace halos_step
