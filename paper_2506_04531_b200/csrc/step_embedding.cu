@@ -8,7 +8,6 @@
 
 #include <atomic>
 #include <math.h>
-#include <stdlib.h>
 #include <type_traits>
 
 namespace halos_step {
@@ -200,6 +199,19 @@ __device__ __forceinline__ void clear_rows_not_met(const EmbedParams& P, uint32_
     }
 }
 
+// The threads of the warp with this one's digit, among those where `is`: by its bits, which costs less than to look for equal values at once (31 us a sort of
+// 65536 places with __match_any_sync).
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits, bool is) {
+    uint32_t same = __ballot_sync(~0u, is);
+#pragma unroll
+    for (int b = 0; b < kMostBits; ++b)
+        if (b < bits) {
+            const uint32_t set = __ballot_sync(~0u, digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+    return same;
+}
+
 // The sum of the threads' values up to each; s_warp: [warps].
 __device__ __forceinline__ uint32_t sum_up_to(uint32_t v, uint32_t* s_warp) {
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -253,7 +265,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) embedding_sort_kernel(const _
         for (int k = 0; k < ITEMS; ++k) {
             const bool is = (warp * ITEMS + k) * 32 + lane < here;
             const uint32_t digit = (uint32_t)(item[k] >> 32) >> shift & (bins - 1);
-            const uint32_t same = __match_any_sync(~0u, is ? digit : bins), before = __popc(same & ((1u << lane) - 1));
+            const uint32_t same = same_digit(digit, bits, is), before = __popc(same & ((1u << lane) - 1));
             const uint32_t had = is ? s_count[warp][digit] : 0;
             __syncwarp();
             if (is && before == 0) s_count[warp][digit] = (uint16_t)(had + __popc(same));
@@ -353,31 +365,39 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
     const uint32_t key_before = from && n ? key[from - 1] : P.vocab, key_after = from + n < P.tokens ? key[from + n] : P.vocab;
     const uint32_t tokens_here = __popc(__ballot_sync(~0u, my_key < P.vocab));     // those that are none come last
     const uint32_t columns = min((uint32_t)kSlab, P.dim - slab * kSlab);
-    // Pieces of 16 bytes that cover the row's columns here; the first begins `off` bytes before them.
-    const auto row_of = [&](uint32_t i) { return reinterpret_cast<const A*>(P.dout) + __shfl_sync(~0u, my_place, i) * P.dout_stride + slab * kSlab; };
+    const A* here = reinterpret_cast<const A*>(P.dout) + slab * kSlab;
+    const auto row_of = [&](uint32_t i) { return here + __shfl_sync(~0u, my_place, i) * P.dout_stride; };
     const auto fetch = [&](uint32_t i) {
         if (i < tokens_here) {
             const A* row = row_of(i);
-            const char* first = reinterpret_cast<const char*>((uintptr_t)row & ~(uintptr_t)15);
-            const uint32_t bytes = (uint32_t)(reinterpret_cast<const char*>(row + columns) - first);
             char* to = rows + i % kRing * kRow;
+            if constexpr (V > 1) {                              // each lane its own columns
 #pragma unroll
-            for (int q = 0; q < (kRow + 511) / 512; ++q) {
-                const uint32_t at = (q * 32 + lane) * 16;
-                if (at >= bytes) break;
-                const char* p = first + at;
-                if (V > 1 || (p >= P.dout_span[0] && p + 16 <= P.dout_span[1])) copy_16(to + at, p);
-                else {                                          // the tensor's own ends
+                for (int j = 0; j < J; ++j)
+                    if (column(j) < P.dim) copy_16(to + (j * 32 + lane) * 16, row + (j * 32 + lane) * V);
+            } else {                                            // pieces of 16 bytes that cover the columns; the first begins up to 15 bytes before them
+                const char* first = reinterpret_cast<const char*>((uintptr_t)row & ~(uintptr_t)15);
+                const uint32_t bytes = (uint32_t)(reinterpret_cast<const char*>(row + columns) - first);
 #pragma unroll
-                    for (int e = 0; e < 16 / (int)sizeof(A); ++e) {
-                        const A* one = reinterpret_cast<const A*>(p) + e;
-                        if (one >= row && one < row + columns) reinterpret_cast<A*>(to + at)[e] = *one;
+                for (int q = 0; q < (kRow + 511) / 512; ++q) {
+                    const uint32_t at = (q * 32 + lane) * 16;
+                    if (at >= bytes) break;
+                    const char* p = first + at;
+                    if (p >= P.dout_span[0] && p + 16 <= P.dout_span[1]) copy_16(to + at, p);
+                    else {                                      // the tensor's own ends
+#pragma unroll
+                        for (int e = 0; e < 16 / (int)sizeof(A); ++e) {
+                            const A* one = reinterpret_cast<const A*>(p) + e;
+                            if (one >= row && one < row + columns) reinterpret_cast<A*>(to + at)[e] = *one;
+                        }
                     }
                 }
             }
         }
         copies_end();
     };
+    // A bit for each place that is its token's last in this chunk.
+    const uint32_t next_key = __shfl_down_sync(~0u, my_key, 1), ends_here = __ballot_sync(~0u, lane + 1 >= n || next_key != my_key);
     float sum[J][V];
     const auto clear = [&] {
 #pragma unroll
@@ -416,22 +436,33 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
 #pragma unroll 1
     for (uint32_t i = 0; i < tokens_here; ++i) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
-        __syncwarp();                                           // pieces are other lanes' columns
-        const uint32_t k = __shfl_sync(~0u, my_key, i), next = i + 1 < n ? __shfl_sync(~0u, my_key, i + 1) : key_after;
-        const uint32_t off = V > 1 ? 0 : (uint32_t)((uintptr_t)row_of(i) & 15);
-        const A* row = reinterpret_cast<const A*>(rows + i % kRing * kRow + off);
+        const char* from_row = rows + i % kRing * kRow;
+        if constexpr (V > 1) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            float v[V];
-            widen<A, V>(load_words<A, V>(row + (j * 32 + lane) * V), v);
+            for (int j = 0; j < J; ++j) {
+                float2 v[V / 2];
+                if (column(j) < P.dim) {
+                    widen<A, V>(load_words<A, V>(reinterpret_cast<const A*>(from_row) + (j * 32 + lane) * V), v);
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum[j][e] += v[e];
+                    for (int e = 0; e < V / 2; ++e) {
+                        const float2 t = add2(make_float2(sum[j][2 * e], sum[j][2 * e + 1]), v[e]);
+                        sum[j][2 * e] = t.x, sum[j][2 * e + 1] = t.y;
+                    }
+                }
+            }
+        } else {
+            __syncwarp();                                       // pieces are other lanes' columns
+            const A* row = reinterpret_cast<const A*>(from_row + ((uintptr_t)row_of(i) & 15));
+#pragma unroll
+            for (int j = 0; j < J; ++j) sum[j][0] += to_f32<A>(row[j * 32 + lane]);
+            __syncwarp();
         }
-        __syncwarp();
         fetch(i + kRing);
-        if (next != k || i + 1 == n) {
-            if (began_before) keep(s_head[warp]), through = next == k;
-            else if (next == k) keep(s_tail[warp]), tail = true;
+        if (ends_here >> i & 1) {
+            const uint32_t k = __shfl_sync(~0u, my_key, i);
+            const bool on = i + 1 == n && key_after == k;       // goes on behind the chunk
+            if (began_before) keep(s_head[warp]), through = on;
+            else if (on) keep(s_tail[warp]), tail = true;
             else write(k);
             began_before = false;
             clear();
@@ -570,7 +601,6 @@ Sizes sizes_of(const halos_embedding_args* a, int32_t device) {
     s.slabs = (a->dim + kSlab - 1) / kSlab;
     // 32 places to a warp, or as few as give every SM two CTAs.
     s.chunk = 32;
-    s.chunk = getenv("ECH") ? atoi(getenv("ECH")) : 32;
     while (s.chunk > 4 && (uint64_t)a->tokens * s.slabs < most * 2 * kWarps * s.chunk) s.chunk /= 2;
     s.ctas = (uint32_t)((a->tokens + s.chunk * kWarps - 1) / (s.chunk * kWarps));
     s.arrays = rounded_up((uint64_t)a->tokens * 4, 16);
