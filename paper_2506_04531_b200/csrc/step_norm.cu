@@ -127,14 +127,14 @@ __global__ void __launch_bounds__(kThreads) rms_norm_any_kernel(const __grid_con
 
 // ------------------------------------------------------------------------------------------------ rows that a CTA holds
 
-template <typename T, int N, Mode M, bool QUANTIZED, int ARRAYS>
+template <typename T, int N, int L, Mode M, bool QUANTIZED, int ARRAYS>
 __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWide<T, N, M> ? 1 : 4) rms_norm_kernel(const __grid_constant__ Params P) {
-    using A = Threads<T, N, M, kWide<T, N, M> ? kMostThreads : kThreads, ARRAYS>;
+    using A = Threads<T, N, L, M, kWide<T, N, M> ? kMostThreads : kThreads, ARRAYS>;
     constexpr int V = A::V, H = A::H;
     extern __shared__ __align__(16) char s_dynamic[];
     __shared__ uint32_t s_part[2 * kMostThreads / 32];
     const A t(P, s_dynamic, false);
-    RowSums<(N > 1)> S(t.lanes, s_part);
+    RowSums<(N > 1 && L == 32)> S(t.lanes, s_part);
     const int stages = (int)P.stages, dim = t.dim;
     constexpr bool added = ARRAYS > 1;
     for (int k = 0; k < stages - 1; ++k) t.fetch(k, k, false);
@@ -355,10 +355,10 @@ Mode mode_of(const Params& P, uint32_t size, uint32_t outs, uint32_t out_size) {
     return whole ? kWhole : alike ? kShifted : kLoose;
 }
 
-static Shape shape_of(const Params& P, uint32_t size, Mode mode, uint32_t groups) {
+static Shape shape_of(const Params& P, uint32_t size, Mode mode, uint32_t groups, uint32_t least) {
     const uint32_t v = mode == kLoose ? 2 : 16 / size, accesses = accesses_of(P.dim, v, mode);
     Shape s{};
-    spread_over(s, P.dim, v, mode, accesses);
+    spread_over(s, v, mode, accesses, least);
     if (!s.n) return s;
     const bool wide = s.n * v > kFew;
     s.threads = wide ? kMostThreads : kThreads, s.resident = wide ? 1 : 4;
@@ -394,7 +394,7 @@ extern "C" int halos_rms_norm_fwd(const halos_rms_norm_args* a) {
     if (int rc = enter(a->device)) return rc;
     cudaStream_t st = (cudaStream_t)a->stream;
     const Mode mode = mode_of(P, size, P.arrays, a->quantized ? 1 : size);
-    const Shape s = shape_of(P, size, mode, a->quantized && mode != kWhole ? P.groups : 0);
+    const Shape s = shape_of(P, size, mode, a->quantized && mode != kWhole ? P.groups : 0, a->quantized && P.group < P.dim ? P.group * size / 16 : 1);
     return by_type(a->dtype, [&](auto t) -> int {
         using T = decltype(t);
         if (!s.n) {
@@ -407,17 +407,17 @@ extern "C" int halos_rms_norm_fwd(const halos_rms_norm_args* a) {
         const uint32_t room = (uint32_t)sm_count(a->device) * s.resident, once = (P.row_blocks + room - 1) / room, long_run = P.row_blocks * 2 / (room * 7);
         P.apart = mode == kShifted && s.per() < 8 ? 8 / s.per() : 1, P.run = long_run > 4 ? long_run : once < 4 ? once : 4;
         const uint32_t grid = (P.row_blocks + P.apart * P.run - 1) / (P.apart * P.run) * P.apart;
-        return by_accesses<T>(s.n, mode, [&](auto n, auto m) -> int {
+        return by_accesses<T>(s.n, s.apart, mode, [&](auto n, auto l, auto m) -> int {
             const auto launch = [&](auto* kernel, Allowed& allowed) -> int {
                 if (int rc = allow_smem(kernel, (int)s.shared, allowed)) return rc;
                 kernel<<<grid, s.threads, s.shared, st>>>(P);
                 return cuda_status(cudaGetLastError(), "norm launch");
             };
             static Allowed allowed[4];
-            constexpr int N = decltype(n)::value;
+            constexpr int N = decltype(n)::value, L = decltype(l)::value;
             constexpr Mode M = decltype(m)::value;
-            if (P.arrays > 1) return a->quantized ? launch(rms_norm_kernel<T, N, M, true, 2>, allowed[0]) : launch(rms_norm_kernel<T, N, M, false, 2>, allowed[1]);
-            return a->quantized ? launch(rms_norm_kernel<T, N, M, true, 1>, allowed[2]) : launch(rms_norm_kernel<T, N, M, false, 1>, allowed[3]);
+            if (P.arrays > 1) return a->quantized ? launch(rms_norm_kernel<T, N, L, M, true, 2>, allowed[0]) : launch(rms_norm_kernel<T, N, L, M, false, 2>, allowed[1]);
+            return a->quantized ? launch(rms_norm_kernel<T, N, L, M, true, 1>, allowed[2]) : launch(rms_norm_kernel<T, N, L, M, false, 1>, allowed[3]);
         });
     });
 }

@@ -105,9 +105,9 @@ __device__ __forceinline__ void store_part(T* row, int c, int dim, const float2 
 constexpr uint32_t kMostStages = 3;
 
 // A thread's part of rows.  What it will need is copied to places of its own in shared memory while it works on the rows before: registers would hold
-// half of what has to be on its way.  Threads of one warp at most have one access each (N = 1); whole warps have N, 32 accesses apart, so that all
-// addresses but a row's first are constants.
-template <typename T, int N, Mode M, int THREADS, int ARRAYS>
+// half of what has to be on its way.  A thread's N accesses are L apart, so that all addresses but a row's first are constants: rows of whole warps have
+// L = 32, short ones L = 4 or 8 threads (or, with N = 1, any number).
+template <typename T, int N, int L, Mode M, int THREADS, int ARRAYS>
 struct Threads {
     static constexpr int V = kVector<T, M>, H = V / 2, kAccess = V * (int)sizeof(T);
     static constexpr int kArray = N * THREADS * kAccess, kStage = ARRAYS * kArray;          // bytes
@@ -127,7 +127,7 @@ struct Threads {
         own = lanes < 32 ? threadIdx.x % 32 / lanes * (THREADS / 32) + threadIdx.x / 32 : threadIdx.x / lanes;
         from = blockIdx.x / P.apart * P.apart * P.run + blockIdx.x % P.apart;
         off = M == kShifted ? (int)((uintptr_t)(reinterpret_cast<T*>(P.in[0].at) + (int64_t)row_of(0) * P.in[0].stride[0]) / sizeof(T) % V) : 0;  // of rows that are not there, too
-        first = (int)(lane / 32 * N * 32 + lane % 32) * V - off;
+        first = (int)(lane / L * N * L + lane % L) * V - off;
         mine = shared + threadIdx.x * kAccess;
         float* behind = reinterpret_cast<float*>(shared + P.stages * kStage);
         rstd = behind + threadIdx.x;
@@ -136,10 +136,10 @@ struct Threads {
         weight = behind + (M == kShifted ? threadIdx.x * kPart : first / V * kPart);
     }
     __device__ __forceinline__ bool leads() const { return threadIdx.x % lanes == 0; }
-    __device__ __forceinline__ int column(int j) const { return first + j * 32 * V; }
+    __device__ __forceinline__ int column(int j) const { return first + j * L * V; }
 
     // kShifted: [N][parts][threads] of kPart floats; else [parts][accesses], for all rows
-    __device__ __forceinline__ float* weight_at_part(int j, int p) const { return M == kShifted ? weight + (j * kParts + p) * THREADS * kPart : weight + p * weight_step + j * 32 * kPart; }
+    __device__ __forceinline__ float* weight_at_part(int j, int p) const { return M == kShifted ? weight + (j * kParts + p) * THREADS * kPart : weight + p * weight_step + j * L * kPart; }
     __device__ __forceinline__ void load_weights() const {
         if (M == kShifted || threadIdx.x < lanes) {
 #pragma unroll
@@ -172,7 +172,7 @@ struct Threads {
                 const T* at = from + first;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const char* p = reinterpret_cast<const char*>(at + j * 32 * V);
+                    const char* p = reinterpret_cast<const char*>(at + j * L * V);
                     char* t = to + array * kArray + j * THREADS * kAccess;
                     if (column(j) >= dim) continue;
                     if (M == kWhole || (M == kShifted && p >= R.span[0] && p + 16 <= R.span[1])) copy_16(t, p);
@@ -183,11 +183,13 @@ struct Threads {
         }
         copies_end();
     }
-    // An access that has arrived, as floats; 0 where there is none.
+    // An access that has arrived, as floats; 0 where there is none, and (OWN) where it is not the row's.
+    template <bool OWN = true>
     __device__ __forceinline__ void arrived(int stage, int array, int j, bool here, float2 (&v)[H]) const {
         Words<T, V> w = no_words<T, V>();
         if (here && column(j) < dim) w = load_words<T, V>(reinterpret_cast<const T*>(mine + stage * kStage + array * kArray + j * THREADS * kAccess));
-        widen<T, V>(w, v), keep_own<V, M>(v, column(j), dim);
+        widen<T, V>(w, v);
+        if (OWN) keep_own<V, M>(v, column(j), dim);
     }
 };
 
@@ -247,7 +249,7 @@ struct RowSums {
 
 // How rows are spread over threads, and how many of the CTAs an SM holds.  n = 0: no CTA holds such rows.
 struct Shape {
-    uint32_t n, lanes, threads, resident, stages, shared;
+    uint32_t n, lanes, apart, threads, resident, stages, shared;   // apart: a thread's accesses
     uint32_t per() const { return threads / lanes; }
 };
 
@@ -260,24 +262,33 @@ inline void set(Rows& R, const void* at, const int64_t (&stride)[3]) {
     for (int i = 0; i < 3; ++i) R.stride[i] = stride[i];
 }
 
-// Rows of `accesses`: up to 32 of them take a thread each, more take whole warps with N accesses to a thread, few first.
+// Rows of many accesses take whole warps with N accesses to a thread, few first.
 inline void spread_over(Shape& s, uint32_t accesses, uint32_t v, Mode mode, uint32_t elements, uint32_t most_lanes, uint32_t above) {
     if (s.n) return;
-    if (accesses <= 32) {
-        for (s.n = 1, s.lanes = 4; s.lanes < accesses;) s.lanes *= 2;
-        return;
-    }
-    for (uint32_t n : {16u, 8u, 6u, 4u, 3u, 2u, 1u})
+    s.apart = 32;
+    for (uint32_t n : {2u, 3u, 1u, 4u, 6u, 8u, 16u})   // of equals the first
         if (n * v <= elements && n * v > above && !(mode == kLoose && (n == 6 || n == 3)))
             for (uint32_t lanes = 32; lanes <= most_lanes; lanes *= 2)
                 if (lanes * n >= accesses && (!s.n || lanes * n < s.lanes * s.n)) s.n = n, s.lanes = lanes;
 }
+// Rows of up to 32 accesses: 4 or 8 threads with two or three each where rows are whole (what a row costs beside its accesses then falls on few threads: 410000 rows of
+// 56 f32 in 8 bits 70 us with a thread to an access, 55 us with eight of them), else a thread to an access.  `least` threads stay neighbours.
+inline void spread_short(Shape& s, uint32_t accesses, Mode mode, uint32_t least) {
+    if (mode == kWhole)
+        for (uint32_t lanes : {4u, 8u})
+            for (uint32_t n : {2u, 3u})
+                if (lanes >= least && lanes * n >= accesses && lanes < accesses && (!s.n || lanes * n < s.lanes * s.n)) s.n = n, s.lanes = s.apart = lanes;
+    if (s.n) return;
+    for (s.n = 1, s.apart = 32, s.lanes = 4; s.lanes < accesses;) s.lanes *= 2;
+}
+
 // One warp to a row where that takes kFew elements to a thread at most, else warps with few accesses to a thread: what they cost at the barrier is
 // less than what long threads cost in registers (2048 bf16: two accesses to each of 128 threads 47 us, eight to each of 32 51 us).
 constexpr uint32_t kFew = 24;
-inline void spread_over(Shape& s, uint32_t dim, uint32_t v, Mode mode, uint32_t accesses) {
+inline void spread_over(Shape& s, uint32_t v, Mode mode, uint32_t accesses, uint32_t least) {
+    if (accesses <= 32) return spread_short(s, accesses, mode, least);
     spread_over(s, accesses, v, mode, kFew, 32, 0);
-    spread_over(s, accesses, v, mode, (mode == kWhole ? 2 : mode == kShifted ? 3 : 8) * v, kThreads, 0);
+    spread_over(s, accesses, v, mode, (mode == kLoose ? 8 : 3) * v, kThreads, 0);
     spread_over(s, accesses, v, mode, kFew, kThreads, 0);
     spread_over(s, accesses, v, mode, 32, kMostThreads, kFew);
 }
@@ -292,21 +303,27 @@ int by_type(uint32_t type, F f) {
 }
 // Numbers of accesses that there are kernels for; 32 elements to a thread at most.
 template <typename T, typename F>
-int by_accesses(uint32_t n, Mode mode, F f) {
+int by_accesses(uint32_t n, uint32_t apart, Mode mode, F f) {
+    if (apart < 32) {
+        constexpr std::integral_constant<Mode, kWhole> whole;
+        const auto counts = [&](auto l) { return n == 2 ? f(std::integral_constant<int, 2>(), l, whole) : f(std::integral_constant<int, 3>(), l, whole); };
+        return apart == 4 ? counts(std::integral_constant<int, 4>()) : counts(std::integral_constant<int, 8>());
+    }
+    constexpr std::integral_constant<int, 32> l;
     const auto counts = [&](auto m) -> int {
         constexpr Mode M = decltype(m)::value;
         constexpr int kMost = 32 / kVector<T, M>;
         if constexpr (kMost >= 16)
-            if (n == 16) return f(std::integral_constant<int, 16>(), m);
+            if (n == 16) return f(std::integral_constant<int, 16>(), l, m);
         if constexpr (kMost >= 8)
-            if (n == 8) return f(std::integral_constant<int, 8>(), m);
+            if (n == 8) return f(std::integral_constant<int, 8>(), l, m);
         if constexpr (kMost >= 8 && M != kLoose)
-            if (n == 6) return f(std::integral_constant<int, 6>(), m);
+            if (n == 6) return f(std::integral_constant<int, 6>(), l, m);
         if constexpr (M != kLoose)
-            if (n == 3) return f(std::integral_constant<int, 3>(), m);
-        if (n == 4) return f(std::integral_constant<int, 4>(), m);
-        if (n == 2) return f(std::integral_constant<int, 2>(), m);
-        return f(std::integral_constant<int, 1>(), m);
+            if (n == 3) return f(std::integral_constant<int, 3>(), l, m);
+        if (n == 4) return f(std::integral_constant<int, 4>(), l, m);
+        if (n == 2) return f(std::integral_constant<int, 2>(), l, m);
+        return f(std::integral_constant<int, 1>(), l, m);
     };
     if (mode == kWhole) return counts(std::integral_constant<Mode, kWhole>());
     if (mode == kShifted) return counts(std::integral_constant<Mode, kShifted>());

@@ -62,15 +62,15 @@ template <int V> __device__ __forceinline__ int spread(int c) { return c + c / V
 
 // A thread has the same columns in all its rows and adds up its part of dweight in registers; a CTA's rows are added in shared memory, and CTAs' by
 // the kernel that joins.
-template <typename T, int N, Mode M, int ARRAYS>
+template <typename T, int N, int L, Mode M, int ARRAYS>
 __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWide<T, N, M> ? 1 : 3) rms_norm_back_kernel(const __grid_constant__ Params P) {
     constexpr int THREADS = kWide<T, N, M> ? kMostThreads : kThreads;
-    using A = Threads<T, N, M, THREADS, ARRAYS>;
+    using A = Threads<T, N, L, M, THREADS, ARRAYS>;
     constexpr int V = A::V, H = A::H;
     extern __shared__ __align__(16) char s_dynamic[];
     __shared__ uint32_t s_part[2 * kMostThreads / 32];
     const A t(P, s_dynamic, true);
-    RowSums<(N > 1)> S(t.lanes, s_part);
+    RowSums<(N > 1 && L == 32)> S(t.lanes, s_part);
     const int stages = (int)P.stages, dim = t.dim;
     for (int k = 0; k < stages - 1; ++k) t.fetch(k, k, true);
     t.load_weights();
@@ -104,8 +104,9 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             float2 u[H], a[H], w[H], d[H];
-            t.arrived(stage, 0, j, here, u), t.arrived(stage, 1, j, here, a), t.weights(j, w);   // from shared memory once more: registers would be too many
-            if (ARRAYS > 2) t.arrived(stage, 2, j, here, d);
+            // from shared memory once more: registers would be too many
+            t.template arrived<false>(stage, 0, j, here, u), t.template arrived<false>(stage, 1, j, here, a), t.weights(j, w);
+            if (ARRAYS > 2) t.template arrived<false>(stage, 2, j, here, d);
             else {
 #pragma unroll
                 for (int i = 0; i < H; ++i) d[i] = both(0.f);
@@ -149,7 +150,7 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
 static Shape back_shape_of(const Params& P, uint32_t size, Mode mode) {
     const uint32_t v = mode == kLoose ? 2 : 16 / size, accesses = accesses_of(P.dim, v, mode);
     Shape s{};
-    spread_over(s, P.dim, v, mode, accesses);
+    spread_over(s, v, mode, accesses, 1);
     if (!s.n) return s;
     const bool wide = s.n * v > kFew;
     s.threads = wide ? kMostThreads : kThreads, s.resident = wide ? 1 : 3;
@@ -220,16 +221,16 @@ extern "C" int halos_rms_norm_bwd(const halos_rms_norm_args* a) {
         const uint32_t most = (uint32_t)sm_count(a->device) * s.resident / 8 * 8;
         P.splits = P.row_blocks < most ? (P.row_blocks + 7) / 8 * 8 : most;
         P.apart = P.splits, P.run = (P.row_blocks + P.splits - 1) / P.splits;
-        return by_accesses<T>(s.n, mode, [&](auto n, auto m) -> int {
+        return by_accesses<T>(s.n, s.apart, mode, [&](auto n, auto l, auto m) -> int {
             const auto launch = [&](auto* kernel, Allowed& allowed) -> int {
                 if (int rc = allow_smem(kernel, (int)s.shared, allowed)) return rc;
                 kernel<<<P.splits, s.threads, s.shared, st>>>(P);
                 return cuda_status(cudaGetLastError(), "norm launch");
             };
             static Allowed allowed[2];
-            constexpr int N = decltype(n)::value;
+            constexpr int N = decltype(n)::value, L = decltype(l)::value;
             constexpr Mode M = decltype(m)::value;
-            return P.arrays > 2 ? launch(rms_norm_back_kernel<T, N, M, 3>, allowed[0]) : launch(rms_norm_back_kernel<T, N, M, 2>, allowed[1]);
+            return P.arrays > 2 ? launch(rms_norm_back_kernel<T, N, L, M, 3>, allowed[0]) : launch(rms_norm_back_kernel<T, N, L, M, 2>, allowed[1]);
         });
     });
     if (rc) return rc;

@@ -531,6 +531,20 @@ def distill_loss(logits, labels, teacher_idx=None, teacher_logits=None, *, tempe
 _STREAM = struct.Struct("=IiQ")              # what every args struct begins with: its size, device and stream
 
 
+@functools.lru_cache(maxsize=1024)
+def _plain_strides(shape):
+    strides, step_ = [], 1
+    for n in reversed(shape):
+        strides.append(step_)
+        step_ *= max(n, 1)
+    return tuple(reversed(strides))
+
+
+def _new(shape, dtype, device):
+    """A contiguous tensor: with strides given, half of what torch.empty takes."""
+    return torch.empty_strided(shape, _plain_strides(shape), dtype=dtype, device=device)
+
+
 def _as_rows(x, dim: int):
     """x, or a copy of it, as a matrix of rows whose elements lie side by side."""
     if x.dim() != 2:
@@ -568,7 +582,7 @@ def embedding_forward(weight, tokens, *, scale: float = 1.0, dtype=None):
     out_kind = kind if dtype is None else _DTYPES.get(dtype)
     if out_kind is None:
         _refuse(f"dtype: {dtype} is not float32, bfloat16 or float16")
-    out = weight.new_empty((*tokens.shape, dim), dtype=dtype)
+    out = _new((*tokens.shape, dim), dtype or weight.dtype, device)
     index = device.index
     _call("halos_embedding_fwd", _pack(
         _EMBEDDING, _EMBEDDING.size, index, _raw_stream(index), out_kind, kind, wide, 0, tokens.numel(), vocab, dim, scale,
@@ -593,7 +607,7 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
             _refuse("accumulate needs out")
         if vocab < 0 or (dtype is not None and dtype not in _DTYPES):
             _refuse("vocab must be positive and dtype float32, bfloat16 or float16")
-        out = dout.new_empty((vocab, dim), dtype=dtype)
+        out = _new((vocab, dim), dtype or dout.dtype, device)
     else:
         _on(out, device, "out")
         if out.shape != (vocab, dim) or (dtype is not None and out.dtype != dtype) or (out.stride(1) != 1 and dim > 1) or (vocab > 1 and out.stride(0) < dim):
@@ -601,7 +615,7 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
         _overwritten(out, "out")
     index, count, kind, out_kind = device.index, tokens.numel(), _dtype(dout, "dout"), _dtype(out, "out")
     size = _embedding_workspace(index, kind, out_kind, count, vocab, dim)
-    space = dout.new_empty(size, dtype=torch.uint8)
+    space = torch.empty(size, dtype=torch.uint8, device=device)
     _call("halos_embedding_bwd", _pack(
         _EMBEDDING, _EMBEDDING.size, index, _raw_stream(index), kind, out_kind, wide, bool(accumulate), count, vocab, dim, scale,
         tokens.data_ptr(), 0, 0, 0, 0, rows.data_ptr(), rows.stride(0), out.data_ptr(), out.stride(0), space.data_ptr(), size), index)
@@ -698,12 +712,13 @@ def _rms_norm(x, weight, residual, eps, quantized, group):
     if residual is not None:
         _like(residual, x, "residual")
         r3 = _side_by_side(residual)
-        summed = x.new_empty(shape)
+        summed = torch.empty_like(x) if x.is_contiguous() else _new(shape, x.dtype, device)
         at_r, at_s, r_stride, s_stride = r3.data_ptr(), summed.data_ptr(), r3.stride()[:-1], True
     layout, strides = _norm_layout(shape, (x3.stride()[:-1], r_stride, s_stride, True, None, None, None), kind, weight_kind, quantized, group, eps)
-    y, rstd, scales, at_scales = x.new_empty(shape, dtype=torch.float8_e4m3fn if quantized else None), x.new_empty(shape[:-1], dtype=torch.float32), None, 0
+    y, scales, at_scales = _new(shape, torch.float8_e4m3fn if quantized else x.dtype, device), None, 0
+    rstd = _new(shape[:-1], torch.float32, device)
     if quantized:
-        scales = x.new_empty((*shape[:-1], -(-shape[-1] // (group or shape[-1] or 1))), dtype=torch.float32)
+        scales = _new((*shape[:-1], -(-shape[-1] // (group or shape[-1] or 1))), torch.float32, device)
         at_scales = scales.data_ptr()
     index = device.index
     _call("halos_rms_norm_fwd", b"".join((_STREAM.pack(_RMS_NORM.size, index, _raw_stream(index)), layout, _NORM_POINTERS.pack(
@@ -745,7 +760,7 @@ def rms_norm_backward(dy, summed, weight, rstd, *, dsummed=None):
     index = device.index
     layout, strides = _norm_layout(shape, (None, None, s3.stride()[:-1], None, dy3.stride()[:-1], d_stride, True), kind, weight_kind, False, 0, 0.0)
     size = _norm_workspace(index, shape, kind, weight_kind)
-    dx, dweight, space = dy.new_empty(shape), weight.new_empty(shape[-1:]), dy.new_empty(size, dtype=torch.uint8)
+    dx, dweight, space = _new(shape, dy.dtype, device), torch.empty_like(weight), torch.empty(size, dtype=torch.uint8, device=device)
     _call("halos_rms_norm_bwd", b"".join((_STREAM.pack(_RMS_NORM.size, index, _raw_stream(index)), layout, _NORM_POINTERS.pack(
         0, 0, s3.data_ptr(), 0, 0, rstd.data_ptr(), weight.data_ptr(), dy3.data_ptr(), at_d, dx.data_ptr(), dweight.data_ptr(), space.data_ptr(), size), strides)), index)
     return dx, dweight
@@ -840,8 +855,8 @@ def _grads_call(name: str, grads, outs, max_norm: float, rate: float, with_norm:
         o_kinds = bytes(kinds[n:])
         (o_words, o_at), o_kinds_at = _words(map(torch.Tensor.data_ptr, outs)), C.cast(C.c_char_p(o_kinds), _vp).value
     if with_norm:
-        norm, size = grads[0].new_empty((), dtype=torch.float32), _grads_workspace(index, n)
-        space = grads[0].new_empty(size, dtype=torch.uint8)
+        norm, size = torch.empty_strided((), (), dtype=torch.float32, device=device), _grads_workspace(index, n)
+        space = torch.empty(size, dtype=torch.uint8, device=device)
     _call(name, _pack(_GRADS, _GRADS.size, index, _raw_stream(index), n, g_at, o_at, sizes_at, kinds_at, o_kinds_at, max_norm, rate,
                       norm.data_ptr() if with_norm else 0, space.data_ptr() if with_norm else 0, size), index)
     return norm

@@ -40,7 +40,7 @@ def test_against_64_bits(dtype, wtype, vocab, dim, shape, scale):
     assert torch.equal(dw, step.embedding_backward(dout, tokens, vocab, scale=scale, dtype=wtype))
 
 
-@pytest.mark.parametrize("tokens,vocab", [(1, 50304), (31, 5), (32, 33), (33, 600), (1024, 70000), (1025, 511), (1025, 512), (1025, 513), (5000, 300000), (40000, 97), (200000, 2000), (3000, 2 ** 27 + 5)])
+@pytest.mark.parametrize("tokens,vocab", [(1, 50304), (31, 5), (32, 33), (33, 600), (1024, 70000), (1025, 511), (1025, 512), (1025, 513), (5000, 300000), (8192, 700), (8193, 40), (16385, 9), (40000, 97), (65536, 3000), (65537, 3000), (200000, 2000), (3000, 2 ** 27 + 5)])
 def test_many_tokens_and_large_vocabularies(tokens, vocab):
     """One pass of the sort to four; more tokens than one block of it takes."""
     dim = 12 if vocab < 2 ** 20 else 2

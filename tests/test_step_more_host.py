@@ -231,3 +231,28 @@ def test_what_the_norm_saved_is_noticed_when_overwritten(plain):
     x += 1
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.sum().backward()
+
+
+@pytest.mark.parametrize("status", [0, 4])
+def test_the_callers_device_stays_current(monkeypatch, status):
+    """Asking for a workspace makes its device current, as every C call does."""
+    class Library:
+        current = 0
+
+        def halos_embedding_workspace(self, args, out):
+            self.current = 1
+            return status
+
+        def halos_step_error(self):
+            return b"as asked"
+
+    lib = Library()
+    monkeypatch.setattr(step, "_lib", lib)
+    monkeypatch.setattr(step, "_current_device", lambda: lib.current)
+    monkeypatch.setattr(step, "_set_device", lambda d: setattr(lib, "current", d))
+    if status:
+        with pytest.raises(step.HalosError):
+            step._workspace("halos_embedding_workspace", b"", 1)
+    else:
+        step._workspace("halos_embedding_workspace", b"", 1)
+    assert lib.current == 0
