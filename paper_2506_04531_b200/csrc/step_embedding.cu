@@ -346,7 +346,7 @@ __device__ __forceinline__ void write_part(const EmbedParams& P, uint32_t v, uin
 
 constexpr int kAhead = 4096;                                   // bytes of dout that a warp has on their way
 
-// A CTA takes 8 `chunk` neighbouring places in the sorted order and 256 columns, a warp `chunk` of the places (32 at most).  Rows of dout are copied into shared memory
+// A CTA takes 8 `chunk` neighbouring places in the sorted order and 256 columns, a warp `chunk` of the places, whose keys it holds 32 at a time.  Rows of dout are copied into shared memory
 // ahead of their turn, in pieces of 16 bytes wherever the row begins; lanes have the columns of whole accesses where rows allow (V = 16 bytes), else every 32nd.
 // A token whose places lie in one warp's chunk is written there.  What goes on from warp to warp is joined in shared memory; what goes on from CTA to
 // CTA is left in memory, and the CTA that comes last, whichever it is, adds up the parts, in their order.
@@ -361,14 +361,17 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
     const auto column = [&](int j) { return slab * kSlab + (j * 32 + lane) * V; };
     char* rows = s_rows + warp * kRing * kRow;
     after_previous();
-    const uint32_t my_key = lane < n ? key[from + lane] : P.vocab, my_place = lane < n ? place[from + lane] : 0;
+    // Keys and places of 32 places and of the next 32: lane l has those of place l, l + 32, ...
+    const auto key_at = [&](uint32_t i) { return i < n ? key[from + i] : P.vocab; };
+    const auto place_at = [&](uint32_t i) { return i < n ? place[from + i] : 0; };
+    uint32_t my_key = key_at(lane), my_place = place_at(lane), next_key = key_at(lane + 32), next_place = place_at(lane + 32), base = 0;
     const uint32_t key_before = from && n ? key[from - 1] : P.vocab, key_after = from + n < P.tokens ? key[from + n] : P.vocab;
-    const uint32_t tokens_here = __popc(__ballot_sync(~0u, my_key < P.vocab));     // those that are none come last
+    const auto of = [&](uint32_t mine, uint32_t next, uint32_t i) { return i - base < 32 ? __shfl_sync(~0u, mine, i - base) : __shfl_sync(~0u, next, i - base - 32); };
     const uint32_t columns = min((uint32_t)kSlab, P.dim - slab * kSlab);
     const A* here = reinterpret_cast<const A*>(P.dout) + slab * kSlab;
-    const auto row_of = [&](uint32_t i) { return here + __shfl_sync(~0u, my_place, i) * P.dout_stride; };
+    const auto row_of = [&](uint32_t i) { return here + of(my_place, next_place, i) * P.dout_stride; };
     const auto fetch = [&](uint32_t i) {
-        if (i < tokens_here) {
+        if (i < n && of(my_key, next_key, i) < P.vocab) {       // places of no token come last
             const A* row = row_of(i);
             char* to = rows + i % kRing * kRow;
             if constexpr (V > 1) {                              // each lane its own columns
@@ -396,8 +399,7 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
         }
         copies_end();
     };
-    // A bit for each place that is its token's last in this chunk.
-    const uint32_t next_key = __shfl_down_sync(~0u, my_key, 1), ends_here = __ballot_sync(~0u, lane + 1 >= n || next_key != my_key);
+    uint32_t ends_here = 0;                                     // a bit for each of the first 31 places that is its token's last in this chunk
     float sum[J][V];
     const auto clear = [&] {
 #pragma unroll
@@ -434,7 +436,17 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
     if (threadIdx.x == 0) s_comes = began_before, s_key[0] = my_key;
     for (uint32_t i = 0; i < kRing; ++i) fetch(i);
 #pragma unroll 1
-    for (uint32_t i = 0; i < tokens_here; ++i) {
+    for (uint32_t i = 0; i < n; ++i) {
+        if (i - base == 32) {
+            base = i, my_key = next_key, my_place = next_place, next_key = key_at(base + 32 + lane), next_place = place_at(base + 32 + lane);
+            if (__shfl_sync(~0u, my_key, 0) >= P.vocab) break;
+        }
+        if (i == base) {
+            const uint32_t behind = __shfl_down_sync(~0u, my_key, 1);
+            ends_here = __ballot_sync(~0u, base + lane + 1 >= n || behind != my_key);
+        }
+        const uint32_t k = __shfl_sync(~0u, my_key, i - base);
+        if (k >= P.vocab) break;
         asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
         const char* from_row = rows + i % kRing * kRow;
         if constexpr (V > 1) {
@@ -458,8 +470,7 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
             __syncwarp();
         }
         fetch(i + kRing);
-        if (ends_here >> i & 1) {
-            const uint32_t k = __shfl_sync(~0u, my_key, i);
+        if (i - base < 31 ? ends_here >> (i - base) & 1 : i + 1 == n || __shfl_sync(~0u, next_key, 0) != k) {
             const bool on = i + 1 == n && key_after == k;       // goes on behind the chunk
             if (began_before) keep(s_head[warp]), through = on;
             else if (on) keep(s_tail[warp]), tail = true;
@@ -492,7 +503,7 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
             add(s_head[w]);
             if (!s_through[w]) break;
         }
-        if (w < kWarps) write(__shfl_sync(~0u, my_key, n - 1));
+        if (w < kWarps) write(key_after);
         else leave(P.tail);
     }
     if (!comes && !goes) return;
@@ -599,9 +610,10 @@ Sizes sizes_of(const halos_embedding_args* a, int32_t device) {
     if (s.blocks == 0) s.blocks = 1;
     s.span = (uint32_t)rounded_up((a->tokens + s.blocks - 1) / s.blocks, kSortThreads);
     s.slabs = (a->dim + kSlab - 1) / kSlab;
-    // 32 places to a warp, or as few as give every SM two CTAs.
-    s.chunk = 32;
-    while (s.chunk > 4 && (uint64_t)a->tokens * s.slabs < most * 2 * kWarps * s.chunk) s.chunk /= 2;
+    // As many places to a warp as fill the SMs once with four CTAs each, 8 at least; where these are over 96, as often as it takes.
+    const uint64_t jobs = (uint64_t)a->tokens * s.slabs, at_once = most * 4 * kWarps, times = (jobs + at_once * 96 - 1) / (at_once * 96);
+    const uint64_t chunk = times ? (jobs + at_once * times - 1) / (at_once * times) : 0;
+    s.chunk = chunk < 8 ? 8 : (uint32_t)chunk;
     s.ctas = (uint32_t)((a->tokens + s.chunk * kWarps - 1) / (s.chunk * kWarps));
     s.arrays = rounded_up((uint64_t)a->tokens * 4, 16);
     s.counts = ((uint64_t)s.blocks << kMostBits) * 4;
