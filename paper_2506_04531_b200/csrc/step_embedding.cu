@@ -175,7 +175,7 @@ __device__ __forceinline__ void clear_rows_not_met(const EmbedParams& P, uint32_
     const uint32_t words = (P.vocab + 31) / 32, warp = threadIdx.x / 32;
     // short rows take part of a warp each
     uint32_t lanes = 32;
-    while (lanes > 1 && lanes * 16 / 2 >= P.dim * sizeof(W)) lanes /= 2;
+    while (lanes > 8 && lanes * 16 / 2 >= P.dim * sizeof(W)) lanes /= 2;
     const uint32_t lane = threadIdx.x % lanes, sub = threadIdx.x % 32 / lanes;
     for (uint32_t first = 0; (uint64_t)first * many + mine < words; first += kMetWords) {       // word i of this CTA is word i * many + mine of all
         for (uint32_t i = threadIdx.x; i < kMetWords; i += kSortThreads) s_met[i] = 0;
@@ -186,11 +186,12 @@ __device__ __forceinline__ void clear_rows_not_met(const EmbedParams& P, uint32_
             if (v < P.vocab && word - i * many == mine && i - first < kMetWords) atomicOr(&s_met[i - first], 1u << v % 32);
         }
         __syncthreads();
-        for (uint32_t i = warp; i < kMetWords; i += kSortWarps) {
+        for (uint32_t part = warp; part < kMetWords * 8; part += kSortWarps) {   // four rows at a time
+            const uint32_t i = part / 8, four = part % 8 * 4;
             const uint64_t word = (uint64_t)(first + i) * many + mine;
             if (word >= words) break;
             const uint32_t met = s_met[i];
-            for (uint32_t r = sub; r < 32; r += 32 / lanes) {
+            for (uint32_t r = four + sub; r < four + 4; r += 32 / lanes) {
                 const uint32_t v = (uint32_t)word * 32 + r;
                 if (v < P.vocab && !(met >> r & 1)) clear_row(reinterpret_cast<W*>(P.dweight) + v * P.dweight_stride, P.dim, lane, lanes);
             }
