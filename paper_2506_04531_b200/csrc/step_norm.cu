@@ -152,7 +152,10 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
         const bool here = row < P.rows;
         float2 v[N][H], sums = both(0.f);
 #pragma unroll
-        for (int j = 0; j < N; ++j) t.arrived(stage, 0, j, here, v[j]);
+        for (int j = 0; j < N; ++j) {
+            t.arrived(stage, 0, j, here, v[j]);
+            if (!added) keep_own<V, M>(v[j], t.column(j), dim);
+        }
         if (added) {
             T* out = here ? row_at<T>(P, P.out[1], row) : nullptr;
 #pragma unroll
@@ -161,6 +164,7 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
                 t.arrived(stage, 1, j, here, r);
 #pragma unroll
                 for (int i = 0; i < H; ++i) v[j][i] = add2(v[j][i], r[i]);
+                keep_own<V, M>(v[j], t.column(j), dim);
                 if (here) store_part<T, V, M>(out, t.column(j), dim, v[j]);
             }
         }

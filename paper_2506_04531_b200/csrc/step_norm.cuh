@@ -170,12 +170,13 @@ struct Threads {
                 const Rows& R = P.in[array];
                 const T* from = row_at<const T>(P, R, row);
                 const T* at = from + first;
+                // accesses at the ends of all rows but the tensor's first and last stay within it
+                const bool inside = M == kWhole || (M == kShifted && reinterpret_cast<const char*>(from) >= R.span[0] + 16 && reinterpret_cast<const char*>(from + dim) + 16 <= R.span[1]);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const char* p = reinterpret_cast<const char*>(at + j * L * V);
                     char* t = to + array * kArray + j * THREADS * kAccess;
                     if (column(j) >= dim) continue;
-                    if (M == kWhole || (M == kShifted && p >= R.span[0] && p + 16 <= R.span[1])) copy_16(t, p);
+                    if (inside) copy_16(t, at + j * L * V);
                     else *reinterpret_cast<Words<T, V>*>(t) = pick<T, V>(from, column(j), dim);
                 }
             }
@@ -183,13 +184,11 @@ struct Threads {
         }
         copies_end();
     }
-    // An access that has arrived, as floats; 0 where there is none, and (OWN) where it is not the row's.
-    template <bool OWN = true>
+    // An access that has arrived, as floats; 0 where there is none.  At a row's ends it holds what lies beside it.
     __device__ __forceinline__ void arrived(int stage, int array, int j, bool here, float2 (&v)[H]) const {
         Words<T, V> w = no_words<T, V>();
         if (here && column(j) < dim) w = load_words<T, V>(reinterpret_cast<const T*>(mine + stage * kStage + array * kArray + j * THREADS * kAccess));
         widen<T, V>(w, v);
-        if (OWN) keep_own<V, M>(v, column(j), dim);
     }
 };
 

@@ -94,10 +94,10 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
             float2 u[H], a[H], w[H];
             t.arrived(stage, 0, j, here, u), t.arrived(stage, 1, j, here, a), t.weights(j, w);
 #pragma unroll
-            for (int i = 0; i < H; ++i) {
-                const float2 p = mul2(a[i], mul2(u[i], both(rstd)));
-                dw[j][i] = add2(dw[j][i], p), dots = fma2(p, w[i], dots);
-            }
+            for (int i = 0; i < H; ++i) a[i] = mul2(a[i], mul2(u[i], both(rstd)));
+            keep_own<V, M>(a, t.column(j), dim);
+#pragma unroll
+            for (int i = 0; i < H; ++i) dw[j][i] = add2(dw[j][i], a[i]), dots = fma2(a[i], w[i], dots);
         }
         const float mean = S.sum(dots.x + dots.y) * P.inverse_dim;
         T* dx = here ? row_at<T>(P, P.out[0], row) : nullptr;
@@ -105,8 +105,8 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
         for (int j = 0; j < N; ++j) {
             float2 u[H], a[H], w[H], d[H];
             // from shared memory once more: registers would be too many
-            t.template arrived<false>(stage, 0, j, here, u), t.template arrived<false>(stage, 1, j, here, a), t.weights(j, w);
-            if (ARRAYS > 2) t.template arrived<false>(stage, 2, j, here, d);
+            t.arrived(stage, 0, j, here, u), t.arrived(stage, 1, j, here, a), t.weights(j, w);
+            if (ARRAYS > 2) t.arrived(stage, 2, j, here, d);
             else {
 #pragma unroll
                 for (int i = 0; i < H; ++i) d[i] = both(0.f);
