@@ -18,8 +18,8 @@
  *    args->stream (cudaStream_t, NULL = the legacy default stream) and returns without waiting.  Tensors are
  *    borrowed until those kernels have completed in stream order.
  *  - Pointers are device pointers.  Strides are in elements; the innermost dimension is contiguous.
- *  - Nothing is allocated but 256 bytes of host memory in the first call: workspaces are the caller's
- *    (halos_*_workspace say how much).
+ *  - Nothing is allocated but 256 bytes of host memory in the first call (and, in calls that write lists of tensors, 24 bytes
+ *    for each until the call returns): workspaces are the caller's (halos_*_workspace say how much).
  *  - The same inputs give the same bits, call after call: no result depends on the order of atomics.
  *  - Sums, statistics and everything between load and store are held in 32 bits, and results are rounded once, except that attention rounds p
  *    and ds to the inputs' type where they enter matrix products, and forms D from the o that was returned.
@@ -167,7 +167,8 @@ int halos_distill_fwd_bwd(const halos_distill_args* args);
 /* fwd:  out[t][c] = scale weight[token[t]][c];   bwd:  dweight[v][c] = scale sum of dout[t][c] over the t with token[t] = v, and 0 where there
  * is none; accumulate: that is added to what dweight holds, and rows that no token names are not touched.
  * A token outside [0, vocab) gives a row of NaN and takes no part in the gradient.  dtype is that of out and dout, weight_dtype that of weight
- * and dweight, any pair of the three.  Products and sums are in 32 bits, the sums of a row in a fixed order, and each result is rounded once. */
+ * and dweight, any pair of the three.  Products and sums are in 32 bits, the sums of a row in a fixed order, and each result is rounded once.
+ * What is written may overlap nothing that is read. */
 typedef struct halos_embedding_args {
     uint32_t struct_size;
     int32_t device;
@@ -206,7 +207,8 @@ int halos_embedding_workspace(const halos_embedding_args* args, uint64_t* bytes)
  * bwd, from s as it was rounded (x, without a residual), rstd, dy and dsummed (the gradient of summed, or NULL), with u = s rstd and g = dy weight:
  *     dx = rstd (g - u mean of g u) + dsummed,  which is the gradient of x and of residual;   dweight = sum over rows of dy u.
  * The sums of dweight are in 32 bits and a fixed order, and each result is rounded once.
- * Rows are those of three outer sizes (1 where there are fewer) with strides of their own; the elements of a row lie side by side. */
+ * Rows are those of three outer sizes (1 where there are fewer) with strides of their own; the elements of a row lie side by side.  Rows that are
+ * written may overlap none that are read or written. */
 typedef struct halos_rms_norm_args {
     uint32_t struct_size;
     int32_t device;

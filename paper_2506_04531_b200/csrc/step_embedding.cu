@@ -1,9 +1,17 @@
 // The embedding with scaling, and its gradient by sorted tokens.
 //
-// The gradient's row for a token is the sum of the rows of dout where it stands.  Places are sorted by token, stably, with a radix sort of up to
-// 9 bits a pass; then a warp takes 32 places in that order and 256 columns, and adds up what belongs together.  A token whose places go on
-// into the next warps' is added up from those warps' sums, in order, by a kernel of its own.  So sums of a token's rows are in a fixed order, and no
+// Both are bound by memory: the forward reads the rows that are asked for and writes as many as there are tokens; the gradient reads dout and writes every row
+// of the table, most of them zeros.
+//
+// The gradient's row for a token is the sum of the rows of dout where it stands.  Up to 65536 places are sorted by token by one cluster of CTAs, in its shared memory, while
+// the launch's other CTAs clear the rows that no token names; more are sorted by a radix sort over the GPU, and rows are cleared by a kernel of their own.  Both sorts
+// are stable.  Then warps take equal runs of places in that order and 256 columns, and add up what belongs together; what goes on from warp to warp is joined in
+// shared memory, and what goes on from CTA to CTA by the one that comes last, part by part in their order.  So the sums of a token's rows are in a fixed order, and no
 // token, however frequent, waits for one warp.
+//
+// Measured: 65536 tokens x 768, bf16 from a table of 50304 in f32: forward 31 us (75% of the copy rate), gradient 70 us (56%): the sort takes 27 us, a third of them ranking places
+// within a warp by ballots and a third moving them, in which 117 MB of rows are cleared (20 us alone); the sums, 38 us, read dout at 5 TB/s while the cleared rows leave the L2 cache.
+// 7147 tokens x 1021 f16, half of them one token: 33 us.
 #include "step_vector.cuh"
 
 #include <atomic>
