@@ -475,7 +475,8 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
             __syncwarp();                                       // pieces are other lanes' columns
             const A* row = reinterpret_cast<const A*>(from_row + ((uintptr_t)row_of(i) & 15));
 #pragma unroll
-            for (int j = 0; j < J; ++j) sum[j][0] += to_f32<A>(row[j * 32 + lane]);
+            for (int j = 0; j < J; ++j)
+                if (j * 32 < columns) sum[j][0] += to_f32<A>(row[j * 32 + lane]);
             __syncwarp();
         }
         fetch(i + kRing);

@@ -594,7 +594,7 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
     """The gradient [vocab, dim] of the table from that of the rows, dout [*tokens.shape, dim]: for every token scale times the sum of dout where it
     stands, in a fixed order, 0 where it does not.  Of dtype (dout's unless given), or written to out (rows any distance apart, detached if it is in a graph);
     accumulate: added to what out holds, whose other rows are not touched.  Tokens outside the vocabulary take no part."""
-    device = dout.device
+    device, vocab = dout.device, int(vocab)
     _on(dout, device, "dout")
     shape = dout.shape
     if not shape or shape[:-1] != tokens.shape:
@@ -703,7 +703,7 @@ def _like(a, b, what: str):
 
 
 def _rms_norm(x, weight, residual, eps, quantized, group):
-    device, shape = x.device, x.shape
+    device, shape, eps, group = x.device, x.shape, float(eps), int(group)
     _on(x, device, "x")
     if not shape:
         _refuse("rows must have a last dimension")
