@@ -370,17 +370,28 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
     const auto column = [&](int j) { return slab * kSlab + (j * 32 + lane) * V; };
     char* rows = s_rows + warp * kRing * kRow;
     after_previous();
-    // Keys and places of 32 places and of the next 32: lane l has those of place l, l + 32, ...
-    const auto key_at = [&](uint32_t i) { return i < n ? key[from + i] : P.vocab; };
-    const auto place_at = [&](uint32_t i) { return i < n ? place[from + i] : 0; };
-    uint32_t my_key = key_at(lane), my_place = place_at(lane), next_key = key_at(lane + 32), next_place = place_at(lane + 32), base = 0;
-    const uint32_t key_before = from && n ? key[from - 1] : P.vocab, key_after = from + n < P.tokens ? key[from + n] : P.vocab;
-    const auto of = [&](uint32_t mine, uint32_t next, uint32_t i) { return i - base < 32 ? __shfl_sync(~0u, mine, i - base) : __shfl_sync(~0u, next, i - base - 32); };
-    const uint32_t columns = min((uint32_t)kSlab, P.dim - slab * kSlab);
+    // Of 32 places and of the next 32 a lane has the key of one each, and where its row's columns begin.  Places of no token come last; `limit` is how many there
+    // are before them, from `base` on, as far as is known: 64 at most.
     const A* here = reinterpret_cast<const A*>(P.dout) + slab * kSlab;
-    const auto row_of = [&](uint32_t i) { return here + of(my_place, next_place, i) * P.dout_stride; };
+    const uint32_t columns = min((uint32_t)kSlab, P.dim - slab * kSlab);
+    uint32_t base = 0, my_key, next_key, limit;
+    const A *my_row, *next_row;
+    const auto load = [&](uint32_t i, uint32_t& k, const A*& row) {
+        k = i < n ? key[from + i] : P.vocab;
+        row = here + (i < n ? place[from + i] : 0) * P.dout_stride;
+    };
+    const auto known = [&] {
+        const uint32_t first = __ballot_sync(~0u, my_key < P.vocab), second = __ballot_sync(~0u, next_key < P.vocab);
+        return ~first ? __popc(first) : 32 + __popc(second);
+    };
+    load(lane, my_key, my_row), load(lane + 32, next_key, next_row);
+    const uint32_t key_before = from && n ? key[from - 1] : P.vocab, key_after = from + n < P.tokens ? key[from + n] : P.vocab;
+    limit = known();
+    const auto row_of = [&](uint32_t i) {                       // i: from `base` on
+        return reinterpret_cast<const A*>(__shfl_sync(~0u, reinterpret_cast<uintptr_t>(i < 32 ? my_row : next_row), i % 32));
+    };
     const auto fetch = [&](uint32_t i) {
-        if (i < n && of(my_key, next_key, i) < P.vocab) {       // places of no token come last
+        if (i < limit) {
             const A* row = row_of(i);
             char* to = rows + i % kRing * kRow;
             if constexpr (V > 1) {                              // each lane its own columns
@@ -408,7 +419,6 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
         }
         copies_end();
     };
-    uint32_t ends_here = 0;                                     // a bit for each of the first 31 places that is its token's last in this chunk
     float sum[J][V];
     const auto clear = [&] {
 #pragma unroll
@@ -444,50 +454,48 @@ __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_co
     bool through = false, tail = false;
     if (threadIdx.x == 0) s_comes = began_before, s_key[0] = my_key;
     for (uint32_t i = 0; i < kRing; ++i) fetch(i);
+    for (;;) {
+        // a bit for each of the first 31 places that is its token's last in this chunk; the 32nd's neighbour may still be on its way
+        const uint32_t behind = __shfl_down_sync(~0u, my_key, 1), ends = __ballot_sync(~0u, base + lane + 1 >= n || behind != my_key), many = min(limit, 32u);
 #pragma unroll 1
-    for (uint32_t i = 0; i < n; ++i) {
-        if (i - base == 32) {
-            base = i, my_key = next_key, my_place = next_place, next_key = key_at(base + 32 + lane), next_place = place_at(base + 32 + lane);
-            if (__shfl_sync(~0u, my_key, 0) >= P.vocab) break;
-        }
-        if (i == base) {
-            const uint32_t behind = __shfl_down_sync(~0u, my_key, 1);
-            ends_here = __ballot_sync(~0u, base + lane + 1 >= n || behind != my_key);
-        }
-        const uint32_t k = __shfl_sync(~0u, my_key, i - base);
-        if (k >= P.vocab) break;
-        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
-        const char* from_row = rows + i % kRing * kRow;
-        if constexpr (V > 1) {
+        for (uint32_t i = 0; i < many; ++i) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+            const char* slot = rows + i % kRing * kRow;
+            if constexpr (V > 1) {
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                float2 v[V / 2];
-                if (column(j) < P.dim) {
-                    widen<A, V>(load_words<A, V>(reinterpret_cast<const A*>(from_row) + (j * 32 + lane) * V), v);
+                for (int j = 0; j < J; ++j) {
+                    float2 v[V / 2];
+                    if (column(j) < P.dim) {
+                        widen<A, V>(load_words<A, V>(reinterpret_cast<const A*>(slot) + (j * 32 + lane) * V), v);
 #pragma unroll
-                    for (int e = 0; e < V / 2; ++e) {
-                        const float2 t = add2(make_float2(sum[j][2 * e], sum[j][2 * e + 1]), v[e]);
-                        sum[j][2 * e] = t.x, sum[j][2 * e + 1] = t.y;
+                        for (int e = 0; e < V / 2; ++e) {
+                            const float2 t = add2(make_float2(sum[j][2 * e], sum[j][2 * e + 1]), v[e]);
+                            sum[j][2 * e] = t.x, sum[j][2 * e + 1] = t.y;
+                        }
                     }
                 }
-            }
-        } else {
-            __syncwarp();                                       // pieces are other lanes' columns
-            const A* row = reinterpret_cast<const A*>(from_row + ((uintptr_t)row_of(i) & 15));
+            } else {
+                __syncwarp();                                   // pieces are other lanes' columns
+                const A* row = reinterpret_cast<const A*>(slot + ((uintptr_t)row_of(i) & 15));
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-                if (j * 32 < columns) sum[j][0] += to_f32<A>(row[j * 32 + lane]);
-            __syncwarp();
+                for (int j = 0; j < J; ++j)
+                    if (j * 32 < columns) sum[j][0] += to_f32<A>(row[j * 32 + lane]);
+                __syncwarp();
+            }
+            fetch(i + kRing);
+            if (i < 31 ? ends >> i & 1 : base + 32 >= n || __shfl_sync(~0u, next_key, 0) != __shfl_sync(~0u, my_key, 31)) {
+                const uint32_t k = __shfl_sync(~0u, my_key, i);
+                const bool on = base + i + 1 == n && key_after == k;    // goes on behind the chunk
+                if (began_before) keep(s_head[warp]), through = on;
+                else if (on) keep(s_tail[warp]), tail = true;
+                else write(k);
+                began_before = false;
+                clear();
+            }
         }
-        fetch(i + kRing);
-        if (i - base < 31 ? ends_here >> (i - base) & 1 : i + 1 == n || __shfl_sync(~0u, next_key, 0) != k) {
-            const bool on = i + 1 == n && key_after == k;       // goes on behind the chunk
-            if (began_before) keep(s_head[warp]), through = on;
-            else if (on) keep(s_tail[warp]), tail = true;
-            else write(k);
-            began_before = false;
-            clear();
-        }
+        if (limit <= 32) break;
+        base += 32, my_key = next_key, my_row = next_row;
+        load(base + 32 + lane, next_key, next_row), limit = known();
     }
     wait_copies(false);
     if (lane == 0) {
