@@ -601,7 +601,10 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
         _refuse("dout must be [*tokens.shape, dim]")
     tokens, wide = _tokens_checked(tokens, device)
     dim = shape[-1]
-    rows = _as_rows(dout, dim) if dim else dout
+    rows, stride = dout, dim
+    if dim and not dout.is_contiguous():
+        rows = _as_rows(dout, dim)
+        stride = rows.stride(0)
     if out is None:
         if accumulate:
             _refuse("accumulate needs out")
@@ -618,7 +621,7 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
     space = torch.empty(size, dtype=torch.uint8, device=device)
     _call("halos_embedding_bwd", _pack(
         _EMBEDDING, _EMBEDDING.size, index, _raw_stream(index), kind, out_kind, wide, bool(accumulate), count, vocab, dim, scale,
-        tokens.data_ptr(), 0, 0, 0, 0, rows.data_ptr(), rows.stride(0), out.data_ptr(), out.stride(0), space.data_ptr(), size), index)
+        tokens.data_ptr(), 0, 0, 0, 0, rows.data_ptr(), stride, out.data_ptr(), out.stride(0), space.data_ptr(), size), index)
     return out
 
 
@@ -659,10 +662,14 @@ _NORM_LAYOUT = struct.Struct("=IIII3qIf")
 
 
 def _side_by_side(x):
-    """x, or a copy of it whose rows' elements lie side by side; more than three outer sizes as one."""
+    """x, or a copy of it whose rows' elements lie side by side (more than three outer sizes as one), and the strides of its outer sizes, True where it is contiguous."""
+    if x.is_contiguous():
+        return x, True
     if x.stride(-1) != 1 and x.size(-1) > 1:
-        x = x.contiguous()
-    return x if x.dim() <= 4 else x.reshape(-1, x.size(-1))
+        return x.contiguous(), True
+    if x.dim() > 4:
+        x = x.reshape(-1, x.size(-1))
+    return x, x.stride()[:-1]
 
 
 @functools.lru_cache(maxsize=256)
@@ -708,14 +715,14 @@ def _rms_norm(x, weight, residual, eps, quantized, group):
     if not shape:
         _refuse("rows must have a last dimension")
     kind, weight_kind = _dtype(x, "x"), _norm_weight(weight, x, device)
-    x3, summed, at_r, at_s, r_stride, s_stride = _side_by_side(x), x, 0, 0, None, None
+    (x3, x_stride), summed, at_r, at_s, r_stride, s_stride = _side_by_side(x), x, 0, 0, None, None
     if residual is not None:
         _like(residual, x, "residual")
-        r3 = _side_by_side(residual)
+        r3, r_stride = _side_by_side(residual)
         summed = torch.empty_like(x) if x.is_contiguous() else _new(shape, x.dtype, device)
-        at_r, at_s, r_stride, s_stride = r3.data_ptr(), summed.data_ptr(), r3.stride()[:-1], True
-    layout, strides = _norm_layout(shape, (x3.stride()[:-1], r_stride, s_stride, True, None, None, None), kind, weight_kind, quantized, group, eps)
-    y, scales, at_scales = _new(shape, torch.float8_e4m3fn if quantized else x.dtype, device), None, 0
+        at_r, at_s, s_stride = r3.data_ptr(), summed.data_ptr(), True
+    layout, strides = _norm_layout(shape, (x_stride, r_stride, s_stride, True, None, None, None), kind, weight_kind, quantized, group, eps)
+    y, scales, at_scales = torch.empty_like(x) if x.is_contiguous() and not quantized else _new(shape, torch.float8_e4m3fn if quantized else x.dtype, device), None, 0
     rstd = _new(shape[:-1], torch.float32, device)
     if quantized:
         scales = _new((*shape[:-1], -(-shape[-1] // (group or shape[-1] or 1))), torch.float32, device)
@@ -752,15 +759,15 @@ def rms_norm_backward(dy, summed, weight, rstd, *, dsummed=None):
     _on(rstd, device, "rstd")
     if rstd.dtype != torch.float32 or rstd.shape != shape[:-1] or not rstd.is_contiguous():
         _refuse("rstd must be contiguous float32 [...]")
-    dy3, s3, at_d, d_stride = _side_by_side(dy), _side_by_side(summed), 0, None
+    (dy3, dy_stride), (s3, s_stride), at_d, d_stride = _side_by_side(dy), _side_by_side(summed), 0, None
     if dsummed is not None:
         _like(dsummed, dy, "dsummed")
-        d3 = _side_by_side(dsummed)
-        at_d, d_stride = d3.data_ptr(), d3.stride()[:-1]
+        d3, d_stride = _side_by_side(dsummed)
+        at_d = d3.data_ptr()
     index = device.index
-    layout, strides = _norm_layout(shape, (None, None, s3.stride()[:-1], None, dy3.stride()[:-1], d_stride, True), kind, weight_kind, False, 0, 0.0)
+    layout, strides = _norm_layout(shape, (None, None, s_stride, None, dy_stride, d_stride, True), kind, weight_kind, False, 0, 0.0)
     size = _norm_workspace(index, shape, kind, weight_kind)
-    dx, dweight, space = _new(shape, dy.dtype, device), torch.empty_like(weight), torch.empty(size, dtype=torch.uint8, device=device)
+    dx, dweight, space = torch.empty_like(dy) if dy.is_contiguous() else _new(shape, dy.dtype, device), torch.empty_like(weight), torch.empty(size, dtype=torch.uint8, device=device)
     _call("halos_rms_norm_bwd", b"".join((_STREAM.pack(_RMS_NORM.size, index, _raw_stream(index)), layout, _NORM_POINTERS.pack(
         0, 0, s3.data_ptr(), 0, 0, rstd.data_ptr(), weight.data_ptr(), dy3.data_ptr(), at_d, dx.data_ptr(), dweight.data_ptr(), space.data_ptr(), size), strides)), index)
     return dx, dweight
