@@ -43,6 +43,12 @@ __global__ void __launch_bounds__(kThreads) rms_norm_any_dweight_kernel(const __
     P.partial[(int64_t)blockIdx.y * P.dim + c] = sum;
 }
 
+__device__ __forceinline__ void write_dweight(const Params& P, uint32_t c, float sum) {
+    if (P.weight_type == HALOS_F32) reinterpret_cast<float*>(P.dweight)[c] = sum;
+    else if (P.weight_type == HALOS_BF16) reinterpret_cast<__nv_bfloat16*>(P.dweight)[c] = __float2bfloat16_rn(sum);
+    else reinterpret_cast<__half*>(P.dweight)[c] = __float2half_rn(sum);
+}
+
 constexpr int kJoinColumns = 32, kJoinRows = 32;
 __global__ void __launch_bounds__(kJoinColumns * kJoinRows) rms_norm_join_kernel(const __grid_constant__ Params P) {
     __shared__ float s[kJoinRows][kJoinColumns];
@@ -57,9 +63,7 @@ __global__ void __launch_bounds__(kJoinColumns * kJoinRows) rms_norm_join_kernel
     if (y || c >= P.dim) return;
 #pragma unroll
     for (int i = 1; i < kJoinRows; ++i) sum += s[i][x];
-    if (P.weight_type == HALOS_F32) reinterpret_cast<float*>(P.dweight)[c] = sum;
-    else if (P.weight_type == HALOS_BF16) reinterpret_cast<__nv_bfloat16*>(P.dweight)[c] = __float2bfloat16_rn(sum);
-    else reinterpret_cast<__half*>(P.dweight)[c] = __float2half_rn(sum);
+    write_dweight(P, c, sum);
 }
 
 // ------------------------------------------------------------------------------------------------ rows that a CTA holds
@@ -149,7 +153,11 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
         }
         __syncthreads();
     }
-    for (uint32_t c = threadIdx.x; c < P.dim; c += blockDim.x) P.partial[(int64_t)blockIdx.x * P.dim + c] = s_dw[spread<V>(c)];
+    for (uint32_t c = threadIdx.x; c < P.dim; c += blockDim.x) {
+        const float sum = s_dw[spread<V>(c)];
+        if (gridDim.x == 1) write_dweight(P, c, sum);
+        else P.partial[(int64_t)blockIdx.x * P.dim + c] = sum;
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -227,6 +235,8 @@ extern "C" int halos_rms_norm_bwd(const halos_rms_norm_args* a) {
         // a multiple of 8, so that steps of as many rows keep every shift
         const uint32_t most = (uint32_t)sm_count(a->device) * s.resident / 8 * 8;
         P.splits = P.row_blocks < most ? (P.row_blocks + 7) / 8 * 8 : most;
+        // A few rows are one CTA's, which needs no other kernel to join its sums.
+        if (P.row_blocks <= 4 && (mode != kShifted || s.per() >= 8)) P.splits = 1;
         P.apart = P.splits, P.run = (P.row_blocks + P.splits - 1) / P.splits;
         return by_accesses<T>(s.n, s.apart, mode, [&](auto n, auto l, auto m) -> int {
             const auto launch = [&](auto* kernel, Allowed& allowed) -> int {
@@ -240,6 +250,6 @@ extern "C" int halos_rms_norm_bwd(const halos_rms_norm_args* a) {
             return P.arrays > 2 ? launch(rms_norm_back_kernel<T, N, L, M, 3>, allowed[0]) : launch(rms_norm_back_kernel<T, N, L, M, 2>, allowed[1]);
         });
     });
-    if (rc) return rc;
+    if (rc || (s.n && P.splits == 1)) return rc;
     return launch_after(rms_norm_join_kernel, (P.dim + kJoinColumns - 1) / kJoinColumns, kJoinColumns * kJoinRows, 0, st, "norm launch", P);
 }
