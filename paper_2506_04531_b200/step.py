@@ -9,7 +9,8 @@
 
 As in ``binding``, the arithmetic is the CUDA library's; what happens here is checking, marshalling and output
 allocation, on the current stream of the tensors' device.  The caller's current device stays what it was.  There is no CPU path.
-Errors are ``HalosError``.
+Errors are ``HalosError``.  Everything can be captured into CUDA graphs; a backward pass by autograd while no graph of the same leaves that was
+built outside the capture is alive, since torch accumulates on that graph's stream.
 """
 from __future__ import annotations
 
@@ -592,7 +593,7 @@ def embedding_forward(weight, tokens, *, scale: float = 1.0, dtype=None):
 
 def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False):
     """The gradient [vocab, dim] of the table from that of the rows, dout [*tokens.shape, dim]: for every token scale times the sum of dout where it
-    stands, in a fixed order, 0 where it does not.  Of dtype (dout's unless given), or written to out (rows any distance apart, detached if it is in a graph);
+    stands, in a fixed order, 0 where it does not.  Of dtype (dout's unless given), or written to out (rows any distance apart, detached if it is in a graph, sharing no memory with dout or tokens);
     accumulate: added to what out holds, whose other rows are not touched.  Tokens outside the vocabulary take no part."""
     device, vocab = dout.device, int(vocab)
     _on(dout, device, "dout")
