@@ -154,6 +154,41 @@ def test_capture_from_the_first_call_on():
     assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
 
 
+# Forward and backward by autograd on static leaves, then the parameters' clipped step, in one graph: replays walk the way that eager steps walk.
+AUTOGRAD = """
+import torch
+from paper_2506_04531_b200 import step
+def state():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = lambda *s: torch.randn(s, generator=g, device="cuda")
+    return [x(500, 72), x(72), x(72)], torch.randint(0, 500, (3, 41), generator=g, device="cuda"), x(3, 41, 72)
+def one(params, tokens, target):
+    leaves = [p.detach().requires_grad_() for p in params]
+    e = step.embedding(leaves[0], tokens, scale=2.0)
+    y = step.rms_norm(e, leaves[1])
+    z, s = step.rms_norm(y, leaves[2], residual=e)
+    grads = torch.autograd.grad((z * target).sum() + (s * s).mean(), leaves)
+    return step.sgd_step(params, grads, 0.1, max_norm=1.0)
+params, tokens, target = state()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    norm = one(params, tokens, target)
+eager, _, _ = state()
+for k in range(4):
+    graph.replay()
+    want = one(eager, tokens, target)
+    assert torch.equal(norm, want), k
+    assert all(torch.equal(a, b) for a, b in zip(params, eager)), k
+assert not torch.equal(params[0], state()[0][0])
+print("same")
+"""
+
+
+def test_autograd_captured():
+    r = subprocess.run([sys.executable, "-c", AUTOGRAD], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
+
+
 def test_threads_with_streams_of_their_own():
     widths, got, errors = [96, 1021, 2048, 4096, 9000, 12288], {}, []
 
