@@ -353,6 +353,49 @@ __device__ __forceinline__ void write_part(const EmbedParams& P, uint32_t v, uin
     store_words<W, V>(to, narrow<W, V>(r));
 }
 
+// A few places, onto a table that is there: nothing is sorted or cleared.  A CTA to each place and 256 columns, which returns where an earlier place has the same token;
+// the token's rows go round the warps, whose sums are joined in their order.  One launch: 8 to 100 places take 2.1 to 2.5 us and 9.6 of the host, sorted and then summed 10.8 to 13.4 and
+// 12.  More places than threads would be looked through in turns by every CTA; they are sorted.
+constexpr uint32_t kFewPlaces = kThreads;
+template <typename A, typename W>
+__global__ void __launch_bounds__(kThreads) embedding_few_kernel(const __grid_constant__ EmbedParams P) {
+    constexpr int J = kSlab / 32;
+    __shared__ uint32_t s_same[kWarps], s_place[kFewPlaces];
+    __shared__ float s_sum[kWarps][kSlab];
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, place = blockIdx.y, key = token_at(P, place);
+    const bool same = threadIdx.x < P.tokens && token_at(P, threadIdx.x) == key;
+    const uint32_t in_warp = __ballot_sync(~0u, same);
+    if (lane == 0) s_same[warp] = in_warp;
+    if (__syncthreads_or((same && threadIdx.x < place) || key >= P.vocab)) return;
+    uint32_t before = 0, many = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) {
+        const uint32_t n = __popc(s_same[w]);
+        before += w < warp ? n : 0, many += n;
+    }
+    if (same) s_place[before + __popc(in_warp & ((1u << lane) - 1))] = threadIdx.x;
+    __syncthreads();
+    const uint32_t first = blockIdx.x * kSlab + lane;
+    float sum[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) sum[j] = 0.f;
+#pragma unroll 4
+    for (uint32_t k = warp; k < many; k += kWarps) {
+        const A* row = reinterpret_cast<const A*>(P.dout) + s_place[k] * P.dout_stride;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (first + j * 32 < P.dim) sum[j] += to_f32<A>(row[first + j * 32]);
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) s_sum[warp][j * 32 + lane] = sum[j];
+    __syncthreads();
+    const uint32_t column = blockIdx.x * kSlab + threadIdx.x;
+    if (column >= P.dim) return;
+    float all = s_sum[0][threadIdx.x];
+    for (uint32_t w = 1; w < min(many, (uint32_t)kWarps); ++w) all += s_sum[w][threadIdx.x];
+    write_part<W, 1>(P, key, column, &all);
+}
+
 constexpr int kAhead = 4096;                                   // bytes of dout that a warp has on their way
 
 // A CTA takes 8 `chunk` neighbouring places in the sorted order and 256 columns, a warp `chunk` of the places, whose keys it holds 32 at a time.  Rows of dout are copied into shared memory
@@ -748,6 +791,13 @@ extern "C" int halos_embedding_bwd(const halos_embedding_args* a) {
     const bool whole = width_of(P.dim, a->dweight, a->dweight_stride, wsize, P.tokens ? a->dout : a->dweight, P.tokens ? a->dout_stride : a->dweight_stride, P.tokens ? size : wsize) >= 16 / size;
     const int64_t far = P.tokens ? (int64_t)(P.tokens - 1) * a->dout_stride : 0;
     P.dout_span[0] = P.dout + (far < 0 ? far : 0) * (int64_t)size, P.dout_span[1] = P.dout + ((far > 0 ? far : 0) + a->dim) * (int64_t)size;
+    if (P.accumulate && P.tokens && P.tokens <= kFewPlaces)
+        return by_type(a->weight_dtype, [&](auto wt) -> int {
+            return by_type(a->dtype, [&](auto x) -> int {
+                embedding_few_kernel<decltype(x), decltype(wt)><<<dim3(P.slabs, P.tokens), kThreads, 0, st>>>(P);
+                return cuda_status(cudaGetLastError(), "embedding launch");
+            });
+        });
     int sorted = 0;                                    // which of the two arrays holds the sorted places
     if (P.tokens && P.tokens <= kMostClustered) {
         // eight CTAs as soon as there is work for them

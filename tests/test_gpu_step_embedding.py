@@ -135,6 +135,34 @@ def test_onto_what_is_there(dtype, wtype, dim):
     assert same(room[:, dim:].contiguous(), before[:, dim:].contiguous())
 
 
+@pytest.mark.parametrize("dtype,wtype", [(BF16, F32), (F32, F32), (F16, F16), (F32, BF16)])
+@pytest.mark.parametrize("n", [1, 2, 31, 33, 255, 256, 257])
+@pytest.mark.parametrize("how", ["apart", "one", "half", "none"])
+def test_few_onto_what_is_there(dtype, wtype, n, how):
+    """Every place another token, one token everywhere, one at every other place among others that are none, and none at all; a column more than whole warps take, rows apart."""
+    vocab, dim = 400, 289
+    room = _x((vocab, dim + 3), wtype, 60)
+    room[399] = float("nan")
+    t = torch.randperm(399, generator=_gen(61), device="cuda")[:n]
+    if how != "apart":
+        t = {"one": torch.full_like(t, 7), "half": torch.where(torch.arange(n, device="cuda") % 2 == 0, 7, torch.where(t % 3 == 0, -t - 1, t)), "none": t + vocab}[how]
+    wide = _x((n, 2 * dim), dtype, 62)
+    dout, before = wide[:, dim:], room.clone()
+    if how == "half":
+        dout[t < 0] = float("nan")       # no row's
+    got = step.embedding_backward(dout, t, vocab, scale=0.5, out=room[:, :dim], accumulate=True)
+    ok = (t >= 0) & (t < vocab)
+    want, bound = mo.embedding_backward(dout[ok], t[ok], vocab, 0.5, wtype, before[:, :dim])
+    mo.close(got[:399], want[:399], bound[:399])
+    bits = torch.int16 if room.element_size() == 2 else torch.int32
+    rest = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    rest[t[ok]] = False
+    assert torch.equal(room[rest].view(bits), before[rest].view(bits)) and torch.equal(room[:, dim:].contiguous().view(bits), before[:, dim:].contiguous().view(bits))
+    again = before.clone()
+    step.embedding_backward(dout, t, vocab, scale=0.5, out=again[:, :dim], accumulate=True)
+    assert torch.equal(again.view(bits), room.view(bits))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_strides(dtype):
     wide = _x((90, 3, 40), dtype, 16)
