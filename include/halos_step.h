@@ -200,8 +200,9 @@ int halos_embedding_workspace(const halos_embedding_args* args, uint64_t* bytes)
 
 /* For every row of dim elements, with s = x + residual (x, without one) in 32 bits:
  *     rstd = 1 / sqrt(mean of s^2 + eps);  y = s rstd weight;  summed = s, rounded to dtype (written if there is a residual).
- * quantized: y is written in 8 bits (4 of exponent, 3 of mantissa, largest 448) as the nearest to y / scale, and scales has for every `group`
- * neighbouring elements of a row (the last of a row may be fewer; group = 0: the whole row)  scale = max(max |y| / 448, 2^-126).
+ * quantized: y is written in 8 bits (4 of exponent, 3 of mantissa, largest 448) as the nearest to the quotient y / scale in 32 bits, of two equally near
+ * the even one, and scales has for every `group` neighbouring elements of a row (the last of a row may be fewer; group = 0: the whole row)
+ * scale = max(max |y| (1/448), 2^-126), a product in 32 bits.
  * Rows of any size, those whose squares 32 bits do not hold included, give what the formula does: 1 / 0 is infinity, a NaN makes its row NaN, an
  * infinity its own place and the rest 0.
  * bwd, from s as it was rounded (x, without a residual), rstd, dy and dsummed (the gradient of summed, or NULL), with u = s rstd and g = dy weight:

@@ -49,12 +49,19 @@ __device__ __forceinline__ float scale_of(uint32_t top) {
     const float s = __uint_as_float(top) * (1.f / kLargest8);
     return s < kLeastScale ? kLeastScale : s;  // a NaN stays one
 }
-// Off by 2^-23 of itself: a value within that of the middle between two 8-bit ones may go to either.
-__device__ __forceinline__ float reciprocal(float v) {
-    float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
+// A scale and its reciprocal as the sum of two floats, which is off by 2^-46 of itself: the reciprocal's approximation is off by 2^-23, `left` is what it leaves of 1, exactly, and
+// `low` is off by 2^-23 of itself.  A product with it that is rounded once is the quotient rounded once, as far as 8 bits can show it: a quotient that is the middle between two 8-bit
+// values comes out as that, and only one within 2^-24 of the middle without being it may go to either side, as if it had been divided in 32 bits.
+struct Scale {
+    float scale, high, low;
+    __device__ __forceinline__ explicit Scale(uint32_t top) : scale(scale_of(top)) {
+        asm("rcp.approx.f32 %0, %1;" : "=f"(high) : "f"(scale));
+        const float left = fmaf(-scale, high, 1.f);
+        low = scale <= 0x1p127f ? left * high : 0.f;   // an infinite scale has a reciprocal of 0, of which nothing is left
+    }
+};
+// Two elements over the scales that are theirs.
+__device__ __forceinline__ float2 over(float2 v, const Scale& a, const Scale& b) { return fma2(v, make_float2(a.high, b.high), mul2(v, make_float2(a.low, b.low))); }
 __device__ __forceinline__ uint8_t to_8_bits(float v) { return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
 template <int V>
 __device__ __forceinline__ void store_8_bits(uint8_t* to, const float2 (&v)[V / 2]) {
@@ -113,6 +120,7 @@ __global__ void __launch_bounds__(kThreads) rms_norm_any_kernel(const __grid_con
         whole = cta_max(whole);
         if (threadIdx.x == 0) P.scales[row] = scale_of(whole);
     }
+    const float scale_of_row = scale_of(whole);
     const int64_t y0 = start_of(P, P.out[0], row);
     for (uint32_t tile = 0; tile < P.dim; tile += kTile) {
         const uint32_t end = min(P.dim, tile + kTile);
@@ -129,7 +137,7 @@ __global__ void __launch_bounds__(kThreads) rms_norm_any_kernel(const __grid_con
             const float v = sum_at<T>(x, r, c), y = v * rstd * weight_at(P, c);
             if (out) out[c] = from_f32<T>(v);
             if (!quantized) reinterpret_cast<T*>(P.out[0].at)[y0 + c] = from_f32<T>(y);
-            else reinterpret_cast<uint8_t*>(P.out[0].at)[y0 + c] = to_8_bits(y * reciprocal(scale_of(grouped ? s_top[(c - tile) / P.group] : whole)));
+            else reinterpret_cast<uint8_t*>(P.out[0].at)[y0 + c] = to_8_bits(y / (grouped ? scale_of(s_top[(c - tile) / P.group]) : scale_of_row));
         }
     }
 }
@@ -222,28 +230,31 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
             float* scales = P.scales + (int64_t)row * P.groups;
             const uint32_t group = P.group;
             if constexpr (M == kWhole) {   // the threads of a group are neighbours in a warp, or the group is the row
-                uint32_t top = 0;
+                uint32_t top[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) top[j] = largest<V>(v[j]);
                 if (group == P.dim) {
 #pragma unroll
-                    for (int j = 0; j < N; ++j) top = max(top, largest<V>(v[j]));
-                    top = S.top(top);
-                    if (here && t.leads()) scales[0] = scale_of(top);
+                    for (int j = 1; j < N; ++j) top[0] = max(top[0], top[j]);
+                    top[0] = S.top(top[0]);
+#pragma unroll
+                    for (int j = 1; j < N; ++j) top[j] = top[0];
+                    if (here && t.leads()) scales[0] = scale_of(top[0]);
+                } else {
+#pragma unroll
+                    for (uint32_t o = 128 / V / 2; o; o >>= 1)
+                        if (o * V < group)
+#pragma unroll
+                            for (int j = 0; j < N; ++j) top[j] = max(top[j], __shfl_xor_sync(~0u, top[j], o));
                 }
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     const int c = t.column(j);
-                    if (group != P.dim) {
-                        top = largest<V>(v[j]);
-#pragma unroll
-                        for (uint32_t o = 128 / V / 2; o; o >>= 1)
-                            if (o * V < group) top = max(top, __shfl_xor_sync(~0u, top, o));
-                    }
                     if (!here || c >= dim) continue;
-                    const float scale = scale_of(top);
-                    if (group != P.dim && ((uint32_t)c & (group - 1)) == 0) scales[(uint32_t)c >> P.group_bits] = scale;
-                    const float2 inverse = both(reciprocal(scale));
+                    const Scale scale(top[j]);
+                    if (group != P.dim && ((uint32_t)c & (group - 1)) == 0) scales[(uint32_t)c >> P.group_bits] = scale.scale;
 #pragma unroll
-                    for (int i = 0; i < H; ++i) v[j][i] = mul2(v[j][i], inverse);
+                    for (int i = 0; i < H; ++i) v[j][i] = over(v[j][i], scale, scale);
                     store_8_bits<V>(y + c, v[j]);
                 }
             } else {
@@ -276,9 +287,9 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
                     if (!here || c >= dim) continue;
                     const uint32_t g = group == P.dim ? 0 : (uint32_t)max(c, 0) >> P.group_bits;
                     const int border = group == P.dim ? dim : (int)(g + 1) << P.group_bits;
-                    const float first = reciprocal(scale_of(s_group[g])), second = border < c + V && border < dim ? reciprocal(scale_of(s_group[g + 1])) : 0.f;
+                    const Scale first(s_group[g]), second(border < c + V && border < dim ? s_group[g + 1] : 0);
 #pragma unroll
-                    for (int i = 0; i < H; ++i) v[j][i] = mul2(v[j][i], make_float2(c + 2 * i < border ? first : second, c + 2 * i + 1 < border ? first : second));
+                    for (int i = 0; i < H; ++i) v[j][i] = over(v[j][i], c + 2 * i < border ? first : second, c + 2 * i + 1 < border ? first : second);
                     if (M == kShifted && c >= 0 && c + V <= dim) store_8_bits<V>(y + c, v[j]);
                     else {
 #pragma unroll
