@@ -204,7 +204,8 @@ int halos_embedding_workspace(const halos_embedding_args* args, uint64_t* bytes)
  * the even one, and scales has for every `group` neighbouring elements of a row (the last of a row may be fewer; group = 0: the whole row)
  * scale = max(max |y| (1/448), 2^-126), a product in 32 bits.
  * Rows of any size, those whose squares 32 bits do not hold included, give what the formula does: 1 / 0 is infinity, a NaN makes its row NaN, an
- * infinity its own place and the rest 0.
+ * infinity its own place and the rest 0.  Where rstd is above what 32 bits hold (a root mean square below 2^-128) it is infinity, y is what the formula
+ * gives, and bwd, which has rstd alone, gives no finite gradients.
  * bwd, from s as it was rounded (x, without a residual), rstd, dy and dsummed (the gradient of summed, or NULL), with u = s rstd and g = dy weight:
  *     dx = rstd (g - u mean of g u) + dsummed,  which is the gradient of x and of residual;   dweight = sum over rows of dy u.
  * The sums of dweight are in 32 bits and a fixed order, and each result is rounded once.

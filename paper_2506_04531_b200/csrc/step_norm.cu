@@ -43,7 +43,10 @@ __device__ __forceinline__ float step_for(uint32_t top) {
     const int e = min(max((int)(top >> 23) - 127, -100), 100);
     return __uint_as_float((uint32_t)(127 - e) << 23);
 }
-__device__ __forceinline__ float root_of(float sum, float step, const Params& P) { return step * rsqrtf(sum * P.inverse_dim + P.eps * step * step); }
+__device__ __forceinline__ float root_of(float sum, float step, const Params& P, float lift = 1.f) { return step / lift * rsqrtf(sum * P.inverse_dim + P.eps * step * step); }
+// Rows that are not all zeros and still so small that 32 bits do not hold one over their root: it is formed divided by kLift, and the products with it are taken times that.
+constexpr float kLift = 0x1p64f;
+__device__ __forceinline__ bool to_be_lifted(float rstd, float sum) { return isinf(rstd) && sum > 0.f; }
 
 __device__ __forceinline__ float scale_of(uint32_t top) {
     const float s = __uint_as_float(top) * (1.f / kLargest8);
@@ -112,11 +115,12 @@ __global__ void __launch_bounds__(kThreads) rms_norm_any_kernel(const __grid_con
         }
         sum = cta_sum(sum);
     }
-    const float rstd = root_of(sum, step, P);
+    const float rstd = root_of(sum, step, P), lift = to_be_lifted(rstd, sum) ? kLift : 1.f, root = root_of(sum, step, P, lift);
     if (threadIdx.x == 0) P.rstd[row] = rstd;
+    const auto y_of = [&](float v, uint32_t c) { return v * root * lift * weight_at(P, c); };
     uint32_t whole = 0;
     if (quantized && P.group == P.dim) {
-        for (uint32_t c = threadIdx.x; c < P.dim; c += kThreads) whole = max(whole, size_bits(sum_at<T>(x, r, c) * rstd * weight_at(P, c)));
+        for (uint32_t c = threadIdx.x; c < P.dim; c += kThreads) whole = max(whole, size_bits(y_of(sum_at<T>(x, r, c), c)));
         whole = cta_max(whole);
         if (threadIdx.x == 0) P.scales[row] = scale_of(whole);
     }
@@ -129,12 +133,12 @@ __global__ void __launch_bounds__(kThreads) rms_norm_any_kernel(const __grid_con
             __syncthreads();
             for (uint32_t g = threadIdx.x; g < kTile / 32; g += kThreads) s_top[g] = 0;
             __syncthreads();
-            for (uint32_t c = tile + threadIdx.x; c < end; c += kThreads) atomicMax(&s_top[(c - tile) / P.group], size_bits(sum_at<T>(x, r, c) * rstd * weight_at(P, c)));
+            for (uint32_t c = tile + threadIdx.x; c < end; c += kThreads) atomicMax(&s_top[(c - tile) / P.group], size_bits(y_of(sum_at<T>(x, r, c), c)));
             __syncthreads();
             for (uint32_t g = threadIdx.x; g * P.group < end - tile; g += kThreads) P.scales[(int64_t)row * P.groups + tile / P.group + g] = scale_of(s_top[g]);
         }
         for (uint32_t c = tile + threadIdx.x; c < end; c += kThreads) {
-            const float v = sum_at<T>(x, r, c), y = v * rstd * weight_at(P, c);
+            const float v = sum_at<T>(x, r, c), y = y_of(v, c);
             if (out) out[c] = from_f32<T>(v);
             if (!quantized) reinterpret_cast<T*>(P.out[0].at)[y0 + c] = from_f32<T>(y);
             else reinterpret_cast<uint8_t*>(P.out[0].at)[y0 + c] = to_8_bits(y / (grouped ? scale_of(s_top[(c - tile) / P.group]) : scale_of_row));
@@ -210,14 +214,21 @@ __global__ void __launch_bounds__(kWide<T, N, M> ? kMostThreads : kThreads, kWid
                 }
             total = S.sum(sums.x + sums.y);
         }
-        const float rstd = root_of(total, step, P);
+        float rstd = root_of(total, step, P);
         if (here && t.leads()) P.rstd[row] = rstd;
+        const bool lifted = to_be_lifted(rstd, total);
+        if (lifted) rstd = root_of(total, step, P, kLift);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             float2 w[H];
             t.weights(j, w);
 #pragma unroll
-            for (int i = 0; i < H; ++i) v[j][i] = mul2(mul2(v[j][i], both(rstd)), w[i]);
+            for (int i = 0; i < H; ++i) v[j][i] = mul2(v[j][i], both(rstd));
+            if (lifted)
+#pragma unroll
+                for (int i = 0; i < H; ++i) v[j][i] = mul2(v[j][i], both(kLift));
+#pragma unroll
+            for (int i = 0; i < H; ++i) v[j][i] = mul2(v[j][i], w[i]);
         }
         const int64_t y0 = here ? start_of(P, P.out[0], row) : 0;
         if constexpr (!QUANTIZED) {

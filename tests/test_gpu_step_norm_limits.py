@@ -43,3 +43,31 @@ def test_8_bits_are_the_nearest_to_the_quotient(d, loose, dtype, group):
         want, want_scales = _in_8_bits(x, residual, w, rstd, group)
         assert torch.equal(scales, want_scales)
         assert int((q.view(torch.uint8) != want).sum()) == 0
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d,loose", [(8, False), (250, True), (1021, False), (2048, False), (9000, False), (40000, False)])
+def test_rows_of_subnormal_elements(d, loose, dtype, residual):
+    """One over their root mean square is more than 32 bits hold; the normalised row is not."""
+    least = 2.0 ** (-149 if dtype == F32 else -133)
+    k = torch.randint(-15, 16, (5, d), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")
+    k[:, 0] = 7
+    k[3] *= 1 << 20                                     # a row that 32 bits do hold
+    x = (k.double() * least).to(dtype)
+    if loose:
+        x = torch.cat([x, x[:, :1]], 1)[:, :d]
+    r = x.contiguous() if residual else None
+    w = _x((d,), F32, 5)
+    y, summed, rstd = step.rms_norm_forward(x, w, residual=r, eps=0.0)
+    o = mo.rms_norm(x, w, r, 0.0)
+    mo.close(y, o["y"], mo.rounded(o["y"], o["y_off"], dtype))
+    held = o["rstd"] < 3.4e38
+    assert int(held.sum()) == 1 and bool(rstd[~held].isinf().all())
+    mo.close(rstd[held], o["rstd"][held], o["rstd_bound"][held])
+    for group in (0, 64):
+        q, scales, _, again = step.rms_norm_quantized(x, w, residual=r, eps=0.0, group=group)
+        assert torch.equal(again, rstd)
+        wide = torch.repeat_interleave(scales.double(), group or d, -1)[..., :d]
+        # half a step of what is held: 2^-4 of a normal value, 2^-10 below 2^-6; the quotient is rounded once before, and the scale once
+        mo.close(q.double() * wide, o["y"], torch.maximum(2.0 ** -4 * (o["y"].abs() + o["y_off"]) * (1 + 4 * mo.E), 2.0 ** -10 * wide) + o["y_off"] + 4 * mo.E * o["y"].abs())
