@@ -243,7 +243,8 @@ int halos_rms_norm_workspace(const halos_rms_norm_args* args, uint64_t* bytes);
 
 /* ------------------------------------------------------------------ gradients ----------- */
 
-/* n = sqrt(sum of the squares of every element of every gradient), f = n > max_norm ? max_norm / n : 1  (n, f in 64 bits; a NaN n has f = 1)
+/* n = sqrt(sum of the squares of every element of every gradient), f = n > max_norm ? max_norm / n : 1  (n, f in 64 bits; a NaN n has f = 1;
+ * elements are multiplied by f, or rate f, as rounded to 32 bits where those hold it, that is from 2^-126 on, and in 64 bits below)
  *     halos_grad_norm    *norm = n
  *     halos_clip_grads   *norm = n;  out_i = f grad_i;  out_i may be grad_i
  *     halos_sgd_step     out_i = out_i - rate f grad_i;  *norm = n where norm is not NULL.  norm NULL: no norm is formed, f = 1

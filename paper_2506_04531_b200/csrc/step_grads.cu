@@ -135,6 +135,9 @@ __global__ void __launch_bounds__(kThreads) grads_norm_kernel(const double* part
     if (threadIdx.x == 0) *norm = (float)d;
 }
 
+// Whether 32 bits hold the factor to their last one.
+__device__ __forceinline__ bool held_in_32_bits(double f) { return f == (double)(float)f || !(fabs(f) < 0x1p-126); }
+
 template <Mode M, typename A, typename B>
 __device__ __forceinline__ void apply_to_chunk(const A* x, B* y, int n, float f) {
     constexpr int kUnits = kChunkBytes / sizeof(A) / 8 / kThreads, kAtOnce = 2;
@@ -174,8 +177,23 @@ __device__ __forceinline__ void apply_to_chunk(const A* x, B* y, int n, float f)
     }
 }
 
+// The same where 32 bits do not hold the factor, in 64: gradients so large that the norm is 2^126 times what they are clipped to, or more.
+template <Mode M, typename A, typename B>
+__device__ __noinline__ void apply_in_64_bits(const A* x, B* y, int n, double f) {
+    for (int c = threadIdx.x; c < n; c += kThreads) {
+        const double g = f * (double)to_f32<A>(x[c]);
+        y[c] = from_f32<B>((float)(M == kStep ? (double)to_f32<B>(y[c]) - g : g));
+    }
+}
+
+template <Mode M, typename A, typename B>
+__device__ __forceinline__ void apply_to_chunk(const A* x, B* y, int n, double f) {
+    if (held_in_32_bits(f)) apply_to_chunk<M>(x, y, n, (float)f);
+    else apply_in_64_bits<M>(x, y, n, f);
+}
+
 template <Mode M, typename A>
-__device__ __forceinline__ void apply_by_out(const Piece& p, int64_t at, int n, float f) {
+__device__ __forceinline__ void apply_by_out(const Piece& p, int64_t at, int n, double f) {
     const A* x = (const A*)p.in + at;
     if (p.out_type == HALOS_F32) apply_to_chunk<M>(x, (float*)p.out + at, n, f);
     else if (p.out_type == HALOS_BF16) apply_to_chunk<M>(x, (__nv_bfloat16*)p.out + at, n, f);
@@ -192,12 +210,12 @@ __global__ void __launch_bounds__(kThreads, kResident) grads_apply_kernel(const 
         if (n > (double)t.max_norm) f = (double)t.max_norm / n;
         if (t.norm && blockIdx.x == 0 && threadIdx.x == 0) *t.norm = (float)n;
     }
-    const float factor = M == kStep ? (float)((double)t.rate * f) : (float)f;
+    const double factor = M == kStep ? (double)t.rate * f : f;
     const uint32_t end = min(t.chunks, (blockIdx.x + 1) * t.run);
     for (uint32_t c = blockIdx.x * t.run; c < end; ++c) {
         const uint32_t chunk = t.chunks - 1 - c;
         const Piece& p = t.piece[piece_of(t, chunk)];
-        if (M == kClip && p.in == p.out && factor == 1.f) continue;
+        if (M == kClip && p.in == p.out && (float)factor == 1.f) continue;
         const uint32_t size = p.in_type == HALOS_F32 ? 4 : 2;
         const int64_t at = (int64_t)(chunk - p.first) * (kChunkBytes / size), left = p.n - at;
         const int n = (int)(left < kChunkBytes / size ? left : kChunkBytes / size);
