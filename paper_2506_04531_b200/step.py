@@ -648,7 +648,10 @@ class _EmbeddingBack(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dweight):
-        return _Embedding.apply(dweight if dweight.stride(1) == 1 else dweight.contiguous(), *ctx.saved_tensors, *ctx.how), None, None, None, None
+        tokens, = ctx.saved_tensors
+        rows = _Embedding.apply(dweight if dweight.stride(1) == 1 else dweight.contiguous(), tokens, *ctx.how)
+        none = (tokens < 0) | (tokens >= dweight.size(0))     # take no part in the gradient: its derivative there is 0, not the NaN of their rows
+        return rows.masked_fill(none.unsqueeze(-1), 0.0), None, None, None, None
 
 
 def embedding(weight, tokens, *, scale: float = 1.0, dtype=None):

@@ -1,0 +1,41 @@
+"""CPU-side checks at the limits of the embedding's, the norms' and the gradients' calls, with stand-ins for the kernels."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2506_04531_b200 import step
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    """The embedding as the interface has it: a token outside the vocabulary gives a row of NaN and takes no part in the gradient."""
+    def embedding_forward(weight, tokens, *, scale=1.0, dtype=None):
+        known = (tokens >= 0) & (tokens < weight.size(0))
+        rows = weight.detach()[tokens.clamp(0, weight.size(0) - 1)] * scale
+        return torch.where(known[..., None], rows, float("nan")).to(dtype or weight.dtype)
+
+    def embedding_backward(dout, tokens, vocab, *, scale=1.0, dtype=None, **kw):
+        flat, rows = tokens.reshape(-1), dout.detach().reshape(-1, dout.size(-1))
+        known = (flat >= 0) & (flat < vocab)
+        return (dout.new_zeros(vocab, dout.size(-1)).index_add(0, flat[known], rows[known]) * scale).to(dtype or dout.dtype)
+
+    for f in (embedding_forward, embedding_backward):
+        monkeypatch.setattr(step, f.__name__, f)
+
+
+def test_second_derivatives_leave_out_tokens_that_are_none(plain):
+    w, t = torch.randn(6, 4, dtype=torch.float64, requires_grad=True), torch.tensor([[1, -1, 5], [6, 1, -100]])
+    known = (t >= 0) & (t < 6)
+    dout = torch.randn(2, 3, 4, dtype=torch.float64, requires_grad=True)
+    y = step.embedding(w, t, scale=2.0)
+    g, = torch.autograd.grad(y, w, dout, create_graph=True)
+    first, = torch.autograd.grad(g.pow(3).sum(), dout, create_graph=True)
+    with torch.no_grad():
+        want = torch.where(known[..., None], 2.0 * 3 * g.pow(2)[t.clamp(0, 5)], 0.0)
+    assert torch.equal(first, want)
+    again, = torch.autograd.grad(first.sum(), dout)     # and once more: 24 g of each row, for every place of its token
+    counts = torch.bincount(t[known], minlength=6).double()
+    with torch.no_grad():
+        want = torch.where(known[..., None], (24.0 * g * counts[:, None])[t.clamp(0, 5)], 0.0)
+    assert torch.allclose(again, want)
