@@ -243,7 +243,7 @@ __device__ __forceinline__ uint32_t sum_up_to(uint32_t v, uint32_t* s_warp) {
 template <int ITEMS>
 __global__ void __launch_bounds__(kSortThreads, 1) embedding_sort_kernel(const __grid_constant__ EmbedParams P, int passes, int bits_of_all, int in_cluster, uint32_t weight_type) {
     extern __shared__ __align__(16) uint64_t s_item[];         // [span]: key << 32 | place, as the cluster has sorted them; [span]: as this CTA has
-    __shared__ uint16_t s_count[kSortWarps][1 << kMostBits];
+    __shared__ __align__(16) uint16_t s_count[kSortWarps][1 << kMostBits];   // cleared by accesses of 16 bytes
     __shared__ uint32_t s_total[1 << kMostBits], s_base[1 << kMostBits], s_warp[kSortWarps];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if ((int)blockIdx.x >= in_cluster) {
@@ -406,7 +406,8 @@ template <typename A, typename W, int V>
 __global__ void __launch_bounds__(kThreads) embedding_sum_kernel(const __grid_constant__ EmbedParams P, const uint32_t* key, const uint32_t* place) {
     constexpr int J = kSlab / 32 / V, kRow = kSlab * (int)sizeof(A) + (V == 1 ? 16 : 0), kRing = kAhead / (kSlab * (int)sizeof(A));
     extern __shared__ __align__(16) char s_rows[];             // [warps][ring] rows
-    __shared__ float s_head[kWarps][kSlab], s_tail[kWarps][kSlab];
+    __shared__ __align__(16) float s_head[kWarps][kSlab], s_tail[kWarps][kSlab];   // of V floats to an access
+    static_assert(__alignof__(s_head) == 16 && __alignof__(s_tail) == 16, "the attribute is every declarator's");
     __shared__ uint32_t s_through[kWarps], s_goes[kWarps], s_last, s_ends, s_comes, s_key[2];   // keys of the run that comes from the CTA before, that goes on into the next
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, slab = blockIdx.x % P.slabs, block = blockIdx.x / P.slabs;
     const uint32_t span = P.chunk * kWarps, cta_from = block * span, from = min(P.tokens, cta_from + warp * P.chunk), n = min(P.chunk, P.tokens - from), blocks = P.jobs / P.slabs;

@@ -1,10 +1,15 @@
 """CPU-side checks at the limits of the embedding's, the norms' and the gradients' calls, with stand-ins for the kernels."""
 from __future__ import annotations
 
+import re
+from pathlib import Path
+
 import pytest
 import torch
 
 from paper_2506_04531_b200 import step
+
+CSRC = Path(step.__file__).resolve().parent / "csrc"
 
 
 @pytest.fixture
@@ -39,3 +44,12 @@ def test_second_derivatives_leave_out_tokens_that_are_none(plain):
     with torch.no_grad():
         want = torch.where(known[..., None], (24.0 * g * counts[:, None])[t.clamp(0, 5)], 0.0)
     assert torch.allclose(again, want)
+
+
+@pytest.mark.parametrize("kernel,names", [("embedding_sort_kernel", ["s_count"]), ("embedding_sum_kernel", ["s_head", "s_tail"])])
+def test_shared_arrays_with_accesses_of_16_bytes_are_aligned_to_them(kernel, names):
+    """Their types alone ask for 2 or 4 bytes, and smaller variables lie beside them."""
+    body = (CSRC / "step_embedding.cu").read_text().split(kernel + "(", 1)[1].split("\n}\n", 1)[0]
+    for name in names:
+        line, = re.findall(rf"^ *(__shared__ [^;]*\b{name}\[[^;]*);", body, re.M)
+        assert line.startswith("__shared__ __align__(16) "), line
