@@ -553,6 +553,17 @@ def _as_rows(x, dim: int):
     return x if x.stride(1) == 1 or dim == 1 else x.contiguous()
 
 
+def _share(a, b) -> bool:
+    """Whether two matrices, each (address, rows, distance of rows, bytes of a row), have a byte in common.  Rows of one may lie between those of the other."""
+    (a_at, a_rows, a_step, a_row), (b_at, b_rows, b_step, b_row) = a, b
+    if not (a_rows and b_rows and a_row and b_row) or a_at + (a_rows - 1) * a_step + a_row <= b_at or b_at + (b_rows - 1) * b_step + b_row <= a_at:
+        return False
+    starts = a_at + torch.arange(a_rows) * a_step
+    before = torch.div(starts - b_at, b_step or 1, rounding_mode="floor")         # b's last row that begins there or in front, and the one behind it
+    near = [b_at + (before + k).clamp(0, b_rows - 1) * b_step for k in (0, 1)]
+    return any(bool(((x < starts + a_row) & (starts < x + b_row)).any()) for x in near)
+
+
 def _tokens_checked(tokens, device):
     _on(tokens, device, "tokens")
     wide = tokens.dtype == torch.int64
@@ -606,7 +617,8 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
     if dim and not dout.is_contiguous():
         rows = _as_rows(dout, dim)
         stride = rows.stride(0)
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             _refuse("accumulate needs out")
         if vocab < 0 or (dtype is not None and dtype not in _DTYPES):
@@ -616,13 +628,22 @@ def embedding_backward(dout, tokens, vocab: int, *, scale: float = 1.0, dtype=No
         _on(out, device, "out")
         if out.shape != (vocab, dim) or (dtype is not None and out.dtype != dtype) or (out.stride(1) != 1 and dim > 1) or (vocab > 1 and out.stride(0) < dim):
             _refuse("out must be [vocab, dim] of dtype, a row's elements side by side and rows apart")
-        _overwritten(out, "out")
     index, count, kind, out_kind = device.index, tokens.numel(), _dtype(dout, "dout"), _dtype(out, "out")
-    size = _embedding_workspace(index, kind, out_kind, count, vocab, dim)
-    space = torch.empty(size, dtype=torch.uint8, device=device)
+    out_at, out_stride, at, token_at = out.data_ptr(), out.stride(0), rows.data_ptr(), tokens.data_ptr()
+    if given:
+        # whole runs of memory first: what lies apart, as nearly everything does, is seen at once
+        out_size, size, token_bytes = 4 if out_kind == F32 else 2, 4 if kind == F32 else 2, count * (8 if wide else 4)
+        end = out_at + ((vocab - 1) * out_stride + dim) * out_size
+        if (at < end and out_at < at + ((count - 1) * stride + dim) * size) or (token_at < end and out_at < token_at + token_bytes):
+            written = (out_at, vocab, out_stride * out_size, dim * out_size)
+            if _share(written, (at, count, stride * size, dim * size)) or _share(written, (token_at, 1, 0, token_bytes)):
+                _refuse("out shares memory with dout or tokens")
+        _overwritten(out, "out")
+    space_bytes = _embedding_workspace(index, kind, out_kind, count, vocab, dim)
+    space = torch.empty(space_bytes, dtype=torch.uint8, device=device)
     _call("halos_embedding_bwd", _pack(
         _EMBEDDING, _EMBEDDING.size, index, _raw_stream(index), kind, out_kind, wide, bool(accumulate), count, vocab, dim, scale,
-        tokens.data_ptr(), 0, 0, 0, 0, rows.data_ptr(), stride, out.data_ptr(), out.stride(0), space.data_ptr(), size), index)
+        token_at, 0, 0, 0, 0, at, stride, out_at, out_stride, space.data_ptr(), space_bytes), index)
     return out
 
 

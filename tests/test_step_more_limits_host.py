@@ -53,3 +53,16 @@ def test_shared_arrays_with_accesses_of_16_bytes_are_aligned_to_them(kernel, nam
     for name in names:
         line, = re.findall(rf"^ *(__shared__ [^;]*\b{name}\[[^;]*);", body, re.M)
         assert line.startswith("__shared__ __align__(16) "), line
+
+
+def test_matrices_that_share_memory():
+    """Against sets of bytes: rows of any distance, one row, rows that overlap one another or are all the same, and rows of one between those of the other."""
+    import random
+    rng, seen = random.Random(0), {False: 0, True: 0}
+    for _ in range(4000):
+        a, b = ((rng.randrange(60), rng.randrange(5), rng.choice([0, 3, 8, 12, 16, 24]), rng.randrange(9)) for _ in range(2))
+        bytes_of = lambda m: {m[0] + i * m[2] + k for i in range(m[1]) for k in range(m[3])}  # noqa: E731
+        want = bool(bytes_of(a) & bytes_of(b))
+        assert step._share(a, b) is want and step._share(b, a) is want, (a, b)
+        seen[want] += 1
+    assert min(seen.values()) > 500
