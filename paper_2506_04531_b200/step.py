@@ -558,7 +558,7 @@ def _share(a, b) -> bool:
     (a_at, a_rows, a_step, a_row), (b_at, b_rows, b_step, b_row) = a, b
     if not (a_rows and b_rows and a_row and b_row) or a_at + (a_rows - 1) * a_step + a_row <= b_at or b_at + (b_rows - 1) * b_step + b_row <= a_at:
         return False
-    starts = a_at + torch.arange(a_rows) * a_step
+    starts = a_at + torch.arange(a_rows, device="cpu") * a_step
     before = torch.div(starts - b_at, b_step or 1, rounding_mode="floor")         # b's last row that begins there or in front, and the one behind it
     near = [b_at + (before + k).clamp(0, b_rows - 1) * b_step for k in (0, 1)]
     return any(bool(((x < starts + a_row) & (starts < x + b_row)).any()) for x in near)

@@ -66,3 +66,12 @@ def test_matrices_that_share_memory():
         assert step._share(a, b) is want and step._share(b, a) is want, (a, b)
         seen[want] += 1
     assert min(seen.values()) > 500
+
+
+def test_shared_memory_is_looked_for_on_the_host():
+    """Whatever device new tensors go to by default: a device's would have to be waited for, which a captured stream cannot be."""
+    try:
+        torch.set_default_device("meta")
+        assert step._share((0, 3, 8, 4), (4, 3, 8, 4)) is False and step._share((0, 3, 8, 4), (3, 3, 8, 4)) is True
+    finally:
+        torch.set_default_device(None)
