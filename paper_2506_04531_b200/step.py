@@ -4,7 +4,7 @@
     attention_forward, _backward      masked attention and its gradients; attention: with autograd
     distill_forward, _backward, distill_loss_and_grad      the loss against labels and a teacher's top logits; distill_loss: with autograd
     embedding_forward, _backward      rows of a table by tokens, scaled, and the table's gradient; embedding: with autograd
-    rms_norm_forward, _quantized, _backward      root-mean-square norm with the residual's addition; rms_norm: with autograd
+    rms_norm_forward, _quantized, _backward      root-mean-square norm with the residual's addition; rms_norm: with autograd (not in 8 bits)
     grad_norm, clip_grads, sgd_step   the norm of many gradients at once, clipping by it, and a step of plain descent
 
 As in ``binding``, the arithmetic is the CUDA library's; what happens here is checking, marshalling and output
@@ -768,7 +768,8 @@ def rms_norm_forward(x, weight, *, residual=None, eps: float = 1e-5):
 
 def rms_norm_quantized(x, weight, *, residual=None, eps: float = 1e-5, group: int = 0):
     """(q, scales, summed, rstd): ``rms_norm_forward`` with y in 8 bits (float8_e4m3fn), q scales being nearest to y.  scales [..., n] in float32 has one value for
-    every group (32, 64 or 128) of a row's elements, or one for the row (0): the largest of them over 448."""
+    every group (32, 64 or 128) of a row's elements, or one for the row (0): the largest of them over 448.  Without autograd: all four, summed among
+    them, are cut from the graph that x, the residual and weight may be in."""
     return _rms_norm(x, weight, residual, eps, True, group)
 
 
