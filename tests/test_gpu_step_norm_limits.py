@@ -71,3 +71,31 @@ def test_rows_of_subnormal_elements(d, loose, dtype, residual):
         wide = torch.repeat_interleave(scales.double(), group or d, -1)[..., :d]
         # half a step of what is held: 2^-4 of a normal value, 2^-10 below 2^-6; the quotient is rounded once before, and the scale once
         mo.close(q.double() * wide, o["y"], torch.maximum(2.0 ** -4 * (o["y"].abs() + o["y_off"]) * (1 + 4 * mo.E), 2.0 ** -10 * wide) + o["y_off"] + 4 * mo.E * o["y"].abs())
+
+
+@pytest.mark.parametrize("dtype,wtype", [(F32, F32), (BF16, F32), (F16, F16)])
+@pytest.mark.parametrize("d", [508, 510, 516, 765, 766, 772, 3076, 4093, 4094, 4100, 6141, 6142, 6144, 6148, 8190, 8196, 12287, 12289, 12296, 16376, 16377, 16378, 16384, 16385, 16392])
+def test_on_both_sides_of_where_other_kernels_take_over(d, dtype, wtype):
+    """Rows that a CTA holds in one way or another, and rows that go through loops; on 16 bytes as they lie in memory of their own, off them, and in strides apart."""
+    rows = 19
+    for how in ("whole", "apart"):
+        x, r, dy, ds = (_x((rows, d), dtype, s) for s in (6, 7, 8, 9))
+        if how == "apart":
+            x = torch.cat([x, x[:, :1]], 1)[:, :d]
+        w = (1 + _x((d,), F32, 10, 0.2)).to(wtype)
+        for residual in (None, r):
+            got = step.rms_norm_forward(x, w, residual=residual)
+            o = mo.rms_norm(x, w, residual, 1e-5)
+            mo.close(got[0], o["y"], mo.rounded(o["y"], o["y_off"], dtype))
+            mo.close(got[2], o["rstd"], o["rstd_bound"])
+            if residual is not None:
+                mo.close(got[1], o["summed"], o["summed_bound"])
+            for group in (0, 64):
+                q, scales, _, rstd = step.rms_norm_quantized(x, w, residual=residual, group=group)
+                want, want_scales = _in_8_bits(x, residual, w, rstd, group)
+                assert torch.equal(scales, want_scales) and torch.equal(q.view(torch.uint8), want)
+            for dsummed in (None, ds):
+                dx, dw = step.rms_norm_backward(dy, got[1], w, got[2], dsummed=dsummed)
+                b = mo.rms_norm_backward(dy, got[1], w, got[2], dsummed)
+                mo.close(dx, b["dx"], b["dx_bound"])
+                mo.close(dw, b["dw"], b["dw_bound"])
