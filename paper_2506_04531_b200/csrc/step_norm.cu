@@ -6,8 +6,9 @@
 // the instructions is what keeps the shorter cases from the memory's rate.  y is formed from the 32-bit sum, not from `summed`, which is rounded; in 8 bits it is
 // rounded once, from 32.
 //
-// Measured (a pass among others; floor by bytes at the copy rate): 65536 x 768 bf16 with residual 67 us (92%), 16384 x 2048 bf16 46.5 us (88%), the same in 8 bits with
-// a scale for 128 elements 46.7 us (77%), 16384 x 1021 bf16 74 us (55%: rows off every boundary, a third of the threads' places unused), 262144 heads of 128 46 us (90%).
+// Measured (a pass among others; floor by bytes at the copy rate): 65536 x 768 bf16 with residual 67 us (92%), 16384 x 2048 bf16 with residual 46.5 us (88%), the same in 8 bits with
+// a scale for 128 elements 49 us (73%), 32768 x 1021 bf16 with residual 75 us (54%: rows off every boundary, a third of the threads' places unused; f32, 16384 of them, 50 us, 82%),
+// 262144 heads of 128 bf16 with residual 46 us (89%), 65536 x 768 f32 with residual 131 us (94%).  The kernel that goes over rows in loops: 16384 x 5120 f32 with residual 250 us (82%).
 #include "step_norm.cuh"
 
 #include <cuda_fp8.h>

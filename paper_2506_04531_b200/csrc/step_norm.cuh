@@ -246,7 +246,9 @@ struct RowSums {
 
 // ------------------------------------------------------------------------------------------------ host
 
-// How rows are spread over threads, and how many of the CTAs an SM holds.  n = 0: no CTA holds such rows.
+// How rows are spread over threads, and how many of the CTAs an SM holds.  n = 0: no CTA holds such rows, for want of registers (over 16384 elements or a little less), or of shared
+// memory for one row of each input to every thread under the spread that registers alone have chosen (f32 with two or three inputs: widths of 510 to 768, of 4094 to 6144, and backward
+// with dsummed from 8193, off 16 bytes from 4094, on).  Kernels with loops take them.
 struct Shape {
     uint32_t n, lanes, apart, threads, resident, stages, shared;   // apart: a thread's accesses
     uint32_t per() const { return threads / lanes; }

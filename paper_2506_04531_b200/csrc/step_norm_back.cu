@@ -4,8 +4,10 @@
 // two passes over its threads' parts, which lie in shared memory, there is one sum.  dweight is added up in registers over all rows that a thread sees, then over the CTA's
 // threads, and a second kernel adds up the CTAs' parts, in their order: no atomics, the same bits every time.
 //
-// Measured: 16384 x 2048 bf16 51.7 us (79% of the copy rate by bytes; the second kernel and its start take 4 of them), 24576 x 768 61.7 us (75%), 16384 x 1024 f32 48 us (85%),
-// 16384 x 1021 bf16 80 us (51%), 3063 x 10 heads of 80 f32, strided, 17 us, of which the call takes 14.
+// Measured (by bytes at the copy rate), with dsummed: 16384 x 2048 bf16 55 us among other passes (74%), 52 by itself (the second kernel and its start take 4 of them), 65536 x 768 bf16
+// 76 us (81%), 16384 x 1024 f32 48 us (85%), 8192 x 8192 f32 174 us (94%), 32768 x 1021 bf16 80 us (51%), 16384 x 1021 f32 54 us (76%); without: 4096 x 16384 f32 150 us (82%), 180560 heads of 80
+// f16 33 us (40%), 3063 x 10 heads of 80 f32, strided, 16 us, of which the call takes 14.  The kernels that go over rows in loops, which read summed and dy twice: 24576 x 768 f32 with dsummed
+// 122 us (38%), 13107 x 5120 342 us (48%), 4096 x 16384 409 us (40%).
 #include "step_norm.cuh"
 
 
